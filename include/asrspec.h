@@ -403,6 +403,156 @@ int asr_spec_test_gemm(int32_t impl, const void* A, const void* B, float* C, int
 int asr_spec_gemm_noalloc(const void* A, const void* B, float* C, int32_t M, int32_t N, int32_t K,
                           int32_t splits, void* stream);
 
+/* ---- Sampled decoding over a paged cache ----------------------------------
+ * The paper verifies greedily over a dense cache of at most max_pos slots; the
+ * four operators below serve the same speculative loop (Sec. 3 "Speculative
+ * Loop") where tokens are drawn at a temperature and where many sessions of
+ * any length share one pool of cache pages.  They take no handle: every array
+ * is a device pointer owned by the caller, nothing is allocated, calls are
+ * asynchronous on `stream` and may be captured in a graph, and calls that
+ * overlap on the GPU need workspaces of their own.  A round is
+ *   attend (per layer) -> accept_sampled -> weigh (per layer) -> kv_len += step
+ *   -> now and then evict (per layer).
+ * Conditions in device data are found by the kernels, which leave out the
+ * sequence concerned, as each entry says, and set bits of the status word
+ * (an int32 on the device, or NULL); the caller reads and clears it.
+ *
+ * A pool of pages.  Slot s of sequence b's head h lies at element
+ *   page_table[b * table_stride + s / page_size] * page_stride + h * head_stride
+ *   + (s % page_size) * slot_stride
+ * of k_pages and of v_pages, head_dim consecutive elements.  Bases and strides
+ * are multiples of 16 bytes.  A page that is written belongs to one sequence. */
+typedef struct {
+  void *k_pages, *v_pages;
+  int64_t page_stride, head_stride, slot_stride;   /* elements */
+  const int32_t* page_table;   /* [batch][table_stride]; the first max_pages of a row are used */
+  int64_t table_stride;
+  int32_t n_pages;             /* pages of the pool; a page id outside [0, n_pages) sets ASR_ST_BOUNDS */
+  int32_t page_size;           /* slots, a multiple of 16 */
+  int32_t max_pages;           /* max_pages * page_size <= 2^30 */
+  int32_t kv_heads;
+  int32_t head_dim;            /* 64 or 128 */
+  int32_t batch;               /* sequences, 1 .. 1024 */
+  int32_t dtype;               /* 0 = fp32, 1 = bf16, 2 = fp16: pages, queries and outputs */
+  int32_t* status;
+} asr_paged_cache;
+
+/* The rows of one call: up to max_rows per sequence (the pending token and its
+ * drafts; 1 for single tokens).  Query head h reads K/V head h / (heads /
+ * kv_heads).  The last axis is contiguous; strides are in elements, multiples
+ * of 16 bytes, so rows may be slices of a fused projection's output. */
+typedef struct {
+  const void* q;               /* [batch][max_rows][heads][head_dim] */
+  int64_t q_batch_stride, q_row_stride, q_head_stride;
+  const void *k_new, *v_new;   /* [batch][max_rows][kv_heads][head_dim], or both NULL */
+  int64_t new_batch_stride, new_row_stride, new_head_stride;
+  const int32_t* kv_len;       /* [batch] committed slots */
+  const int32_t* rows;         /* [batch] rows in use, 0 .. max_rows; NULL: max_rows each */
+  int32_t max_rows, heads;
+  int32_t causal;              /* 1: row i sees slots 0 .. kv_len + i; 0: every row sees slots below kv_len */
+  float scale;
+} asr_paged_rows;
+
+/* Attention of the rows over the cache, and the append of their K/V.
+ *   out[b][i][h] = sum_j p_j v_j,  p = softmax_j(scale q.k_j) over the slots row i sees;
+ *   lse[b][i][h] = log sum_j exp(scale q.k_j)   (natural log; may be NULL).
+ * With k_new / v_new (causal only) row i's K/V are also written to slot kv_len
+ * + i; without them a causal call finds the block's K/V in the pages.  A row
+ * past rows[b], and a row that sees no slot, gets zeros and lse = -inf.  A
+ * slot that a row does not see never reaches it, whatever it holds.
+ * out: [batch][max_rows][heads][head_dim] contiguous, 16-byte aligned; lse
+ * [batch][max_rows][heads] fp32.  ws: asr_spec_paged_attend_ws bytes, 16-byte
+ * aligned, no initial contents.  Arithmetic: 16-bit types multiply in 16 bits
+ * with fp32 accumulation (weights rounded to the type for the second
+ * product); fp32 in fp32 throughout; softmax statistics in fp32.
+ * Data errors: kv_len or kv_len + rows outside the table (ASR_ST_CAPACITY) and
+ * rows outside [0, max_rows] (ASR_ST_BAD_LENS) leave that sequence's rows zero
+ * and its pages unwritten; a bad page id (ASR_ST_BOUNDS) reads page 0 in its
+ * place, and new rows that belong there are not written.
+ * Errors: ASR_E_INVAL (arguments), ASR_E_CAPACITY (workspace, sizes), ASR_E_CUDA. */
+int64_t asr_spec_paged_attend_ws(const asr_paged_cache* cache, const asr_paged_rows* rows);
+int asr_spec_paged_attend(const asr_paged_cache* cache, const asr_paged_rows* rows, void* out, float* lse, void* ws,
+                          int64_t ws_bytes, void* stream);
+
+/* Per (sequence, K/V head, slot): the accumulated attention weight and the
+ * position of the token held there.  Strides in elements. */
+typedef struct {
+  const float* score;          /* [batch][kv_heads][slots]; NULL in weigh: zeros */
+  int32_t* pos;                /* the same shape and strides */
+  int64_t batch_stride, head_stride;
+  int32_t slots;
+  float* score_out;            /* may be score itself */
+  int32_t* pos_out;            /* evict only; may be pos itself */
+  int64_t out_batch_stride, out_head_stride;   /* evict only; weigh writes score_out with score's strides */
+  int32_t slots_out;           /* evict only: at least min(len, budget) */
+  const int32_t* first_pos;    /* weigh only: [batch] position of the sequence's row 0, or NULL with pos */
+} asr_paged_scores;
+
+/* Add the attention weight that the rows gave each slot:
+ *   score_out[j] = (j < kv_len ? score[j] : 0) + sum_i sum_h exp(scale q_ih.k_j - lse[i][h])
+ * over rows i < rows[b] that see slot j and the query heads h of the K/V head.
+ * Called after the verification with rows = the committed rows (step of
+ * asr_spec_accept_sampled) and the kv_len of the attention before it; k_new /
+ * v_new are not read (the block's K are in the pages).  With pos, the new
+ * slots' positions are set: pos[kv_len + i] = first_pos + i.  Entries past the
+ * last slot are left as they are.  lse: as the attention wrote it (strides in
+ * elements); a row with lse = -inf weighs nothing.
+ * Data errors as asr_spec_paged_attend, and slots beyond `slots` (ASR_ST_CAPACITY): that sequence is left out. */
+int asr_spec_paged_weigh(const asr_paged_cache* cache, const asr_paged_rows* rows, const asr_paged_scores* scores,
+                         const float* lse, int64_t lse_batch_stride, int64_t lse_row_stride, void* stream);
+
+/* Cut every (sequence, K/V head) to `budget` slots.  Where len[b] > budget the
+ * slots that stay are those of highest rank: first the protected ones (pos >=
+ * seen[b] - recent, or pos < first; seen = tokens seen so far), then by score,
+ * equal scores by lowest slot (NaN last).  The j-th freed slot below the
+ * budget takes K, V, score and position of the j-th kept slot at or past it;
+ * other kept slots stay in place.  len_out[b] = min(len[b], budget); may be
+ * len itself.  score_out / pos_out receive the entries of the slots in use.
+ * Pages past the budget are free afterwards.  The K/V of slots at or past the
+ * budget are left as they are.
+ * Data errors: len outside [0, slots] or the table, or more slots left than
+ * slots_out (ASR_ST_CAPACITY): that sequence stays as it is, len_out = len; a
+ * bad page id (ASR_ST_BOUNDS): the slot is not moved.
+ * ws: asr_spec_paged_evict_ws bytes, no initial contents. */
+int64_t asr_spec_paged_evict_ws(const asr_paged_cache* cache, const asr_paged_scores* scores, int32_t budget);
+int asr_spec_paged_evict(const asr_paged_cache* cache, const asr_paged_scores* scores, const int32_t* len,
+                         const int32_t* seen, int32_t budget, int32_t recent, int32_t first, int32_t* len_out, void* ws,
+                         int64_t ws_bytes, void* stream);
+
+/* Logits of one verification.  Rows need only their element's alignment; strides in elements. */
+typedef struct {
+  const void* target;          /* [batch][k + 1][vocab]: row i scores position i of the block */
+  int64_t target_batch_stride, target_row_stride;
+  const void* draft_logits;    /* [batch][k][vocab]: what draft i was drawn from; NULL: drafts were certain (greedy) */
+  int64_t draft_batch_stride, draft_row_stride;
+  int32_t batch, k, vocab, dtype;   /* k 0 .. 31; dtype 0 = fp32, 1 = bf16, 2 = fp16 */
+} asr_sampled_logits;
+
+/* Verification against the target's probabilities, from given random numbers.
+ * With p_i = softmax(target_i / temperature) and q_i = softmax(draft_logits_i /
+ * temperature) (or one at the draft itself), draft i is accepted while
+ *   u[b][i] q_i(x_i) < p_i(x_i);
+ * accepted[b] = n = the drafts accepted before the first that is not;
+ * token[b] = argmax_j w_j / race[b][j] (lowest id on ties) with w = max(0, p_n
+ * - q_n) after a rejection and w = p_n after none: with race drawn from the
+ * standard exponential distribution and u from [0, 1), accepted drafts and
+ * token are distributed as the target's own samples.  Where w has no positive
+ * entry, w = p_n; where p_n has none either (every logit masked), token = -1.
+ * step[b] = n + 1, the positions to commit; 0 where there is no token.
+ * prob[b][i] = min(1, p_i(x_i) / q_i(x_i)) for i < lens[b], else 0.
+ *   draft [batch][k], lens [batch] (0 .. k, -1 sits out; NULL: k each), u [batch][k],
+ *   race [batch][race_stride] fp32 > 0, at least vocab a row.
+ * A logit of -inf or NaN is masked; +inf counts as the largest float.  An
+ * utterance that sits out returns accepted 0, token -1, step 0, prob 0; so
+ * does one with a token outside [0, vocab) (ASR_ST_BAD_TOKEN) or lens outside
+ * [-1, k] (ASR_ST_BAD_LENS).  All arithmetic is fp32.
+ * ws: asr_spec_accept_sampled_ws bytes, 8-byte aligned, no initial contents.
+ * status: as the cache's, may be NULL. */
+int64_t asr_spec_accept_sampled_ws(int32_t batch, int32_t k);
+int asr_spec_accept_sampled(const asr_sampled_logits* logits, const int32_t* draft, const int32_t* lens, const float* u,
+                            const float* race, int64_t race_stride, float temperature, int32_t* accepted, int32_t* token,
+                            int32_t* step, float* prob, int32_t* status, void* ws, int64_t ws_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

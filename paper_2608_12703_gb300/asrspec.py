@@ -30,7 +30,8 @@ EXPORTED = [
     "asr_spec_gemm_noalloc", "asr_spec_timeline", "asr_spec_timeline_read",
     "asr_spec_verify_tree", "asr_spec_restart", "asr_spec_fewrow_trace", "asr_spec_fewrow_trace_read",
     "asr_spec_debug_anchor_profile", "asr_spec_draft_create", "asr_spec_draft_propose",
-    "asr_spec_draft_set_threshold",
+    "asr_spec_draft_set_threshold", "asr_spec_paged_attend", "asr_spec_paged_attend_ws", "asr_spec_paged_weigh",
+    "asr_spec_paged_evict", "asr_spec_paged_evict_ws", "asr_spec_accept_sampled", "asr_spec_accept_sampled_ws",
 ]
 DRAFT_WIN = {"anchor": 0, "shifted": 1, "random": 2, None: 3}
 PROF_CLASSES = ["qkv", "resid", "query", "mlp_up", "self_attn", "cross_attn", "lm_head", "layernorm", "other",
@@ -58,6 +59,37 @@ class AsrModelDims(ctypes.Structure):
 
 class AsrWeights(ctypes.Structure):
     _fields_ = [("blob", ctypes.POINTER(ctypes.c_float)), ("n_floats", ctypes.c_size_t)]
+
+
+class AsrPagedCache(ctypes.Structure):
+    _fields_ = [("k_pages", ctypes.c_void_p), ("v_pages", ctypes.c_void_p), ("page_stride", ctypes.c_int64),
+                ("head_stride", ctypes.c_int64), ("slot_stride", ctypes.c_int64), ("page_table", ctypes.c_void_p),
+                ("table_stride", ctypes.c_int64)] + [(n, ctypes.c_int32) for n in (
+                    "n_pages", "page_size", "max_pages", "kv_heads", "head_dim", "batch", "dtype")] + [
+                ("status", ctypes.c_void_p)]
+
+
+class AsrPagedRows(ctypes.Structure):
+    _fields_ = [("q", ctypes.c_void_p), ("q_batch_stride", ctypes.c_int64), ("q_row_stride", ctypes.c_int64),
+                ("q_head_stride", ctypes.c_int64), ("k_new", ctypes.c_void_p), ("v_new", ctypes.c_void_p),
+                ("new_batch_stride", ctypes.c_int64), ("new_row_stride", ctypes.c_int64),
+                ("new_head_stride", ctypes.c_int64), ("kv_len", ctypes.c_void_p), ("rows", ctypes.c_void_p),
+                ("max_rows", ctypes.c_int32), ("heads", ctypes.c_int32), ("causal", ctypes.c_int32),
+                ("scale", ctypes.c_float)]
+
+
+class AsrPagedScores(ctypes.Structure):
+    _fields_ = [("score", ctypes.c_void_p), ("pos", ctypes.c_void_p), ("batch_stride", ctypes.c_int64),
+                ("head_stride", ctypes.c_int64), ("slots", ctypes.c_int32), ("score_out", ctypes.c_void_p),
+                ("pos_out", ctypes.c_void_p), ("out_batch_stride", ctypes.c_int64), ("out_head_stride", ctypes.c_int64),
+                ("slots_out", ctypes.c_int32), ("first_pos", ctypes.c_void_p)]
+
+
+class AsrSampledLogits(ctypes.Structure):
+    _fields_ = [("target", ctypes.c_void_p), ("target_batch_stride", ctypes.c_int64),
+                ("target_row_stride", ctypes.c_int64), ("draft_logits", ctypes.c_void_p),
+                ("draft_batch_stride", ctypes.c_int64), ("draft_row_stride", ctypes.c_int64)] + [
+                (n, ctypes.c_int32) for n in ("batch", "k", "vocab", "dtype")]
 
 
 class AsrSpecError(RuntimeError):
@@ -106,9 +138,17 @@ def lib():
     L.asr_spec_gemm_noalloc.argtypes = [vp, vp, vp, i32, i32, i32, i32, vp]
     L.asr_spec_timeline.argtypes = [vp, i32]
     L.asr_spec_timeline_read.argtypes = [vp, vp, vp, i32, vp]
+    i64 = ctypes.c_int64
+    L.asr_spec_paged_attend.argtypes = [vp, vp, vp, vp, vp, i64, vp]
+    L.asr_spec_paged_attend_ws.argtypes = [vp, vp]
+    L.asr_spec_paged_weigh.argtypes = [vp, vp, vp, vp, i64, i64, vp]
+    L.asr_spec_paged_evict.argtypes = [vp, vp, vp, vp, i32, i32, i32, vp, vp, i64, vp]
+    L.asr_spec_paged_evict_ws.argtypes = [vp, vp, i32]
+    L.asr_spec_accept_sampled.argtypes = [vp, p32, p32, vp, vp, i64, ctypes.c_float, p32, p32, p32, vp, p32, vp, i64, vp]
+    L.asr_spec_accept_sampled_ws.argtypes = [i32, i32]
     for name in EXPORTED:
         if name not in ("asr_spec_last_error", "asr_spec_destroy"):
-            getattr(L, name).restype = ctypes.c_int
+            getattr(L, name).restype = i64 if name.endswith("_ws") else ctypes.c_int
     _lib = L
     return L
 
@@ -124,6 +164,11 @@ def ptr(x) -> Optional[int]:
     if not x.is_contiguous():
         raise ValueError("tensor must be contiguous")
     return x.data_ptr()
+
+
+def addr(x) -> Optional[int]:
+    """Address of a torch tensor of any strides, or None."""
+    return None if x is None else x.data_ptr()
 
 
 def _check(h, rc, what):
@@ -282,3 +327,27 @@ def asr_spec_gemm_noalloc(A, B, C, M, N, K, splits, stream=None):
     return _check(None, lib().asr_spec_gemm_noalloc(ptr(A), ptr(B), ptr(C), M, N, K, splits,
                                                     None if stream is None else ctypes.c_void_p(stream)),
                   "asr_spec_gemm_noalloc")
+
+
+# The operators over a paged cache take no handle; tensors are passed by address, their strides in the structures.
+def asr_spec_paged_attend(cache, rows, out, lse, ws, ws_bytes, stream=None):
+    return _check(None, lib().asr_spec_paged_attend(cache, ctypes.byref(rows), ptr(out), ptr(lse), ptr(ws), ws_bytes, stream),
+                  "asr_spec_paged_attend")
+
+
+def asr_spec_paged_weigh(cache, rows, scores, lse, lse_batch_stride, lse_row_stride, stream=None):
+    return _check(None, lib().asr_spec_paged_weigh(cache, ctypes.byref(rows), ctypes.byref(scores), addr(lse),
+                                                   lse_batch_stride, lse_row_stride, stream), "asr_spec_paged_weigh")
+
+
+def asr_spec_paged_evict(cache, scores, lens, seen, budget, recent, first, lens_out, ws, ws_bytes, stream=None):
+    return _check(None, lib().asr_spec_paged_evict(cache, ctypes.byref(scores), ptr(lens), ptr(seen), budget, recent, first,
+                                                   ptr(lens_out), ptr(ws), ws_bytes, stream), "asr_spec_paged_evict")
+
+
+def asr_spec_accept_sampled(logits, draft, lens, u, race, race_stride, temperature, accepted, token, step, prob, status, ws,
+                            ws_bytes, stream=None):
+    return _check(None, lib().asr_spec_accept_sampled(ctypes.byref(logits), ptr(draft), ptr(lens), ptr(u), addr(race),
+                                                      race_stride, temperature, ptr(accepted), ptr(token), ptr(step),
+                                                      ptr(prob), ptr(status), ptr(ws), ws_bytes, stream),
+                  "asr_spec_accept_sampled")

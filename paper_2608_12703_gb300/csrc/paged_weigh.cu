@@ -1,0 +1,267 @@
+// The attention weight that each cached slot received from a block's committed
+// rows, added to a running score per (sequence, K/V head, slot):
+//
+//   score'[j] = (j < kv_len ? score[j] : 0) + sum_r sum_h exp(scale q_rh k_j - lse_rh)
+//
+// over rows r < rows[b] that see slot j (j <= kv_len + r, or j < kv_len when
+// not causal) and the query heads h of the K/V head.  It runs after the
+// verification, when the number of committed rows is known, on the lse that
+// the attention left: one pass over K, no join.  Bound by the bytes of K and
+// of the scores; keys are read as in the attention (paged.cuh), each warp a
+// contiguous run of steps.  Products are exact in fp32 accumulators and all
+// sums are fp32 in a fixed order.
+#include "kernels.h"
+#include "paged.cuh"
+
+namespace asrspec {
+namespace {
+
+constexpr int PW_WARPS = 4;
+
+struct WeighArgs {
+  PagedView c;
+  PagedRows r;
+  const float *lse, *score;   // score may be null (zeros)
+  float* out;
+  long long lse_b, lse_r, score_b, score_h;   // elements
+  int* pos;                   // or null; strides as score's
+  const int* first_pos;
+  int cap;
+};
+
+struct WeighSeq {
+  int len, rows, keys, steps, tiles;
+};
+template <int KS, int TR>
+__device__ __forceinline__ WeighSeq weigh_seq(const WeighArgs& a, int len, int rows) {
+  WeighSeq s;
+  s.len = len;
+  s.rows = rows;
+  s.keys = len + (a.r.causal ? rows : 0);   // a sequence without rows keeps its scores
+  if (s.keys > a.cap) {
+    if (a.c.status) set_status(a.c.status, ST_CAPACITY);
+    s.len = s.rows = s.keys = 0;
+  }
+  s.steps = (s.keys + KS - 1) / KS;
+  s.tiles = (s.rows * a.r.group + TR - 1) / TR;
+  return s;
+}
+
+// One lane's slot: add the weight, or start the slot of a new row.
+__device__ __forceinline__ void put_score(const WeighArgs& a, const WeighSeq& s, int b, int kvh, int key, float w) {
+  if (key >= s.keys) return;
+  const long long at = b * a.score_b + kvh * a.score_h + key;
+  a.out[at] = (key < s.len && a.score ? a.score[at] : 0.f) + w;
+  if (a.pos && key >= s.len) a.pos[at] = a.first_pos[b] + key - s.len;
+}
+
+template <typename T, int D>
+__global__ void __launch_bounds__(PW_WARPS * 32, 4) weigh16_kernel(WeighArgs a, int max_workers) {
+  constexpr int KS = Cfg16<D>::KS, NG = KS / PG_GROUP, NC = D / 32, TR = 16;
+  const PagedView& c = a.c;
+  const PagedRows& r = a.r;
+  PlanMem mem;
+  const WorkPlan plan = work_plan(c, r, mem, max_workers, 1, [&](int len, int rows) {
+    return (long long)c.kv_heads * weigh_seq<KS, TR>(a, len, rows).steps;
+  });
+  const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+  const int worker = (threadIdx.x >> 5) * gridDim.x + blockIdx.x;
+  if (worker >= plan.workers) return;
+  long long u = work_start(plan, worker);
+  const long long u_end = work_start(plan, worker + 1);
+  const float sc = r.scale * LOG2E;
+
+  while (u < u_end) {
+    const int b = work_find(mem.pre, c.batch, u);
+    const WeighSeq s = weigh_seq<KS, TR>(a, mem.lens[b].x, mem.lens[b].y);
+    const int rem = (int)(u - mem.pre[b]), kvh = rem / s.steps, s0 = rem - kvh * s.steps;
+    const int n = (int)min((long long)(s.steps - s0), u_end - u);
+    u += n;
+    Keys16<T, D> ks{c, r, c.table + b * c.table_stride, kvh * c.head_stride, nullptr, nullptr, s.keys, s.keys, g, t};
+    int pid[NG];
+    uint4 kf[KS / 8][NC];
+    if (s.tiles) {
+#pragma unroll
+      for (int x = 0; x < NG; ++x) pid[x] = ks.id(s0, x);
+      ks.load_k(s0, pid, kf);
+      if (n > 1)
+#pragma unroll
+        for (int x = 0; x < NG; ++x) pid[x] = ks.id(s0 + 1, x);
+    }
+    uint32_t qa[NC * 2][4];
+    float ls[2];
+    int lim[2];
+    auto rows_of = [&](int tile) {
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int m = tile * TR + e * 8 + g, row = m / r.group, hq = kvh * r.group + m - row * r.group;
+        const bool in = row < s.rows;
+        lim[e] = !in ? 0 : r.causal ? s.len + row + 1 : s.keys;
+        const float x = in ? a.lse[b * a.lse_b + row * a.lse_r + hq] : -INFINITY;
+        ls[e] = x == -INFINITY ? INFINITY : x * LOG2E;   // an empty row weighs nothing
+#pragma unroll
+        for (int j = 0; j < NC; ++j) {
+          const uint4 v = in ? __ldg(reinterpret_cast<const uint4*>(r.q + b * r.q_b + row * r.q_r + hq * r.q_h +
+                                                                    j * 64 + t * 16))
+                             : make_uint4(0, 0, 0, 0);
+          qa[2 * j][e] = v.x;
+          qa[2 * j][2 + e] = v.y;
+          qa[2 * j + 1][e] = v.z;
+          qa[2 * j + 1][2 + e] = v.w;
+        }
+      }
+    };
+    if (s.tiles) rows_of(0);
+    for (int i = 0; i < n; ++i) {
+      const int step = s0 + i;
+      float w[KS / 8][2];
+#pragma unroll
+      for (int kt = 0; kt < KS / 8; ++kt) w[kt][0] = w[kt][1] = 0.f;
+      for (int tile = 0; tile < s.tiles; ++tile) {
+        if (s.tiles > 1) rows_of(tile);
+        float S[KS / 8][4];
+#pragma unroll
+        for (int kt = 0; kt < KS / 8; ++kt) {
+          S[kt][0] = S[kt][1] = S[kt][2] = S[kt][3] = 0.f;
+#pragma unroll
+          for (int j = 0; j < NC; ++j) {
+            Mma16<T>::mma(S[kt], qa[2 * j], kf[kt][j].x, kf[kt][j].y);
+            Mma16<T>::mma(S[kt], qa[2 * j + 1], kf[kt][j].z, kf[kt][j].w);
+          }
+        }
+#pragma unroll
+        for (int kt = 0; kt < KS / 8; ++kt)
+#pragma unroll
+          for (int x = 0; x < 4; ++x)
+            if (step * KS + kt * 8 + 2 * t + (x & 1) < lim[x >> 1]) w[kt][x & 1] += exp2f(fmaf(S[kt][x], sc, -ls[x >> 1]));
+      }
+      if (s.tiles && i + 1 < n) {
+        ks.load_k(step + 1, pid, kf);
+        if (i + 2 < n)
+#pragma unroll
+          for (int x = 0; x < NG; ++x) pid[x] = ks.id(step + 2, x);
+      }
+#pragma unroll
+      for (int kt = 0; kt < KS / 8; ++kt)
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          float v = w[kt][x];
+          v += __shfl_xor_sync(0xffffffffu, v, 4);
+          v += __shfl_xor_sync(0xffffffffu, v, 8);
+          v += __shfl_xor_sync(0xffffffffu, v, 16);
+          if (g == (kt * 2 + x) % 8) put_score(a, s, b, kvh, step * KS + kt * 8 + 2 * t + x, v);
+        }
+    }
+  }
+}
+
+// fp32 (no TF32): eight lanes share a key, four keys at a time; rows from L1.
+template <int D>
+__global__ void __launch_bounds__(PW_WARPS * 32) weigh32_kernel(WeighArgs a, int max_workers) {
+  constexpr int KS = 16, IT = KS / 4, NC = D / 32;
+  const PagedView& c = a.c;
+  const PagedRows& r = a.r;
+  PlanMem mem;
+  const WorkPlan plan = work_plan(c, r, mem, max_workers, 1, [&](int len, int rows) {
+    return (long long)c.kv_heads * weigh_seq<KS, 1>(a, len, rows).steps;
+  });
+  const int lane = threadIdx.x & 31, kg = lane >> 3, e = lane & 7;
+  const int worker = (threadIdx.x >> 5) * gridDim.x + blockIdx.x;
+  if (worker >= plan.workers) return;
+  long long u = work_start(plan, worker);
+  const long long u_end = work_start(plan, worker + 1);
+  const float sc = r.scale * LOG2E;
+
+  while (u < u_end) {
+    const int b = work_find(mem.pre, c.batch, u);
+    const WeighSeq s = weigh_seq<KS, 1>(a, mem.lens[b].x, mem.lens[b].y);
+    const int rem = (int)(u - mem.pre[b]), kvh = rem / s.steps, step = rem - kvh * s.steps;
+    ++u;
+    const int grp = step;
+    float4 kf[IT][NC];
+    if (s.tiles) {
+      const char* p = c.k + paged_offset(c, paged_id(c, c.table + b * c.table_stride, grp), grp) + kvh * c.head_stride +
+                      kg * c.slot_stride + e * 16;
+#pragma unroll
+      for (int k = 0; k < IT; ++k)
+#pragma unroll
+        for (int j = 0; j < NC; ++j)
+          kf[k][j] = step * KS + 4 * k + kg < s.keys
+                         ? *reinterpret_cast<const float4*>(p + (long long)(4 * k) * c.slot_stride + j * 128)
+                         : make_float4(0.f, 0.f, 0.f, 0.f);
+    }
+    float w[IT];
+#pragma unroll
+    for (int k = 0; k < IT; ++k) w[k] = 0.f;
+    for (int m = 0; m < s.tiles; ++m) {
+      const int row = m / r.group, hq = kvh * r.group + m - row * r.group;
+      const int lim = r.causal ? s.len + row + 1 : s.keys;
+      const float x = a.lse[b * a.lse_b + row * a.lse_r + hq], ls = x == -INFINITY ? INFINITY : x * LOG2E;
+      float d[IT];
+#pragma unroll
+      for (int k = 0; k < IT; ++k) d[k] = 0.f;
+#pragma unroll
+      for (int j = 0; j < NC; ++j) {
+        const float4 q = __ldg(reinterpret_cast<const float4*>(r.q + b * r.q_b + row * r.q_r + hq * r.q_h + (e + 8 * j) * 16));
+#pragma unroll
+        for (int k = 0; k < IT; ++k) d[k] += (q.x * kf[k][j].x + q.y * kf[k][j].y) + (q.z * kf[k][j].z + q.w * kf[k][j].w);
+      }
+#pragma unroll
+      for (int k = 0; k < IT; ++k) {
+        float v = d[k];
+        v += __shfl_xor_sync(0xffffffffu, v, 1);
+        v += __shfl_xor_sync(0xffffffffu, v, 2);
+        v += __shfl_xor_sync(0xffffffffu, v, 4);
+        if (step * KS + 4 * k + kg < lim) w[k] += exp2f(fmaf(v, sc, -ls));
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < IT; ++k)
+      if (e == k) put_score(a, s, b, kvh, step * KS + 4 * k + kg, w[k]);
+  }
+}
+
+}  // namespace
+}  // namespace asrspec
+
+using namespace asrspec;
+
+extern "C" int asr_spec_paged_weigh(const asr_paged_cache* c, const asr_paged_rows* r, const asr_paged_scores* sc,
+                                    const float* lse, int64_t lse_batch_stride, int64_t lse_row_stride, void* stream) {
+  WeighArgs a{};
+  if (int rc = paged_view(c, &a.c)) return rc;
+  if (int rc = paged_rows(c, r, &a.r)) return rc;
+  a.r.k_new = a.r.v_new = nullptr;   // the block's rows are in their pages
+  if (!sc || !sc->score_out || !lse || sc->slots < 1 || sc->head_stride < sc->slots || sc->batch_stride < 0)
+    return ASR_E_INVAL;
+  if ((sc->pos != nullptr) != (sc->first_pos != nullptr)) return ASR_E_INVAL;
+  if (((uintptr_t)sc->score | (uintptr_t)sc->score_out | (uintptr_t)sc->pos | (uintptr_t)sc->first_pos | (uintptr_t)lse) % 4)
+    return ASR_E_INVAL;
+  if ((long long)c->kv_heads * (a.c.max_slots / PG_GROUP) > 0x7fffffffll) return ASR_E_CAPACITY;
+  a.lse = lse;
+  a.lse_b = lse_batch_stride;
+  a.lse_r = lse_row_stride;
+  a.score = sc->score;
+  a.out = sc->score_out;
+  a.score_b = sc->batch_stride;
+  a.score_h = sc->head_stride;
+  a.pos = sc->pos;
+  a.first_pos = sc->first_pos;
+  a.cap = sc->slots;
+  const int grid = paged_sm_count() * 4, workers = grid * PW_WARPS;
+  const size_t smem = plan_bytes(c->batch);
+  cudaStream_t st = static_cast<cudaStream_t>(stream);
+  const dim3 g(grid), b(PW_WARPS * 32);
+  cudaError_t e;
+  const bool wide = c->head_dim == 128;
+  if (c->dtype == 0)
+    e = wide ? launch_ex(weigh32_kernel<128>, g, b, smem, st, false, 1, a, workers)
+             : launch_ex(weigh32_kernel<64>, g, b, smem, st, false, 1, a, workers);
+  else if (c->dtype == 1)
+    e = wide ? launch_ex(weigh16_kernel<__nv_bfloat16, 128>, g, b, smem, st, false, 1, a, workers)
+             : launch_ex(weigh16_kernel<__nv_bfloat16, 64>, g, b, smem, st, false, 1, a, workers);
+  else
+    e = wide ? launch_ex(weigh16_kernel<__half, 128>, g, b, smem, st, false, 1, a, workers)
+             : launch_ex(weigh16_kernel<__half, 64>, g, b, smem, st, false, 1, a, workers);
+  return e == cudaSuccess ? ASR_OK : ASR_E_CUDA;
+}
