@@ -421,7 +421,8 @@ int asr_spec_gemm_noalloc(const void* A, const void* B, float* C, int32_t M, int
  *   page_table[b * table_stride + s / page_size] * page_stride + h * head_stride
  *   + (s % page_size) * slot_stride
  * of k_pages and of v_pages, head_dim consecutive elements.  Bases and strides
- * are multiples of 16 bytes.  A page that is written belongs to one sequence. */
+ * are multiples of 16 bytes (slot_stride at most 64 MB).  A page that is written
+ * belongs to one sequence. */
 typedef struct {
   void *k_pages, *v_pages;
   int64_t page_stride, head_stride, slot_stride;   /* elements */

@@ -30,7 +30,8 @@ int paged_view(const asr_paged_cache* c, PagedView* v) {
   const long long es = c->dtype == 0 ? 4 : 2;
   if (((uintptr_t)c->k_pages | (uintptr_t)c->v_pages) % 16) return ASR_E_INVAL;
   if (c->page_stride < 0 || c->head_stride < 0 || c->slot_stride < 0 || (c->page_stride * es) % 16 ||
-      (c->head_stride * es) % 16 || (c->slot_stride * es) % 16 || (c->page_size > 1 && c->slot_stride < c->head_dim))
+      (c->head_stride * es) % 16 || (c->slot_stride * es) % 16 || c->slot_stride < c->head_dim ||
+      c->slot_stride * es > (1 << 26))   // 16 slots' offsets fit 32 bits
     return ASR_E_INVAL;
   v->k = static_cast<char*>(c->k_pages);
   v->v = static_cast<char*>(c->v_pages);

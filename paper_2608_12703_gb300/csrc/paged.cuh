@@ -83,6 +83,13 @@ __device__ __forceinline__ long long paged_offset(const PagedView& c, int pid, i
   return (long long)pid * c.page_stride + (long long)(in_page * PG_GROUP) * c.slot_stride;
 }
 
+// 2^x by the hardware's approximation (2 ulp; 0 below 2^-126).
+__device__ __forceinline__ float ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
 __device__ __forceinline__ uint4 ldg_stream(const char* p) {   // read once: no L1 line
   uint4 v;
   asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];"
@@ -221,64 +228,69 @@ struct Keys16 {
   const PagedRows& r;
   const int* table_row;
   long long head_off;
-  const char *kn, *vn;   // this sequence's and head's new rows, or null
+  const char *kn, *vn;   // this sequence's and head's new rows
   int len, keys, g, t;
+  bool fresh;            // slots from len on are read from them
 
   __device__ __forceinline__ int id(int step, int u) const {   // page of group u of a step, fetched ahead
     const int grp = step * NG + u;
     return grp * PG_GROUP < keys ? paged_id(c, table_row, grp) : 0;
   }
   __device__ __forceinline__ bool full(int step) const { return (step + 1) * KS <= len; }
+  __device__ __forceinline__ void offsets(int step, const int* pid, long long* off) const {
+#pragma unroll
+    for (int u = 0; u < NG; ++u) off[u] = paged_offset(c, pid[u], step * NG + u) + head_off;
+  }
 
   // K: kf[key tile][16-byte chunk], lane's key 8 w + g of a group
-  __device__ __forceinline__ void load_k(int step, const int* pid, uint4 (&kf)[KS / 8][NC]) const {
+  __device__ __forceinline__ void load_k(int step, const long long* off, uint4 (&kf)[KS / 8][NC]) const {
+    const int lane_off = g * (int)c.slot_stride + t * 16, row8 = 8 * (int)c.slot_stride;
     if (full(step)) {
 #pragma unroll
       for (int u = 0; u < NG; ++u) {
-        const char* p = c.k + paged_offset(c, pid[u], step * NG + u) + head_off + g * c.slot_stride + t * 16;
+        const char* p = c.k + off[u] + lane_off;
 #pragma unroll
         for (int w = 0; w < 2; ++w)
 #pragma unroll
-          for (int j = 0; j < NC; ++j) kf[u * 2 + w][j] = ldg_stream(p + w * 8 * c.slot_stride + j * 64);
+          for (int j = 0; j < NC; ++j) kf[u * 2 + w][j] = ldg_stream(p + w * row8 + j * 64);
       }
     } else {
 #pragma unroll
       for (int u = 0; u < NG; ++u)
 #pragma unroll
-        for (int w = 0; w < 2; ++w) edge<NC, 64>(c.k, kn, step, u, w * 8 + g, pid[u], t * 16, kf[u * 2 + w]);
+        for (int w = 0; w < 2; ++w)
+          edge<NC, 64>(c.k + off[u] + lane_off + w * row8, kn + t * 16, step * KS + u * PG_GROUP + w * 8 + g, kf[u * 2 + w]);
     }
   }
   // V: vf[group][which of the lane's four keys 2t, 2t+1, 2t+8, 2t+9][64-wide half]
-  __device__ __forceinline__ void load_v(int step, const int* pid, uint4 (&vf)[NG][4][NV]) const {
-    if (full(step)) {
+  __device__ __forceinline__ void load_v(int step, const long long* off, uint4 (&vf)[NG][4][NV]) const {
+    const int slot = (int)c.slot_stride, lane_off = 2 * t * slot + g * 16;
 #pragma unroll
-      for (int u = 0; u < NG; ++u) {
-        const char* p = c.v + paged_offset(c, pid[u], step * NG + u) + head_off + 2 * t * c.slot_stride + g * 16;
+    for (int u = 0; u < NG; ++u) {
+      const char* p = c.v + off[u] + lane_off;
+      if (full(step)) {
 #pragma unroll
         for (int w = 0; w < 4; ++w)
 #pragma unroll
-          for (int j = 0; j < NV; ++j)
-            vf[u][w][j] = ldg_stream(p + ((w & 1) + (w >> 1) * 8) * c.slot_stride + j * 128);
+          for (int j = 0; j < NV; ++j) vf[u][w][j] = ldg_stream(p + ((w & 1) + (w >> 1) * 8) * slot + j * 128);
+      } else {
+#pragma unroll
+        for (int w = 0; w < 4; ++w)
+          edge<NV, 128>(p + ((w & 1) + (w >> 1) * 8) * slot, vn + g * 16,
+                        step * KS + u * PG_GROUP + 2 * t + (w & 1) + (w >> 1) * 8, vf[u][w]);
       }
-    } else {
-#pragma unroll
-      for (int u = 0; u < NG; ++u)
-#pragma unroll
-        for (int w = 0; w < 4; ++w)
-          edge<NV, 128>(c.v, vn, step, u, 2 * t + (w & 1) + (w >> 1) * 8, pid[u], g * 16, vf[u][w]);
     }
   }
   // One key of an edge step: from its page, or from the block's rows; zero past the end.
   template <int N, int STRIDE>
-  __device__ __forceinline__ void edge(const char* pages, const char* fresh_rows, int step, int u, int in, int pid,
-                                       int byte, uint4 (&f)[N]) const {
-    const int key = step * KS + u * PG_GROUP + in;
-    const char* src = fresh_rows != nullptr && key >= len
-                          ? fresh_rows + (long long)(key - len) * r.n_r + byte
-                          : pages + paged_offset(c, pid, step * NG + u) + head_off + in * c.slot_stride + byte;
+  __device__ __forceinline__ void edge(const char* page, const char* fresh_rows, int key, uint4 (&f)[N]) const {
+    const char* src = fresh && key >= len ? fresh_rows + (long long)(key - len) * r.n_r : page;
 #pragma unroll
-    for (int j = 0; j < N; ++j)
-      f[j] = key < keys ? *reinterpret_cast<const uint4*>(src + j * STRIDE) : make_uint4(0, 0, 0, 0);
+    for (int j = 0; j < N; ++j) f[j] = make_uint4(0, 0, 0, 0);
+    if (key < keys) {
+#pragma unroll
+      for (int j = 0; j < N; ++j) f[j] = *reinterpret_cast<const uint4*>(src + j * STRIDE);
+    }
   }
   // Write the new rows of an edge step to their pages, from the fragments that
   // the step is about to use.  A bad page id is reported by id(); nothing goes there.

@@ -58,6 +58,22 @@ __device__ __forceinline__ uint32_t nonfinite_halves(uint32_t x) {
   return ((x & E) == E ? 0xffffu : 0u) | (((x >> 16) & E) == E ? 0xffff0000u : 0u);
 }
 
+template <typename T> struct Pair;
+template <> struct Pair<__nv_bfloat16> {
+  using type = __nv_bfloat162;
+  static __device__ __forceinline__ type zero() { return __float2bfloat162_rn(0.f); }
+  static __device__ __forceinline__ type add_zero(uint32_t x, type s) {
+    return __hfma2(*reinterpret_cast<const type*>(&x), zero(), s);
+  }
+};
+template <> struct Pair<__half> {
+  using type = __half2;
+  static __device__ __forceinline__ type zero() { return __float2half2_rn(0.f); }
+  static __device__ __forceinline__ type add_zero(uint32_t x, type s) {
+    return __hfma2(*reinterpret_cast<const type*>(&x), zero(), s);
+  }
+};
+
 __device__ __forceinline__ uint32_t reg_of(const uint4& v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
 
 // A key of an edge step may be hidden from some of the tile's rows, and a hidden
@@ -68,12 +84,18 @@ template <typename T, int D, int MT>
 __device__ __forceinline__ void guard_values(const Keys16<T, D>& ks, int step, const int (&lim)[MT][2],
                                              uint4 (&vf)[Keys16<T, D>::NG][4][D / 64], float (&O)[MT][D / 8][4]) {
   using K = Keys16<T, D>;
-  uint32_t bad = 0;
-  auto take_out = [&](uint32_t& x) {
-    const uint32_t n = nonfinite_halves<T>(x);
-    bad |= n;
-    x &= ~n;
-  };
+  // x * 0 is NaN for an infinity or NaN, and stays in the sum
+  typename Pair<T>::type sum = Pair<T>::zero();
+#pragma unroll
+  for (int u = 0; u < K::NG; ++u)
+#pragma unroll
+    for (int w = 0; w < 4; ++w)
+#pragma unroll
+      for (int j = 0; j < K::NV; ++j) {
+        const uint4& v = vf[u][w][j];
+        sum = Pair<T>::add_zero(v.w, Pair<T>::add_zero(v.z, Pair<T>::add_zero(v.y, Pair<T>::add_zero(v.x, sum))));
+      }
+  if (!__any_sync(0xffffffffu, nonfinite_halves<T>(*reinterpret_cast<uint32_t*>(&sum)) != 0)) return;
 #pragma unroll
   for (int u = 0; u < K::NG; ++u)
 #pragma unroll
@@ -81,12 +103,12 @@ __device__ __forceinline__ void guard_values(const Keys16<T, D>& ks, int step, c
 #pragma unroll
       for (int j = 0; j < K::NV; ++j) {
         uint4& v = vf[u][w][j];
-        take_out(v.x), take_out(v.y), take_out(v.z), take_out(v.w);
+        v.x &= ~nonfinite_halves<T>(v.x), v.y &= ~nonfinite_halves<T>(v.y);
+        v.z &= ~nonfinite_halves<T>(v.z), v.w &= ~nonfinite_halves<T>(v.w);
       }
-  if (!__any_sync(0xffffffffu, bad != 0)) return;
   for (int key = step * K::KS; key < min((step + 1) * K::KS, ks.keys); ++key) {
     const int grp = key / PG_GROUP;
-    const char* row = ks.vn != nullptr && key >= ks.len
+    const char* row = ks.fresh && key >= ks.len
                           ? ks.vn + (long long)(key - ks.len) * ks.r.n_r
                           : ks.c.v + paged_offset(ks.c, paged_id(ks.c, ks.table_row, grp), grp) + ks.head_off +
                                 (key % PG_GROUP) * ks.c.slot_stride;
@@ -131,23 +153,15 @@ __global__ void __launch_bounds__(PA_WARPS * 32, MINB) attend16_kernel(AttendArg
     const int kvh = item / s.tiles, tile = item - kvh * s.tiles;
     u += n;
 
-    Keys16<T, D> ks{c,
-                    r,
-                    c.table + b * c.table_stride,
-                    kvh * c.head_stride,
-                    r.k_new ? r.k_new + b * r.n_b + kvh * r.n_h : nullptr,
-                    r.k_new ? r.v_new + b * r.n_b + kvh * r.n_h : nullptr,
-                    s.len,
-                    s.keys,
-                    g,
-                    t};
-    const bool append = r.k_new != nullptr && tile == 0;
+    const bool fresh = r.k_new != nullptr, append = fresh && tile == 0;
+    const long long new_off = b * r.n_b + kvh * r.n_h;
+    Keys16<T, D> ks{c, r, c.table + b * c.table_stride, kvh * c.head_stride, r.k_new + new_off, r.v_new + new_off,
+                    s.len, s.keys, g, t, fresh};
     int pid[NG];
+    long long off[NG];
     uint4 kf[KS / 8][NC], vf[NG][4][NV];
 #pragma unroll
     for (int x = 0; x < NG; ++x) pid[x] = ks.id(s0, x);
-    ks.load_k(s0, pid, kf);
-    ks.load_v(s0, pid, vf);
 
     uint32_t qa[MT][NC * 2][4];
     int lim[MT][2];   // keys the fragment's rows see
@@ -176,101 +190,102 @@ __global__ void __launch_bounds__(PA_WARPS * 32, MINB) attend16_kernel(AttendArg
 #pragma unroll
       for (int d = 0; d < D / 8; ++d) O[mt][d][0] = O[mt][d][1] = O[mt][d][2] = O[mt][d][3] = 0.f;
     }
-    if (n > 1)
-#pragma unroll
-      for (int x = 0; x < NG; ++x) pid[x] = ks.id(s0 + 1, x);
 
-    for (int i = 0; i < n; ++i) {
+    // Step i's products and step i + 1's loads; i = -1 only loads.
+#pragma unroll 1
+    for (int i = -1; i < n; ++i) {
       const int step = s0 + i;
-      const bool full = ks.full(step);
-      if (!full && append) ks.append_k(step, kf);
+      const bool full = ks.full(step), more = i + 1 < n;
       float S[MT][KS / 8][4];
+      if (i >= 0) {
+        if (!full && append) ks.append_k(step, kf);
 #pragma unroll
-      for (int mt = 0; mt < MT; ++mt)
+        for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-        for (int kt = 0; kt < KS / 8; ++kt) {
-          S[mt][kt][0] = S[mt][kt][1] = S[mt][kt][2] = S[mt][kt][3] = 0.f;
+          for (int kt = 0; kt < KS / 8; ++kt) {
+            S[mt][kt][0] = S[mt][kt][1] = S[mt][kt][2] = S[mt][kt][3] = 0.f;
 #pragma unroll
-          for (int j = 0; j < NC; ++j) {
-            Mma16<T>::mma(S[mt][kt], qa[mt][2 * j], kf[kt][j].x, kf[kt][j].y);
-            Mma16<T>::mma(S[mt][kt], qa[mt][2 * j + 1], kf[kt][j].z, kf[kt][j].w);
+            for (int j = 0; j < NC; ++j) {
+              Mma16<T>::mma(S[mt][kt], qa[mt][2 * j], kf[kt][j].x, kf[kt][j].y);
+              Mma16<T>::mma(S[mt][kt], qa[mt][2 * j + 1], kf[kt][j].z, kf[kt][j].w);
+            }
           }
-        }
-      int pid_v[NG];
-#pragma unroll
-      for (int x = 0; x < NG; ++x) pid_v[x] = pid[x];
-      if (i + 1 < n) {
-        ks.load_k(step + 1, pid, kf);
+      }
+      if (more) {
+        ks.offsets(step + 1, pid, off);
+        ks.load_k(step + 1, off, kf);
         if (i + 2 < n)
 #pragma unroll
           for (int x = 0; x < NG; ++x) pid[x] = ks.id(step + 2, x);
       }
-      if (!full) {
+      if (i >= 0) {
+        if (!full) {
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
+          for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-          for (int kt = 0; kt < KS / 8; ++kt)
+            for (int kt = 0; kt < KS / 8; ++kt)
 #pragma unroll
-            for (int x = 0; x < 4; ++x)
-              if (step * KS + kt * 8 + 2 * t + (x & 1) >= min(lim[mt][x >> 1], s.keys)) S[mt][kt][x] = -INFINITY;
-      }
-      uint32_t pf[MT][KS / 8][2];
-#pragma unroll
-      for (int mt = 0; mt < MT; ++mt) {
-        float mx[2];
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          float x = fmaxf(S[mt][0][2 * e], S[mt][0][2 * e + 1]);
-#pragma unroll
-          for (int kt = 1; kt < KS / 8; ++kt) x = fmaxf(x, fmaxf(S[mt][kt][2 * e], S[mt][kt][2 * e + 1]));
-          x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 1));
-          x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 2));
-          mx[e] = fmaxf(m_run[mt][e], x * sc);
+              for (int x = 0; x < 4; ++x)
+                if (step * KS + kt * 8 + 2 * t + (x & 1) >= min(lim[mt][x >> 1], s.keys)) S[mt][kt][x] = -INFINITY;
         }
-        if (__any_sync(0xffffffffu, mx[0] > m_run[mt][0] || mx[1] > m_run[mt][1])) {
+        uint32_t pf[MT][KS / 8][2];
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
+          float mx[2];
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
-            const float f = mx[e] == -INFINITY ? 1.f : exp2f(m_run[mt][e] - mx[e]);
-            m_run[mt][e] = mx[e];
-            l_run[mt][e] *= f;
+            float x = fmaxf(S[mt][0][2 * e], S[mt][0][2 * e + 1]);
 #pragma unroll
-            for (int d = 0; d < D / 8; ++d) {
-              O[mt][d][2 * e] *= f;
-              O[mt][d][2 * e + 1] *= f;
+            for (int kt = 1; kt < KS / 8; ++kt) x = fmaxf(x, fmaxf(S[mt][kt][2 * e], S[mt][kt][2 * e + 1]));
+            x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 1));
+            x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 2));
+            mx[e] = fmaxf(m_run[mt][e], x * sc);
+          }
+          if (__any_sync(0xffffffffu, mx[0] > m_run[mt][0] || mx[1] > m_run[mt][1])) {
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              const float f = mx[e] == -INFINITY ? 1.f : ex2(m_run[mt][e] - mx[e]);
+              m_run[mt][e] = mx[e];
+              l_run[mt][e] *= f;
+#pragma unroll
+              for (int d = 0; d < D / 8; ++d) {
+                O[mt][d][2 * e] *= f;
+                O[mt][d][2 * e + 1] *= f;
+              }
+            }
+          }
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const float m = m_run[mt][e] == -INFINITY ? 0.f : m_run[mt][e];
+#pragma unroll
+            for (int kt = 0; kt < KS / 8; ++kt) {
+              const float p0 = ex2(fmaf(S[mt][kt][2 * e], sc, -m)), p1 = ex2(fmaf(S[mt][kt][2 * e + 1], sc, -m));
+              l_run[mt][e] += p0 + p1;
+              pf[mt][kt][e] = Mma16<T>::pack(p0, p1);
             }
           }
         }
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          const float m = m_run[mt][e] == -INFINITY ? 0.f : m_run[mt][e];
-#pragma unroll
-          for (int kt = 0; kt < KS / 8; ++kt) {
-            const float p0 = exp2f(fmaf(S[mt][kt][2 * e], sc, -m)), p1 = exp2f(fmaf(S[mt][kt][2 * e + 1], sc, -m));
-            l_run[mt][e] += p0 + p1;
-            pf[mt][kt][e] = Mma16<T>::pack(p0, p1);
-          }
+        if (!full) {
+          if (append) ks.append_v(step, vf);
+          guard_values<T, D, MT>(ks, step, lim, vf, O);
         }
-      }
-      if (!full) {
-        if (append) ks.append_v(step, vf);
-        guard_values<T, D, MT>(ks, step, lim, vf, O);
-      }
 #pragma unroll
-      for (int x = 0; x < NG; ++x)
+        for (int x = 0; x < NG; ++x)
 #pragma unroll
-        for (int j = 0; j < NV; ++j)
+          for (int j = 0; j < NV; ++j)
 #pragma unroll
-          for (int d = 0; d < 8; ++d) {   // n-tile d of half j: output column 64 j + 8 n + d
-            const uint32_t sel = d & 1 ? 0x7632 : 0x5410;
-            const uint32_t b0 = __byte_perm(reg_of(vf[x][0][j], d >> 1), reg_of(vf[x][1][j], d >> 1), sel);
-            const uint32_t b1 = __byte_perm(reg_of(vf[x][2][j], d >> 1), reg_of(vf[x][3][j], d >> 1), sel);
+            for (int d = 0; d < 8; ++d) {   // n-tile d of half j: output column 64 j + 8 n + d
+              const uint32_t sel = d & 1 ? 0x7632 : 0x5410;
+              const uint32_t b0 = __byte_perm(reg_of(vf[x][0][j], d >> 1), reg_of(vf[x][1][j], d >> 1), sel);
+              const uint32_t b1 = __byte_perm(reg_of(vf[x][2][j], d >> 1), reg_of(vf[x][3][j], d >> 1), sel);
 #pragma unroll
-            for (int mt = 0; mt < MT; ++mt) {
-              const uint32_t pa[4] = {pf[mt][2 * x][0], pf[mt][2 * x][1], pf[mt][2 * x + 1][0], pf[mt][2 * x + 1][1]};
-              Mma16<T>::mma(O[mt][j * 8 + d], pa, b0, b1);
+              for (int mt = 0; mt < MT; ++mt) {
+                const uint32_t pa[4] = {pf[mt][2 * x][0], pf[mt][2 * x][1], pf[mt][2 * x + 1][0], pf[mt][2 * x + 1][1]};
+                Mma16<T>::mma(O[mt][j * 8 + d], pa, b0, b1);
+              }
             }
-          }
-      if (i + 1 < n) ks.load_v(step + 1, pid_v, vf);
+      }
+      if (more) ks.load_v(step + 1, off, vf);
     }
 
     // the item's result: of row g (+ 8 e) a lane holds columns 64 j + 16 t .. + 15
@@ -424,14 +439,14 @@ __global__ void __launch_bounds__(PA_WARPS * 32) attend32_kernel(AttendArgs a) {
           S[k] = key0 + 4 * k + kg < min(lim[x], s.keys) ? d : -INFINITY;
           mx = fmaxf(mx, S[k]);
         }
-        const float m = mx == -INFINITY ? 0.f : mx, f = exp2f(m_run[x] - m);
+        const float m = mx == -INFINITY ? 0.f : mx, f = ex2(m_run[x] - m);
         m_run[x] = mx;
         l_run[x] *= f;
 #pragma unroll
         for (int j = 0; j < NC * 4; ++j) O[x][j] *= f;
 #pragma unroll
         for (int k = 0; k < IT; ++k) {
-          const float p = exp2f(S[k] - m);
+          const float p = ex2(S[k] - m);
           l_run[x] += p;
           if (key0 + 4 * k + kg >= lim[x]) continue;   // hidden: an infinity or NaN there must not reach the row
 #pragma unroll
@@ -450,7 +465,7 @@ __global__ void __launch_bounds__(PA_WARPS * 32) attend32_kernel(AttendArgs a) {
     for (int x = 0; x < TR; ++x) {
       float mx = fmaxf(m_run[x], __shfl_xor_sync(0xffffffffu, m_run[x], 8));
       mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
-      const float f = mx == -INFINITY ? 0.f : exp2f(m_run[x] - mx);
+      const float f = mx == -INFINITY ? 0.f : ex2(m_run[x] - mx);
       float l = l_run[x] * f;
       l += __shfl_xor_sync(0xffffffffu, l, 8);
       l += __shfl_xor_sync(0xffffffffu, l, 16);
@@ -536,7 +551,7 @@ __global__ void __launch_bounds__(PJ_WARPS * 32) join_kernel(AttendArgs a) {
       const float* part = a.ws + (size_t)(2 * w + (w == wf ? 1 : 0)) * (TR * (D + 2));
       const float pm = part[in], pl = part[TR + in];
       const float4 po = *reinterpret_cast<const float4*>(part + 2 * TR + in * D + col);
-      const float mx = fmaxf(m, pm), z = mx == -INFINITY ? 0.f : mx, f0 = exp2f(m - z), f1 = exp2f(pm - z);
+      const float mx = fmaxf(m, pm), z = mx == -INFINITY ? 0.f : mx, f0 = ex2(m - z), f1 = ex2(pm - z);
       m = mx;
       l = l * f0 + pl * f1;
       o.x = o.x * f0 + po.x * f1;
@@ -548,7 +563,7 @@ __global__ void __launch_bounds__(PJ_WARPS * 32) join_kernel(AttendArgs a) {
       const float pm = __shfl_xor_sync(0xffffffffu, m, 16), pl = __shfl_xor_sync(0xffffffffu, l, 16);
       const float px = __shfl_xor_sync(0xffffffffu, o.x, 16), py = __shfl_xor_sync(0xffffffffu, o.y, 16);
       const float pz = __shfl_xor_sync(0xffffffffu, o.z, 16), pw = __shfl_xor_sync(0xffffffffu, o.w, 16);
-      const float mx = fmaxf(m, pm), z = mx == -INFINITY ? 0.f : mx, f0 = exp2f(m - z), f1 = exp2f(pm - z);
+      const float mx = fmaxf(m, pm), z = mx == -INFINITY ? 0.f : mx, f0 = ex2(m - z), f1 = ex2(pm - z);
       m = mx;
       l = l * f0 + pl * f1;
       o = make_float4(o.x * f0 + px * f1, o.y * f0 + py * f1, o.z * f0 + pz * f1, o.w * f0 + pw * f1);
@@ -571,7 +586,7 @@ __global__ void __launch_bounds__(PJ_WARPS * 32) join_kernel(AttendArgs a) {
     o = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
     for (int w = 0; w < WPT; ++w) {
-      const float f = m == -INFINITY ? 0.f : exp2f(s_m[warp + w] - m);
+      const float f = m == -INFINITY ? 0.f : ex2(s_m[warp + w] - m);
       const float4 po = *reinterpret_cast<const float4*>(&s_o[warp + w][col]);
       l += s_l[warp + w] * f;
       o = make_float4(o.x + po.x * f, o.y + po.y * f, o.z + po.z * f, o.w + po.w * f);

@@ -77,13 +77,15 @@ __global__ void __launch_bounds__(PW_WARPS * 32, 4) weigh16_kernel(WeighArgs a, 
     const int rem = (int)(u - mem.pre[b]), kvh = rem / s.steps, s0 = rem - kvh * s.steps;
     const int n = (int)min((long long)(s.steps - s0), u_end - u);
     u += n;
-    Keys16<T, D> ks{c, r, c.table + b * c.table_stride, kvh * c.head_stride, nullptr, nullptr, s.keys, s.keys, g, t};
+    Keys16<T, D> ks{c, r, c.table + b * c.table_stride, kvh * c.head_stride, nullptr, nullptr, s.keys, s.keys, g, t, false};
     int pid[NG];
+    long long off[NG];
     uint4 kf[KS / 8][NC];
     if (s.tiles) {
 #pragma unroll
       for (int x = 0; x < NG; ++x) pid[x] = ks.id(s0, x);
-      ks.load_k(s0, pid, kf);
+      ks.offsets(s0, pid, off);
+      ks.load_k(s0, off, kf);
       if (n > 1)
 #pragma unroll
         for (int x = 0; x < NG; ++x) pid[x] = ks.id(s0 + 1, x);
@@ -133,10 +135,11 @@ __global__ void __launch_bounds__(PW_WARPS * 32, 4) weigh16_kernel(WeighArgs a, 
         for (int kt = 0; kt < KS / 8; ++kt)
 #pragma unroll
           for (int x = 0; x < 4; ++x)
-            if (step * KS + kt * 8 + 2 * t + (x & 1) < lim[x >> 1]) w[kt][x & 1] += exp2f(fmaf(S[kt][x], sc, -ls[x >> 1]));
+            if (step * KS + kt * 8 + 2 * t + (x & 1) < lim[x >> 1]) w[kt][x & 1] += ex2(fmaf(S[kt][x], sc, -ls[x >> 1]));
       }
       if (s.tiles && i + 1 < n) {
-        ks.load_k(step + 1, pid, kf);
+        ks.offsets(step + 1, pid, off);
+        ks.load_k(step + 1, off, kf);
         if (i + 2 < n)
 #pragma unroll
           for (int x = 0; x < NG; ++x) pid[x] = ks.id(step + 2, x);
@@ -212,7 +215,7 @@ __global__ void __launch_bounds__(PW_WARPS * 32) weigh32_kernel(WeighArgs a, int
         v += __shfl_xor_sync(0xffffffffu, v, 1);
         v += __shfl_xor_sync(0xffffffffu, v, 2);
         v += __shfl_xor_sync(0xffffffffu, v, 4);
-        if (step * KS + 4 * k + kg < lim) w[k] += exp2f(fmaf(v, sc, -ls));
+        if (step * KS + 4 * k + kg < lim) w[k] += ex2(fmaf(v, sc, -ls));
       }
     }
 #pragma unroll

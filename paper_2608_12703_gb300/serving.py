@@ -4,11 +4,17 @@ and acceptance of drafted tokens from given random numbers.
 
 ``PagedCache`` wraps the caller's pool of pages and page table; its methods and
 ``accept_sampled`` are one C-ABI call each (include/asrspec.h), on the current
-CUDA stream of the tensors' device, without a synchronisation.  Workspaces and
-outputs come from torch's allocator on that stream.  Arguments are checked
-here by shape, type and device; what only the device knows (lengths, page ids,
-token ids) is checked by the kernels, which set the status word read by
-``PagedCache.status``.
+CUDA stream of the tensors' device, without a synchronisation.  Outputs come
+from torch's allocator; a cache keeps one workspace per stream.  Arguments are
+checked here by shape, type and device; what only the device knows (lengths,
+page ids, token ids) is checked by the kernels, which set the status word read
+by ``PagedCache.status``.
+
+A small call's kernels take less time than the checks of its arguments, so a
+call whose tensors have the layouts (shape, strides, type, device) of an
+earlier one goes by that call's checks: layouts are what the checks look at,
+and addresses, the only other thing, are checked by the library.  A captured
+graph needs the cache object that it was captured with.
 """
 from __future__ import annotations
 
@@ -21,11 +27,31 @@ import torch
 from . import asrspec as A
 
 _DTYPE = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+_MAX_LAYOUTS = 1024      # layouts remembered by one operator before it starts anew
+_raw_stream = torch._C._cuda_getCurrentRawStream
+_current_device = torch._C._cuda_getDevice
+_capturing = torch._C._cuda_isCurrentStreamCapturing
 
 
 def _need(ok: bool, what: str):
     if not ok:
         raise A.AsrSpecError("ASR_E_INVAL " + what)
+
+
+def _layout(x):
+    if x is None:
+        return None
+    try:
+        return x.shape, x.stride(), x.dtype, x.get_device()
+    except AttributeError:
+        raise A.AsrSpecError(f"ASR_E_INVAL a tensor is required, not {type(x).__name__}") from None
+
+
+def _remember(layouts: dict, key, value):
+    if len(layouts) >= _MAX_LAYOUTS:
+        layouts.clear()
+    layouts[key] = value
+    return value
 
 
 def _tensor(x, name, dtype, shape, device):
@@ -34,8 +60,8 @@ def _tensor(x, name, dtype, shape, device):
     _need(tuple(x.shape) == tuple(shape), f"{name}: shape {tuple(shape)} is required, not {tuple(x.shape)}")
 
 
-def _ints(x, name, shape, device):
-    _tensor(x, name, torch.int32, shape, device)
+def _whole(x, name, dtype, shape, device):
+    _tensor(x, name, dtype, shape, device)
     _need(x.is_contiguous(), f"{name}: must be contiguous")
 
 
@@ -70,12 +96,15 @@ class PagedCache:
         self.batch, self.max_pages = page_table.shape
         self.kv_heads, self.page_size, self.head_dim = kv_heads, page_size, dim
         self.max_slots = self.max_pages * page_size
+        self._index = dev.index
         self._status = torch.zeros(1, dtype=torch.int32, device=dev)
         self._c = A.AsrPagedCache(
             k_pages.data_ptr(), v_pages.data_ptr(), k_pages.stride(0), k_pages.stride(1), k_pages.stride(2),
             page_table.data_ptr(), page_table.stride(0), n_pages, page_size, self.max_pages, kv_heads, dim, self.batch,
             _DTYPE[self.dtype], self._status.data_ptr())
         self._ref = ctypes.byref(self._c)
+        self._lib = A.lib()
+        self._attend_layouts, self._weigh_layouts, self._evict_layouts = {}, {}, {}
         self._ws = {}
 
     def status(self) -> int:
@@ -86,6 +115,15 @@ class PagedCache:
             self._status.zero_()
         return s
 
+    def _workspace(self, stream: int, n: int):
+        """``n`` bytes that only calls on this stream use; a capture gets bytes of its graph's own."""
+        if _capturing():
+            return torch.empty(n, dtype=torch.uint8, device=self.device)
+        ws = self._ws.get(stream)
+        if ws is None or ws.numel() < n:
+            ws = self._ws[stream] = torch.empty(n, dtype=torch.uint8, device=self.device)
+        return ws
+
     def _rows(self, q, kv_len, rows, k_new, v_new, causal, scale):
         B, K, D = self.batch, self.kv_heads, self.head_dim
         _need(isinstance(q, torch.Tensor) and q.dim() == 4 and q.shape[0] == B and q.shape[3] == D,
@@ -94,9 +132,9 @@ class PagedCache:
         _tensor(q, "q", self.dtype, (B, R, H, D), self.device)
         _need(R >= 1 and H >= K and H % K == 0, f"q: heads must be a multiple of the cache's {K}")
         _need(q.stride(3) == 1, "q: the last axis must be contiguous")
-        _ints(kv_len, "kv_len", (B,), self.device)
+        _whole(kv_len, "kv_len", torch.int32, (B,), self.device)
         if rows is not None:
-            _ints(rows, "rows", (B,), self.device)
+            _whole(rows, "rows", torch.int32, (B,), self.device)
         ns = (0, 0, 0)
         _need((k_new is None) == (v_new is None), "k_new and v_new go together")
         if k_new is not None:
@@ -110,30 +148,47 @@ class PagedCache:
         return A.AsrPagedRows(q.data_ptr(), s[0], s[1], s[2], A.addr(k_new), A.addr(v_new), *ns, kv_len.data_ptr(),
                               A.addr(rows), R, H, int(bool(causal)), 1.0 / math.sqrt(D) if scale is None else scale)
 
+    @staticmethod
+    def _rows_at(layout, q, kv_len, rows, k_new, v_new):
+        """The rows of an earlier call with this call's addresses."""
+        r = A.AsrPagedRows.from_buffer_copy(layout)
+        r.q, r.kv_len = q.data_ptr(), kv_len.data_ptr()
+        if rows is not None:
+            r.rows = rows.data_ptr()
+        if k_new is not None:
+            r.k_new, r.v_new = k_new.data_ptr(), v_new.data_ptr()
+        return r
+
     def attend(self, q, kv_len, *, k_new=None, v_new=None, rows=None, causal=True, scale: Optional[float] = None,
                out=None, lse=None):
         """Attention of the block's rows ``q [B, R, H, D]`` over the cache; ``k_new`` / ``v_new`` ``[B, R, K, D]`` are
         appended at ``kv_len``.  ``rows`` (int32 ``[B]``) are the rows in use.  Causal: row i sees slots 0 .. kv_len + i;
         else slots below kv_len.  Returns ``(out [B, R, H, D], lse [B, R, H])``; ``scale`` defaults to 1 / sqrt(D)."""
-        r = self._rows(q, kv_len, rows, k_new, v_new, causal, scale)
-        B, R, H, D = q.shape
-        with torch.cuda.device(self.device):
-            if out is None:
-                out = torch.empty((B, R, H, D), dtype=self.dtype, device=self.device)
-            else:
-                _tensor(out, "out", self.dtype, (B, R, H, D), self.device)
-                _need(out.is_contiguous(), "out: must be contiguous")
-            if lse is None:
-                lse = torch.empty((B, R, H), dtype=torch.float32, device=self.device)
-            else:
-                _tensor(lse, "lse", torch.float32, (B, R, H), self.device)
-                _need(lse.is_contiguous(), "lse: must be contiguous")
-            n = self._ws.get((R, H))
-            if n is None:
-                n = _check(A.lib().asr_spec_paged_attend_ws(self._ref, ctypes.byref(r)), "asr_spec_paged_attend_ws")
-                self._ws[(R, H)] = n
-            ws = torch.empty(n, dtype=torch.uint8, device=self.device)
-            A.asr_spec_paged_attend(self._ref, r, out, lse, ws, n, torch.cuda.current_stream().cuda_stream)
+        if _current_device() != self._index:
+            with torch.cuda.device(self.device):
+                return self.attend(q, kv_len, k_new=k_new, v_new=v_new, rows=rows, causal=causal, scale=scale, out=out,
+                                   lse=lse)
+        key = (_layout(q), _layout(kv_len), _layout(k_new), _layout(v_new), _layout(rows), causal, scale, _layout(out),
+               _layout(lse))
+        known = self._attend_layouts.get(key)
+        if known is None:
+            r = self._rows(q, kv_len, rows, k_new, v_new, causal, scale)
+            if out is not None:
+                _whole(out, "out", self.dtype, q.shape, self.device)
+            if lse is not None:
+                _whole(lse, "lse", torch.float32, q.shape[:3], self.device)
+            n = _check(self._lib.asr_spec_paged_attend_ws(self._ref, ctypes.byref(r)), "asr_spec_paged_attend_ws")
+            known = _remember(self._attend_layouts, key, (r, n, q.shape, q.shape[:3]))
+        layout, n, out_shape, lse_shape = known
+        r = self._rows_at(layout, q, kv_len, rows, k_new, v_new)
+        if out is None:
+            out = torch.empty(out_shape, dtype=self.dtype, device=self.device)
+        if lse is None:
+            lse = torch.empty(lse_shape, dtype=torch.float32, device=self.device)
+        stream = _raw_stream(self._index)
+        ws = self._workspace(stream, n)
+        _check(self._lib.asr_spec_paged_attend(self._ref, ctypes.byref(r), out.data_ptr(), lse.data_ptr(), ws.data_ptr(), n,
+                                               stream), "asr_spec_paged_attend")
         return out, lse
 
     def weigh(self, q, lse, kv_len, score, *, rows=None, causal=True, scale: Optional[float] = None, out=None, pos=None,
@@ -142,9 +197,32 @@ class PagedCache:
         None: zeros, then ``out`` is required).  Call it after the verification with the committed rows, and the
         ``kv_len`` and ``lse`` of the attention.  Writes ``out`` (default: ``score`` in place) and, with ``pos`` (int32,
         as score) and ``first_pos`` (int32 ``[B]``), the new slots' positions.  Returns ``out``."""
+        if _current_device() != self._index:
+            with torch.cuda.device(self.device):
+                return self.weigh(q, lse, kv_len, score, rows=rows, causal=causal, scale=scale, out=out, pos=pos,
+                                  first_pos=first_pos)
+        out = score if out is None else out
+        key = (_layout(q), _layout(kv_len), _layout(rows), causal, scale, _layout(lse), _layout(score), _layout(out),
+               _layout(pos), _layout(first_pos))
+        known = self._weigh_layouts.get(key)
+        if known is None:
+            known = _remember(self._weigh_layouts, key, self._weigh_layout(q, lse, kv_len, score, rows, causal, scale, out,
+                                                                           pos, first_pos))
+        layout, slots, lse_strides = known
+        r = self._rows_at(layout, q, kv_len, rows, None, None)
+        s = A.AsrPagedScores.from_buffer_copy(slots)
+        s.score_out = out.data_ptr()
+        if score is not None:
+            s.score = score.data_ptr()
+        if pos is not None:
+            s.pos, s.first_pos = pos.data_ptr(), first_pos.data_ptr()
+        _check(self._lib.asr_spec_paged_weigh(self._ref, ctypes.byref(r), ctypes.byref(s), lse.data_ptr(), *lse_strides,
+                                              _raw_stream(self._index)), "asr_spec_paged_weigh")
+        return out
+
+    def _weigh_layout(self, q, lse, kv_len, score, rows, causal, scale, out, pos, first_pos):
         r = self._rows(q, kv_len, rows, None, None, causal, scale)
         B, R, H = q.shape[:3]
-        out = score if out is None else out
         _need(out is not None, "out: required without score")
         _need(out.dim() == 3, "score: [batch, kv_heads, slots] is required")
         shape = (B, self.kv_heads, out.shape[2])
@@ -156,14 +234,11 @@ class PagedCache:
                 _need(x.stride() == out.stride(), f"{name}: out's strides are required")
         _need((pos is None) == (first_pos is None), "pos and first_pos go together")
         if first_pos is not None:
-            _ints(first_pos, "first_pos", (B,), self.device)
+            _whole(first_pos, "first_pos", torch.int32, (B,), self.device)
         _tensor(lse, "lse", torch.float32, (B, R, H), self.device)
         _need(lse.stride(2) == 1, "lse: the last axis must be contiguous")
-        s = A.AsrPagedScores(A.addr(score), A.addr(pos), out.stride(0), out.stride(1), shape[2], out.data_ptr(), None, 0, 0, 0,
-                             A.addr(first_pos))
-        with torch.cuda.device(self.device):
-            A.asr_spec_paged_weigh(self._ref, r, s, lse, lse.stride(0), lse.stride(1), torch.cuda.current_stream().cuda_stream)
-        return out
+        s = A.AsrPagedScores(None, None, out.stride(0), out.stride(1), shape[2], None, None, 0, 0, 0, None)
+        return r, s, (lse.stride(0), lse.stride(1))
 
     def evict(self, lens, score, pos, seen, *, budget: int, recent: int = 0, first: int = 0, lens_out=None, score_out=None,
               pos_out=None):
@@ -171,33 +246,49 @@ class PagedCache:
         (of ``seen`` ``[B]`` tokens) and the ``first`` oldest go last.  Freed slots below the budget take the kept ones
         past it.  ``score`` / ``pos`` ``[B, K, slots]`` and the pages' K/V move along: into ``score_out`` / ``pos_out``
         (default: in place) and in place.  Returns ``(lens_out, score_out, pos_out)``."""
-        B, K = self.batch, self.kv_heads
-        _ints(lens, "lens", (B,), self.device)
-        _ints(seen, "seen", (B,), self.device)
-        _need(isinstance(score, torch.Tensor) and score.dim() == 3, "score: [batch, kv_heads, slots] is required")
-        _tensor(score, "score", torch.float32, (B, K, score.shape[2]), self.device)
-        _tensor(pos, "pos", torch.int32, score.shape, self.device)
+        if _current_device() != self._index:
+            with torch.cuda.device(self.device):
+                return self.evict(lens, score, pos, seen, budget=budget, recent=recent, first=first, lens_out=lens_out,
+                                  score_out=score_out, pos_out=pos_out)
         score_out = score if score_out is None else score_out
         pos_out = pos if pos_out is None else pos_out
-        _need(isinstance(score_out, torch.Tensor) and score_out.dim() == 3, "score_out: [batch, kv_heads, slots] is required")
-        _tensor(score_out, "score_out", torch.float32, (B, K, score_out.shape[2]), self.device)
-        _tensor(pos_out, "pos_out", torch.int32, score_out.shape, self.device)
-        _need(score.stride() == pos.stride() and score.stride(2) == 1 and score_out.stride() == pos_out.stride() and
-              score_out.stride(2) == 1, "score and pos: the same strides and a contiguous last axis are required")
-        _need(budget >= 1 and recent >= 0 and first >= 0, "budget >= 1, recent >= 0 and first >= 0 are required")
-        with torch.cuda.device(self.device):
-            if lens_out is None:
-                lens_out = torch.empty_like(lens)
-            else:
-                _ints(lens_out, "lens_out", (B,), self.device)
-            s = A.AsrPagedScores(score.data_ptr(), pos.data_ptr(), score.stride(0), score.stride(1), score.shape[2],
-                                 score_out.data_ptr(), pos_out.data_ptr(), score_out.stride(0), score_out.stride(1),
-                                 score_out.shape[2], None)
-            n = _check(A.lib().asr_spec_paged_evict_ws(self._ref, ctypes.byref(s), budget), "asr_spec_paged_evict_ws")
-            ws = torch.empty(n, dtype=torch.uint8, device=self.device)
-            A.asr_spec_paged_evict(self._ref, s, lens, seen, budget, recent, first, lens_out, ws, n,
-                                   torch.cuda.current_stream().cuda_stream)
+        key = (_layout(lens), _layout(score), _layout(pos), _layout(seen), budget, recent, first, _layout(lens_out),
+               _layout(score_out), _layout(pos_out))
+        known = self._evict_layouts.get(key)
+        if known is None:
+            known = _remember(self._evict_layouts, key, self._evict_layout(lens, score, pos, seen, budget, recent, first,
+                                                                           lens_out, score_out, pos_out))
+        slots, n = known
+        if lens_out is None:
+            lens_out = torch.empty_like(lens)
+        s = A.AsrPagedScores.from_buffer_copy(slots)
+        s.score, s.pos, s.score_out, s.pos_out = score.data_ptr(), pos.data_ptr(), score_out.data_ptr(), pos_out.data_ptr()
+        stream = _raw_stream(self._index)
+        ws = self._workspace(stream, n)
+        _check(self._lib.asr_spec_paged_evict(self._ref, ctypes.byref(s), lens.data_ptr(), seen.data_ptr(), budget, recent,
+                                              first, lens_out.data_ptr(), ws.data_ptr(), n, stream), "asr_spec_paged_evict")
         return lens_out, score_out, pos_out
+
+    def _evict_layout(self, lens, score, pos, seen, budget, recent, first, lens_out, score_out, pos_out):
+        B, K = self.batch, self.kv_heads
+        _whole(lens, "lens", torch.int32, (B,), self.device)
+        _whole(seen, "seen", torch.int32, (B,), self.device)
+        if lens_out is not None:
+            _whole(lens_out, "lens_out", torch.int32, (B,), self.device)
+        for x, y, name in ((score, pos, "score"), (score_out, pos_out, "score_out")):
+            _need(isinstance(x, torch.Tensor) and x.dim() == 3, f"{name}: [batch, kv_heads, slots] is required")
+            _tensor(x, name, torch.float32, (B, K, x.shape[2]), self.device)
+            _tensor(y, name.replace("score", "pos"), torch.int32, x.shape, self.device)
+            _need(x.stride() == y.stride() and x.stride(2) == 1,
+                  "score and pos: the same strides and a contiguous last axis are required")
+        _need(budget >= 1 and recent >= 0 and first >= 0, "budget >= 1, recent >= 0 and first >= 0 are required")
+        s = A.AsrPagedScores(None, None, score.stride(0), score.stride(1), score.shape[2], None, None, score_out.stride(0),
+                             score_out.stride(1), score_out.shape[2], None)
+        n = _check(self._lib.asr_spec_paged_evict_ws(self._ref, ctypes.byref(s), budget), "asr_spec_paged_evict_ws")
+        return s, n
+
+
+_accept_layouts: dict = {}
 
 
 def accept_sampled(target, draft, lens, u, race, *, draft_logits=None, temperature: float = 1.0, status=None):
@@ -208,17 +299,43 @@ def accept_sampled(target, draft, lens, u, race, *, draft_logits=None, temperatu
     [0, 1) and ``race [B, V]`` standard exponential, float32.  Returns ``(accepted [B], token [B], step [B], prob [B, k])``:
     the drafts accepted, the token drawn after them, the positions to commit and each draft's acceptance probability.
     ``status``: an int32 device tensor that collects ``asrspec.ST_*`` bits."""
+    key = (_layout(target), _layout(draft), _layout(lens), _layout(u), _layout(race), _layout(draft_logits),
+           _layout(status), temperature)
+    known = _accept_layouts.get(key)
+    if known is None:
+        known = _remember(_accept_layouts, key, _accept_layout(target, draft, lens, u, race, draft_logits, temperature, status))
+    layout, n, device, index, race_stride = known
+    if _current_device() != index:
+        with torch.cuda.device(device):
+            return accept_sampled(target, draft, lens, u, race, draft_logits=draft_logits, temperature=temperature, status=status)
+    B, k = draft.shape
+    x = A.AsrSampledLogits.from_buffer_copy(layout)
+    x.target = target.data_ptr()
+    if draft_logits is not None and k:
+        x.draft_logits = draft_logits.data_ptr()
+    ints = torch.empty((3, B), dtype=torch.int32, device=device)
+    prob = torch.empty((B, k), dtype=torch.float32, device=device)
+    ws = torch.empty(n, dtype=torch.uint8, device=device)
+    at = ints.data_ptr()
+    _check(A.lib().asr_spec_accept_sampled(
+        ctypes.byref(x), draft.data_ptr(), None if lens is None else lens.data_ptr(), u.data_ptr(), race.data_ptr(), race_stride,
+        temperature, at, at + 4 * B, at + 8 * B, prob.data_ptr(), None if status is None else status.data_ptr(), ws.data_ptr(), n,
+        _raw_stream(index)), "asr_spec_accept_sampled")
+    accepted, token, step = ints.unbind(0)
+    return accepted, token, step, prob
+
+
+def _accept_layout(target, draft, lens, u, race, draft_logits, temperature, status):
     _need(isinstance(target, torch.Tensor) and target.is_cuda and target.dim() == 3 and target.dtype in _DTYPE,
           "target: [batch, k + 1, vocab] of float32, bfloat16 or float16 on a CUDA device is required")
     dev = target.device
     B, k, V = target.shape[0], target.shape[1] - 1, target.shape[2]
     _need(0 <= k <= 31 and B >= 1 and V >= 1, "target: 1 to 32 rows are required")
     _need(target.stride(2) == 1, "target: the last axis must be contiguous")
-    _ints(draft, "draft", (B, k), dev)
+    _whole(draft, "draft", torch.int32, (B, k), dev)
     if lens is not None:
-        _ints(lens, "lens", (B,), dev)
-    _tensor(u, "u", torch.float32, (B, k), dev)
-    _need(u.is_contiguous(), "u: must be contiguous")
+        _whole(lens, "lens", torch.int32, (B,), dev)
+    _whole(u, "u", torch.float32, (B, k), dev)
     _tensor(race, "race", torch.float32, (B, V), dev)
     _need(race.stride(1) == 1, "race: the last axis must be contiguous")
     ds = (0, 0)
@@ -227,16 +344,8 @@ def accept_sampled(target, draft, lens, u, race, *, draft_logits=None, temperatu
         _need(k == 0 or draft_logits.stride(2) == 1, "draft_logits: the last axis must be contiguous")
         ds = draft_logits.stride()[:2]
     if status is not None:
-        _ints(status, "status", (1,), dev)
+        _whole(status, "status", torch.int32, (1,), dev)
     _need(temperature > 0 and math.isfinite(temperature), "temperature: a positive number is required")
-    with torch.cuda.device(dev):
-        ints = torch.empty((3, B), dtype=torch.int32, device=dev)
-        prob = torch.empty((B, k), dtype=torch.float32, device=dev)
-        n = _check(A.lib().asr_spec_accept_sampled_ws(B, k), "asr_spec_accept_sampled_ws")
-        ws = torch.empty(n, dtype=torch.uint8, device=dev)
-        x = A.AsrSampledLogits(target.data_ptr(), target.stride(0), target.stride(1), A.addr(draft_logits) if k else None, *ds,
-                               B, k, V, _DTYPE[target.dtype])
-        accepted, token, step = ints.unbind(0)
-        A.asr_spec_accept_sampled(x, draft, lens, u, race, race.stride(0), temperature, accepted, token, step, prob, status, ws,
-                                  n, torch.cuda.current_stream().cuda_stream)
-    return accepted, token, step, prob
+    n = _check(A.lib().asr_spec_accept_sampled_ws(B, k), "asr_spec_accept_sampled_ws")
+    return (A.AsrSampledLogits(None, target.stride(0), target.stride(1), None, *ds, B, k, V, _DTYPE[target.dtype]), n, dev,
+            dev.index, race.stride(0))
