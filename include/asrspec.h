@@ -463,7 +463,8 @@ typedef struct {
  * slot that a row does not see never reaches it, whatever it holds.
  * out: [batch][max_rows][heads][head_dim] contiguous, 16-byte aligned; lse
  * [batch][max_rows][heads] fp32.  ws: asr_spec_paged_attend_ws bytes, 16-byte
- * aligned, no initial contents.  Arithmetic: 16-bit types multiply in 16 bits
+ * aligned, zero before its first use; every call leaves it ready for the next
+ * on its stream, whatever that one's sizes.  Arithmetic: 16-bit types multiply in 16 bits
  * with fp32 accumulation (weights rounded to the type for the second
  * product); fp32 in fp32 throughout; softmax statistics in fp32.
  * Data errors: kv_len or kv_len + rows outside the table (ASR_ST_CAPACITY) and

@@ -62,6 +62,7 @@ int paged_rows(const asr_paged_cache* c, const asr_paged_rows* r, PagedRows* v) 
                          r->new_batch_stride, r->new_row_stride, r->new_head_stride};
   for (int i = 0; i < (r->k_new ? 6 : 3); ++i)
     if (st[i] < 0 || (st[i] * es) % 16) return ASR_E_INVAL;
+  if (r->k_new && r->new_row_stride * es > (1 << 26)) return ASR_E_INVAL;   // 16 rows' offsets fit 32 bits
   if (((uintptr_t)r->q | (uintptr_t)r->k_new | (uintptr_t)r->v_new) % 16) return ASR_E_INVAL;
   v->q = static_cast<const char*>(r->q);
   v->q_b = r->q_batch_stride * es;

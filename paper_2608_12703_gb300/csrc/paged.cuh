@@ -98,40 +98,50 @@ __device__ __forceinline__ uint4 ldg_stream(const char* p) {   // read once: no 
   return v;
 }
 
+__device__ __forceinline__ uint4 ldg_if(bool in, const char* p) {   // zero where not `in`
+  uint4 v;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %5, 0;\n\t"
+      "mov.b32 %0, 0;\n\tmov.b32 %1, 0;\n\tmov.b32 %2, 0;\n\tmov.b32 %3, 0;\n\t"
+      "@p ld.global.nc.v4.u32 {%0,%1,%2,%3}, [%4];\n\t}"
+      : "=&r"(v.x), "=&r"(v.y), "=&r"(v.z), "=&r"(v.w)
+      : "l"(p), "r"((int)in));
+  return v;
+}
+
 // ---------------------------------------------------------------------------
 // Work distribution.  The units of a call are key steps in the order
 // (sequence, item, step), an item being what one warp keeps in registers (a
 // K/V head and a tile of rows).  U units are dealt to W warps in contiguous
-// runs, warp w taking [w U / W, (w + 1) U / W): equal shares whatever the
-// lengths, at most two items of a warp are shared with others.
+// runs of U / W or one more: equal shares whatever the lengths; at most two
+// items of a warp are shared with other warps.  The warps of a block are
+// neighbours.  U < 2^31 (checked on the host).
 // ---------------------------------------------------------------------------
 struct WorkPlan {
-  long long units;   // U
-  int workers;       // W in use
+  int units, workers;   // U, W in use
+  int share, more;      // every warp takes `share` units, the first `more` one more
+  __device__ __forceinline__ int start(int w) const { return w * share + min(w, more); }
+  __device__ __forceinline__ int owner(int u) const {   // the warp whose run holds unit u
+    const unsigned edge = (unsigned)more * (share + 1);
+    return (unsigned)u < edge ? (unsigned)u / (share + 1u) : more + ((unsigned)u - edge) / (unsigned)share;
+  }
 };
-__device__ __forceinline__ long long work_start(const WorkPlan& p, long long w) { return w * p.units / p.workers; }
-// the warp whose run holds unit u
-__device__ __forceinline__ int work_owner(const WorkPlan& p, long long u) {
-  return (int)(((u + 1) * p.workers - 1) / p.units);
-}
 
 // The block's copy of the call's lengths and the prefix sums of the sequences'
 // units, so that later look-ups stay on chip: shared memory of plan_bytes(B).
 struct PlanMem {
-  long long* pre;   // [B + 1]
-  int2* lens;       // [B] committed slots, rows
+  int2* lens;   // [B] committed slots, rows
+  int* pre;     // [B + 1]
 };
-inline size_t plan_bytes(int B) { return (2 * (size_t)B + 1) * sizeof(long long); }
+constexpr size_t plan_bytes(int B) { return ((size_t)B * 12 + 4 + 15) / 16 * 16; }
 
-// Every thread of the block calls it.  units(len, rows): a sequence's units;
-// fewer units than min_units are not dealt to a warp of their own.
+// Every thread of the block calls it.  units(len, rows): a sequence's units.
 template <typename F>
-__device__ __forceinline__ WorkPlan work_plan(const PagedView& c, const PagedRows& r, PlanMem& mem, int max_workers,
-                                              int min_units, F units) {
-  extern __shared__ __align__(16) long long plan_smem[];
+__device__ __forceinline__ WorkPlan work_plan(const PagedView& c, const PagedRows& r, PlanMem& mem, int max_workers, F units) {
+  extern __shared__ __align__(16) unsigned char plan_smem[];
   const int B = c.batch, lane = threadIdx.x & 31;
-  mem.pre = plan_smem;
-  mem.lens = reinterpret_cast<int2*>(plan_smem + B + 1);
+  mem.lens = reinterpret_cast<int2*>(plan_smem);
+  mem.pre = reinterpret_cast<int*>(mem.lens + B);
   for (int b = threadIdx.x; b < B; b += blockDim.x) {
     int2 n;
     paged_lens(c, r, b, n.x, n.y);
@@ -140,12 +150,12 @@ __device__ __forceinline__ WorkPlan work_plan(const PagedView& c, const PagedRow
   }
   __syncthreads();
   if (threadIdx.x < 32) {
-    long long base = 0;
+    int base = 0;
     for (int b0 = 0; b0 < B; b0 += 32) {
-      long long x = b0 + lane < B ? mem.pre[b0 + lane + 1] : 0;
+      int x = b0 + lane < B ? mem.pre[b0 + lane + 1] : 0;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
-        const long long y = __shfl_up_sync(0xffffffffu, x, o);
+        const int y = __shfl_up_sync(0xffffffffu, x, o);
         if (lane >= o) x += y;
       }
       if (b0 + lane < B) mem.pre[b0 + lane + 1] = base + x;
@@ -156,19 +166,21 @@ __device__ __forceinline__ WorkPlan work_plan(const PagedView& c, const PagedRow
   __syncthreads();
   WorkPlan p;
   p.units = mem.pre[B];
-  const long long w = (p.units + min_units - 1) / min_units;
-  p.workers = (int)(w < 1 ? 1 : w < max_workers ? w : max_workers);
+  p.workers = max(1, min(p.units, max_workers));
+  p.share = p.units / p.workers;
+  p.more = p.units - p.share * p.workers;
   return p;
 }
-// the sequence that holds unit u: pre[b] <= u < pre[b + 1]
-__device__ __forceinline__ int work_find(const long long* pre, int B, long long u) {
-  int lo = 0, hi = B;
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (pre[mid] <= u) lo = mid;
-    else hi = mid;
+// the sequence that holds unit u, pre[b] <= u < pre[b + 1]; a warp's lanes search together
+__device__ __forceinline__ int work_find(const int* pre, int B, int u) {
+  const int lane = threadIdx.x & 31;
+  int lo = 0;
+  if (B > 32) {
+    const int step = (B + 31) >> 5, at = lane * step;
+    lo = (__popc(__ballot_sync(0xffffffffu, at < B && pre[at] <= u)) - 1) * step;
+    B = min(B, lo + step);
   }
-  return lo;
+  return lo + __popc(__ballot_sync(0xffffffffu, lo + lane < B && pre[lo + lane] <= u)) - 1;
 }
 
 // ---------------------------------------------------------------------------
@@ -204,39 +216,49 @@ template <> struct Mma16<__half> {
 
 template <int D> struct Cfg16 { static constexpr int KS = D == 64 ? 32 : 16; };   // keys a step
 
-// one sequence's share of the work
+// One sequence's share of the work.  Keys come in steps of KS: first the slots
+// in pages, then, where the block's own rows are passed, those rows.
 struct SeqWork {
-  int len, rows, keys, steps, tiles;
+  int len, rows;       // committed slots, rows
+  int paged, fresh;    // keys in pages, keys in the block's own rows
+  int psteps, steps, tiles;
 };
 template <int KS, int TR>
 __device__ __forceinline__ SeqWork seq_work(const PagedRows& r, int len, int rows) {
   SeqWork s;
   s.len = len;
   s.rows = rows;
-  s.keys = s.rows ? s.len + (r.causal ? s.rows : 0) : 0;
-  s.steps = (s.keys + KS - 1) / KS;
-  s.tiles = (s.rows * r.group + TR - 1) / TR;
+  s.fresh = r.k_new != nullptr ? rows : 0;
+  s.paged = rows == 0 ? 0 : len + (r.causal ? rows - s.fresh : 0);
+  s.psteps = (s.paged + KS - 1) / KS;
+  s.steps = s.psteps + (s.fresh + KS - 1) / KS;
+  s.tiles = (rows * r.group + TR - 1) / TR;
   return s;
 }
 
-// The step's fragments of one head.  Full steps lie below kv_len; the others
-// pick each key's source and zero what is past the end.
+// A warp's reader of one head's keys and values, step by step, as mma B
+// fragments.  A step whose slots are all committed is full; in the others keys
+// past the end are zero.
 template <typename T, int D>
 struct Keys16 {
   static constexpr int KS = Cfg16<D>::KS, NG = KS / PG_GROUP, NC = D / 32, NV = D / 64;
   const PagedView& c;
   const PagedRows& r;
+  SeqWork s;
   const int* table_row;
   long long head_off;
   const char *kn, *vn;   // this sequence's and head's new rows
-  int len, keys, g, t;
-  bool fresh;            // slots from len on are read from them
+  int g, t;
+
+  __device__ __forceinline__ bool full(int step) const { return (step + 1) * KS <= min(s.len, s.paged); }
+  // slot of a step's first key, and the end of the run of slots that it reads from
+  __device__ __forceinline__ int first(int step) const { return step < s.psteps ? step * KS : s.len + (step - s.psteps) * KS; }
+  __device__ __forceinline__ int end(int step) const { return step < s.psteps ? s.paged : s.len + s.fresh; }
 
   __device__ __forceinline__ int id(int step, int u) const {   // page of group u of a step, fetched ahead
     const int grp = step * NG + u;
-    return grp * PG_GROUP < keys ? paged_id(c, table_row, grp) : 0;
+    return grp * PG_GROUP < s.paged ? paged_id(c, table_row, grp) : 0;
   }
-  __device__ __forceinline__ bool full(int step) const { return (step + 1) * KS <= len; }
   __device__ __forceinline__ void offsets(int step, const int* pid, long long* off) const {
 #pragma unroll
     for (int u = 0; u < NG; ++u) off[u] = paged_offset(c, pid[u], step * NG + u) + head_off;
@@ -244,79 +266,83 @@ struct Keys16 {
 
   // K: kf[key tile][16-byte chunk], lane's key 8 w + g of a group
   __device__ __forceinline__ void load_k(int step, const long long* off, uint4 (&kf)[KS / 8][NC]) const {
-    const int lane_off = g * (int)c.slot_stride + t * 16, row8 = 8 * (int)c.slot_stride;
     if (full(step)) {
+      const int slot = (int)c.slot_stride, lane_off = g * slot + t * 16;
 #pragma unroll
       for (int u = 0; u < NG; ++u) {
         const char* p = c.k + off[u] + lane_off;
 #pragma unroll
         for (int w = 0; w < 2; ++w)
 #pragma unroll
-          for (int j = 0; j < NC; ++j) kf[u * 2 + w][j] = ldg_stream(p + w * row8 + j * 64);
+          for (int j = 0; j < NC; ++j) kf[u * 2 + w][j] = ldg_stream(p + w * 8 * slot + j * 64);
       }
     } else {
+      const bool paged = step < s.psteps;
+      const int stride = paged ? (int)c.slot_stride : (int)r.n_r, left = end(step) - first(step);
+      const char* rows = kn + (long long)(step - s.psteps) * KS * r.n_r;
 #pragma unroll
-      for (int u = 0; u < NG; ++u)
+      for (int u = 0; u < NG; ++u) {
+        const char* p = (paged ? c.k + off[u] : rows + u * PG_GROUP * stride) + g * stride + t * 16;
 #pragma unroll
         for (int w = 0; w < 2; ++w)
-          edge<NC, 64>(c.k + off[u] + lane_off + w * row8, kn + t * 16, step * KS + u * PG_GROUP + w * 8 + g, kf[u * 2 + w]);
+#pragma unroll
+          for (int j = 0; j < NC; ++j) kf[u * 2 + w][j] = ldg_if(u * PG_GROUP + w * 8 + g < left, p + w * 8 * stride + j * 64);
+      }
     }
   }
   // V: vf[group][which of the lane's four keys 2t, 2t+1, 2t+8, 2t+9][64-wide half]
   __device__ __forceinline__ void load_v(int step, const long long* off, uint4 (&vf)[NG][4][NV]) const {
-    const int slot = (int)c.slot_stride, lane_off = 2 * t * slot + g * 16;
+    if (full(step)) {
+      const int slot = (int)c.slot_stride, lane_off = 2 * t * slot + g * 16;
 #pragma unroll
-    for (int u = 0; u < NG; ++u) {
-      const char* p = c.v + off[u] + lane_off;
-      if (full(step)) {
+      for (int u = 0; u < NG; ++u) {
+        const char* p = c.v + off[u] + lane_off;
 #pragma unroll
         for (int w = 0; w < 4; ++w)
 #pragma unroll
           for (int j = 0; j < NV; ++j) vf[u][w][j] = ldg_stream(p + ((w & 1) + (w >> 1) * 8) * slot + j * 128);
-      } else {
+      }
+    } else {
+      const bool paged = step < s.psteps;
+      const int stride = paged ? (int)c.slot_stride : (int)r.n_r, left = end(step) - first(step);
+      const char* rows = vn + (long long)(step - s.psteps) * KS * r.n_r;
 #pragma unroll
-        for (int w = 0; w < 4; ++w)
-          edge<NV, 128>(p + ((w & 1) + (w >> 1) * 8) * slot, vn + g * 16,
-                        step * KS + u * PG_GROUP + 2 * t + (w & 1) + (w >> 1) * 8, vf[u][w]);
+      for (int u = 0; u < NG; ++u) {
+        const char* p = (paged ? c.v + off[u] : rows + u * PG_GROUP * stride) + 2 * t * stride + g * 16;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          const int in = (w & 1) + (w >> 1) * 8;
+#pragma unroll
+          for (int j = 0; j < NV; ++j) vf[u][w][j] = ldg_if(u * PG_GROUP + 2 * t + in < left, p + in * stride + j * 128);
+        }
       }
     }
   }
-  // One key of an edge step: from its page, or from the block's rows; zero past the end.
-  template <int N, int STRIDE>
-  __device__ __forceinline__ void edge(const char* page, const char* fresh_rows, int key, uint4 (&f)[N]) const {
-    const char* src = fresh && key >= len ? fresh_rows + (long long)(key - len) * r.n_r : page;
-#pragma unroll
-    for (int j = 0; j < N; ++j) f[j] = make_uint4(0, 0, 0, 0);
-    if (key < keys) {
-#pragma unroll
-      for (int j = 0; j < N; ++j) f[j] = *reinterpret_cast<const uint4*>(src + j * STRIDE);
-    }
-  }
-  // Write the new rows of an edge step to their pages, from the fragments that
-  // the step is about to use.  A bad page id is reported by id(); nothing goes there.
-  __device__ __forceinline__ void append_k(int step, const uint4 (&kf)[KS / 8][NC]) const {
-#pragma unroll
-    for (int u = 0; u < NG; ++u)
-#pragma unroll
-      for (int w = 0; w < 2; ++w) append<NC, 64>(c.k, step, u, w * 8 + g, t * 16, kf[u * 2 + w]);
-  }
-  __device__ __forceinline__ void append_v(int step, const uint4 (&vf)[NG][4][NV]) const {
-#pragma unroll
-    for (int u = 0; u < NG; ++u)
-#pragma unroll
-      for (int w = 0; w < 4; ++w) append<NV, 128>(c.v, step, u, 2 * t + (w & 1) + (w >> 1) * 8, g * 16, vf[u][w]);
-  }
-  template <int N, int STRIDE>
-  __device__ __forceinline__ void append(char* pages, int step, int u, int in, int byte, const uint4 (&f)[N]) const {
-    const int key = step * KS + u * PG_GROUP + in, grp = step * NG + u;
-    if (key < len || key >= keys) return;
-    const int pid = __ldg(table_row + c.groups.div((uint32_t)grp));
-    if ((unsigned)pid >= (unsigned)c.n_pages) return;
-    char* p = pages + paged_offset(c, pid, grp) + head_off + in * c.slot_stride + byte;
-#pragma unroll
-    for (int j = 0; j < N; ++j) *reinterpret_cast<uint4*>(p + j * STRIDE) = f[j];
-  }
 };
+
+// A warp writes one head's new rows to their pages, 16 bytes a lane, K and V
+// side by side.  A bad page id is reported and nothing goes there.
+__device__ __forceinline__ void append_rows(const PagedView& c, const PagedRows& r, const SeqWork& s, int b, int kvh,
+                                            int row_bytes) {
+  const int lane = threadIdx.x & 31, chunks = row_bytes / 16;      // 8, 16 or 32 a row
+  const bool is_v = (lane / (chunks < 16 ? chunks : 16)) & 1;
+  const int* table_row = c.table + b * c.table_stride;
+  const char* src0 = (is_v ? r.v_new : r.k_new) + b * r.n_b + kvh * r.n_h;
+  char* dst0 = (is_v ? c.v : c.k) + kvh * c.head_stride;
+  const int at_once = chunks < 16 ? 32 / (2 * chunks) : 1;
+  for (int i = chunks < 16 ? lane / (2 * chunks) : 0; i < s.rows; i += at_once) {
+    const int slot = s.len + i, page = slot / c.page_size;
+    const int pid = __ldg(table_row + page);
+    if ((unsigned)pid >= (unsigned)c.n_pages) {
+      if (c.status) set_status(c.status, ST_BOUNDS);
+      continue;
+    }
+    const char* src = src0 + (long long)i * r.n_r;
+    char* dst = dst0 + pid * c.page_stride + (slot - page * c.page_size) * c.slot_stride;
+    for (int x = lane % (chunks < 16 ? chunks : 16); x < chunks; x += 16)
+      *reinterpret_cast<uint4*>(dst + x * 16) = __ldg(reinterpret_cast<const uint4*>(src + x * 16));
+  }
+}
 
 // ---- Host: argument checks shared by the entry points ------------------------
 int paged_view(const asr_paged_cache* c, PagedView* v);

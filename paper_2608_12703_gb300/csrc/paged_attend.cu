@@ -19,17 +19,19 @@
 //     V of step i + 1 as soon as its product is: one of the two is always in
 //     flight, 8 KB a warp;
 //   * equal shares whatever the lengths: the (sequence, head, tile, step) units
-//     are dealt in contiguous runs over all resident warps (paged.cuh), and a
-//     second kernel joins the items that more than one warp worked on, in key
-//     order, so results do not depend on timing;
-//   * steps below kv_len are read from the pages; the last ones take the
-//     block's own rows from k_new / v_new, which the warp that holds them also
-//     writes to the pages (other tiles read them from k_new, never from a page
-//     written in the same launch).
+//     are dealt in contiguous runs over all resident warps (paged.cuh).  Warps
+//     of a block that all work on one item combine in shared memory; where an
+//     item has several such partial results they go through the workspace,
+//     and whoever delivers the last one joins them, in key order, so results
+//     do not depend on timing;
+//   * committed slots are read from the pages and the block's own rows, in
+//     steps after them, from k_new / v_new; one warp also copies those to the
+//     pages (nobody reads a page's slot that this launch writes).
 // Scores, running maximum and sum, and the output accumulate in fp32.  p is
 // rounded to the cache's 16-bit type for the second product (relative error at
 // most 2^-8 for bf16 and 2^-11 for fp16 a weight, as that of the rounded
 // output); the sum takes p before rounding, so lse is exact to fp32.
+#include <atomic>
 #include <type_traits>
 
 #include "kernels.h"
@@ -38,7 +40,7 @@
 namespace asrspec {
 namespace {
 
-constexpr int PA_WARPS = 4;
+constexpr int PA_WARPS = 8;   // one block an SM: registers for a step of K and V in flight a warp
 
 
 
@@ -47,9 +49,11 @@ struct AttendArgs {
   PagedRows r;
   char* out;     // [B][R][H][D]
   float* lse;    // [B][R][H] or null
-  float* ws;     // partial results: 2 per warp, [TR] max, [TR] sum, [TR][D] output
-  int max_workers, min_units;
+  int* tickets;  // [MAX_WORKERS] zero between calls: partial results delivered of the item that a warp begins
+  float* ws;     // partial results: 2 a warp, [TR] max, [TR] sum, [TR][D] output
+  int max_workers;
 };
+constexpr int MAX_WORKERS = 4096;
 
 // The halves of a pair of 16-bit values that are infinite or NaN, as a mask.
 template <typename T>
@@ -106,10 +110,11 @@ __device__ __forceinline__ void guard_values(const Keys16<T, D>& ks, int step, c
         v.x &= ~nonfinite_halves<T>(v.x), v.y &= ~nonfinite_halves<T>(v.y);
         v.z &= ~nonfinite_halves<T>(v.z), v.w &= ~nonfinite_halves<T>(v.w);
       }
-  for (int key = step * K::KS; key < min((step + 1) * K::KS, ks.keys); ++key) {
+  const int first = ks.first(step), end = min(first + K::KS, ks.end(step));
+  for (int key = first; key < end; ++key) {
     const int grp = key / PG_GROUP;
-    const char* row = ks.fresh && key >= ks.len
-                          ? ks.vn + (long long)(key - ks.len) * ks.r.n_r
+    const char* row = step >= ks.s.psteps
+                          ? ks.vn + (long long)(key - ks.s.len) * ks.r.n_r
                           : ks.c.v + paged_offset(ks.c, paged_id(ks.c, ks.table_row, grp), grp) + ks.head_off +
                                 (key % PG_GROUP) * ks.c.slot_stride;
 #pragma unroll
@@ -127,36 +132,227 @@ __device__ __forceinline__ void guard_values(const Keys16<T, D>& ks, int step, c
   }
 }
 
-template <typename T, int D, int MT, int MINB>
-__global__ void __launch_bounds__(PA_WARPS * 32, MINB) attend16_kernel(AttendArgs a) {
-  constexpr int KS = Cfg16<D>::KS, NG = KS / PG_GROUP, NC = D / 32, NV = D / 64, TR = 16 * MT;
+// ---------------------------------------------------------------------------
+// The end of an item.  Every warp leaves its (max, sum, output) in shared
+// memory, [TR] max, [TR] sum, [TR][D] output; `regions` of them are combined by
+// a warp, or by the block where all its warps worked on the item.  This code
+// runs once an item, mostly from a cold instruction cache: its loops stay
+// rolled, and the round trips to L2 are overlapped by asynchronous copies.
+// ---------------------------------------------------------------------------
+template <int D, int TR>
+struct Part {
+  static constexpr int FLOATS = TR * (D + 2);
+  static constexpr int STAGE = FLOATS * 4 > 4300 ? 2 : 3;   // regions a warp has to fetch partial results into, its own among them
+};
+
+__device__ __forceinline__ void copy16(float* smem, const float* gmem) {   // by L2: another SM wrote it
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(smem)), "l"(gmem) : "memory");
+}
+
+struct Acc {   // four columns of a row
+  float m = -INFINITY, l = 0.f;
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+  __device__ __forceinline__ void add(float pm, float pl, float4 po) {
+    const float mx = fmaxf(m, pm), z = mx == -INFINITY ? 0.f : mx, f0 = ex2(m - z), f1 = ex2(pm - z);
+    m = mx;
+    // the products' rounding is written out: a warp and a block must join alike, whichever comes last
+    l = fmaf(pl, f1, __fmul_rn(l, f0));
+    o = make_float4(fmaf(po.x, f1, __fmul_rn(o.x, f0)), fmaf(po.y, f1, __fmul_rn(o.y, f0)),
+                    fmaf(po.z, f1, __fmul_rn(o.z, f0)), fmaf(po.w, f1, __fmul_rn(o.w, f0)));
+  }
+};
+
+template <typename T, int D>
+__device__ __forceinline__ void put_row(const AttendArgs& a, int b, int kvh, int m, int col, const Acc& x) {
+  const int row = m / a.r.group, hq = kvh * a.r.group + m - row * a.r.group;
+  const size_t at = ((size_t)b * a.r.max_rows + row) * a.r.heads + hq;
+  const float inv = x.l > 0.f ? 1.f / x.l : 0.f;
+  if (a.lse && col == 0) a.lse[at] = (x.m + log2f(x.l)) * LN2;
+  T* out = reinterpret_cast<T*>(a.out) + at * D + col;
+  if constexpr (sizeof(T) == 4) {
+    *reinterpret_cast<float4*>(out) = make_float4(x.o.x * inv, x.o.y * inv, x.o.z * inv, x.o.w * inv);
+  } else {
+    *reinterpret_cast<uint2*>(out) =
+        make_uint2(Mma16<T>::pack(x.o.x * inv, x.o.y * inv), Mma16<T>::pack(x.o.z * inv, x.o.w * inv));
+  }
+}
+
+template <typename T, int D, int TR, bool BLOCK>
+__device__ __noinline__ void finish_item(const AttendArgs& a, const WorkPlan& plan, float* sm, int regions, int b, int kvh,
+                                         int tile, int rows, int u0, int u1, int worker, bool begins, bool whole) {
+  using PT = Part<D, TR>;
+  constexpr int PART = PT::FLOATS, C4 = D / 4;
+  __shared__ int s_last;
+  const int tid = BLOCK ? threadIdx.x : threadIdx.x & 31, nt = BLOCK ? PA_WARPS * 32 : 32;
+  const int nr = min(TR, rows - tile * TR);
+  auto sync = [] {
+    if (BLOCK) __syncthreads();
+    else __syncwarp();
+  };
+  sync();
+  float* part = a.ws + (size_t)(2 * worker + (begins ? 1 : 0)) * PART;
+#pragma unroll 1
+  for (int x = tid; x < nr * C4; x += nt) {
+    const int in = x / C4, col = (x - in * C4) * 4;
+    Acc acc;
+#pragma unroll 1
+    for (int w = 0; w < regions; ++w) {
+      const float* p = sm + w * PT::STAGE * PART;
+      acc.add(p[in], p[TR + in], *reinterpret_cast<const float4*>(p + 2 * TR + in * D + col));
+    }
+    if (whole) {
+      put_row<T, D>(a, b, kvh, tile * TR + in, col, acc);
+    } else {
+      if (col == 0) {
+        __stcg(part + in, acc.m);
+        __stcg(part + TR + in, acc.l);
+      }
+      __stcg(reinterpret_cast<float4*>(part + 2 * TR + in * D + col), acc.o);
+    }
+  }
+  if (whole) {
+    sync();   // the next item's results go to the same shared memory
+    return;
+  }
+  __threadfence();
+  // The parts of the item, in key order: single warps wf .., then blocks c0 ..
+  // c1 whose warps all work on it, then single warps again.
+  const int wf = plan.owner(u0), wl = plan.owner(u1 - 1);
+  const bool from_first = wf % PA_WARPS == 0 && plan.start(wf) == u0;
+  const bool to_last = (wl % PA_WARPS == PA_WARPS - 1 || wl == plan.workers - 1) && plan.start(wl + 1) == u1;
+  const int c0 = wf / PA_WARPS + (from_first ? 0 : 1), c1 = wl / PA_WARPS - (to_last ? 0 : 1);
+  const int n0 = c0 <= c1 ? c0 * PA_WARPS - wf : wl - wf + 1;
+  const int n1 = c0 <= c1 ? c1 - c0 + 1 : 0;
+  const int parts = n0 + n1 + (c0 <= c1 ? max(0, wl + 1 - (c1 + 1) * PA_WARPS) : 0);
+  sync();
+  int last = 0;
+  if (tid == 0) {
+    last = atomicAdd(a.tickets + wf, 1) == parts - 1;
+    if (last) {
+      a.tickets[wf] = 0;   // all have come: as the next call needs it
+      __threadfence();
+    }
+    if (BLOCK) s_last = last;
+  }
+  if (BLOCK) {
+    __syncthreads();
+    last = s_last;
+  } else {
+    last = __shfl_sync(0xffffffffu, last, 0);
+  }
+  if (!last) return;
+
+  // Fetch as many parts at a time as there is room for, and add them up.
+  constexpr int ROOM = (BLOCK ? PA_WARPS : 1) * PT::STAGE, MAX_X = (TR * C4 + (BLOCK ? PA_WARPS * 32 : 32) - 1) / (BLOCK ? PA_WARPS * 32 : 32);
+  const int used = 2 * TR + nr * D;   // floats of a part
+  Acc acc[MAX_X];
+  for (int p0 = 0; p0 < parts; p0 += ROOM) {
+    const int np = min(ROOM, parts - p0);
+    sync();
+#pragma unroll 1
+    for (int i = 0; i < np; ++i) {
+      const int p = p0 + i;
+      const int w = p < n0 ? wf + p : p < n0 + n1 ? (c0 + p - n0) * PA_WARPS : (c1 + 1) * PA_WARPS + p - n0 - n1;
+      const float* src = a.ws + (size_t)(2 * w + (p == 0 ? 1 : 0)) * PART;
+#pragma unroll 1
+      for (int x = tid * 4; x < used; x += nt * 4) copy16(sm + i * PART + x, src + x);
+    }
+    asm volatile("cp.async.wait_all;" ::: "memory");
+    sync();
+#pragma unroll
+    for (int e = 0; e < MAX_X; ++e) {
+      const int x = tid + e * nt, in = x / C4, col = (x - in * C4) * 4;
+      if (x >= nr * C4) break;
+#pragma unroll 1
+      for (int i = 0; i < np; ++i) {
+        const float* p = sm + i * PART;
+        acc[e].add(p[in], p[TR + in], *reinterpret_cast<const float4*>(p + 2 * TR + in * D + col));
+      }
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < MAX_X; ++e) {
+    const int x = tid + e * nt, in = x / C4;
+    if (x < nr * C4) put_row<T, D>(a, b, kvh, tile * TR + in, (x - in * C4) * 4, acc[e]);
+  }
+  sync();   // the next item's results go to the same shared memory
+}
+
+// Rows without keys: zeros, and -inf for the log-sum-exp.
+template <typename T, int D>
+__device__ __forceinline__ void clear_rows(const AttendArgs& a, const PlanMem& mem) {
+  for (int b = blockIdx.x; b < a.c.batch; b += gridDim.x) {
+    const int2 n = mem.lens[b];
+    const int from = n.x + (a.r.causal ? n.y : 0) == 0 ? 0 : n.y;
+    const size_t heads0 = ((size_t)b * a.r.max_rows + from) * a.r.heads, count = (size_t)(a.r.max_rows - from) * a.r.heads;
+    uint4* o = reinterpret_cast<uint4*>(a.out + heads0 * D * sizeof(T));
+    for (size_t i = threadIdx.x; i < count * (D * sizeof(T) / 16); i += blockDim.x) o[i] = make_uint4(0, 0, 0, 0);
+    if (a.lse)
+      for (size_t i = threadIdx.x; i < count; i += blockDim.x) a.lse[heads0 + i] = -INFINITY;
+  }
+}
+
+// What the two kernels below share: the plan, the walk over a warp's items and
+// their ends.  `item` computes keys [s0, s0 + n) steps of one item and leaves
+// the result in the warp's shared memory.
+template <typename T, int D, int KS, int TR, typename F>
+__device__ __forceinline__ void attend_items(const AttendArgs& a, F item) {
+  constexpr int REGION = Part<D, TR>::FLOATS * Part<D, TR>::STAGE;
   const PagedView& c = a.c;
   const PagedRows& r = a.r;
   PlanMem mem;
-  const WorkPlan plan = work_plan(c, r, mem, a.max_workers, a.min_units, [&](int len, int rows) {
+  const WorkPlan plan = work_plan(c, r, mem, a.max_workers, [&](int len, int rows) {
     const SeqWork s = seq_work<KS, TR>(r, len, rows);
-    return (long long)c.kv_heads * s.tiles * s.steps;
+    return c.kv_heads * s.tiles * s.steps;
   });
-  pdl_launch();
+  clear_rows<T, D>(a, mem);
+  const int warp = threadIdx.x >> 5, w0 = blockIdx.x * PA_WARPS, worker = w0 + warp;
+  if (plan.units == 0 || w0 >= plan.workers) return;
+  extern __shared__ __align__(16) unsigned char smem[];
+  float* sm = reinterpret_cast<float*>(smem + plan_bytes(c.batch));
+
+  const int w1 = min(w0 + PA_WARPS, plan.workers), block0 = plan.start(w0), block1 = plan.start(w1);
+  int u = worker < plan.workers ? plan.start(worker) : block1;
+  const int u_end = worker < plan.workers ? plan.start(worker + 1) : block1;
+  bool team = true;   // all warps of the block work on one item
+  for (int at = block0;;) {
+    const int b = work_find(mem.pre, c.batch, at);
+    const SeqWork s = seq_work<KS, TR>(r, mem.lens[b].x, mem.lens[b].y);
+    const int rem = at - mem.pre[b], it = rem / s.steps, kvh = it / s.tiles, tile = it - kvh * s.tiles;
+    const int u0 = mem.pre[b] + it * s.steps, u1 = u0 + s.steps;
+    if (team && block1 > u1) {   // uniform over the block, at its first item only
+      team = false;
+      if (worker >= plan.workers) return;
+      if (u > block0) {
+        at = u;
+        continue;
+      }
+    }
+    const int s0 = u - u0, n = min(u1, u_end) - u;
+    if (n > 0) item(s, b, kvh, tile, s0, n, sm + warp * REGION);
+    if (team) {
+      finish_item<T, D, TR, true>(a, plan, sm, w1 - w0, b, kvh, tile, s.rows * r.group, u0, u1, w0, block0 == u0,
+                                  block0 == u0 && block1 == u1);
+      return;
+    }
+    finish_item<T, D, TR, false>(a, plan, sm + warp * REGION, 1, b, kvh, tile, s.rows * r.group, u0, u1, worker, s0 == 0,
+                                 n == s.steps);
+    at = u += n;
+    if (u >= u_end) return;
+  }
+}
+
+template <typename T, int D, int MT>
+__global__ void __launch_bounds__(PA_WARPS * 32, 1) attend16_kernel(AttendArgs a) {
+  constexpr int KS = Cfg16<D>::KS, NG = KS / PG_GROUP, NC = D / 32, NV = D / 64, TR = 16 * MT;
+  const PagedView& c = a.c;
+  const PagedRows& r = a.r;
   const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-  const int worker = (threadIdx.x >> 5) * gridDim.x + blockIdx.x;   // few workers spread over the SMs
-  if (worker >= plan.workers) return;
-  long long u = work_start(plan, worker);
-  const long long u_end = work_start(plan, worker + 1);
   const float sc = r.scale * LOG2E;
 
-  while (u < u_end) {
-    const int b = work_find(mem.pre, c.batch, u);
-    const SeqWork s = seq_work<KS, TR>(r, mem.lens[b].x, mem.lens[b].y);
-    const int rem = (int)(u - mem.pre[b]), item = rem / s.steps, s0 = rem - item * s.steps;
-    const int n = (int)min((long long)(s.steps - s0), u_end - u);
-    const int kvh = item / s.tiles, tile = item - kvh * s.tiles;
-    u += n;
-
-    const bool fresh = r.k_new != nullptr, append = fresh && tile == 0;
+  attend_items<T, D, KS, TR>(a, [&](const SeqWork& s, int b, int kvh, int tile, int s0, int n, float* sm) {
     const long long new_off = b * r.n_b + kvh * r.n_h;
-    Keys16<T, D> ks{c, r, c.table + b * c.table_stride, kvh * c.head_stride, r.k_new + new_off, r.v_new + new_off,
-                    s.len, s.keys, g, t, fresh};
+    Keys16<T, D> ks{c, r, s, c.table + b * c.table_stride, kvh * c.head_stride, r.k_new + new_off, r.v_new + new_off, g, t};
     int pid[NG];
     long long off[NG];
     uint4 kf[KS / 8][NC], vf[NG][4][NV];
@@ -164,18 +360,16 @@ __global__ void __launch_bounds__(PA_WARPS * 32, MINB) attend16_kernel(AttendArg
     for (int x = 0; x < NG; ++x) pid[x] = ks.id(s0, x);
 
     uint32_t qa[MT][NC * 2][4];
-    int lim[MT][2];   // keys the fragment's rows see
+    int lim[MT][2];   // slots that the fragment's rows see
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
         const int m = tile * TR + mt * 16 + e * 8 + g, row = m / r.group, hq = kvh * r.group + m - row * r.group;
-        lim[mt][e] = r.causal ? s.len + row + 1 : s.keys;
+        lim[mt][e] = r.causal ? s.len + row + 1 : s.len;
 #pragma unroll
         for (int j = 0; j < NC; ++j) {
-          const uint4 x = row < s.rows ? __ldg(reinterpret_cast<const uint4*>(r.q + b * r.q_b + row * r.q_r +
-                                                                              hq * r.q_h + j * 64 + t * 16))
-                                       : make_uint4(0, 0, 0, 0);
+          const uint4 x = ldg_if(row < s.rows, r.q + b * r.q_b + row * r.q_r + hq * r.q_h + j * 64 + t * 16);
           qa[mt][2 * j][e] = x.x;
           qa[mt][2 * j][2 + e] = x.y;
           qa[mt][2 * j + 1][e] = x.z;
@@ -198,7 +392,6 @@ __global__ void __launch_bounds__(PA_WARPS * 32, MINB) attend16_kernel(AttendArg
       const bool full = ks.full(step), more = i + 1 < n;
       float S[MT][KS / 8][4];
       if (i >= 0) {
-        if (!full && append) ks.append_k(step, kf);
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
@@ -220,13 +413,14 @@ __global__ void __launch_bounds__(PA_WARPS * 32, MINB) attend16_kernel(AttendArg
       }
       if (i >= 0) {
         if (!full) {
+          const int first = ks.first(step), end = ks.end(step);
 #pragma unroll
           for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
             for (int kt = 0; kt < KS / 8; ++kt)
 #pragma unroll
               for (int x = 0; x < 4; ++x)
-                if (step * KS + kt * 8 + 2 * t + (x & 1) >= min(lim[mt][x >> 1], s.keys)) S[mt][kt][x] = -INFINITY;
+                if (first + kt * 8 + 2 * t + (x & 1) >= min(lim[mt][x >> 1], end)) S[mt][kt][x] = -INFINITY;
         }
         uint32_t pf[MT][KS / 8][2];
 #pragma unroll
@@ -265,10 +459,7 @@ __global__ void __launch_bounds__(PA_WARPS * 32, MINB) attend16_kernel(AttendArg
             }
           }
         }
-        if (!full) {
-          if (append) ks.append_v(step, vf);
-          guard_values<T, D, MT>(ks, step, lim, vf, O);
-        }
+        if (!full && ks.end(step) > s.len) guard_values<T, D, MT>(ks, step, lim, vf, O);
 #pragma unroll
         for (int x = 0; x < NG; ++x)
 #pragma unroll
@@ -287,10 +478,9 @@ __global__ void __launch_bounds__(PA_WARPS * 32, MINB) attend16_kernel(AttendArg
       }
       if (more) ks.load_v(step + 1, off, vf);
     }
+    if (tile == 0 && s.fresh && s0 <= s.psteps && s.psteps < s0 + n) append_rows(c, r, s, b, kvh, D * sizeof(T));
 
-    // the item's result: of row g (+ 8 e) a lane holds columns 64 j + 16 t .. + 15
-    const bool whole = n == s.steps;
-    float* part = a.ws + (size_t)(2 * worker + (s0 == 0 ? 1 : 0)) * (TR * (D + 2));
+    // of row g (+ 8 e) a lane holds columns 64 j + 16 t .. + 15
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
@@ -298,46 +488,23 @@ __global__ void __launch_bounds__(PA_WARPS * 32, MINB) attend16_kernel(AttendArg
         float l = l_run[mt][e];
         l += __shfl_xor_sync(0xffffffffu, l, 1);
         l += __shfl_xor_sync(0xffffffffu, l, 2);
-        const int in = mt * 16 + e * 8 + g, m = tile * TR + in, row = m / r.group;
-        if (row >= s.rows) continue;
-        const int hq = kvh * r.group + m - row * r.group;
-        if (whole) {
-          const size_t at = ((size_t)b * r.max_rows + row) * r.heads + hq;
-          const float inv = l > 0.f ? 1.f / l : 0.f;
-          if (a.lse && t == 0) a.lse[at] = (m_run[mt][e] + log2f(l)) * LN2;
-          uint32_t* o = reinterpret_cast<uint32_t*>(a.out + at * D * sizeof(T));
-#pragma unroll
-          for (int j = 0; j < NV; ++j)
-#pragma unroll
-            for (int x = 0; x < 2; ++x) {
-              const float* f[8];
-#pragma unroll
-              for (int d = 0; d < 8; ++d) f[d] = &O[mt][j * 8 + d][2 * e + x];
-              uint4 w;
-              w.x = Mma16<T>::pack(*f[0] * inv, *f[1] * inv);
-              w.y = Mma16<T>::pack(*f[2] * inv, *f[3] * inv);
-              w.z = Mma16<T>::pack(*f[4] * inv, *f[5] * inv);
-              w.w = Mma16<T>::pack(*f[6] * inv, *f[7] * inv);
-              *reinterpret_cast<uint4*>(o + (j * 64 + t * 16 + x * 8) / 2) = w;
-            }
-        } else {
-          if (t == 0) {
-            part[in] = m_run[mt][e];
-            part[TR + in] = l;
-          }
-          float* o = part + 2 * TR + in * D;
-#pragma unroll
-          for (int j = 0; j < NV; ++j)
-#pragma unroll
-            for (int x = 0; x < 2; ++x)
-#pragma unroll
-              for (int d = 0; d < 8; d += 4)
-                *reinterpret_cast<float4*>(o + j * 64 + t * 16 + x * 8 + d) =
-                    make_float4(O[mt][j * 8 + d][2 * e + x], O[mt][j * 8 + d + 1][2 * e + x],
-                                O[mt][j * 8 + d + 2][2 * e + x], O[mt][j * 8 + d + 3][2 * e + x]);
+        const int in = mt * 16 + e * 8 + g;
+        if (t == 0) {
+          sm[in] = m_run[mt][e];
+          sm[TR + in] = l;
         }
+        float* o = sm + 2 * TR + in * D;
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+#pragma unroll
+          for (int x = 0; x < 2; ++x)
+#pragma unroll
+            for (int d = 0; d < 8; d += 4)
+              *reinterpret_cast<float4*>(o + j * 64 + t * 16 + x * 8 + d) =
+                  make_float4(O[mt][j * 8 + d][2 * e + x], O[mt][j * 8 + d + 1][2 * e + x], O[mt][j * 8 + d + 2][2 * e + x],
+                              O[mt][j * 8 + d + 3][2 * e + x]);
       }
-  }
+  });
 }
 
 // fp32: plain fp32 products (no TF32), four rows a warp.  Eight lanes share a
@@ -345,38 +512,21 @@ __global__ void __launch_bounds__(PA_WARPS * 32, MINB) attend16_kernel(AttendArg
 // time; each group of eight lanes keeps its own running maximum, sum and
 // output over its keys, combined at the end of the item.
 template <int D>
-__global__ void __launch_bounds__(PA_WARPS * 32) attend32_kernel(AttendArgs a) {
+__global__ void __launch_bounds__(PA_WARPS * 32, 1) attend32_kernel(AttendArgs a) {
   constexpr int TR = 4, KS = D == 64 ? 16 : 8, IT = KS / 4, NC = D / 32;
   const PagedView& c = a.c;
   const PagedRows& r = a.r;
-  PlanMem mem;
-  const WorkPlan plan = work_plan(c, r, mem, a.max_workers, a.min_units, [&](int len, int rows) {
-    const SeqWork s = seq_work<KS, TR>(r, len, rows);
-    return (long long)c.kv_heads * s.tiles * s.steps;
-  });
-  pdl_launch();
   const int lane = threadIdx.x & 31, kg = lane >> 3, e = lane & 7;
-  const int worker = (threadIdx.x >> 5) * gridDim.x + blockIdx.x;
-  if (worker >= plan.workers) return;
-  long long u = work_start(plan, worker);
-  const long long u_end = work_start(plan, worker + 1);
   const float sc = r.scale * LOG2E;
 
-  while (u < u_end) {
-    const int b = work_find(mem.pre, c.batch, u);
-    const SeqWork s = seq_work<KS, TR>(r, mem.lens[b].x, mem.lens[b].y);
-    const int rem = (int)(u - mem.pre[b]), item = rem / s.steps, s0 = rem - item * s.steps;
-    const int n = (int)min((long long)(s.steps - s0), u_end - u);
-    const int kvh = item / s.tiles, tile = item - kvh * s.tiles;
-    u += n;
+  attend_items<float, D, KS, TR>(a, [&](const SeqWork& s, int b, int kvh, int tile, int s0, int n, float* sm) {
     const int* table_row = c.table + b * c.table_stride;
-
     float q[TR][NC * 4], O[TR][NC * 4], m_run[TR], l_run[TR];
     int lim[TR];
 #pragma unroll
     for (int x = 0; x < TR; ++x) {
       const int m = tile * TR + x, row = m / r.group, hq = kvh * r.group + m - row * r.group;
-      lim[x] = row < s.rows ? (r.causal ? s.len + row + 1 : s.keys) : 0;
+      lim[x] = row < s.rows ? (r.causal ? s.len + row + 1 : s.len) : 0;
       m_run[x] = -INFINITY;
       l_run[x] = 0.f;
 #pragma unroll
@@ -389,38 +539,30 @@ __global__ void __launch_bounds__(PA_WARPS * 32) attend32_kernel(AttendArgs a) {
       }
     }
     for (int i = 0; i < n; ++i) {
-      const int key0 = (s0 + i) * KS;
-      const int grp = key0 / PG_GROUP;
-      const int pid = paged_id(c, table_row, grp);
-      const bool pid_ok = pid != 0 || __ldg(table_row + c.groups.div((uint32_t)grp)) == 0;   // no stand-in
-      const long long off =
-          paged_offset(c, pid, grp) + kvh * c.head_stride + (long long)(key0 % PG_GROUP + kg) * c.slot_stride + e * 16;
+      const int step = s0 + i;
+      const bool paged = step < s.psteps;
+      const int first = paged ? step * KS : s.len + (step - s.psteps) * KS, end = paged ? s.paged : s.len + s.fresh;
+      const char *kp, *vp;
+      long long stride;
+      if (paged) {
+        const int grp = first / PG_GROUP;
+        const long long off = paged_offset(c, paged_id(c, table_row, grp), grp) + kvh * c.head_stride +
+                              (long long)(first % PG_GROUP) * c.slot_stride;
+        kp = c.k + off, vp = c.v + off, stride = c.slot_stride;
+      } else {
+        const long long off = b * r.n_b + (long long)(first - s.len) * r.n_r + kvh * r.n_h;
+        kp = r.k_new + off, vp = r.v_new + off, stride = r.n_r;
+      }
       float4 kf[IT][NC], vf[IT][NC];
 #pragma unroll
       for (int k = 0; k < IT; ++k) {
-        const int key = key0 + 4 * k + kg;
-        const bool fresh = r.k_new != nullptr && key >= s.len, in = key < s.keys;
-        const char* kp = c.k + off + (long long)(4 * k) * c.slot_stride;
-        const char* vp = c.v + off + (long long)(4 * k) * c.slot_stride;
-        const long long no = b * r.n_b + (long long)(key - s.len) * r.n_r + kvh * r.n_h + e * 16;
-        const char* ksrc = fresh ? r.k_new + no : kp;
-        const char* vsrc = fresh ? r.v_new + no : vp;
+        const bool in = first + 4 * k + kg < end;
+        const long long at = (4 * k + kg) * stride + e * 16;
 #pragma unroll
         for (int j = 0; j < NC; ++j) {
-          kf[k][j] = in ? *reinterpret_cast<const float4*>(ksrc + j * 128) : make_float4(0.f, 0.f, 0.f, 0.f);
-          vf[k][j] = in ? *reinterpret_cast<const float4*>(vsrc + j * 128) : make_float4(0.f, 0.f, 0.f, 0.f);
-        }
-      }
-      if (r.k_new != nullptr && tile == 0 && pid_ok && key0 + KS > s.len) {   // the step's new rows go to their page
-#pragma unroll
-        for (int k = 0; k < IT; ++k) {
-          const int key = key0 + 4 * k + kg;
-          if (key < s.len || key >= s.keys) continue;
-#pragma unroll
-          for (int j = 0; j < NC; ++j) {
-            *reinterpret_cast<float4*>(c.k + off + (long long)(4 * k) * c.slot_stride + j * 128) = kf[k][j];
-            *reinterpret_cast<float4*>(c.v + off + (long long)(4 * k) * c.slot_stride + j * 128) = vf[k][j];
-          }
+          const uint4 x = ldg_if(in, kp + at + j * 128), y = ldg_if(in, vp + at + j * 128);
+          kf[k][j] = *reinterpret_cast<const float4*>(&x);
+          vf[k][j] = *reinterpret_cast<const float4*>(&y);
         }
       }
 #pragma unroll
@@ -436,7 +578,7 @@ __global__ void __launch_bounds__(PA_WARPS * 32) attend32_kernel(AttendArgs a) {
           d += __shfl_xor_sync(0xffffffffu, d, 1);
           d += __shfl_xor_sync(0xffffffffu, d, 2);
           d += __shfl_xor_sync(0xffffffffu, d, 4);
-          S[k] = key0 + 4 * k + kg < min(lim[x], s.keys) ? d : -INFINITY;
+          S[k] = first + 4 * k + kg < min(lim[x], end) ? d : -INFINITY;
           mx = fmaxf(mx, S[k]);
         }
         const float m = mx == -INFINITY ? 0.f : mx, f = ex2(m_run[x] - m);
@@ -448,7 +590,7 @@ __global__ void __launch_bounds__(PA_WARPS * 32) attend32_kernel(AttendArgs a) {
         for (int k = 0; k < IT; ++k) {
           const float p = ex2(S[k] - m);
           l_run[x] += p;
-          if (key0 + 4 * k + kg >= lim[x]) continue;   // hidden: an infinity or NaN there must not reach the row
+          if (first + 4 * k + kg >= lim[x]) continue;   // hidden: an infinity or NaN there must not reach the row
 #pragma unroll
           for (int j = 0; j < NC; ++j) {
             O[x][4 * j] += p * vf[k][j].x;
@@ -459,8 +601,7 @@ __global__ void __launch_bounds__(PA_WARPS * 32) attend32_kernel(AttendArgs a) {
         }
       }
     }
-    const bool whole = n == s.steps;
-    float* part = a.ws + (size_t)(2 * worker + (s0 == 0 ? 1 : 0)) * (TR * (D + 2));
+    if (tile == 0 && s.fresh && s0 <= s.psteps && s.psteps < s0 + n) append_rows(c, r, s, b, kvh, D * sizeof(float));
 #pragma unroll
     for (int x = 0; x < TR; ++x) {
       float mx = fmaxf(m_run[x], __shfl_xor_sync(0xffffffffu, m_run[x], 8));
@@ -476,168 +617,48 @@ __global__ void __launch_bounds__(PA_WARPS * 32) attend32_kernel(AttendArgs a) {
         o += __shfl_xor_sync(0xffffffffu, o, 16);
         O[x][j] = o;
       }
-      const int m = tile * TR + x, row = m / r.group;
-      if (row >= s.rows || kg != 0) continue;
-      if (whole) {
-        const size_t at = ((size_t)b * r.max_rows + row) * r.heads + kvh * r.group + m - row * r.group;
-        const float inv = l > 0.f ? 1.f / l : 0.f;
-        if (a.lse && e == 0) a.lse[at] = (mx + log2f(l)) * LN2;
-        float4* o = reinterpret_cast<float4*>(a.out + at * D * sizeof(float));
-#pragma unroll
-        for (int j = 0; j < NC; ++j)
-          o[e + 8 * j] = make_float4(O[x][4 * j] * inv, O[x][4 * j + 1] * inv, O[x][4 * j + 2] * inv, O[x][4 * j + 3] * inv);
-      } else {
-        if (e == 0) {
-          part[x] = mx;
-          part[TR + x] = l;
-        }
-        float4* o = reinterpret_cast<float4*>(part + 2 * TR + x * D);
-#pragma unroll
-        for (int j = 0; j < NC; ++j) o[e + 8 * j] = make_float4(O[x][4 * j], O[x][4 * j + 1], O[x][4 * j + 2], O[x][4 * j + 3]);
+      if (kg != 0) continue;
+      if (e == 0) {
+        sm[x] = mx;
+        sm[TR + x] = l;
       }
+      float4* o = reinterpret_cast<float4*>(sm + 2 * TR + x * D);
+#pragma unroll
+      for (int j = 0; j < NC; ++j) o[e + 8 * j] = make_float4(O[x][4 * j], O[x][4 * j + 1], O[x][4 * j + 2], O[x][4 * j + 3]);
     }
-  }
-}
-
-// Joins the items that several warps worked on, in key order, and fills the
-// rows that have no keys.  WPT warps share one (sequence, row, head): many
-// partials and few rows with one long sequence, the reverse in a batch.
-constexpr int PJ_WARPS = 8;
-
-template <typename T, int D, int KS, int TR, int WPT>
-__global__ void __launch_bounds__(PJ_WARPS * 32) join_kernel(AttendArgs a) {
-  constexpr int LP = D / 4;            // lanes that hold one output row, 4 columns each
-  constexpr int PP = 32 / LP * WPT;    // partials at a time
-  __shared__ float s_m[PJ_WARPS], s_l[PJ_WARPS], s_o[PJ_WARPS][D];
-  const PagedView& c = a.c;
-  const PagedRows& r = a.r;
-  PlanMem mem;
-  const WorkPlan plan = work_plan(c, r, mem, a.max_workers, a.min_units, [&](int len, int rows) {
-    const SeqWork s = seq_work<KS, TR>(r, len, rows);
-    return (long long)c.kv_heads * s.tiles * s.steps;
   });
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const long long tasks = (long long)c.batch * r.max_rows * r.heads;
-  const long long task = (long long)blockIdx.x * (PJ_WARPS / WPT) + warp / WPT;
-  const bool live = task < tasks;
-  pdl_wait();
-  int wf = 0, wl = 0, in = 0;
-  long long at = task;
-  if (live) {
-    const int hq = (int)(task % r.heads), row = (int)(task / r.heads % r.max_rows), b = (int)(task / r.heads / r.max_rows);
-    const SeqWork s = seq_work<KS, TR>(r, mem.lens[b].x, mem.lens[b].y);
-    if (row >= s.rows || s.keys == 0) {
-      if (warp % WPT == 0) {
-        if (a.lse && lane == 0) a.lse[at] = -INFINITY;
-        T* o = reinterpret_cast<T*>(a.out) + at * D;
-        for (int d = lane; d < D; d += 32) o[d] = T(0.f);
-      }
-    } else {
-      const int kvh = hq / r.group, m = row * r.group + hq - kvh * r.group, tile = m / TR;
-      in = m - tile * TR;
-      const long long u0 = mem.pre[b] + (long long)(kvh * s.tiles + tile) * s.steps;
-      wf = work_owner(plan, u0);
-      wl = work_owner(plan, u0 + s.steps - 1);
-    }
-  }
-  const bool join = live && wl > wf;
-  if (WPT == 1 && !join) return;
-  const int sub = lane / LP, col = (lane % LP) * 4;
-  float m = -INFINITY, l = 0.f;
-  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-  if (join) {
-#pragma unroll 4
-    for (int w = wf + (warp % WPT) * (32 / LP) + sub; w <= wl; w += PP) {
-      const float* part = a.ws + (size_t)(2 * w + (w == wf ? 1 : 0)) * (TR * (D + 2));
-      const float pm = part[in], pl = part[TR + in];
-      const float4 po = *reinterpret_cast<const float4*>(part + 2 * TR + in * D + col);
-      const float mx = fmaxf(m, pm), z = mx == -INFINITY ? 0.f : mx, f0 = ex2(m - z), f1 = ex2(pm - z);
-      m = mx;
-      l = l * f0 + pl * f1;
-      o.x = o.x * f0 + po.x * f1;
-      o.y = o.y * f0 + po.y * f1;
-      o.z = o.z * f0 + po.z * f1;
-      o.w = o.w * f0 + po.w * f1;
-    }
-    if (LP < 32) {
-      const float pm = __shfl_xor_sync(0xffffffffu, m, 16), pl = __shfl_xor_sync(0xffffffffu, l, 16);
-      const float px = __shfl_xor_sync(0xffffffffu, o.x, 16), py = __shfl_xor_sync(0xffffffffu, o.y, 16);
-      const float pz = __shfl_xor_sync(0xffffffffu, o.z, 16), pw = __shfl_xor_sync(0xffffffffu, o.w, 16);
-      const float mx = fmaxf(m, pm), z = mx == -INFINITY ? 0.f : mx, f0 = ex2(m - z), f1 = ex2(pm - z);
-      m = mx;
-      l = l * f0 + pl * f1;
-      o = make_float4(o.x * f0 + px * f1, o.y * f0 + py * f1, o.z * f0 + pz * f1, o.w * f0 + pw * f1);
-    }
-  }
-  if (WPT > 1) {
-    if (join && sub == 0) {
-      if (lane == 0) {
-        s_m[warp] = m;
-        s_l[warp] = l;
-      }
-      *reinterpret_cast<float4*>(&s_o[warp][col]) = o;
-    }
-    __syncthreads();
-    if (!join || warp % WPT != 0 || sub != 0) return;
-    m = -INFINITY;
-#pragma unroll
-    for (int w = 0; w < WPT; ++w) m = fmaxf(m, s_m[warp + w]);
-    l = 0.f;
-    o = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-    for (int w = 0; w < WPT; ++w) {
-      const float f = m == -INFINITY ? 0.f : ex2(s_m[warp + w] - m);
-      const float4 po = *reinterpret_cast<const float4*>(&s_o[warp + w][col]);
-      l += s_l[warp + w] * f;
-      o = make_float4(o.x + po.x * f, o.y + po.y * f, o.z + po.z * f, o.w + po.w * f);
-    }
-  }
-  if (sub != 0) return;
-  const float inv = l > 0.f ? 1.f / l : 0.f;
-  if (a.lse && lane == 0) a.lse[at] = (m + log2f(l)) * LN2;
-  T* out = reinterpret_cast<T*>(a.out) + at * D + col;
-  if constexpr (sizeof(T) == 4) {
-    *reinterpret_cast<float4*>(out) = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
-  } else {
-    *reinterpret_cast<uint2*>(out) = make_uint2(Mma16<T>::pack(o.x * inv, o.y * inv), Mma16<T>::pack(o.z * inv, o.w * inv));
-  }
 }
 
-struct Shape {   // of one call's kernels
-  int tr, blocks_per_sm;
-};
-Shape attend_shape(int dtype, int dim, int m_rows) {
-  if (dtype == 0) return {4, 2};
-  if (dim == 128) return {16, 2};
-  return m_rows > 16 ? Shape{32, 2} : Shape{16, 3};
+int attend_tile(int dtype, int dim, int m_rows) { return dtype == 0 ? 4 : dim == 64 && m_rows > 16 ? 32 : 16; }
+int attend_grid() {
+  const int most = MAX_WORKERS / PA_WARPS, sms = paged_sm_count();
+  return sms < most ? sms : most;
 }
+int64_t attend_ws_bytes(int tr, int dim) { return MAX_WORKERS * 4 + (int64_t)attend_grid() * PA_WARPS * 2 * tr * (dim + 2) * 4; }
 
-template <typename T, int D, int KS, int TR>
-cudaError_t launch_join(const AttendArgs& a, size_t smem, cudaStream_t st) {
-  const long long tasks = (long long)a.c.batch * a.r.max_rows * a.r.heads;
-  // Whole blocks join one row each while the rows alone do not fill the SMs.
-  if (tasks < 152 * 2)
-    return launch_ex(join_kernel<T, D, KS, TR, PJ_WARPS>, dim3((unsigned)tasks), dim3(PJ_WARPS * 32), smem, st, true, 1, a);
-  return launch_ex(join_kernel<T, D, KS, TR, 1>, dim3((unsigned)((tasks + PJ_WARPS - 1) / PJ_WARPS)), dim3(PJ_WARPS * 32),
-                   smem, st, true, 1, a);
-}
-
-template <typename T, int D, int MT, int MINB>
-cudaError_t launch16(const AttendArgs& a, int grid, size_t smem, cudaStream_t st) {
-  cudaError_t e = launch_ex(attend16_kernel<T, D, MT, MINB>, dim3(grid), dim3(PA_WARPS * 32), smem, st, false, 1, a);
+// One block an SM.  The shared memory above 48 KB that a kernel needs is asked for once a device.
+template <auto kernel, int D, int TR>
+cudaError_t launch_attend(const AttendArgs& a, cudaStream_t st) {
+  constexpr size_t REGIONS = (size_t)PA_WARPS * Part<D, TR>::STAGE * Part<D, TR>::FLOATS * 4;
+  static std::atomic<uint64_t> ready{0};
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
-  return launch_join<T, D, Cfg16<D>::KS, 16 * MT>(a, smem, st);
+  const uint64_t bit = 1ull << (dev & 63);
+  if (!(ready.load(std::memory_order_acquire) & bit)) {
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(REGIONS + plan_bytes(PG_MAX_BATCH)));
+    if (e != cudaSuccess) return e;
+    ready.fetch_or(bit, std::memory_order_release);
+  }
+  kernel<<<a.max_workers / PA_WARPS, PA_WARPS * 32, REGIONS + plan_bytes(a.c.batch), st>>>(a);
+  return cudaGetLastError();
 }
-template <int D>
-cudaError_t launch32(const AttendArgs& a, int grid, size_t smem, cudaStream_t st) {
-  cudaError_t e = launch_ex(attend32_kernel<D>, dim3(grid), dim3(PA_WARPS * 32), smem, st, false, 1, a);
-  if (e != cudaSuccess) return e;
-  return launch_join<float, D, D == 64 ? 16 : 8, 4>(a, smem, st);
-}
+
 template <typename T>
-cudaError_t launch16_dim(const AttendArgs& a, int dim, int tr, int grid, size_t smem, cudaStream_t st) {
-  if (dim == 128) return launch16<T, 128, 1, 2>(a, grid, smem, st);
-  return tr == 32 ? launch16<T, 64, 2, 2>(a, grid, smem, st) : launch16<T, 64, 1, 3>(a, grid, smem, st);
+cudaError_t launch16(const AttendArgs& a, int dim, int tr, cudaStream_t st) {
+  if (dim == 128) return launch_attend<attend16_kernel<T, 128, 1>, 128, 16>(a, st);
+  if (tr == 32) return launch_attend<attend16_kernel<T, 64, 2>, 64, 32>(a, st);
+  return launch_attend<attend16_kernel<T, 64, 1>, 64, 16>(a, st);
 }
 
 }  // namespace
@@ -652,8 +673,7 @@ int64_t asr_spec_paged_attend_ws(const asr_paged_cache* c, const asr_paged_rows*
   PagedRows w;
   if (int rc = paged_view(c, &v)) return rc;
   if (int rc = paged_rows(c, r, &w)) return rc;
-  const Shape s = attend_shape(c->dtype, c->head_dim, w.max_rows * w.group);
-  return (int64_t)paged_sm_count() * s.blocks_per_sm * PA_WARPS * 2 * s.tr * (c->head_dim + 2) * 4;
+  return attend_ws_bytes(attend_tile(c->dtype, c->head_dim, w.max_rows * w.group), c->head_dim);
 }
 
 int asr_spec_paged_attend(const asr_paged_cache* c, const asr_paged_rows* r, void* out, float* lse, void* ws,
@@ -662,23 +682,23 @@ int asr_spec_paged_attend(const asr_paged_cache* c, const asr_paged_rows* r, voi
   if (int rc = paged_view(c, &a.c)) return rc;
   if (int rc = paged_rows(c, r, &a.r)) return rc;
   if (!out || !ws || ((uintptr_t)out | (uintptr_t)ws) % 16 || (uintptr_t)lse % 4) return ASR_E_INVAL;
-  const Shape s = attend_shape(c->dtype, c->head_dim, a.r.max_rows * a.r.group);
-  const int grid = paged_sm_count() * s.blocks_per_sm;
-  if (ws_bytes < (int64_t)grid * PA_WARPS * 2 * s.tr * (c->head_dim + 2) * 4) return ASR_E_CAPACITY;
-  const long long tiles = ((long long)a.r.max_rows * a.r.group + s.tr - 1) / s.tr;
-  if (tiles * c->kv_heads * ((long long)a.c.max_slots / 8 + 1) > 0x7fffffffll) return ASR_E_CAPACITY;   // 32-bit units a sequence
-  if ((long long)c->batch * a.r.max_rows * a.r.heads > 0x7fffffffll) return ASR_E_CAPACITY;
+  const int tr = attend_tile(c->dtype, c->head_dim, a.r.max_rows * a.r.group);
+  if (ws_bytes < attend_ws_bytes(tr, c->head_dim)) return ASR_E_CAPACITY;
+  const long long tiles = ((long long)a.r.max_rows * a.r.group + tr - 1) / tr;
+  if (tiles * c->kv_heads * c->batch * ((long long)a.c.max_slots / 8 + a.r.max_rows / 8 + 2) > 0x7fffffffll)
+    return ASR_E_CAPACITY;   // 32-bit units
   a.out = static_cast<char*>(out);
   a.lse = lse;
-  a.ws = static_cast<float*>(ws);
-  a.max_workers = grid * PA_WARPS;
-  a.min_units = 1;
-  const size_t smem = plan_bytes(c->batch);
+  a.tickets = static_cast<int*>(ws);
+  a.ws = reinterpret_cast<float*>(a.tickets + MAX_WORKERS);
+  a.max_workers = attend_grid() * PA_WARPS;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   cudaError_t e;
-  if (c->dtype == 0) e = c->head_dim == 64 ? launch32<64>(a, grid, smem, st) : launch32<128>(a, grid, smem, st);
-  else if (c->dtype == 1) e = launch16_dim<__nv_bfloat16>(a, c->head_dim, s.tr, grid, smem, st);
-  else e = launch16_dim<__half>(a, c->head_dim, s.tr, grid, smem, st);
+  if (c->dtype == 0)
+    e = c->head_dim == 64 ? launch_attend<attend32_kernel<64>, 64, 4>(a, st)
+                          : launch_attend<attend32_kernel<128>, 128, 4>(a, st);
+  else if (c->dtype == 1) e = launch16<__nv_bfloat16>(a, c->head_dim, tr, st);
+  else e = launch16<__half>(a, c->head_dim, tr, st);
   return e == cudaSuccess ? ASR_OK : ASR_E_CUDA;
 }
 

@@ -29,27 +29,22 @@ struct WeighArgs {
   int cap;
 };
 
-struct WeighSeq {
-  int len, rows, keys, steps, tiles;
-};
+// A sequence without rows keeps its scores: its slots still take part.
 template <int KS, int TR>
-__device__ __forceinline__ WeighSeq weigh_seq(const WeighArgs& a, int len, int rows) {
-  WeighSeq s;
-  s.len = len;
-  s.rows = rows;
-  s.keys = len + (a.r.causal ? rows : 0);   // a sequence without rows keeps its scores
-  if (s.keys > a.cap) {
+__device__ __forceinline__ SeqWork weigh_seq(const WeighArgs& a, int len, int rows) {
+  SeqWork s = seq_work<KS, TR>(a.r, len, rows);
+  s.paged = len + (a.r.causal ? rows : 0);
+  if (s.paged > a.cap) {
     if (a.c.status) set_status(a.c.status, ST_CAPACITY);
-    s.len = s.rows = s.keys = 0;
+    s.len = s.rows = s.paged = s.tiles = 0;
   }
-  s.steps = (s.keys + KS - 1) / KS;
-  s.tiles = (s.rows * a.r.group + TR - 1) / TR;
+  s.psteps = s.steps = (s.paged + KS - 1) / KS;
   return s;
 }
 
 // One lane's slot: add the weight, or start the slot of a new row.
-__device__ __forceinline__ void put_score(const WeighArgs& a, const WeighSeq& s, int b, int kvh, int key, float w) {
-  if (key >= s.keys) return;
+__device__ __forceinline__ void put_score(const WeighArgs& a, const SeqWork& s, int b, int kvh, int key, float w) {
+  if (key >= s.paged) return;
   const long long at = b * a.score_b + kvh * a.score_h + key;
   a.out[at] = (key < s.len && a.score ? a.score[at] : 0.f) + w;
   if (a.pos && key >= s.len) a.pos[at] = a.first_pos[b] + key - s.len;
@@ -61,23 +56,23 @@ __global__ void __launch_bounds__(PW_WARPS * 32, 4) weigh16_kernel(WeighArgs a, 
   const PagedView& c = a.c;
   const PagedRows& r = a.r;
   PlanMem mem;
-  const WorkPlan plan = work_plan(c, r, mem, max_workers, 1, [&](int len, int rows) {
-    return (long long)c.kv_heads * weigh_seq<KS, TR>(a, len, rows).steps;
+  const WorkPlan plan = work_plan(c, r, mem, max_workers, [&](int len, int rows) {
+    return c.kv_heads * weigh_seq<KS, TR>(a, len, rows).steps;
   });
   const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   const int worker = (threadIdx.x >> 5) * gridDim.x + blockIdx.x;
-  if (worker >= plan.workers) return;
-  long long u = work_start(plan, worker);
-  const long long u_end = work_start(plan, worker + 1);
+  if (plan.units == 0 || worker >= plan.workers) return;
+  int u = plan.start(worker);
+  const int u_end = plan.start(worker + 1);
   const float sc = r.scale * LOG2E;
 
   while (u < u_end) {
     const int b = work_find(mem.pre, c.batch, u);
-    const WeighSeq s = weigh_seq<KS, TR>(a, mem.lens[b].x, mem.lens[b].y);
-    const int rem = (int)(u - mem.pre[b]), kvh = rem / s.steps, s0 = rem - kvh * s.steps;
-    const int n = (int)min((long long)(s.steps - s0), u_end - u);
+    const SeqWork s = weigh_seq<KS, TR>(a, mem.lens[b].x, mem.lens[b].y);
+    const int rem = u - mem.pre[b], kvh = rem / s.steps, s0 = rem - kvh * s.steps;
+    const int n = min(s.steps - s0, u_end - u);
     u += n;
-    Keys16<T, D> ks{c, r, c.table + b * c.table_stride, kvh * c.head_stride, nullptr, nullptr, s.keys, s.keys, g, t, false};
+    Keys16<T, D> ks{c, r, s, c.table + b * c.table_stride, kvh * c.head_stride, nullptr, nullptr, g, t};
     int pid[NG];
     long long off[NG];
     uint4 kf[KS / 8][NC];
@@ -98,7 +93,7 @@ __global__ void __launch_bounds__(PW_WARPS * 32, 4) weigh16_kernel(WeighArgs a, 
       for (int e = 0; e < 2; ++e) {
         const int m = tile * TR + e * 8 + g, row = m / r.group, hq = kvh * r.group + m - row * r.group;
         const bool in = row < s.rows;
-        lim[e] = !in ? 0 : r.causal ? s.len + row + 1 : s.keys;
+        lim[e] = !in ? 0 : r.causal ? s.len + row + 1 : s.paged;
         const float x = in ? a.lse[b * a.lse_b + row * a.lse_r + hq] : -INFINITY;
         ls[e] = x == -INFINITY ? INFINITY : x * LOG2E;   // an empty row weighs nothing
 #pragma unroll
@@ -165,20 +160,20 @@ __global__ void __launch_bounds__(PW_WARPS * 32) weigh32_kernel(WeighArgs a, int
   const PagedView& c = a.c;
   const PagedRows& r = a.r;
   PlanMem mem;
-  const WorkPlan plan = work_plan(c, r, mem, max_workers, 1, [&](int len, int rows) {
-    return (long long)c.kv_heads * weigh_seq<KS, 1>(a, len, rows).steps;
+  const WorkPlan plan = work_plan(c, r, mem, max_workers, [&](int len, int rows) {
+    return c.kv_heads * weigh_seq<KS, 1>(a, len, rows).steps;
   });
   const int lane = threadIdx.x & 31, kg = lane >> 3, e = lane & 7;
   const int worker = (threadIdx.x >> 5) * gridDim.x + blockIdx.x;
-  if (worker >= plan.workers) return;
-  long long u = work_start(plan, worker);
-  const long long u_end = work_start(plan, worker + 1);
+  if (plan.units == 0 || worker >= plan.workers) return;
+  int u = plan.start(worker);
+  const int u_end = plan.start(worker + 1);
   const float sc = r.scale * LOG2E;
 
   while (u < u_end) {
     const int b = work_find(mem.pre, c.batch, u);
-    const WeighSeq s = weigh_seq<KS, 1>(a, mem.lens[b].x, mem.lens[b].y);
-    const int rem = (int)(u - mem.pre[b]), kvh = rem / s.steps, step = rem - kvh * s.steps;
+    const SeqWork s = weigh_seq<KS, 1>(a, mem.lens[b].x, mem.lens[b].y);
+    const int rem = u - mem.pre[b], kvh = rem / s.steps, step = rem - kvh * s.steps;
     ++u;
     const int grp = step;
     float4 kf[IT][NC];
@@ -189,7 +184,7 @@ __global__ void __launch_bounds__(PW_WARPS * 32) weigh32_kernel(WeighArgs a, int
       for (int k = 0; k < IT; ++k)
 #pragma unroll
         for (int j = 0; j < NC; ++j)
-          kf[k][j] = step * KS + 4 * k + kg < s.keys
+          kf[k][j] = step * KS + 4 * k + kg < s.paged
                          ? *reinterpret_cast<const float4*>(p + (long long)(4 * k) * c.slot_stride + j * 128)
                          : make_float4(0.f, 0.f, 0.f, 0.f);
     }
@@ -198,7 +193,7 @@ __global__ void __launch_bounds__(PW_WARPS * 32) weigh32_kernel(WeighArgs a, int
     for (int k = 0; k < IT; ++k) w[k] = 0.f;
     for (int m = 0; m < s.tiles; ++m) {
       const int row = m / r.group, hq = kvh * r.group + m - row * r.group;
-      const int lim = r.causal ? s.len + row + 1 : s.keys;
+      const int lim = r.causal ? s.len + row + 1 : s.paged;
       const float x = a.lse[b * a.lse_b + row * a.lse_r + hq], ls = x == -INFINITY ? INFINITY : x * LOG2E;
       float d[IT];
 #pragma unroll
@@ -240,7 +235,7 @@ extern "C" int asr_spec_paged_weigh(const asr_paged_cache* c, const asr_paged_ro
   if ((sc->pos != nullptr) != (sc->first_pos != nullptr)) return ASR_E_INVAL;
   if (((uintptr_t)sc->score | (uintptr_t)sc->score_out | (uintptr_t)sc->pos | (uintptr_t)sc->first_pos | (uintptr_t)lse) % 4)
     return ASR_E_INVAL;
-  if ((long long)c->kv_heads * (a.c.max_slots / PG_GROUP) > 0x7fffffffll) return ASR_E_CAPACITY;
+  if ((long long)c->kv_heads * c->batch * (a.c.max_slots / PG_GROUP + 1) > 0x7fffffffll) return ASR_E_CAPACITY;   // 32-bit units
   a.lse = lse;
   a.lse_b = lse_batch_stride;
   a.lse_r = lse_row_stride;

@@ -115,14 +115,15 @@ class PagedCache:
             self._status.zero_()
         return s
 
-    def _workspace(self, stream: int, n: int):
-        """``n`` bytes that only calls on this stream use; a capture gets bytes of its graph's own."""
-        if _capturing():
-            return torch.empty(n, dtype=torch.uint8, device=self.device)
-        ws = self._ws.get(stream)
+    def _workspace(self, op: str, stream: int, n: int) -> int:
+        """Address of ``n`` bytes, zero at first, that only this operator's calls on this stream use; a capture gets
+        bytes of its graph's own."""
+        ws = None if _capturing() else self._ws.get((op, stream))
         if ws is None or ws.numel() < n:
-            ws = self._ws[stream] = torch.empty(n, dtype=torch.uint8, device=self.device)
-        return ws
+            ws = torch.zeros(n, dtype=torch.uint8, device=self.device)
+            if not _capturing():
+                self._ws[(op, stream)] = ws
+        return ws.data_ptr()
 
     def _rows(self, q, kv_len, rows, k_new, v_new, causal, scale):
         B, K, D = self.batch, self.kv_heads, self.head_dim
@@ -186,9 +187,8 @@ class PagedCache:
         if lse is None:
             lse = torch.empty(lse_shape, dtype=torch.float32, device=self.device)
         stream = _raw_stream(self._index)
-        ws = self._workspace(stream, n)
-        _check(self._lib.asr_spec_paged_attend(self._ref, ctypes.byref(r), out.data_ptr(), lse.data_ptr(), ws.data_ptr(), n,
-                                               stream), "asr_spec_paged_attend")
+        _check(self._lib.asr_spec_paged_attend(self._ref, ctypes.byref(r), out.data_ptr(), lse.data_ptr(),
+                                               self._workspace("attend", stream, n), n, stream), "asr_spec_paged_attend")
         return out, lse
 
     def weigh(self, q, lse, kv_len, score, *, rows=None, causal=True, scale: Optional[float] = None, out=None, pos=None,
@@ -264,9 +264,9 @@ class PagedCache:
         s = A.AsrPagedScores.from_buffer_copy(slots)
         s.score, s.pos, s.score_out, s.pos_out = score.data_ptr(), pos.data_ptr(), score_out.data_ptr(), pos_out.data_ptr()
         stream = _raw_stream(self._index)
-        ws = self._workspace(stream, n)
         _check(self._lib.asr_spec_paged_evict(self._ref, ctypes.byref(s), lens.data_ptr(), seen.data_ptr(), budget, recent,
-                                              first, lens_out.data_ptr(), ws.data_ptr(), n, stream), "asr_spec_paged_evict")
+                                              first, lens_out.data_ptr(), self._workspace("evict", stream, n), n, stream),
+               "asr_spec_paged_evict")
         return lens_out, score_out, pos_out
 
     def _evict_layout(self, lens, score, pos, seen, budget, recent, first, lens_out, score_out, pos_out):
