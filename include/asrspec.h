@@ -548,12 +548,10 @@ typedef struct {
  * utterance that sits out returns accepted 0, token -1, step 0, prob 0; so
  * does one with a token outside [0, vocab) (ASR_ST_BAD_TOKEN) or lens outside
  * [-1, k] (ASR_ST_BAD_LENS).  All arithmetic is fp32.
- * ws: asr_spec_accept_sampled_ws bytes, 8-byte aligned, no initial contents.
  * status: as the cache's, may be NULL. */
-int64_t asr_spec_accept_sampled_ws(int32_t batch, int32_t k);
 int asr_spec_accept_sampled(const asr_sampled_logits* logits, const int32_t* draft, const int32_t* lens, const float* u,
                             const float* race, int64_t race_stride, float temperature, int32_t* accepted, int32_t* token,
-                            int32_t* step, float* prob, int32_t* status, void* ws, int64_t ws_bytes, void* stream);
+                            int32_t* step, float* prob, int32_t* status, void* stream);
 
 #ifdef __cplusplus
 }

@@ -31,7 +31,7 @@ EXPORTED = [
     "asr_spec_verify_tree", "asr_spec_restart", "asr_spec_fewrow_trace", "asr_spec_fewrow_trace_read",
     "asr_spec_debug_anchor_profile", "asr_spec_draft_create", "asr_spec_draft_propose",
     "asr_spec_draft_set_threshold", "asr_spec_paged_attend", "asr_spec_paged_attend_ws", "asr_spec_paged_weigh",
-    "asr_spec_paged_evict", "asr_spec_paged_evict_ws", "asr_spec_accept_sampled", "asr_spec_accept_sampled_ws",
+    "asr_spec_paged_evict", "asr_spec_paged_evict_ws", "asr_spec_accept_sampled",
 ]
 DRAFT_WIN = {"anchor": 0, "shifted": 1, "random": 2, None: 3}
 PROF_CLASSES = ["qkv", "resid", "query", "mlp_up", "self_attn", "cross_attn", "lm_head", "layernorm", "other",
@@ -144,8 +144,7 @@ def lib():
     L.asr_spec_paged_weigh.argtypes = [vp, vp, vp, vp, i64, i64, vp]
     L.asr_spec_paged_evict.argtypes = [vp, vp, vp, vp, i32, i32, i32, vp, vp, i64, vp]
     L.asr_spec_paged_evict_ws.argtypes = [vp, vp, i32]
-    L.asr_spec_accept_sampled.argtypes = [vp, p32, p32, vp, vp, i64, ctypes.c_float, p32, p32, p32, vp, p32, vp, i64, vp]
-    L.asr_spec_accept_sampled_ws.argtypes = [i32, i32]
+    L.asr_spec_accept_sampled.argtypes = [vp, p32, p32, vp, vp, i64, ctypes.c_float, p32, p32, p32, vp, p32, vp]
     for name in EXPORTED:
         if name not in ("asr_spec_last_error", "asr_spec_destroy"):
             getattr(L, name).restype = i64 if name.endswith("_ws") else ctypes.c_int
@@ -345,9 +344,8 @@ def asr_spec_paged_evict(cache, scores, lens, seen, budget, recent, first, lens_
                                                    ptr(lens_out), ptr(ws), ws_bytes, stream), "asr_spec_paged_evict")
 
 
-def asr_spec_accept_sampled(logits, draft, lens, u, race, race_stride, temperature, accepted, token, step, prob, status, ws,
-                            ws_bytes, stream=None):
+def asr_spec_accept_sampled(logits, draft, lens, u, race, race_stride, temperature, accepted, token, step, prob, status, stream=None):
     return _check(None, lib().asr_spec_accept_sampled(ctypes.byref(logits), ptr(draft), ptr(lens), ptr(u), addr(race),
                                                       race_stride, temperature, ptr(accepted), ptr(token), ptr(step),
-                                                      ptr(prob), ptr(status), ptr(ws), ws_bytes, stream),
+                                                      ptr(prob), ptr(status), stream),
                   "asr_spec_accept_sampled")

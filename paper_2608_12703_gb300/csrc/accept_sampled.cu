@@ -11,24 +11,25 @@
 // j with probability w_j / sum w), without a prefix sum over the vocabulary.
 // So accepted drafts and token follow the target's distribution exactly.
 //
-// Two launches.  Statistics: every live row's (max, sum exp) in one pass, a
-// row split over blocks so that one utterance fills the GPU too.  Decision:
-// a cluster of 8 blocks per utterance; each combines the statistics, finds n
-// and runs the race over an eighth of the vocabulary, and block 0 takes the
-// best.  Bound by the bytes of the logits: rows past the first rejection are
-// read as well (which rows those are is known only when all have been read).
-// Everything is fp32; a maximum of (value, lowest index) keys does not depend
-// on order, and the partial sums are combined in a fixed one.
+// One launch, a cluster of blocks per utterance, each on its share of the
+// vocabulary.  First every live row's (max, sum exp) in one pass; the blocks
+// exchange them through distributed shared memory, and each finds n for itself
+// and runs the race over its share; rank 0 takes the best.  Bound by the bytes
+// of the logits: rows past the first rejection are read as well (which rows
+// those are is known only when all have been read).  Everything is fp32; a
+// maximum of (value, lowest index) keys does not depend on order, and the
+// partial sums are combined in a fixed one.
+#include <atomic>
+
 #include "kernels.h"
 #include "paged.cuh"
 
 namespace asrspec {
 namespace {
 
-constexpr int AS_THREADS = 256;
-constexpr int AS_CLUSTER = 8;
+constexpr int AS_ROW = 256;       // threads on one row at a time
 constexpr int AS_MAX_K = 31;
-constexpr int AS_MAX_SPLIT = 32;
+constexpr int AS_ROWS = 2 * AS_MAX_K + 1;
 
 struct SampleArgs {
   const char *target, *draft_logits;         // draft_logits may be null
@@ -37,10 +38,9 @@ struct SampleArgs {
   const float *u, *race;
   long long race_b;                          // elements
   float inv_t;
-  int B, k, V, splits;
+  int k, V;
   int *accepted, *token, *step;
   float* prob;
-  float2* part;                              // [B][2 k + 1][splits] (max, sum)
   int* status;
 };
 
@@ -55,12 +55,10 @@ __device__ __forceinline__ int live_drafts(const SampleArgs& a, int b) {
 }
 
 // logit -> finite or -inf: NaN counts as masked, +inf as the largest float
-__device__ __forceinline__ float clean(float x) { return x != x ? -INFINITY : fminf(x, 3.4028234e38f); }
+__device__ __forceinline__ float clean(float x) { return fminf(fmaxf(x, -INFINITY), 3.4028234e38f); }
 
-// exp((x - m) / T); 0 for a masked x or an empty row (m = -inf)
-__device__ __forceinline__ float weight(float x, float m, float c) {
-  return x == -INFINITY ? 0.f : exp2f((x - m) * c);
-}
+// exp((x - m) / T) for finite m; 0 for a masked x
+__device__ __forceinline__ float weight(float x, float m, float c) { return ex2((x - m) * c); }
 
 template <typename T> struct Vec16 {   // the values of 16 bytes
   static constexpr int N = 8;
@@ -83,146 +81,113 @@ template <> struct Vec16<float> {
   }
 };
 
-template <typename T>
-__global__ void __launch_bounds__(AS_THREADS) sample_stats_kernel(SampleArgs a) {
-  constexpr int N = Vec16<T>::N, UN = 4;
-  __shared__ float s_m[AS_THREADS / 32], s_l[AS_THREADS / 32];
-  const int split = blockIdx.x, rr = blockIdx.y, b = blockIdx.z;
-  const int n = live_drafts(a, b);
-  pdl_launch();
-  const bool is_draft = rr > a.k;
-  const int row = is_draft ? rr - a.k - 1 : rr;
-  if (n < 0 || row > n || (is_draft && row >= n)) return;
-  const T* x = reinterpret_cast<const T*>(is_draft ? a.draft_logits + b * a.d_b + row * a.d_r : a.target + b * a.t_b + row * a.t_r);
-  const float c = a.inv_t * LOG2E;
-  // elements before the first 16-byte boundary, whole vectors, rest
-  const int head = min(a.V, (int)(((16 - (reinterpret_cast<uintptr_t>(x) & 15)) & 15) / sizeof(T)));
-  const int nv = (a.V - head) / N, tail = head + nv * N;
-  const int v0 = (int)((long long)nv * split / a.splits), v1 = (int)((long long)nv * (split + 1) / a.splits);
-  const uint4* xv = reinterpret_cast<const uint4*>(x + head);
+struct Stat {   // max and sum of weights relative to it
   float m = -INFINITY, l = 0.f;
-  auto add = [&](const float* f, int cnt) {
-    float mx = m;
-    for (int i = 0; i < cnt; ++i) mx = fmaxf(mx, f[i]);
-    if (mx == -INFINITY) return;
-    if (mx > m) {
-      l *= exp2f((m - mx) * c);
-      m = mx;
-    }
-    for (int i = 0; i < cnt; ++i) l += weight(f[i], m, c);
-  };
-  for (int i = v0 + threadIdx.x; i < v1; i += AS_THREADS * UN) {
-    uint4 v[UN];
-    float f[UN * N];
-#pragma unroll
-    for (int j = 0; j < UN; ++j)
-      if (i + j * AS_THREADS < v1) v[j] = ldg_stream(reinterpret_cast<const char*>(xv + i + j * AS_THREADS));
-#pragma unroll
-    for (int j = 0; j < UN; ++j) {
-      if (i + j * AS_THREADS < v1) {
-        Vec16<T>::get(v[j], f + j * N);
-#pragma unroll
-        for (int y = 0; y < N; ++y) f[j * N + y] = clean(f[j * N + y]);
-      } else {
-#pragma unroll
-        for (int y = 0; y < N; ++y) f[j * N + y] = -INFINITY;
-      }
-    }
-    float mx = m;
-#pragma unroll
-    for (int y = 0; y < UN * N; ++y) mx = fmaxf(mx, f[y]);
-    if (mx == -INFINITY) continue;
-    if (mx > m) {
-      l *= exp2f((m - mx) * c);
-      m = mx;
-    }
-#pragma unroll
-    for (int y = 0; y < UN * N; ++y) l += weight(f[y], m, c);
-  }
-  if (split == 0 && threadIdx.x < 32) {   // the ragged ends
-    const int lane = threadIdx.x;
-    if (lane < head) {
-      const float f = clean(to_f32(x[lane]));
-      add(&f, 1);
-    }
-    if (tail + lane < a.V) {
-      const float f = clean(to_f32(x[tail + lane]));
-      add(&f, 1);
-    }
-  }
-  auto combine = [&](float pm, float pl) {
+  __device__ __forceinline__ void add(float pm, float pl, float c) {
     const float mx = fmaxf(m, pm);
     if (mx == -INFINITY) return;
-    l = l * (m == -INFINITY ? 0.f : exp2f((m - mx) * c)) + pl * (pm == -INFINITY ? 0.f : exp2f((pm - mx) * c));
+    l = fmaf(pl, weight(pm, mx, c), __fmul_rn(l, weight(m, mx, c)));
     m = mx;
-  };
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) {
-    const float pm = __shfl_xor_sync(0xffffffffu, m, o), pl = __shfl_xor_sync(0xffffffffu, l, o);
-    combine(pm, pl);
   }
-  const int warp = threadIdx.x >> 5;
-  if ((threadIdx.x & 31) == 0) {
-    s_m[warp] = m;
-    s_l[warp] = l;
-  }
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    for (int w = 1; w < AS_THREADS / 32; ++w) combine(s_m[w], s_l[w]);
-    a.part[((long long)b * (2 * a.k + 1) + rr) * a.splits + split] = make_float2(m, l);
-  }
-}
+};
 
-template <typename T>
-__global__ void __launch_bounds__(AS_THREADS) sample_decide_kernel(SampleArgs a) {
-  __shared__ float s_px[AS_MAX_K + 1], s_qx[AS_MAX_K + 1];   // p_i(x_i), q_i(x_i)
-  __shared__ float s_pm[AS_MAX_K + 1], s_pl[AS_MAX_K + 1], s_qm[AS_MAX_K + 1], s_ql[AS_MAX_K + 1];
-  __shared__ unsigned long long s_key[2][AS_THREADS / 32], s_best[2];
-  __shared__ int s_bad;
+// CL blocks a cluster, GROUPS rows at a time in a block.
+template <typename T, int CL, int GROUPS>
+__global__ void __launch_bounds__(AS_ROW * GROUPS, GROUPS == 1 ? 4 : 1) accept_kernel(SampleArgs a) {
+  constexpr int N = Vec16<T>::N, UN = 4, THREADS = AS_ROW * GROUPS, WARPS = THREADS / 32, ROW_WARPS = AS_ROW / 32;
+  __shared__ float2 s_warp[AS_ROWS][ROW_WARPS];          // a warp's part of a row
+  __shared__ float2 s_block[AS_ROWS];                    // this block's part, read by the cluster
+  __shared__ float s_m[AS_ROWS], s_inv[AS_ROWS], s_x[AS_ROWS];   // the row's max, 1 / sum, probability of its draft
+  __shared__ unsigned long long s_key[2][WARPS], s_best[2];
   const int b = blockIdx.y, part = blockIdx.x, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int n_draft = live_drafts(a, b);
   const float c = a.inv_t * LOG2E;
-  if (tid == 0) s_bad = 0;
-  __syncthreads();
-  for (int i = tid; i < n_draft; i += AS_THREADS) {
-    const int x = a.draft[(long long)b * a.k + i];
-    if (x < 0 || x >= a.V) s_bad = 1;
+  bool bad = false;
+  if (lane < n_draft) {
+    const int x = a.draft[(long long)b * a.k + lane];
+    bad = x < 0 || x >= a.V;
   }
-  pdl_wait();
-  __syncthreads();
-  const bool out = n_draft < 0 || s_bad;   // uniform over the cluster
-  if (s_bad && tid == 0 && part == 0 && a.status) set_status(a.status, ST_BAD_TOKEN);
-  if (out) {
+  bad = __any_sync(0xffffffffu, bad);
+  if (n_draft < 0 || bad) {   // uniform over the cluster
     if (part == 0) {
       if (tid == 0) {
+        if (bad && a.status) set_status(a.status, ST_BAD_TOKEN);
         a.accepted[b] = 0;
         a.token[b] = -1;
         a.step[b] = 0;
       }
-      for (int i = tid; i < a.k; i += AS_THREADS) a.prob[(long long)b * a.k + i] = 0.f;
+      if (tid < a.k) a.prob[(long long)b * a.k + tid] = 0.f;
     }
     return;
   }
-  // a warp per row: combine its statistics, read the drafted token's probability
-  for (int rr = warp; rr < 2 * a.k + 1; rr += AS_THREADS / 32) {
-    const bool is_draft = rr > a.k;
-    const int row = is_draft ? rr - a.k - 1 : rr;
-    if (row > n_draft || (is_draft && (row >= n_draft || !a.draft_logits))) continue;
-    float2 s = make_float2(-INFINITY, 0.f);
-    if (lane < a.splits) s = a.part[((long long)b * (2 * a.k + 1) + rr) * a.splits + lane];
-    const float m = warp_max(s.x);
-    const float l = warp_sum(s.x == -INFINITY ? 0.f : s.y * exp2f((s.x - m) * c));
-    if (lane == 0) {
-      float px = 0.f;
-      if (row < n_draft) {
-        const int x = a.draft[(long long)b * a.k + row];
-        const T* p = reinterpret_cast<const T*>(is_draft ? a.draft_logits + b * a.d_b + row * a.d_r
-                                                         : a.target + b * a.t_b + row * a.t_r);
-        px = l > 0.f ? weight(clean(to_f32(p[x])), m, c) / l : 0.f;
+  // rows: target 0 .. n_draft, then draft 0 .. n_draft - 1
+  const int n_rows = n_draft + 1 + (a.draft_logits ? n_draft : 0);
+  auto row_ptr = [&](int r) {
+    return reinterpret_cast<const T*>(r > n_draft ? a.draft_logits + b * a.d_b + (r - n_draft - 1) * a.d_r
+                                                  : a.target + b * a.t_b + r * a.t_r);
+  };
+
+  const int rt = tid % AS_ROW;
+  for (int r = tid / AS_ROW; r < n_rows; r += GROUPS) {
+    const T* x = row_ptr(r);
+    // elements before the first 16-byte boundary, whole vectors, rest
+    const int head = min(a.V, (int)(((16 - (reinterpret_cast<uintptr_t>(x) & 15)) & 15) / sizeof(T)));
+    const int nv = (a.V - head) / N, tail = head + nv * N;
+    const int v0 = (int)((long long)nv * part / CL), v1 = (int)((long long)nv * (part + 1) / CL);
+    const char* xv = reinterpret_cast<const char*>(x + head);
+    Stat s;
+    for (int i = v0 + rt; i < v1; i += AS_ROW * UN) {
+      uint4 v[UN];
+      float mx = s.m, l = 0.f;
+#pragma unroll
+      for (int j = 0; j < UN; ++j)
+        if (i + j * AS_ROW < v1) v[j] = ldg_stream(xv + (long long)(i + j * AS_ROW) * 16);
+#pragma unroll
+      for (int j = 0; j < UN; ++j) {
+        if (i + j * AS_ROW >= v1) break;
+        float f[N];
+        Vec16<T>::get(v[j], f);
+#pragma unroll
+        for (int y = 0; y < N; ++y) mx = fmaxf(mx, f[y]);   // passes over NaN
       }
-      (is_draft ? s_qx : s_px)[row] = px;
-      (is_draft ? s_qm : s_pm)[row] = m;
-      (is_draft ? s_ql : s_pl)[row] = l;
+      if (mx == -INFINITY) continue;
+      mx = fminf(mx, 3.4028234e38f);
+#pragma unroll
+      for (int j = 0; j < UN; ++j) {
+        if (i + j * AS_ROW >= v1) break;
+        float f[N];
+        Vec16<T>::get(v[j], f);
+#pragma unroll
+        for (int y = 0; y < N; ++y) l += weight(clean(f[y]), mx, c);
+      }
+      s.l = fmaf(s.l, weight(s.m, mx, c), l);
+      s.m = mx;
+    }
+    if (part == 0 && rt < 32) {   // the ragged ends
+      if (lane < head) s.add(clean(to_f32(x[lane])), 1.f, c);
+      if (tail + lane < a.V) s.add(clean(to_f32(x[tail + lane])), 1.f, c);
+    }
+    const float m = warp_max(s.m);
+    const float l = m == -INFINITY ? 0.f : warp_sum(s.l * weight(s.m, m, c));
+    if (lane == 0) s_warp[r][rt >> 5] = make_float2(m, l);
+  }
+  __syncthreads();
+  for (int r = tid; r < n_rows; r += THREADS) {
+    Stat s;
+    for (int w = 0; w < ROW_WARPS; ++w) s.add(s_warp[r][w].x, s_warp[r][w].y, c);
+    s_block[r] = make_float2(s.m, s.l);
+  }
+  cluster_sync();
+  for (int r = warp; r < n_rows; r += WARPS) {
+    float pm = -INFINITY, pl = 0.f;
+    if (lane < CL) asm volatile("ld.shared::cluster.v2.f32 {%0,%1}, [%2];" : "=f"(pm), "=f"(pl) : "r"(dsmem_addr(&s_block[r], lane)));
+    const float m = warp_max(pm), l = m == -INFINITY ? 0.f : warp_sum(pl * weight(pm, m, c));
+    if (lane == 0) {
+      const int i = r > n_draft ? r - n_draft - 1 : r;
+      const float inv = l > 0.f ? 1.f / l : 0.f;
+      s_m[r] = l > 0.f ? m : 0.f;
+      s_inv[r] = inv;
+      s_x[r] = i < n_draft ? weight(clean(to_f32(row_ptr(r)[a.draft[(long long)b * a.k + i]])), s_m[r], c) * inv : 0.f;
     }
   }
   __syncthreads();
@@ -230,57 +195,64 @@ __global__ void __launch_bounds__(AS_THREADS) sample_decide_kernel(SampleArgs a)
   float px = 0.f, qx = 1.f;
   bool take = false;
   if (lane < n_draft) {
-    px = s_px[lane];
-    if (a.draft_logits) qx = s_qx[lane];
+    px = s_x[lane];
+    if (a.draft_logits) qx = s_x[n_draft + 1 + lane];
     take = a.u[(long long)b * a.k + lane] * qx < px;
   }
   const int n = __ffs(~__ballot_sync(0xffffffffu, take)) - 1;   // n_draft <= 31: lane n_draft never takes
   if (part == 0 && warp == 0 && lane < a.k)
     a.prob[(long long)b * a.k + lane] = lane < n_draft ? (px >= qx ? (px > 0.f ? 1.f : 0.f) : px / qx) : 0.f;
+
   // the race over this block's share of the vocabulary
-  const bool rejected = n < n_draft;
-  const T* pr = reinterpret_cast<const T*>(a.target + b * a.t_b + n * a.t_r);
-  const T* qr = rejected && a.draft_logits ? reinterpret_cast<const T*>(a.draft_logits + b * a.d_b + n * a.d_r) : nullptr;
+  const bool rejected = n < n_draft, minus = rejected && a.draft_logits;
+  const T *pr = row_ptr(n), *qr = minus ? row_ptr(n_draft + 1 + n) : pr;
   const int gone = rejected && !a.draft_logits ? a.draft[(long long)b * a.k + n] : -1;
-  const float pm = s_pm[n], pi = s_pl[n] > 0.f ? 1.f / s_pl[n] : 0.f;
-  const float qm = qr ? s_qm[n] : 0.f, qi = qr && s_ql[n] > 0.f ? 1.f / s_ql[n] : 0.f;
+  const float pm = s_m[n], pi = s_inv[n];
+  const float qm = minus ? s_m[n_draft + 1 + n] : 0.f, qi = minus ? s_inv[n_draft + 1 + n] : 0.f;
   const float* e = a.race + b * a.race_b;
-  const int v0 = (int)((long long)a.V * part / AS_CLUSTER), v1 = (int)((long long)a.V * (part + 1) / AS_CLUSTER);
-  unsigned long long best = 0, best_p = 0;   // keys of positive values are above 2^63
-#pragma unroll 4
-  for (int j = v0 + tid; j < v1; j += AS_THREADS) {
-    const float p = weight(clean(to_f32(pr[j])), pm, c) * pi;
-    if (!(p > 0.f)) continue;
-    const float ej = e[j];
-    float w = p;
-    if (qr) w = fmaxf(p - weight(clean(to_f32(qr[j])), qm, c) * qi, 0.f);
-    if (j == gone) w = 0.f;
-    const float vp = p / ej, vw = w / ej;
-    if (vp > 0.f) {
-      const unsigned long long x = argmax_key(vp, j);
-      best_p = x > best_p ? x : best_p;
+  const int j0 = (int)((long long)a.V * part / CL), j1 = (int)((long long)a.V * (part + 1) / CL);
+  // The best of w / e and, in case that w has no positive entry, of p / e.  Of
+  // equal values the lowest index: a thread meets its indices in order.
+  float best = 0.f, best_p = 0.f;
+  int at = 0, at_p = 0;
+  constexpr int RU = 8;
+  for (int jj = j0 + tid; jj < j1; jj += THREADS * RU) {
+    float p[RU], q[RU], ej[RU];
+#pragma unroll
+    for (int y = 0; y < RU; ++y) {
+      const int j = min(jj + y * THREADS, j1 - 1);
+      p[y] = to_f32(pr[j]);
+      ej[y] = __ldg(e + j);
+      q[y] = minus ? to_f32(qr[j]) : 0.f;
     }
-    if (vw > 0.f) {
-      const unsigned long long x = argmax_key(vw, j);
-      best = x > best ? x : best;
+#pragma unroll
+    for (int y = 0; y < RU; ++y) {
+      const int j = jj + y * THREADS;
+      if (j >= j1) break;
+      const float pj = weight(clean(p[y]), pm, c) * pi;
+      float w = pj;
+      if (minus) w = fmaxf(pj - weight(clean(q[y]), qm, c) * qi, 0.f);
+      if (j == gone) w = 0.f;
+      const float vp = pj / ej[y], vw = w / ej[y];
+      if (vp > best_p) best_p = vp, at_p = j;
+      if (vw > best) best = vw, at = j;
     }
   }
-  best = warp_max_u64(best);
-  best_p = warp_max_u64(best_p);
+  const unsigned long long key = warp_max_u64(best > 0.f ? argmax_key(best, at) : 0ull);
+  const unsigned long long key_p = warp_max_u64(best_p > 0.f ? argmax_key(best_p, at_p) : 0ull);
   if (lane == 0) {
-    s_key[0][warp] = best;
-    s_key[1][warp] = best_p;
+    s_key[0][warp] = key;
+    s_key[1][warp] = key_p;
   }
   __syncthreads();
-  if (tid < 2) {
-    unsigned long long x = 0;
-    for (int w = 0; w < AS_THREADS / 32; ++w) x = s_key[tid][w] > x ? s_key[tid][w] : x;
-    s_best[tid] = x;
+  if (warp < 2) {
+    const unsigned long long x = warp_max_u64(lane < WARPS ? s_key[warp][lane] : 0ull);
+    if (lane == 0) s_best[warp] = x;
   }
   cluster_sync();
   if (part == 0 && warp == 0) {
     unsigned long long x = 0, y = 0;
-    if (lane < AS_CLUSTER) {
+    if (lane < CL) {
       asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(x) : "r"(dsmem_addr(&s_best[0], lane)));
       asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(y) : "r"(dsmem_addr(&s_best[1], lane)));
     }
@@ -293,15 +265,33 @@ __global__ void __launch_bounds__(AS_THREADS) sample_decide_kernel(SampleArgs a)
       a.step[b] = k ? n + 1 : 0;
     }
   }
-  cluster_sync();   // s_best stays until block 0 has read it
+  cluster_sync();   // s_best stays until rank 0 has read it
 }
 
-int pick_splits(int rows, int V) {
-  // A row is cut so that all rows together give each SM a few blocks, none below 2048 elements.
-  int s = (8 * paged_sm_count() + rows - 1) / rows;
-  const int most = V / 2048 < 1 ? 1 : V / 2048;
-  if (s > most) s = most;
-  return s < 1 ? 1 : s > AS_MAX_SPLIT ? AS_MAX_SPLIT : s;
+template <auto kernel, int CL, int GROUPS>
+cudaError_t launch_accept(const SampleArgs& a, int B, cudaStream_t st) {
+  if constexpr (CL > 8) {   // clusters above 8 are asked for once a device
+    static std::atomic<uint64_t> ready{0};
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    const uint64_t bit = 1ull << (dev & 63);
+    if (!(ready.load(std::memory_order_acquire) & bit)) {
+      e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+      if (e != cudaSuccess) return e;
+      ready.fetch_or(bit, std::memory_order_release);
+    }
+  }
+  return launch_ex(kernel, dim3(CL, B), dim3(AS_ROW * GROUPS), 0, st, false, CL, a);
+}
+
+// A few utterances cannot fill the GPU: wide clusters of large blocks shorten
+// the chain of reads.  From 16 on, blocks of 256 threads, four an SM, keep
+// every SM busy in one wave.
+template <typename T>
+cudaError_t launch_accept_t(const SampleArgs& a, int B, cudaStream_t st) {
+  if (B < 16) return launch_accept<accept_kernel<T, 16, 4>, 16, 4>(a, B, st);
+  return launch_accept<accept_kernel<T, 8, 1>, 8, 1>(a, B, st);
 }
 
 }  // namespace
@@ -311,15 +301,10 @@ using namespace asrspec;
 
 extern "C" {
 
-int64_t asr_spec_accept_sampled_ws(int32_t B, int32_t k) {
-  if (B < 1 || B > 65535 || k < 0 || k > AS_MAX_K) return ASR_E_INVAL;
-  return (int64_t)B * (2 * k + 1) * AS_MAX_SPLIT * sizeof(float2);
-}
-
 int asr_spec_accept_sampled(const asr_sampled_logits* x, const int32_t* draft, const int32_t* lens, const float* u,
                             const float* race, int64_t race_stride, float temperature, int32_t* accepted, int32_t* token,
-                            int32_t* step, float* prob, int32_t* status, void* ws, int64_t ws_bytes, void* stream) {
-  if (!x || !x->target || !race || !accepted || !token || !step || !ws) return ASR_E_INVAL;
+                            int32_t* step, float* prob, int32_t* status, void* stream) {
+  if (!x || !x->target || !race || !accepted || !token || !step) return ASR_E_INVAL;
   if (x->dtype < 0 || x->dtype > 2 || x->batch < 1 || x->batch > 65535 || x->k < 0 || x->k > AS_MAX_K || x->vocab < 1 ||
       x->vocab > (1 << 30))
     return ASR_E_INVAL;
@@ -331,10 +316,8 @@ int asr_spec_accept_sampled(const asr_sampled_logits* x, const int32_t* draft, c
     return ASR_E_INVAL;
   if ((uintptr_t)x->target % es || (uintptr_t)x->draft_logits % es ||
       ((uintptr_t)draft | (uintptr_t)lens | (uintptr_t)u | (uintptr_t)race | (uintptr_t)accepted | (uintptr_t)token |
-       (uintptr_t)step | (uintptr_t)prob | (uintptr_t)status) % 4 ||
-      (uintptr_t)ws % 8)
+       (uintptr_t)step | (uintptr_t)prob | (uintptr_t)status) % 4)
     return ASR_E_INVAL;
-  if (ws_bytes < asr_spec_accept_sampled_ws(x->batch, x->k)) return ASR_E_CAPACITY;
   SampleArgs a{};
   a.target = static_cast<const char*>(x->target);
   a.draft_logits = static_cast<const char*>(x->draft_logits);
@@ -348,27 +331,18 @@ int asr_spec_accept_sampled(const asr_sampled_logits* x, const int32_t* draft, c
   a.race = race;
   a.race_b = race_stride;
   a.inv_t = 1.f / temperature;
-  a.B = x->batch;
   a.k = x->k;
   a.V = x->vocab;
   a.accepted = accepted;
   a.token = token;
   a.step = step;
   a.prob = prob;
-  a.part = static_cast<float2*>(ws);
   a.status = status;
-  const int rows = x->draft_logits ? 2 * x->k + 1 : x->k + 1;
-  a.splits = pick_splits(rows * x->batch, x->vocab);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  const dim3 g1(a.splits, rows, x->batch), g2(AS_CLUSTER, x->batch), blk(AS_THREADS);
   cudaError_t e;
-  auto go = [&](auto stats, auto decide) {
-    cudaError_t r = launch_ex(stats, g1, blk, 0, st, false, 1, a);
-    return r != cudaSuccess ? r : launch_ex(decide, g2, blk, 0, st, true, AS_CLUSTER, a);
-  };
-  if (x->dtype == 0) e = go(sample_stats_kernel<float>, sample_decide_kernel<float>);
-  else if (x->dtype == 1) e = go(sample_stats_kernel<__nv_bfloat16>, sample_decide_kernel<__nv_bfloat16>);
-  else e = go(sample_stats_kernel<__half>, sample_decide_kernel<__half>);
+  if (x->dtype == 0) e = launch_accept_t<float>(a, x->batch, st);
+  else if (x->dtype == 1) e = launch_accept_t<__nv_bfloat16>(a, x->batch, st);
+  else e = launch_accept_t<__half>(a, x->batch, st);
   return e == cudaSuccess ? ASR_OK : ASR_E_CUDA;
 }
 

@@ -304,7 +304,7 @@ def accept_sampled(target, draft, lens, u, race, *, draft_logits=None, temperatu
     known = _accept_layouts.get(key)
     if known is None:
         known = _remember(_accept_layouts, key, _accept_layout(target, draft, lens, u, race, draft_logits, temperature, status))
-    layout, n, device, index, race_stride = known
+    layout, device, index, race_stride = known
     if _current_device() != index:
         with torch.cuda.device(device):
             return accept_sampled(target, draft, lens, u, race, draft_logits=draft_logits, temperature=temperature, status=status)
@@ -315,11 +315,10 @@ def accept_sampled(target, draft, lens, u, race, *, draft_logits=None, temperatu
         x.draft_logits = draft_logits.data_ptr()
     ints = torch.empty((3, B), dtype=torch.int32, device=device)
     prob = torch.empty((B, k), dtype=torch.float32, device=device)
-    ws = torch.empty(n, dtype=torch.uint8, device=device)
     at = ints.data_ptr()
     _check(A.lib().asr_spec_accept_sampled(
         ctypes.byref(x), draft.data_ptr(), None if lens is None else lens.data_ptr(), u.data_ptr(), race.data_ptr(), race_stride,
-        temperature, at, at + 4 * B, at + 8 * B, prob.data_ptr(), None if status is None else status.data_ptr(), ws.data_ptr(), n,
+        temperature, at, at + 4 * B, at + 8 * B, prob.data_ptr(), None if status is None else status.data_ptr(),
         _raw_stream(index)), "asr_spec_accept_sampled")
     accepted, token, step = ints.unbind(0)
     return accepted, token, step, prob
@@ -346,6 +345,5 @@ def _accept_layout(target, draft, lens, u, race, draft_logits, temperature, stat
     if status is not None:
         _whole(status, "status", torch.int32, (1,), dev)
     _need(temperature > 0 and math.isfinite(temperature), "temperature: a positive number is required")
-    n = _check(A.lib().asr_spec_accept_sampled_ws(B, k), "asr_spec_accept_sampled_ws")
-    return (A.AsrSampledLogits(None, target.stride(0), target.stride(1), None, *ds, B, k, V, _DTYPE[target.dtype]), n, dev,
+    return (A.AsrSampledLogits(None, target.stride(0), target.stride(1), None, *ds, B, k, V, _DTYPE[target.dtype]), dev,
             dev.index, race.stride(0))
