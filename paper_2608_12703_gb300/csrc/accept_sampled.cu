@@ -96,18 +96,19 @@ template <typename T, int CL, int GROUPS>
 __global__ void __launch_bounds__(AS_ROW * GROUPS, GROUPS == 1 ? 4 : 1) accept_kernel(SampleArgs a) {
   constexpr int N = Vec16<T>::N, UN = 4, THREADS = AS_ROW * GROUPS, WARPS = THREADS / 32, ROW_WARPS = AS_ROW / 32;
   __shared__ float2 s_warp[AS_ROWS][ROW_WARPS];          // a warp's part of a row
-  __shared__ float2 s_block[AS_ROWS];                    // this block's part, read by the cluster
-  __shared__ float s_m[AS_ROWS], s_inv[AS_ROWS], s_x[AS_ROWS];   // the row's max, 1 / sum, probability of its draft
-  __shared__ unsigned long long s_key[2][WARPS], s_best[2];
+  __shared__ float2 s_part[AS_ROWS][CL];                 // every block's part of a row
+  __shared__ float s_m[AS_ROWS], s_inv[AS_ROWS], s_x[AS_ROWS];   // the row's max, 1 / sum, its draft's logit, then probability
+  __shared__ unsigned long long s_key[WARPS], s_best[2][CL];   // every block's best, of w and of the second race
   const int b = blockIdx.y, part = blockIdx.x, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int n_draft = live_drafts(a, b);
   const float c = a.inv_t * LOG2E;
-  bool bad = false;
+  int mine = 0;   // a lane's draft and its random number
+  float u = 1.f;
   if (lane < n_draft) {
-    const int x = a.draft[(long long)b * a.k + lane];
-    bad = x < 0 || x >= a.V;
+    mine = a.draft[(long long)b * a.k + lane];
+    u = a.u[(long long)b * a.k + lane];
   }
-  bad = __any_sync(0xffffffffu, bad);
+  const bool bad = __any_sync(0xffffffffu, mine < 0 || mine >= a.V);
   if (n_draft < 0 || bad) {   // uniform over the cluster
     if (part == 0) {
       if (tid == 0) {
@@ -126,6 +127,11 @@ __global__ void __launch_bounds__(AS_ROW * GROUPS, GROUPS == 1 ? 4 : 1) accept_k
     return reinterpret_cast<const T*>(r > n_draft ? a.draft_logits + b * a.d_b + (r - n_draft - 1) * a.d_r
                                                   : a.target + b * a.t_b + r * a.t_r);
   };
+
+  if (warp == 0 && lane < n_draft) {
+    s_x[lane] = clean(to_f32(row_ptr(lane)[mine]));
+    if (a.draft_logits) s_x[n_draft + 1 + lane] = clean(to_f32(row_ptr(n_draft + 1 + lane)[mine]));
+  }
 
   const int rt = tid % AS_ROW;
   for (int r = tid / AS_ROW; r < n_rows; r += GROUPS) {
@@ -172,22 +178,21 @@ __global__ void __launch_bounds__(AS_ROW * GROUPS, GROUPS == 1 ? 4 : 1) accept_k
     if (lane == 0) s_warp[r][rt >> 5] = make_float2(m, l);
   }
   __syncthreads();
-  for (int r = tid; r < n_rows; r += THREADS) {
+  for (int x = tid; x < n_rows * CL; x += THREADS) {   // this block's part of every row to every block
+    const int r = x / CL, to = x - r * CL;
     Stat s;
     for (int w = 0; w < ROW_WARPS; ++w) s.add(s_warp[r][w].x, s_warp[r][w].y, c);
-    s_block[r] = make_float2(s.m, s.l);
+    asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(dsmem_addr(&s_part[r][part], to)), "f"(s.m), "f"(s.l) : "memory");
   }
   cluster_sync();
   for (int r = warp; r < n_rows; r += WARPS) {
-    float pm = -INFINITY, pl = 0.f;
-    if (lane < CL) asm volatile("ld.shared::cluster.v2.f32 {%0,%1}, [%2];" : "=f"(pm), "=f"(pl) : "r"(dsmem_addr(&s_block[r], lane)));
-    const float m = warp_max(pm), l = m == -INFINITY ? 0.f : warp_sum(pl * weight(pm, m, c));
+    const float2 x = lane < CL ? s_part[r][lane] : make_float2(-INFINITY, 0.f);
+    const float m = warp_max(x.x), l = m == -INFINITY ? 0.f : warp_sum(x.y * weight(x.x, m, c));
     if (lane == 0) {
       const int i = r > n_draft ? r - n_draft - 1 : r;
-      const float inv = l > 0.f ? 1.f / l : 0.f;
       s_m[r] = l > 0.f ? m : 0.f;
-      s_inv[r] = inv;
-      s_x[r] = i < n_draft ? weight(clean(to_f32(row_ptr(r)[a.draft[(long long)b * a.k + i]])), s_m[r], c) * inv : 0.f;
+      s_inv[r] = l > 0.f ? 1.f / l : 0.f;
+      if (i < n_draft) s_x[r] = weight(s_x[r], s_m[r], c) * s_inv[r];
     }
   }
   __syncthreads();
@@ -197,7 +202,7 @@ __global__ void __launch_bounds__(AS_ROW * GROUPS, GROUPS == 1 ? 4 : 1) accept_k
   if (lane < n_draft) {
     px = s_x[lane];
     if (a.draft_logits) qx = s_x[n_draft + 1 + lane];
-    take = a.u[(long long)b * a.k + lane] * qx < px;
+    take = u * qx < px;
   }
   const int n = __ffs(~__ballot_sync(0xffffffffu, take)) - 1;   // n_draft <= 31: lane n_draft never takes
   if (part == 0 && warp == 0 && lane < a.k)
@@ -206,66 +211,55 @@ __global__ void __launch_bounds__(AS_ROW * GROUPS, GROUPS == 1 ? 4 : 1) accept_k
   // the race over this block's share of the vocabulary
   const bool rejected = n < n_draft, minus = rejected && a.draft_logits;
   const T *pr = row_ptr(n), *qr = minus ? row_ptr(n_draft + 1 + n) : pr;
-  const int gone = rejected && !a.draft_logits ? a.draft[(long long)b * a.k + n] : -1;
+  const int gone = rejected && !a.draft_logits ? __shfl_sync(0xffffffffu, mine, n) : -1;
   const float pm = s_m[n], pi = s_inv[n];
   const float qm = minus ? s_m[n_draft + 1 + n] : 0.f, qi = minus ? s_inv[n_draft + 1 + n] : 0.f;
   const float* e = a.race + b * a.race_b;
   const int j0 = (int)((long long)a.V * part / CL), j1 = (int)((long long)a.V * (part + 1) / CL);
-  // The best of w / e and, in case that w has no positive entry, of p / e.  Of
-  // equal values the lowest index: a thread meets its indices in order.
-  float best = 0.f, best_p = 0.f;
-  int at = 0, at_p = 0;
-  constexpr int RU = 8;
-  for (int jj = j0 + tid; jj < j1; jj += THREADS * RU) {
-    float p[RU], q[RU], ej[RU];
+  // Of equal values the lowest index: a thread meets its indices in order.
+  auto race = [&](bool residual, int second) {
+    float best = 0.f;
+    int at = 0;
+    constexpr int RU = 8;
+    for (int jj = j0 + tid; jj < j1; jj += THREADS * RU) {
+      float p[RU], q[RU], ej[RU];
 #pragma unroll
-    for (int y = 0; y < RU; ++y) {
-      const int j = min(jj + y * THREADS, j1 - 1);
-      p[y] = to_f32(pr[j]);
-      ej[y] = __ldg(e + j);
-      q[y] = minus ? to_f32(qr[j]) : 0.f;
-    }
+      for (int y = 0; y < RU; ++y) {
+        const int j = min(jj + y * THREADS, j1 - 1);   // the share's last entry again: never better than itself
+        p[y] = to_f32(pr[j]);
+        ej[y] = __ldg(e + j);
+        q[y] = minus ? to_f32(qr[j]) : -INFINITY;
+      }
 #pragma unroll
-    for (int y = 0; y < RU; ++y) {
-      const int j = jj + y * THREADS;
-      if (j >= j1) break;
-      const float pj = weight(clean(p[y]), pm, c) * pi;
-      float w = pj;
-      if (minus) w = fmaxf(pj - weight(clean(q[y]), qm, c) * qi, 0.f);
-      if (j == gone) w = 0.f;
-      const float vp = pj / ej[y], vw = w / ej[y];
-      if (vp > best_p) best_p = vp, at_p = j;
-      if (vw > best) best = vw, at = j;
+      for (int y = 0; y < RU; ++y) {
+        const int j = min(jj + y * THREADS, j1 - 1);
+        float w = weight(clean(p[y]), pm, c) * pi;
+        if (residual) {
+          w -= weight(clean(q[y]), qm, c) * qi;
+          if (j == gone) w = 0.f;
+        }
+        // A quotient is off by 2 ulp at most: as good as w itself.
+        const float v = __fdividef(w, ej[y]);
+        if (v > best) best = v, at = j;
+      }
     }
-  }
-  const unsigned long long key = warp_max_u64(best > 0.f ? argmax_key(best, at) : 0ull);
-  const unsigned long long key_p = warp_max_u64(best_p > 0.f ? argmax_key(best_p, at_p) : 0ull);
-  if (lane == 0) {
-    s_key[0][warp] = key;
-    s_key[1][warp] = key_p;
-  }
-  __syncthreads();
-  if (warp < 2) {
-    const unsigned long long x = warp_max_u64(lane < WARPS ? s_key[warp][lane] : 0ull);
-    if (lane == 0) s_best[warp] = x;
-  }
-  cluster_sync();
-  if (part == 0 && warp == 0) {
-    unsigned long long x = 0, y = 0;
-    if (lane < CL) {
-      asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(x) : "r"(dsmem_addr(&s_best[0], lane)));
-      asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(y) : "r"(dsmem_addr(&s_best[1], lane)));
+    const unsigned long long key = warp_max_u64(best > 0.f ? argmax_key(best, at) : 0ull);
+    if (lane == 0) s_key[warp] = key;
+    __syncthreads();
+    if (warp == 0) {
+      const unsigned long long x = warp_max_u64(lane < WARPS ? s_key[lane] : 0ull);
+      if (lane < CL) asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(dsmem_addr(&s_best[second][part], lane)), "l"(x) : "memory");
     }
-    x = warp_max_u64(x);
-    y = warp_max_u64(y);
-    if (lane == 0) {
-      const unsigned long long k = x ? x : y;   // no residual left (p = q): draw from p
-      a.accepted[b] = n;
-      a.token[b] = k ? (int)argmax_index(k) : -1;
-      a.step[b] = k ? n + 1 : 0;
-    }
+    cluster_sync();
+    return warp_max_u64(lane < CL ? s_best[second][lane] : 0ull);
+  };
+  unsigned long long best = race(rejected, 0);
+  if (best == 0 && rejected) best = race(false, 1);   // no residual left (p = q): draw from p; uniform over the cluster
+  if (part == 0 && tid == 0) {
+    a.accepted[b] = n;
+    a.token[b] = best ? (int)argmax_index(best) : -1;
+    a.step[b] = best ? n + 1 : 0;
   }
-  cluster_sync();   // s_best stays until rank 0 has read it
 }
 
 template <auto kernel, int CL, int GROUPS>
