@@ -8,18 +8,25 @@
 // takes the j-th kept slot at or past it.  Sources and destinations are
 // disjoint, so the moves run in any order over the whole GPU and move the
 // fewest rows there are to move.
-//   * select: one block per (sequence, head) finds the rank of the last kept
-//     slot by a radix search, 8 bits a pass over a histogram, then lists freed
-//     and kept slots in slot order and writes the kept scores and positions;
-//   * move: one 16-byte chunk a lane, rows of K and V from list to list.
+//
+// One launch, a cluster of 1 to 8 blocks per (sequence, head), each on a
+// contiguous part of the slots:
+//   * the rank of the last kept slot by a radix search, 8 bits a pass over a
+//     histogram (summed over the cluster through distributed shared memory);
+//   * freed and kept slots listed in slot order, from exclusive counts over
+//     warps and blocks;
+//   * the moves, rows dealt out over the cluster: addresses first, for a batch
+//     of rows at a time, then 16-byte chunks with several rows in flight a
+//     thread.  Bound by the bytes of the moved rows where many move, by the
+//     chain of passes where few do.
 #include "kernels.h"
 #include "paged.cuh"
 
 namespace asrspec {
 namespace {
 
-constexpr int EV_THREADS = 512;
-constexpr int EV_WARPS = EV_THREADS / 32;
+constexpr int EV_MAX_CLUSTER = 8;
+constexpr int EV_KEYS = 8192;    // slots whose rank a block keeps in shared memory; past them it is taken anew
 
 struct EvictArgs {
   PagedView c;
@@ -30,8 +37,8 @@ struct EvictArgs {
   float* score_out;
   int *pos_out, *len_out;
   int in_cap, out_cap, budget, recent, first;
-  int *count, *holes, *srcs;            // workspace: [B K], [B K][max_moves] each
-  int max_moves;
+  int *holes, *srcs;                    // workspace: [B K][max_moves] each
+  int max_moves, chunks, keys;          // 16-byte chunks of a row; ranks kept in shared memory
 };
 
 // Slots in use; a length out of range sets the status word and is left alone (-1).
@@ -50,43 +57,80 @@ __device__ __forceinline__ uint32_t rank_key(float score, int pos, int newest, i
   return score != score ? 0u : ordered_bits(score + 0.f);   // -0 ranks as 0
 }
 
-__global__ void __launch_bounds__(EV_THREADS) evict_select_kernel(EvictArgs a) {
-  __shared__ int hist[256];
-  __shared__ uint32_t s_prefix;
-  __shared__ int s_need;
-  __shared__ int s_cnt[3][EV_WARPS];
-  const int h = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int n = evict_len(a, b), task = b * a.c.kv_heads + h;
+__device__ __forceinline__ void st_cluster(int* at, int rank, int v) {
+  asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(dsmem_addr(at, rank)), "r"(v) : "memory");
+}
+__device__ __forceinline__ int ld_cluster(const int* at, int rank) {
+  int v;
+  asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(dsmem_addr(at, rank)) : "memory");
+  return v;
+}
+
+template <int THREADS>
+__global__ void __launch_bounds__(THREADS) evict_kernel(EvictArgs a) {
+  constexpr int WARPS = THREADS / 32;
+  __shared__ int hist[4][256];
+  __shared__ int s_bin, s_need;
+  __shared__ int s_warp[3][WARPS], s_rank[3][EV_MAX_CLUSTER];
+  __shared__ long long s_to[THREADS], s_of[THREADS];
+  extern __shared__ uint32_t s_key[];
+  const int CL = gridDim.x, rank = blockIdx.x, h = blockIdx.y, b = blockIdx.z;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int n = evict_len(a, b);
+  const size_t task = (size_t)b * a.c.kv_heads + h;
   const float* sc = a.score + b * a.in_b + h * a.in_h;
   const int* ps = a.pos + b * a.in_b + h * a.in_h;
   float* so = a.score_out + b * a.out_b + h * a.out_h;
   int* po = a.pos_out + b * a.out_b + h * a.out_h;
-  pdl_launch();
-  if (n <= a.budget) {
+  if (h == 0 && rank == 0 && tid == 0) a.len_out[b] = n < 0 ? a.len[b] : min(n, a.budget);
+  const int i0 = (int)((long long)max(n, 0) * rank / CL), i1 = (int)((long long)max(n, 0) * (rank + 1) / CL);
+  if (n <= a.budget) {   // uniform over the cluster
     if (so != sc)
-      for (int i = tid; i < n; i += EV_THREADS) so[i] = sc[i];
+      for (int i = i0 + tid; i < i1; i += THREADS) so[i] = sc[i];
     if (po != ps)
-      for (int i = tid; i < n; i += EV_THREADS) po[i] = ps[i];
-    if (tid == 0) a.count[task] = 0;
+      for (int i = i0 + tid; i < i1; i += THREADS) po[i] = ps[i];
     return;
   }
+  auto sync = [&] {
+    if (CL > 1) cluster_sync();
+    else __syncthreads();
+  };
   const int newest = a.seen[b] - a.recent;
+  const int cached = min(i1 - i0, a.keys);
+  auto key = [&](int i) { return i - i0 < cached ? s_key[i - i0] : rank_key(sc[i], ps[i], newest, a.first); };
+  for (int i = tid; i < cached; i += THREADS) s_key[i] = rank_key(sc[i0 + i], ps[i0 + i], newest, a.first);
+  for (int i = tid; i < 4 * 256; i += THREADS) hist[0][i] = 0;
+  __syncthreads();
+
   // the key of the budget-th slot: fix 8 bits a pass from the top
   uint32_t prefix = 0;
   int need = a.budget;
-  for (int shift = 24; shift >= 0; shift -= 8) {
-    for (int i = tid; i < 256; i += EV_THREADS) hist[i] = 0;
-    __syncthreads();
-    const uint32_t mask = shift == 24 ? 0u : 0xffffffffu << (shift + 8);
-    for (int i = tid; i < n; i += EV_THREADS) {
-      const uint32_t k = rank_key(sc[i], ps[i], newest, a.first);
-      if ((k & mask) == prefix) atomicAdd(&hist[(k >> shift) & 255], 1);
+#pragma unroll 1
+  for (int pass = 0; pass < 4; ++pass) {
+    const int shift = 24 - 8 * pass;
+    const uint32_t mask = pass == 0 ? 0u : 0xffffffffu << (shift + 8);
+    for (int base = i0 + warp * 32; base < i1; base += THREADS) {
+      const uint32_t k = base + lane < i1 ? key(base + lane) : 0u;
+      const bool in = base + lane < i1 && (k & mask) == prefix;
+      const unsigned live = __ballot_sync(0xffffffffu, in);
+      if (in) {   // equal digits of a warp are one addition: scores crowd in few bins
+        const int digit = (k >> shift) & 255;
+        const unsigned same = __match_any_sync(live, digit);
+        if (lane == __ffs(same) - 1) atomicAdd(&hist[pass][digit], __popc(same));
+      }
     }
-    __syncthreads();
+    sync();
     if (warp == 0) {   // bins from the top, 8 a lane
-      int mine = 0;
+      int x[8], mine = 0;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) mine += hist[255 - (lane * 8 + j)];
+      for (int j = 0; j < 8; ++j) {
+        const int* bin = &hist[pass][255 - (lane * 8 + j)];
+        x[j] = 0;
+        if (CL == 1) x[j] = *bin;
+        else
+          for (int q = 0; q < CL; ++q) x[j] += ld_cluster(bin, q);
+        mine += x[j];
+      }
       int inc = mine;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
@@ -97,101 +141,124 @@ __global__ void __launch_bounds__(EV_THREADS) evict_select_kernel(EvictArgs a) {
       if (before < need && need <= inc) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-          const int bin = 255 - (lane * 8 + j), x = hist[bin];
-          if (before < need && need <= before + x) {
-            s_prefix = prefix | ((uint32_t)bin << shift);
+          if (before < need && need <= before + x[j]) {
+            s_bin = 255 - (lane * 8 + j);
             s_need = need - before;
           }
-          before += x;
+          before += x[j];
         }
       }
     }
     __syncthreads();
-    prefix = s_prefix;
+    prefix |= (uint32_t)s_bin << shift;
     need = s_need;
+    __syncthreads();
   }
-  // in slot order: slots above the key stay, and the first `need` equal to it
-  int *holes = a.holes + (size_t)task * a.max_moves, *srcs = a.srcs + (size_t)task * a.max_moves;
-  int n_eq = 0, n_hole = 0, n_src = 0;
-  for (int i0 = 0; i0 < n; i0 += EV_THREADS) {
-    const int i = i0 + tid;
-    const bool in = i < n;
-    float x = 0.f;
-    int p = 0;
-    uint32_t k = 0;
-    if (in) {
-      x = sc[i];
-      p = ps[i];
-      k = rank_key(x, p, newest, a.first);
-    }
-    const unsigned below = (1u << lane) - 1;
-    const unsigned beq = __ballot_sync(0xffffffffu, in && k == prefix);
-    if (lane == 0) s_cnt[0][warp] = __popc(beq);
+
+  // Slots above the key stay, and of those equal to it the first `need` in slot
+  // order.  Warps and blocks count before they list; warp w has 32-slot rows
+  // [w0, w1) of the block's part.
+  const int per = ((i1 - i0 + 31) / 32 + WARPS - 1) / WARPS * 32;
+  const int w0 = i0 + warp * per, w1 = min(i1, w0 + per);
+  const unsigned below = (1u << lane) - 1;
+  // exclusive count over the cluster of a warp's number; `total` receives the sum
+  auto before_warp = [&](int which, int count, int& total) {
+    if (lane == 0) s_warp[which][warp] = count;
     __syncthreads();
-    int eq = n_eq + __popc(beq & below);
-    for (int w = 0; w < EV_WARPS; ++w) {
-      if (w < warp) eq += s_cnt[0][w];
-      n_eq += s_cnt[0][w];
+    int x = 0, all = 0;
+    for (int w = 0; w < WARPS; ++w) {
+      if (w < warp) x += s_warp[which][w];
+      all += s_warp[which][w];
     }
-    const bool keep = in && (k > prefix || (k == prefix && eq < need));
-    const bool hole = in && !keep && i < a.budget, src = keep && i >= a.budget;
-    const unsigned bh = __ballot_sync(0xffffffffu, hole), bs = __ballot_sync(0xffffffffu, src);
-    if (lane == 0) {
-      s_cnt[1][warp] = __popc(bh);
-      s_cnt[2][warp] = __popc(bs);
-    }
-    __syncthreads();
-    int at_h = n_hole + __popc(bh & below), at_s = n_src + __popc(bs & below);
-    for (int w = 0; w < EV_WARPS; ++w) {
-      if (w < warp) {
-        at_h += s_cnt[1][w];
-        at_s += s_cnt[2][w];
+    total = all;
+    if (CL > 1) {
+      if (tid < CL) st_cluster(&s_rank[which][rank], tid, all);
+      cluster_sync();
+      total = 0;
+      for (int q = 0; q < CL; ++q) {
+        if (q < rank) x += s_rank[which][q];
+        total += s_rank[which][q];
       }
-      n_hole += s_cnt[1][w];
-      n_src += s_cnt[2][w];
     }
-    if (hole) holes[at_h] = i;
-    if (src) srcs[at_s] = i;
-    if (keep && i < a.budget) {
-      so[i] = x;
-      po[i] = p;
+    return x;
+  };
+  int count = 0, total = 0;
+  for (int base = w0; base < w1; base += 32)
+    count += __popc(__ballot_sync(0xffffffffu, base + lane < w1 && key(base + lane) == prefix));
+  const int eq0 = before_warp(0, count, total);
+  // f(slot, kept, its place among the freed below the budget, its place among the kept past it)
+  auto walk = [&](int hole, int src, auto f) {
+    int eq = eq0;
+    for (int base = w0; base < w1; base += 32) {
+      const int i = base + lane;
+      const uint32_t k = i < w1 ? key(i) : 0u;
+      const unsigned e = __ballot_sync(0xffffffffu, i < w1 && k == prefix);
+      const bool keep = i < w1 && (k > prefix || (k == prefix && eq + __popc(e & below) < need));
+      const unsigned bh = __ballot_sync(0xffffffffu, i < w1 && !keep && i < a.budget);
+      const unsigned bs = __ballot_sync(0xffffffffu, keep && i >= a.budget);
+      f(i, keep, bh, bs, hole, src);
+      eq += __popc(e);
+      hole += __popc(bh);
+      src += __popc(bs);
     }
-  }
-  __syncthreads();
-  for (int j = tid; j < n_hole; j += EV_THREADS) {
-    const int to = holes[j], of = srcs[j];
-    so[to] = sc[of];
-    po[to] = ps[of];
-  }
-  if (tid == 0) a.count[task] = n_hole;
-}
+    count = hole;
+    total = src;
+  };
+  walk(0, 0, [](int, bool, unsigned, unsigned, int, int) {});
+  const int my_holes = count, my_srcs = total;
+  int moves, sum;
+  const int hole0 = before_warp(1, my_holes, moves), src0 = before_warp(2, my_srcs, sum);
+  int *holes = a.holes + task * a.max_moves, *srcs = a.srcs + task * a.max_moves;
+  const bool copy = so != sc || po != ps;
+  walk(hole0, src0, [&](int i, bool keep, unsigned bh, unsigned bs, int hole, int src) {
+    if (bh >> lane & 1) __stcg(holes + hole + __popc(bh & below), i);
+    if (bs >> lane & 1) __stcg(srcs + src + __popc(bs & below), i);
+    if (copy && keep && i < a.budget) {
+      so[i] = sc[i];
+      po[i] = ps[i];
+    }
+  });
+  sync();
 
-constexpr int EM_THREADS = 256;
-
-__global__ void __launch_bounds__(EM_THREADS) evict_move_kernel(EvictArgs a, int chunks) {
-  const int h = blockIdx.y, b = blockIdx.z, task = b * a.c.kv_heads + h;
-  pdl_wait();
-  if (h == 0 && blockIdx.x == 0 && threadIdx.x == 0) {
-    const int n = evict_len(a, b);
-    a.len_out[b] = n < 0 ? a.len[b] : min(n, a.budget);
-  }
-  const int n = a.count[task];
+  // the moves: batches of THREADS rows, this block every CL-th batch
   const int* table = a.c.table + b * a.c.table_stride;
-  const long long head = h * a.c.head_stride;
-  const int per = EM_THREADS / chunks;   // rows a block moves at a time
-  const int chunk = threadIdx.x % chunks;
-  for (int j = blockIdx.x * per + threadIdx.x / chunks; j < n; j += gridDim.x * per) {
-    const int to = a.holes[(size_t)task * a.max_moves + j], of = a.srcs[(size_t)task * a.max_moves + j];
-    const int tp = table[to / a.c.page_size], fp = table[of / a.c.page_size];
-    if ((unsigned)tp >= (unsigned)a.c.n_pages || (unsigned)fp >= (unsigned)a.c.n_pages) {
-      if (a.c.status) set_status(a.c.status, ST_BOUNDS);
-      continue;
+  const int in_row = tid % a.chunks, row0 = tid / a.chunks, rows = THREADS / a.chunks;
+  for (int j0 = rank * THREADS; j0 < moves; j0 += CL * THREADS) {
+    const int j = j0 + tid;
+    if (j < moves) {
+      const int to = __ldcg(holes + j), of = __ldcg(srcs + j);
+      const int tp = __ldg(table + to / a.c.page_size), fp = __ldg(table + of / a.c.page_size);
+      const bool ok = (unsigned)tp < (unsigned)a.c.n_pages && (unsigned)fp < (unsigned)a.c.n_pages;
+      if (!ok && a.c.status) set_status(a.c.status, ST_BOUNDS);
+      const long long head = h * a.c.head_stride;
+      s_to[tid] = tp * a.c.page_stride + (to % a.c.page_size) * a.c.slot_stride + head;
+      s_of[tid] = ok ? fp * a.c.page_stride + (of % a.c.page_size) * a.c.slot_stride + head : -1;
+      so[to] = sc[of];
+      po[to] = ps[of];
     }
-    const long long t = tp * a.c.page_stride + (to % a.c.page_size) * a.c.slot_stride + head + chunk * 16;
-    const long long f = fp * a.c.page_stride + (of % a.c.page_size) * a.c.slot_stride + head + chunk * 16;
-    const uint4 k = *reinterpret_cast<const uint4*>(a.c.k + f), v = *reinterpret_cast<const uint4*>(a.c.v + f);
-    *reinterpret_cast<uint4*>(a.c.k + t) = k;
-    *reinterpret_cast<uint4*>(a.c.v + t) = v;
+    __syncthreads();
+    const int m = min(THREADS, moves - j0);
+    constexpr int U = 4;
+    for (int x0 = row0; x0 < m; x0 += rows * U) {
+      uint4 k[U], v[U];
+#pragma unroll
+      for (int y = 0; y < U; ++y) {
+        const int x = x0 + y * rows;
+        if (x < m && s_of[x] >= 0) {
+          k[y] = ldg_stream(a.c.k + s_of[x] + in_row * 16);
+          v[y] = ldg_stream(a.c.v + s_of[x] + in_row * 16);
+        }
+      }
+#pragma unroll
+      for (int y = 0; y < U; ++y) {
+        const int x = x0 + y * rows;
+        if (x < m && s_of[x] >= 0) {
+          *reinterpret_cast<uint4*>(a.c.k + s_to[x] + in_row * 16) = k[y];
+          *reinterpret_cast<uint4*>(a.c.v + s_to[x] + in_row * 16) = v[y];
+        }
+      }
+    }
+    __syncthreads();
   }
 }
 
@@ -212,7 +279,7 @@ int64_t asr_spec_paged_evict_ws(const asr_paged_cache* c, const asr_paged_scores
   PagedView v;
   if (int rc = paged_view(c, &v)) return rc;
   if (!s || s->slots < 1 || budget < 1) return ASR_E_INVAL;
-  return (int64_t)c->batch * c->kv_heads * (1 + 2 * evict_max_moves(s, budget)) * 4;
+  return ((int64_t)c->batch * c->kv_heads * 2 * evict_max_moves(s, budget) + c->batch) * 4;
 }
 
 int asr_spec_paged_evict(const asr_paged_cache* c, const asr_paged_scores* s, const int32_t* len, const int32_t* seen,
@@ -228,7 +295,7 @@ int asr_spec_paged_evict(const asr_paged_cache* c, const asr_paged_scores* s, co
        (uintptr_t)seen | (uintptr_t)len_out | (uintptr_t)ws) % 4)
     return ASR_E_INVAL;
   const int64_t moves = evict_max_moves(s, budget), tasks = (int64_t)c->batch * c->kv_heads;
-  if (ws_bytes < tasks * (1 + 2 * moves) * 4) return ASR_E_CAPACITY;
+  if (ws_bytes < (tasks * 2 * moves + c->batch) * 4) return ASR_E_CAPACITY;
   a.len = len;
   a.seen = seen;
   a.score = s->score;
@@ -246,17 +313,24 @@ int asr_spec_paged_evict(const asr_paged_cache* c, const asr_paged_scores* s, co
   a.recent = recent;
   a.first = first;
   a.max_moves = (int)moves;
-  a.count = static_cast<int*>(ws);
-  a.holes = a.count + tasks;
+  a.holes = static_cast<int*>(ws);
   a.srcs = a.holes + tasks * moves;
+  a.chunks = c->head_dim * (c->dtype == 0 ? 4 : 2) / 16;
+  // Heads read len while others may be done: in place, the lengths go through the workspace.
+  const bool in_place = len_out == len;
+  if (in_place) a.len_out = a.srcs + tasks * moves;
+  // A block takes 2048 slots of a head comfortably; more blocks share a head
+  // while all of them together stay below four an SM.
+  int cluster = 1;
+  while (cluster < EV_MAX_CLUSTER && s->slots > 2048 * cluster && tasks * cluster * 2 <= 4 * paged_sm_count()) cluster *= 2;
+  const int part = (s->slots + cluster - 1) / cluster;
+  a.keys = part < EV_KEYS ? part : EV_KEYS;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  cudaError_t e = launch_ex(evict_select_kernel, dim3(c->kv_heads, c->batch), dim3(EV_THREADS), 0, st, false, 1, a);
-  if (e != cudaSuccess) return ASR_E_CUDA;
-  const int chunks = c->head_dim * (c->dtype == 0 ? 4 : 2) / 16, per = EM_THREADS / chunks;
-  int64_t x = (moves + per - 1) / per;
-  const int64_t most = (paged_sm_count() * 16 + tasks - 1) / tasks;
-  if (x > most) x = most;
-  e = launch_ex(evict_move_kernel, dim3((unsigned)x, c->kv_heads, c->batch), dim3(EM_THREADS), 0, st, true, 1, a, chunks);
+  const dim3 grid(cluster, c->kv_heads, c->batch);
+  cudaError_t e;
+  if (part <= 2048) e = launch_ex(evict_kernel<256>, grid, dim3(256), a.keys * 4, st, false, cluster, a);
+  else e = launch_ex(evict_kernel<512>, grid, dim3(512), a.keys * 4, st, false, cluster, a);
+  if (e == cudaSuccess && in_place) e = cudaMemcpyAsync(len_out, a.len_out, c->batch * 4, cudaMemcpyDeviceToDevice, st);
   return e == cudaSuccess ? ASR_OK : ASR_E_CUDA;
 }
 
