@@ -67,10 +67,10 @@ __device__ __forceinline__ int ld_cluster(const int* at, int rank) {
 }
 
 template <int THREADS>
-__global__ void __launch_bounds__(THREADS) evict_kernel(EvictArgs a) {
+__global__ void __launch_bounds__(THREADS, 1024 / THREADS) evict_kernel(EvictArgs a) {
   constexpr int WARPS = THREADS / 32;
   __shared__ int hist[4][256];
-  __shared__ int s_bin, s_need;
+  __shared__ int s_hist[256], s_cut[4][3];   // the cluster's; a pass's bin, how many of it stay, how many it has
   __shared__ int s_warp[3][WARPS], s_rank[3][EV_MAX_CLUSTER];
   __shared__ long long s_to[THREADS], s_of[THREADS];
   extern __shared__ uint32_t s_key[];
@@ -98,7 +98,16 @@ __global__ void __launch_bounds__(THREADS) evict_kernel(EvictArgs a) {
   const int newest = a.seen[b] - a.recent;
   const int cached = min(i1 - i0, a.keys);
   auto key = [&](int i) { return i - i0 < cached ? s_key[i - i0] : rank_key(sc[i], ps[i], newest, a.first); };
+#pragma unroll 4
   for (int i = tid; i < cached; i += THREADS) s_key[i] = rank_key(sc[i0 + i], ps[i0 + i], newest, a.first);
+  if (so != sc) {   // what stays below the budget, and in the freed slots what the moves overwrite
+#pragma unroll 4
+    for (int i = i0 + tid; i < min(i1, a.budget); i += THREADS) so[i] = sc[i];
+  }
+  if (po != ps) {
+#pragma unroll 4
+    for (int i = i0 + tid; i < min(i1, a.budget); i += THREADS) po[i] = ps[i];
+  }
   for (int i = tid; i < 4 * 256; i += THREADS) hist[0][i] = 0;
   __syncthreads();
 
@@ -120,17 +129,22 @@ __global__ void __launch_bounds__(THREADS) evict_kernel(EvictArgs a) {
       }
     }
     sync();
+    if (CL > 1) {   // the cluster's histogram
+      for (int bin = tid; bin < 256; bin += THREADS) {
+        int x[EV_MAX_CLUSTER], sum = 0;
+#pragma unroll
+        for (int q = 0; q < EV_MAX_CLUSTER; ++q) x[q] = q < CL ? ld_cluster(&hist[pass][bin], q) : 0;
+#pragma unroll
+        for (int q = 0; q < EV_MAX_CLUSTER; ++q) sum += x[q];
+        s_hist[bin] = sum;
+      }
+      __syncthreads();
+    }
     if (warp == 0) {   // bins from the top, 8 a lane
+      const int* bins = CL > 1 ? s_hist : hist[pass];
       int x[8], mine = 0;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const int* bin = &hist[pass][255 - (lane * 8 + j)];
-        x[j] = 0;
-        if (CL == 1) x[j] = *bin;
-        else
-          for (int q = 0; q < CL; ++q) x[j] += ld_cluster(bin, q);
-        mine += x[j];
-      }
+      for (int j = 0; j < 8; ++j) mine += x[j] = bins[255 - (lane * 8 + j)];
       int inc = mine;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
@@ -142,17 +156,22 @@ __global__ void __launch_bounds__(THREADS) evict_kernel(EvictArgs a) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
           if (before < need && need <= before + x[j]) {
-            s_bin = 255 - (lane * 8 + j);
-            s_need = need - before;
+            s_cut[pass][0] = 255 - (lane * 8 + j);
+            s_cut[pass][1] = need - before;
+            s_cut[pass][2] = x[j];
           }
           before += x[j];
         }
       }
     }
     __syncthreads();
-    prefix |= (uint32_t)s_bin << shift;
-    need = s_need;
-    __syncthreads();
+    prefix |= (uint32_t)s_cut[pass][0] << shift;
+    need = s_cut[pass][1];
+    if (need == s_cut[pass][2]) {   // the whole bin stays (never all slots, so prefix > 0): cut just below it
+      prefix -= 1;
+      need = 0;
+      break;
+    }
   }
 
   // Slots above the key stay, and of those equal to it the first `need` in slot
@@ -209,14 +228,9 @@ __global__ void __launch_bounds__(THREADS) evict_kernel(EvictArgs a) {
   int moves, sum;
   const int hole0 = before_warp(1, my_holes, moves), src0 = before_warp(2, my_srcs, sum);
   int *holes = a.holes + task * a.max_moves, *srcs = a.srcs + task * a.max_moves;
-  const bool copy = so != sc || po != ps;
-  walk(hole0, src0, [&](int i, bool keep, unsigned bh, unsigned bs, int hole, int src) {
+  walk(hole0, src0, [&](int i, bool, unsigned bh, unsigned bs, int hole, int src) {
     if (bh >> lane & 1) __stcg(holes + hole + __popc(bh & below), i);
     if (bs >> lane & 1) __stcg(srcs + src + __popc(bs & below), i);
-    if (copy && keep && i < a.budget) {
-      so[i] = sc[i];
-      po[i] = ps[i];
-    }
   });
   sync();
 
@@ -328,8 +342,9 @@ int asr_spec_paged_evict(const asr_paged_cache* c, const asr_paged_scores* s, co
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   const dim3 grid(cluster, c->kv_heads, c->batch);
   cudaError_t e;
-  if (part <= 2048) e = launch_ex(evict_kernel<256>, grid, dim3(256), a.keys * 4, st, false, cluster, a);
-  else e = launch_ex(evict_kernel<512>, grid, dim3(512), a.keys * 4, st, false, cluster, a);
+  // Few slots a block: smaller blocks, so that more heads share an SM and hide one another's passes.
+  if (part <= 512) e = launch_ex(evict_kernel<128>, grid, dim3(128), a.keys * 4, st, false, cluster, a);
+  else e = launch_ex(evict_kernel<256>, grid, dim3(256), a.keys * 4, st, false, cluster, a);
   if (e == cudaSuccess && in_place) e = cudaMemcpyAsync(len_out, a.len_out, c->batch * 4, cudaMemcpyDeviceToDevice, st);
   return e == cudaSuccess ? ASR_OK : ASR_E_CUDA;
 }
