@@ -71,7 +71,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) evict_kernel(EvictArg
   constexpr int WARPS = THREADS / 32;
   __shared__ int hist[4][256];
   __shared__ int s_hist[256], s_cut[4][3];   // the cluster's; a pass's bin, how many of it stay, how many it has
-  __shared__ int s_warp[3][WARPS], s_rank[3][EV_MAX_CLUSTER];
+  __shared__ int2 s_warp[2][WARPS], s_rank[2][EV_MAX_CLUSTER];
   __shared__ long long s_to[THREADS], s_of[THREADS];
   extern __shared__ uint32_t s_key[];
   const int CL = gridDim.x, rank = blockIdx.x, h = blockIdx.y, b = blockIdx.z;
@@ -98,15 +98,26 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) evict_kernel(EvictArg
   const int newest = a.seen[b] - a.recent;
   const int cached = min(i1 - i0, a.keys);
   auto key = [&](int i) { return i - i0 < cached ? s_key[i - i0] : rank_key(sc[i], ps[i], newest, a.first); };
-#pragma unroll 4
-  for (int i = tid; i < cached; i += THREADS) s_key[i] = rank_key(sc[i0 + i], ps[i0 + i], newest, a.first);
-  if (so != sc) {   // what stays below the budget, and in the freed slots what the moves overwrite
-#pragma unroll 4
-    for (int i = i0 + tid; i < min(i1, a.budget); i += THREADS) so[i] = sc[i];
-  }
-  if (po != ps) {
-#pragma unroll 4
-    for (int i = i0 + tid; i < min(i1, a.budget); i += THREADS) po[i] = ps[i];
+  // Ranks to shared memory; scores and positions below the budget to the
+  // outputs, where the moves then overwrite the freed slots.
+  const bool copy_s = so != sc, copy_p = po != ps;
+  const int ends = max(i0 + cached, copy_s || copy_p ? min(i1, a.budget) : 0);
+  for (int i = i0 + tid; i < ends; i += THREADS * 8) {
+    float x[8];
+    int p[8];
+#pragma unroll
+    for (int y = 0; y < 8; ++y) {
+      x[y] = __ldcg(sc + min(i + y * THREADS, ends - 1));
+      p[y] = __ldcg(ps + min(i + y * THREADS, ends - 1));
+    }
+#pragma unroll
+    for (int y = 0; y < 8; ++y) {
+      const int at = i + y * THREADS;
+      if (at >= ends) break;
+      if (at - i0 < cached) s_key[at - i0] = rank_key(x[y], p[y], newest, a.first);
+      if (copy_s && at < a.budget) so[at] = x[y];
+      if (copy_p && at < a.budget) po[at] = p[y];
+    }
   }
   for (int i = tid; i < 4 * 256; i += THREADS) hist[0][i] = 0;
   __syncthreads();
@@ -118,6 +129,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) evict_kernel(EvictArg
   for (int pass = 0; pass < 4; ++pass) {
     const int shift = 24 - 8 * pass;
     const uint32_t mask = pass == 0 ? 0u : 0xffffffffu << (shift + 8);
+#pragma unroll 4
     for (int base = i0 + warp * 32; base < i1; base += THREADS) {
       const uint32_t k = base + lane < i1 ? key(base + lane) : 0u;
       const bool in = base + lane < i1 && (k & mask) == prefix;
@@ -180,34 +192,42 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) evict_kernel(EvictArg
   const int per = ((i1 - i0 + 31) / 32 + WARPS - 1) / WARPS * 32;
   const int w0 = i0 + warp * per, w1 = min(i1, w0 + per);
   const unsigned below = (1u << lane) - 1;
-  // exclusive count over the cluster of a warp's number; `total` receives the sum
-  auto before_warp = [&](int which, int count, int& total) {
+  // exclusive counts over the cluster of two numbers of a warp, and the first one's sum
+  auto before_warp = [&](int which, int2 count, int& total) {
     if (lane == 0) s_warp[which][warp] = count;
     __syncthreads();
-    int x = 0, all = 0;
+    int2 x = make_int2(0, 0), all = x;
     for (int w = 0; w < WARPS; ++w) {
-      if (w < warp) x += s_warp[which][w];
-      all += s_warp[which][w];
+      const int2 y = s_warp[which][w];
+      if (w < warp) x.x += y.x, x.y += y.y;
+      all.x += y.x, all.y += y.y;
     }
-    total = all;
+    total = all.x;
     if (CL > 1) {
-      if (tid < CL) st_cluster(&s_rank[which][rank], tid, all);
+      if (tid < CL) {
+        st_cluster(&s_rank[which][rank].x, tid, all.x);
+        st_cluster(&s_rank[which][rank].y, tid, all.y);
+      }
       cluster_sync();
       total = 0;
       for (int q = 0; q < CL; ++q) {
-        if (q < rank) x += s_rank[which][q];
-        total += s_rank[which][q];
+        const int2 y = s_rank[which][q];
+        if (q < rank) x.x += y.x, x.y += y.y;
+        total += y.x;
       }
     }
     return x;
   };
-  int count = 0, total = 0;
-  for (int base = w0; base < w1; base += 32)
-    count += __popc(__ballot_sync(0xffffffffu, base + lane < w1 && key(base + lane) == prefix));
-  const int eq0 = before_warp(0, count, total);
+  int count = 0, total = 0, eq0 = 0, moves = 0;
+  if (need > 0) {   // uniform over the cluster: some of the slots at the cut stay and some go
+    for (int base = w0; base < w1; base += 32)
+      count += __popc(__ballot_sync(0xffffffffu, base + lane < w1 && key(base + lane) == prefix));
+    eq0 = before_warp(0, make_int2(count, 0), total).x;
+  }
   // f(slot, kept, its place among the freed below the budget, its place among the kept past it)
   auto walk = [&](int hole, int src, auto f) {
     int eq = eq0;
+#pragma unroll 4
     for (int base = w0; base < w1; base += 32) {
       const int i = base + lane;
       const uint32_t k = i < w1 ? key(i) : 0u;
@@ -224,11 +244,9 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) evict_kernel(EvictArg
     total = src;
   };
   walk(0, 0, [](int, bool, unsigned, unsigned, int, int) {});
-  const int my_holes = count, my_srcs = total;
-  int moves, sum;
-  const int hole0 = before_warp(1, my_holes, moves), src0 = before_warp(2, my_srcs, sum);
+  const int2 at0 = before_warp(1, make_int2(count, total), moves);
   int *holes = a.holes + task * a.max_moves, *srcs = a.srcs + task * a.max_moves;
-  walk(hole0, src0, [&](int i, bool, unsigned bh, unsigned bs, int hole, int src) {
+  walk(at0.x, at0.y, [&](int i, bool, unsigned bh, unsigned bs, int hole, int src) {
     if (bh >> lane & 1) __stcg(holes + hole + __popc(bh & below), i);
     if (bs >> lane & 1) __stcg(srcs + src + __popc(bs & below), i);
   });
