@@ -292,9 +292,83 @@ __device__ __forceinline__ void clear_rows(const AttendArgs& a, const PlanMem& m
   }
 }
 
+// Who works on what.  Every end of an item costs its warps a few steps' time
+// (pipeline fill, the way through shared memory), and every item that is split
+// over blocks a way through L2 and a join besides; whole items cost balance
+// instead.  So, by the lengths at hand and in steps:
+//   WARP    a warp takes whole items:   the longest item, or an equal share;
+//   BLOCK   a block takes whole items, its warps each a part of the steps;
+//   SPLIT   equal runs of steps for all warps, items split wherever a run ends.
+// Whole items are dealt longest sequence first, to and fro over the takers.
+// Measured, us a call: 64 sequences of up to 448 slots, 1280 heads: WARP @@, SPLIT 39;
+// 32 of up to 1500, 384 heads: BLOCK @@, SPLIT 31; one sequence of 230, 20
+// heads: BLOCK @@, SPLIT 13.7; one of 100001, 20 heads: SPLIT 110, BLOCK 400.
+enum Deal { DEAL_WARP, DEAL_BLOCK, DEAL_SPLIT };
+constexpr int DEAL_SORT_MAX = PA_WARPS * 32;   // sequences that a block ranks, one a thread
+constexpr float END_COST = 4.f, JOIN_COST = 5.f;   // steps
+
+struct DealMem {
+  int *order, *pre;   // [B] sequences by falling length, [B + 1] items before each
+  int items;
+};
+constexpr size_t deal_bytes(int B) { return B <= DEAL_SORT_MAX ? ((size_t)B * 8 + 4 + 15) / 16 * 16 : 0; }
+
+template <int KS, int TR>
+__device__ __forceinline__ Deal choose_deal(const AttendArgs& a, const WorkPlan& plan, const PlanMem& mem, DealMem& dm,
+                                            int* smem) {
+  __shared__ int s_long;
+  const int B = a.c.batch, b = threadIdx.x, lane = threadIdx.x & 31;
+  if (B > DEAL_SORT_MAX) return DEAL_SPLIT;
+  dm.order = smem;
+  dm.pre = smem + B;
+  int steps = 0, items = 0, rank = 0;
+  if (b == 0) s_long = 0;
+  if (b < B) {
+    const SeqWork s = seq_work<KS, TR>(a.r, mem.lens[b].x, mem.lens[b].y);
+    steps = s.steps;
+    items = s.steps ? a.c.kv_heads * s.tiles : 0;
+    dm.pre[b + 1] = steps;
+  }
+  __syncthreads();
+  if (b < B) {
+    for (int x = 0; x < B; ++x) {
+      const int y = dm.pre[x + 1];
+      rank += y > steps || (y == steps && x < b);
+    }
+    dm.order[rank] = b;
+    if (rank == 0) s_long = steps;
+  }
+  __syncthreads();
+  if (b < B) dm.pre[rank + 1] = items;
+  __syncthreads();
+  if (threadIdx.x < 32) {
+    int base = 0;
+    for (int b0 = 0; b0 < B; b0 += 32) {
+      int x = b0 + lane < B ? dm.pre[b0 + lane + 1] : 0;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int y = __shfl_up_sync(0xffffffffu, x, o);
+        if (lane >= o) x += y;
+      }
+      if (b0 + lane < B) dm.pre[b0 + lane + 1] = base + x;
+      base += __shfl_sync(0xffffffffu, x, 31);
+    }
+    if (lane == 0) dm.pre[0] = 0;
+  }
+  __syncthreads();
+  dm.items = dm.pre[B];
+  const float u = (float)plan.units, n = (float)dm.items, longest = (float)s_long;
+  const float warps = (float)a.max_workers, blocks = warps / PA_WARPS;
+  const float by_warp = fmaxf(longest + END_COST, n <= warps ? 0.f : 1.1f * (u + END_COST * n) / warps);
+  const float by_block = fmaxf(longest / PA_WARPS + END_COST + 1.f,
+                               n <= blocks ? 0.f : 1.1f * (u / PA_WARPS + (END_COST + 1.f) * n) / blocks);
+  const float split = u / warps + 2.f * END_COST + JOIN_COST;
+  return by_warp <= by_block ? (by_warp <= split ? DEAL_WARP : DEAL_SPLIT) : by_block <= split ? DEAL_BLOCK : DEAL_SPLIT;
+}
+
 // What the two kernels below share: the plan, the walk over a warp's items and
-// their ends.  `item` computes keys [s0, s0 + n) steps of one item and leaves
-// the result in the warp's shared memory.
+// their ends.  `item` computes steps [s0, s0 + n) of one item and leaves the
+// result in the warp's shared memory.
 template <typename T, int D, int KS, int TR, typename F>
 __device__ __forceinline__ void attend_items(const AttendArgs& a, F item) {
   constexpr int REGION = Part<D, TR>::FLOATS * Part<D, TR>::STAGE;
@@ -306,39 +380,67 @@ __device__ __forceinline__ void attend_items(const AttendArgs& a, F item) {
     return c.kv_heads * s.tiles * s.steps;
   });
   clear_rows<T, D>(a, mem);
-  const int warp = threadIdx.x >> 5, w0 = blockIdx.x * PA_WARPS, worker = w0 + warp;
-  if (plan.units == 0 || w0 >= plan.workers) return;
+  if (plan.units == 0) return;
   extern __shared__ __align__(16) unsigned char smem[];
-  float* sm = reinterpret_cast<float*>(smem + plan_bytes(c.batch));
+  DealMem dm;
+  const Deal deal = choose_deal<KS, TR>(a, plan, mem, dm, reinterpret_cast<int*>(smem + plan_bytes(c.batch)));
+  float* sm = reinterpret_cast<float*>(smem + plan_bytes(c.batch) + deal_bytes(c.batch));
+  const int warp = threadIdx.x >> 5, w0 = blockIdx.x * PA_WARPS, worker = w0 + warp;
 
-  const int w1 = min(w0 + PA_WARPS, plan.workers), block0 = plan.start(w0), block1 = plan.start(w1);
+  // SPLIT: this warp's run of units [u, u_end), the block's [block0, block1)
+  const int w1 = min(w0 + PA_WARPS, plan.workers), block0 = plan.start(min(w0, plan.workers)), block1 = plan.start(w1);
   int u = worker < plan.workers ? plan.start(worker) : block1;
   const int u_end = worker < plan.workers ? plan.start(worker + 1) : block1;
-  bool team = true;   // all warps of the block work on one item
-  for (int at = block0;;) {
-    const int b = work_find(mem.pre, c.batch, at);
-    const SeqWork s = seq_work<KS, TR>(r, mem.lens[b].x, mem.lens[b].y);
-    const int rem = at - mem.pre[b], it = rem / s.steps, kvh = it / s.tiles, tile = it - kvh * s.tiles;
-    const int u0 = mem.pre[b] + it * s.steps, u1 = u0 + s.steps;
-    if (team && block1 > u1) {   // uniform over the block, at its first item only
-      team = false;
-      if (worker >= plan.workers) return;
-      if (u > block0) {
-        at = u;
-        continue;
+  if (deal == DEAL_SPLIT && w0 >= plan.workers) return;
+  // WARP, BLOCK: taker and takers; consecutive items go to different SMs
+  const int takers = deal == DEAL_WARP ? a.max_workers : gridDim.x;
+  const int taker = deal == DEAL_WARP ? warp * gridDim.x + blockIdx.x : blockIdx.x;
+  bool team = deal != DEAL_WARP;   // all warps of the block work on one item
+  for (int round = 0, at = block0;;) {
+    int b, it, u0 = 0, u1 = 0, s0, n, active = PA_WARPS;
+    SeqWork s;
+    if (deal == DEAL_SPLIT) {
+      b = work_find(mem.pre, c.batch, at);
+      s = seq_work<KS, TR>(r, mem.lens[b].x, mem.lens[b].y);
+      it = (at - mem.pre[b]) / s.steps;
+      u0 = mem.pre[b] + it * s.steps, u1 = u0 + s.steps;
+      if (team && block1 > u1) {   // uniform over the block, at its first item only
+        team = false;
+        if (worker >= plan.workers) return;
+        if (u > block0) {
+          at = u;
+          continue;
+        }
+      }
+      s0 = u - u0, n = min(u1, u_end) - u;
+      active = w1 - w0;
+    } else {
+      const int k = round * takers + (round & 1 ? takers - 1 - taker : taker);
+      if (k >= dm.items) return;
+      ++round;
+      const int rank = work_find(dm.pre, c.batch, k);
+      b = dm.order[rank];
+      it = k - dm.pre[rank];
+      s = seq_work<KS, TR>(r, mem.lens[b].x, mem.lens[b].y);
+      s0 = 0, n = s.steps;
+      if (team) {
+        active = min(PA_WARPS, s.steps);
+        s0 = s.steps * min(warp, active) / active;
+        n = s.steps * min(warp + 1, active) / active - s0;
       }
     }
-    const int s0 = u - u0, n = min(u1, u_end) - u;
+    const int kvh = it / s.tiles, tile = it - kvh * s.tiles;
     if (n > 0) item(s, b, kvh, tile, s0, n, sm + warp * REGION);
     if (team) {
-      finish_item<T, D, TR, true>(a, plan, sm, w1 - w0, b, kvh, tile, s.rows * r.group, u0, u1, w0, block0 == u0,
-                                  block0 == u0 && block1 == u1);
-      return;
+      const bool whole = deal == DEAL_BLOCK || (block0 == u0 && block1 == u1);
+      finish_item<T, D, TR, true>(a, plan, sm, active, b, kvh, tile, s.rows * r.group, u0, u1, w0, block0 == u0, whole);
+      if (deal == DEAL_SPLIT) return;
+    } else {
+      finish_item<T, D, TR, false>(a, plan, sm + warp * REGION, 1, b, kvh, tile, s.rows * r.group, u0, u1, worker, s0 == 0,
+                                   n == s.steps);
+      at = u += n;
+      if (deal == DEAL_SPLIT && u >= u_end) return;
     }
-    finish_item<T, D, TR, false>(a, plan, sm + warp * REGION, 1, b, kvh, tile, s.rows * r.group, u0, u1, worker, s0 == 0,
-                                 n == s.steps);
-    at = u += n;
-    if (u >= u_end) return;
   }
 }
 
@@ -646,11 +748,11 @@ cudaError_t launch_attend(const AttendArgs& a, cudaStream_t st) {
   if (e != cudaSuccess) return e;
   const uint64_t bit = 1ull << (dev & 63);
   if (!(ready.load(std::memory_order_acquire) & bit)) {
-    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(REGIONS + plan_bytes(PG_MAX_BATCH)));
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(REGIONS + plan_bytes(PG_MAX_BATCH) + deal_bytes(DEAL_SORT_MAX)));
     if (e != cudaSuccess) return e;
     ready.fetch_or(bit, std::memory_order_release);
   }
-  kernel<<<a.max_workers / PA_WARPS, PA_WARPS * 32, REGIONS + plan_bytes(a.c.batch), st>>>(a);
+  kernel<<<a.max_workers / PA_WARPS, PA_WARPS * 32, REGIONS + plan_bytes(a.c.batch) + deal_bytes(a.c.batch), st>>>(a);
   return cudaGetLastError();
 }
 
