@@ -308,20 +308,24 @@ def accept_sampled(target, draft, lens, u, race, *, draft_logits=None, temperatu
     if _current_device() != index:
         with torch.cuda.device(device):
             return accept_sampled(target, draft, lens, u, race, draft_logits=draft_logits, temperature=temperature, status=status)
-    B, k = draft.shape
     x = A.AsrSampledLogits.from_buffer_copy(layout)
     x.target = target.data_ptr()
-    if draft_logits is not None and k:
+    if draft_logits is not None and x.k:
         x.draft_logits = draft_logits.data_ptr()
-    ints = torch.empty((3, B), dtype=torch.int32, device=device)
-    prob = torch.empty((B, k), dtype=torch.float32, device=device)
-    at = ints.data_ptr()
-    _check(A.lib().asr_spec_accept_sampled(
+    accepted = torch.empty(x.batch, dtype=torch.int32, device=device)
+    token, step, prob = torch.empty_like(accepted), torch.empty_like(accepted), torch.empty_like(u)
+    _check(_accept(
         ctypes.byref(x), draft.data_ptr(), None if lens is None else lens.data_ptr(), u.data_ptr(), race.data_ptr(), race_stride,
-        temperature, at, at + 4 * B, at + 8 * B, prob.data_ptr(), None if status is None else status.data_ptr(),
-        _raw_stream(index)), "asr_spec_accept_sampled")
-    accepted, token, step = ints.unbind(0)
+        temperature, accepted.data_ptr(), token.data_ptr(), step.data_ptr(), prob.data_ptr(),
+        None if status is None else status.data_ptr(), _raw_stream(index)), "asr_spec_accept_sampled")
     return accepted, token, step, prob
+
+
+def _accept(*args):
+    """The library's entry; looked up at the first call, which loads the library."""
+    global _accept
+    _accept = A.lib().asr_spec_accept_sampled
+    return _accept(*args)
 
 
 def _accept_layout(target, draft, lens, u, race, draft_logits, temperature, status):
