@@ -42,12 +42,15 @@ __device__ __forceinline__ SeqWork weigh_seq(const WeighArgs& a, int len, int ro
   return s;
 }
 
-// One lane's slot: add the weight, or start the slot of a new row.
-__device__ __forceinline__ void put_score(const WeighArgs& a, const SeqWork& s, int b, int kvh, int key, float w) {
+// One lane's slot: its score before, and the end of it.
+__device__ __forceinline__ float old_score(const WeighArgs& a, const SeqWork& s, int b, int kvh, int key) {
+  return key < min(s.len, s.paged) && a.score ? __ldcg(a.score + b * a.score_b + kvh * a.score_h + key) : 0.f;
+}
+__device__ __forceinline__ void put_score(const WeighArgs& a, const SeqWork& s, int b, int kvh, int key, float v) {
   if (key >= s.paged) return;
   const long long at = b * a.score_b + kvh * a.score_h + key;
-  a.out[at] = (key < s.len && a.score ? a.score[at] : 0.f) + w;
-  if (a.pos && key >= s.len) a.pos[at] = a.first_pos[b] + key - s.len;
+  a.out[at] = v;
+  if (a.pos && key >= s.len) a.pos[at] = a.first_pos[b] + key - s.len;   // the slot of a new row
 }
 
 template <typename T, int D>
@@ -109,6 +112,10 @@ __global__ void __launch_bounds__(PW_WARPS * 32, 4) weigh16_kernel(WeighArgs a, 
       }
     };
     if (s.tiles) rows_of(0);
+    // Of a step's KS slots a lane ends with the sum of one, after the exchange below.
+    constexpr int V = KS / 4;
+    const int mine = ((g % V) >> 1) * 8 + 2 * t + (g & 1);
+    float old = old_score(a, s, b, kvh, s0 * KS + mine);
     for (int i = 0; i < n; ++i) {
       const int step = s0 + i;
       float w[KS / 8][2];
@@ -139,16 +146,31 @@ __global__ void __launch_bounds__(PW_WARPS * 32, 4) weigh16_kernel(WeighArgs a, 
 #pragma unroll
           for (int x = 0; x < NG; ++x) pid[x] = ks.id(step + 2, x);
       }
+      const float before = old;
+      if (i + 1 < n) old = old_score(a, s, b, kvh, (step + 1) * KS + mine);
+      // The eight lanes of a column hold the sums of their rows for V slots
+      // each: every exchange halves the slots that a lane goes on with.
+      float v[V];
 #pragma unroll
-      for (int kt = 0; kt < KS / 8; ++kt)
+      for (int x = 0; x < V; ++x) v[x] = w[x >> 1][x & 1];
+      if (V == 8) {
 #pragma unroll
-        for (int x = 0; x < 2; ++x) {
-          float v = w[kt][x];
-          v += __shfl_xor_sync(0xffffffffu, v, 4);
-          v += __shfl_xor_sync(0xffffffffu, v, 8);
-          v += __shfl_xor_sync(0xffffffffu, v, 16);
-          if (g == (kt * 2 + x) % 8) put_score(a, s, b, kvh, step * KS + kt * 8 + 2 * t + x, v);
+        for (int x = 0; x < 4; ++x) {
+          const float give = g & 4 ? v[x] : v[x + V / 2], keep = g & 4 ? v[x + V / 2] : v[x];
+          v[x] = keep + __shfl_xor_sync(0xffffffffu, give, 16);
         }
+      } else {
+#pragma unroll
+        for (int x = 0; x < V; ++x) v[x] += __shfl_xor_sync(0xffffffffu, v[x], 16);
+      }
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        const float give = g & 2 ? v[x] : v[x + 2], keep = g & 2 ? v[x + 2] : v[x];
+        v[x] = keep + __shfl_xor_sync(0xffffffffu, give, 8);
+      }
+      const float give = g & 1 ? v[0] : v[1], keep = g & 1 ? v[1] : v[0];
+      const float sum = keep + __shfl_xor_sync(0xffffffffu, give, 4);
+      if (g < V) put_score(a, s, b, kvh, step * KS + mine, before + sum);
     }
   }
 }
@@ -215,7 +237,10 @@ __global__ void __launch_bounds__(PW_WARPS * 32) weigh32_kernel(WeighArgs a, int
     }
 #pragma unroll
     for (int k = 0; k < IT; ++k)
-      if (e == k) put_score(a, s, b, kvh, step * KS + 4 * k + kg, w[k]);
+      if (e == k) {
+        const int key = step * KS + 4 * k + kg;
+        put_score(a, s, b, kvh, key, old_score(a, s, b, kvh, key) + w[k]);
+      }
   }
 }
 
