@@ -109,6 +109,31 @@ __device__ __forceinline__ uint4 ldg_if(bool in, const char* p) {   // zero wher
   return v;
 }
 
+// Global -> shared copy counted on an mbarrier; addresses and size multiples of 16 bytes.
+__device__ __forceinline__ void bulk_copy(uint32_t smem, const char* p, uint32_t bytes, uint64_t* bar) {
+  asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(smem), "l"(p),
+               "r"(bytes), "r"(smem_u32(bar))
+               : "memory");
+}
+// Waits for a phase, at most about a second; then, and at once from there on,
+// it gives up: the status word says so and the results are invalid.
+__device__ __forceinline__ void bar_wait(uint64_t* bar, uint32_t parity, int* status, bool& gave_up) {
+  if (mbar_try_wait(bar, parity) || gave_up) return;
+  const long long t0 = clock64();
+  while (!mbar_try_wait(bar, parity)) {
+    if (clock64() - t0 > (1ll << 31)) {
+      if (status) set_status(status, ST_WAIT_TIMEOUT);
+      gave_up = true;
+      return;
+    }
+  }
+}
+__device__ __forceinline__ uint4 lds16(uint32_t smem) {
+  uint4 v;
+  asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(smem) : "memory");
+  return v;
+}
+
 // ---------------------------------------------------------------------------
 // Work distribution.  The units of a call are key steps in the order
 // (sequence, item, step), an item being what one warp keeps in registers (a
@@ -288,6 +313,32 @@ struct Keys16 {
 #pragma unroll
           for (int j = 0; j < NC; ++j) kf[u * 2 + w][j] = ldg_if(u * PG_GROUP + w * 8 + g < left, p + w * 8 * stride + j * 64);
       }
+    }
+  }
+  // A step's K (or V) by bulk copies into shared memory, rows of D in slot
+  // order, counted on `bar`: whole groups where a head's slots are contiguous,
+  // else a row a lane.  Keys past the end are not written.
+  __device__ __forceinline__ void fetch(int step, const char* pages, const char* fresh, const long long* off, uint32_t dst,
+                                        uint64_t* bar) const {
+    constexpr int ROW = D * (int)sizeof(T);
+    const int lane = threadIdx.x & 31, left = end(step) - first(step);
+    if (step < s.psteps && c.slot_stride == ROW) {
+      if (lane == 0) {
+        const int groups = min(NG, (left + PG_GROUP - 1) / PG_GROUP);
+        mbar_arrive_expect_tx(bar, groups * PG_GROUP * ROW);
+#pragma unroll
+        for (int u = 0; u < NG; ++u)
+          if (u < groups) bulk_copy(dst + u * PG_GROUP * ROW, pages + off[u], PG_GROUP * ROW, bar);
+      }
+    } else {
+      const int rows = min(KS, left);
+      if (lane == 0) mbar_arrive_expect_tx(bar, rows * ROW);
+      __syncwarp();
+      long long base = off[0];
+      if (NG > 1 && lane >= PG_GROUP) base = off[NG - 1];
+      const char* src = step < s.psteps ? pages + base + (lane % PG_GROUP) * c.slot_stride
+                                        : fresh + (long long)((step - s.psteps) * KS + lane) * r.n_r;
+      if (lane < rows) bulk_copy(dst + lane * ROW, src, ROW, bar);
     }
   }
   // V: vf[group][which of the lane's four keys 2t, 2t+1, 2t+8, 2t+9][64-wide half]

@@ -40,7 +40,8 @@
 namespace asrspec {
 namespace {
 
-constexpr int PA_WARPS = 8;   // one block an SM: registers for a step of K and V in flight a warp
+constexpr int PA_WARPS = 8;   // one block an SM
+constexpr int PA_STAGES = 3;  // steps of K and V (8 KB) that a warp has in flight or in use
 
 
 
@@ -142,7 +143,10 @@ __device__ __forceinline__ void guard_values(const Keys16<T, D>& ks, int step, c
 template <int D, int TR>
 struct Part {
   static constexpr int FLOATS = TR * (D + 2);
-  static constexpr int STAGE = FLOATS * 4 > 4300 ? 2 : 3;   // regions a warp has to fetch partial results into, its own among them
+  // A warp's shared memory: the ring of its loads (16-bit types), then, the ring
+  // drained, its result and room to fetch others' partial results into.
+  static constexpr int RING = TR == 4 ? 0 : PA_STAGES * 8192;
+  static constexpr int REGION = (RING ? RING : 3 * FLOATS * 4) / 4;   // floats
 };
 
 __device__ __forceinline__ void copy16(float* smem, const float* gmem) {   // by L2: another SM wrote it
@@ -197,7 +201,7 @@ __device__ __noinline__ void finish_item(const AttendArgs& a, const WorkPlan& pl
     Acc acc;
 #pragma unroll 1
     for (int w = 0; w < regions; ++w) {
-      const float* p = sm + w * PT::STAGE * PART;
+      const float* p = sm + w * PT::REGION;
       acc.add(p[in], p[TR + in], *reinterpret_cast<const float4*>(p + 2 * TR + in * D + col));
     }
     if (whole) {
@@ -243,7 +247,7 @@ __device__ __noinline__ void finish_item(const AttendArgs& a, const WorkPlan& pl
   if (!last) return;
 
   // Fetch as many parts at a time as there is room for, and add them up.
-  constexpr int ROOM = (BLOCK ? PA_WARPS : 1) * PT::STAGE, MAX_X = (TR * C4 + (BLOCK ? PA_WARPS * 32 : 32) - 1) / (BLOCK ? PA_WARPS * 32 : 32);
+  constexpr int ROOM = (BLOCK ? PA_WARPS : 1) * PT::REGION / PART, MAX_X = (TR * C4 + (BLOCK ? PA_WARPS * 32 : 32) - 1) / (BLOCK ? PA_WARPS * 32 : 32);
   const int used = 2 * TR + nr * D;   // floats of a part
   Acc acc[MAX_X];
   for (int p0 = 0; p0 < parts; p0 += ROOM) {
@@ -371,7 +375,7 @@ __device__ __forceinline__ Deal choose_deal(const AttendArgs& a, const WorkPlan&
 // result in the warp's shared memory.
 template <typename T, int D, int KS, int TR, typename F>
 __device__ __forceinline__ void attend_items(const AttendArgs& a, F item) {
-  constexpr int REGION = Part<D, TR>::FLOATS * Part<D, TR>::STAGE;
+  constexpr int REGION = Part<D, TR>::REGION;
   const PagedView& c = a.c;
   const PagedRows& r = a.r;
   PlanMem mem;
@@ -451,15 +455,37 @@ __global__ void __launch_bounds__(PA_WARPS * 32, 1) attend16_kernel(AttendArgs a
   const PagedRows& r = a.r;
   const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   const float sc = r.scale * LOG2E;
+  __shared__ __align__(8) uint64_t bars[PA_WARPS][PA_STAGES][2];   // K and V of a stage have landed
+  uint64_t(*bar)[2] = bars[threadIdx.x >> 5];
+  if (lane < 2 * PA_STAGES) mbar_init(&bar[lane >> 1][lane & 1], 1);
+  fence_mbar_init();
+  __syncwarp();
+  uint32_t phases = 0;   // a bit a stage
+  bool gave_up = false;
 
   attend_items<T, D, KS, TR>(a, [&](const SeqWork& s, int b, int kvh, int tile, int s0, int n, float* sm) {
     const long long new_off = b * r.n_b + kvh * r.n_h;
     Keys16<T, D> ks{c, r, s, c.table + b * c.table_stride, kvh * c.head_stride, r.k_new + new_off, r.v_new + new_off, g, t};
-    int pid[NG];
+    constexpr int KB = KS * D * 2;   // bytes of a step's K, and of its V
+    const uint32_t ring = smem_u32(sm);
     long long off[NG];
-    uint4 kf[KS / 8][NC], vf[NG][4][NV];
+    int pid[PA_STAGES][NG], next[NG];   // page ids, asked for a step ahead of the copies
 #pragma unroll
-    for (int x = 0; x < NG; ++x) pid[x] = ks.id(s0, x);
+    for (int i = 0; i < PA_STAGES; ++i)
+#pragma unroll
+      for (int x = 0; x < NG; ++x) pid[i][x] = i < n ? ks.id(s0 + i, x) : 0;
+#pragma unroll
+    for (int x = 0; x < NG; ++x) next[x] = PA_STAGES < n ? ks.id(s0 + PA_STAGES, x) : 0;
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // results were written here before
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < PA_STAGES; ++i) {
+      if (i < n) {
+        ks.offsets(s0 + i, pid[i], off);
+        ks.fetch(s0 + i, c.k, ks.kn, off, ring + i * 2 * KB, &bar[i][0]);
+        ks.fetch(s0 + i, c.v, ks.vn, off, ring + i * 2 * KB + KB, &bar[i][1]);
+      }
+    }
 
     uint32_t qa[MT][NC * 2][4];
     int lim[MT][2];   // slots that the fragment's rows see
@@ -487,98 +513,124 @@ __global__ void __launch_bounds__(PA_WARPS * 32, 1) attend16_kernel(AttendArgs a
       for (int d = 0; d < D / 8; ++d) O[mt][d][0] = O[mt][d][1] = O[mt][d][2] = O[mt][d][3] = 0.f;
     }
 
-    // Step i's products and step i + 1's loads; i = -1 only loads.
+    int stage = 0;
 #pragma unroll 1
-    for (int i = -1; i < n; ++i) {
+    for (int i = 0; i < n; ++i) {
       const int step = s0 + i;
-      const bool full = ks.full(step), more = i + 1 < n;
+      const bool full = ks.full(step), more = i + PA_STAGES < n;
+      const uint32_t slot = ring + stage * 2 * KB, parity = phases >> stage & 1;
+      uint64_t* landed = bar[stage];
+      phases ^= 1u << stage;
+      stage = stage + 1 == PA_STAGES ? 0 : stage + 1;
       float S[MT][KS / 8][4];
-      if (i >= 0) {
+      bar_wait(&landed[0], parity, c.status, gave_up);
+      {
+        const uint32_t at = slot + g * (D * 2) + t * 16;
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt)
+        for (int kt = 0; kt < KS / 8; ++kt) {
+          uint4 kf[NC];
 #pragma unroll
-          for (int kt = 0; kt < KS / 8; ++kt) {
+          for (int j = 0; j < NC; ++j) kf[j] = lds16(at + kt * 8 * (D * 2) + j * 64);
+#pragma unroll
+          for (int mt = 0; mt < MT; ++mt) {
             S[mt][kt][0] = S[mt][kt][1] = S[mt][kt][2] = S[mt][kt][3] = 0.f;
 #pragma unroll
             for (int j = 0; j < NC; ++j) {
-              Mma16<T>::mma(S[mt][kt], qa[mt][2 * j], kf[kt][j].x, kf[kt][j].y);
-              Mma16<T>::mma(S[mt][kt], qa[mt][2 * j + 1], kf[kt][j].z, kf[kt][j].w);
+              Mma16<T>::mma(S[mt][kt], qa[mt][2 * j], kf[j].x, kf[j].y);
+              Mma16<T>::mma(S[mt][kt], qa[mt][2 * j + 1], kf[j].z, kf[j].w);
             }
           }
+        }
       }
+      __syncwarp();   // all lanes have read the slot
       if (more) {
-        ks.offsets(step + 1, pid, off);
-        ks.load_k(step + 1, off, kf);
-        if (i + 2 < n)
+        ks.offsets(step + PA_STAGES, next, off);
+        ks.fetch(step + PA_STAGES, c.k, ks.kn, off, slot, &landed[0]);
+        if (i + PA_STAGES + 1 < n)
 #pragma unroll
-          for (int x = 0; x < NG; ++x) pid[x] = ks.id(step + 2, x);
+          for (int x = 0; x < NG; ++x) next[x] = ks.id(step + PA_STAGES + 1, x);
       }
-      if (i >= 0) {
-        if (!full) {
-          const int first = ks.first(step), end = ks.end(step);
+      const int first = ks.first(step), end = ks.end(step);
+      if (!full) {
 #pragma unroll
-          for (int mt = 0; mt < MT; ++mt)
+        for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-            for (int kt = 0; kt < KS / 8; ++kt)
+          for (int kt = 0; kt < KS / 8; ++kt)
 #pragma unroll
-              for (int x = 0; x < 4; ++x)
-                if (first + kt * 8 + 2 * t + (x & 1) >= min(lim[mt][x >> 1], end)) S[mt][kt][x] = -INFINITY;
+            for (int x = 0; x < 4; ++x)
+              if (first + kt * 8 + 2 * t + (x & 1) >= min(lim[mt][x >> 1], end)) S[mt][kt][x] = -INFINITY;
+      }
+      uint32_t pf[MT][KS / 8][2];
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt) {
+        float mx[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          float x = fmaxf(S[mt][0][2 * e], S[mt][0][2 * e + 1]);
+#pragma unroll
+          for (int kt = 1; kt < KS / 8; ++kt) x = fmaxf(x, fmaxf(S[mt][kt][2 * e], S[mt][kt][2 * e + 1]));
+          x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 1));
+          x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 2));
+          mx[e] = fmaxf(m_run[mt][e], x * sc);
         }
-        uint32_t pf[MT][KS / 8][2];
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt) {
-          float mx[2];
+        if (__any_sync(0xffffffffu, mx[0] > m_run[mt][0] || mx[1] > m_run[mt][1])) {
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
-            float x = fmaxf(S[mt][0][2 * e], S[mt][0][2 * e + 1]);
+            const float f = mx[e] == -INFINITY ? 1.f : ex2(m_run[mt][e] - mx[e]);
+            m_run[mt][e] = mx[e];
+            l_run[mt][e] *= f;
 #pragma unroll
-            for (int kt = 1; kt < KS / 8; ++kt) x = fmaxf(x, fmaxf(S[mt][kt][2 * e], S[mt][kt][2 * e + 1]));
-            x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 1));
-            x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 2));
-            mx[e] = fmaxf(m_run[mt][e], x * sc);
-          }
-          if (__any_sync(0xffffffffu, mx[0] > m_run[mt][0] || mx[1] > m_run[mt][1])) {
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              const float f = mx[e] == -INFINITY ? 1.f : ex2(m_run[mt][e] - mx[e]);
-              m_run[mt][e] = mx[e];
-              l_run[mt][e] *= f;
-#pragma unroll
-              for (int d = 0; d < D / 8; ++d) {
-                O[mt][d][2 * e] *= f;
-                O[mt][d][2 * e + 1] *= f;
-              }
-            }
-          }
-#pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            const float m = m_run[mt][e] == -INFINITY ? 0.f : m_run[mt][e];
-#pragma unroll
-            for (int kt = 0; kt < KS / 8; ++kt) {
-              const float p0 = ex2(fmaf(S[mt][kt][2 * e], sc, -m)), p1 = ex2(fmaf(S[mt][kt][2 * e + 1], sc, -m));
-              l_run[mt][e] += p0 + p1;
-              pf[mt][kt][e] = Mma16<T>::pack(p0, p1);
+            for (int d = 0; d < D / 8; ++d) {
+              O[mt][d][2 * e] *= f;
+              O[mt][d][2 * e + 1] *= f;
             }
           }
         }
-        if (!full && ks.end(step) > s.len) guard_values<T, D, MT>(ks, step, lim, vf, O);
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const float m = m_run[mt][e] == -INFINITY ? 0.f : m_run[mt][e];
+#pragma unroll
+          for (int kt = 0; kt < KS / 8; ++kt) {
+            const float p0 = ex2(fmaf(S[mt][kt][2 * e], sc, -m)), p1 = ex2(fmaf(S[mt][kt][2 * e + 1], sc, -m));
+            l_run[mt][e] += p0 + p1;
+            pf[mt][kt][e] = Mma16<T>::pack(p0, p1);
+          }
+        }
+      }
+      bar_wait(&landed[1], parity, c.status, gave_up);
+      uint4 vf[NG][4][NV];
+      {
+        const uint32_t at = slot + KB + 2 * t * (D * 2) + g * 16;
 #pragma unroll
         for (int x = 0; x < NG; ++x)
 #pragma unroll
-          for (int j = 0; j < NV; ++j)
+          for (int w = 0; w < 4; ++w) {
+            const int in = x * PG_GROUP + (w & 1) + (w >> 1) * 8;
 #pragma unroll
-            for (int d = 0; d < 8; ++d) {   // n-tile d of half j: output column 64 j + 8 n + d
-              const uint32_t sel = d & 1 ? 0x7632 : 0x5410;
-              const uint32_t b0 = __byte_perm(reg_of(vf[x][0][j], d >> 1), reg_of(vf[x][1][j], d >> 1), sel);
-              const uint32_t b1 = __byte_perm(reg_of(vf[x][2][j], d >> 1), reg_of(vf[x][3][j], d >> 1), sel);
+            for (int j = 0; j < NV; ++j) vf[x][w][j] = lds16(at + in * (D * 2) + j * 128);
+            if (!full && first + in + 2 * t >= end)   // past the end: whatever the slot held
 #pragma unroll
-              for (int mt = 0; mt < MT; ++mt) {
-                const uint32_t pa[4] = {pf[mt][2 * x][0], pf[mt][2 * x][1], pf[mt][2 * x + 1][0], pf[mt][2 * x + 1][1]};
-                Mma16<T>::mma(O[mt][j * 8 + d], pa, b0, b1);
-              }
-            }
+              for (int j = 0; j < NV; ++j) vf[x][w][j] = make_uint4(0, 0, 0, 0);
+          }
       }
-      if (more) ks.load_v(step + 1, off, vf);
+      if (!full && end > s.len) guard_values<T, D, MT>(ks, step, lim, vf, O);
+#pragma unroll
+      for (int x = 0; x < NG; ++x)
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+#pragma unroll
+          for (int d = 0; d < 8; ++d) {   // n-tile d of half j: output column 64 j + 8 n + d
+            const uint32_t sel = d & 1 ? 0x7632 : 0x5410;
+            const uint32_t b0 = __byte_perm(reg_of(vf[x][0][j], d >> 1), reg_of(vf[x][1][j], d >> 1), sel);
+            const uint32_t b1 = __byte_perm(reg_of(vf[x][2][j], d >> 1), reg_of(vf[x][3][j], d >> 1), sel);
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt) {
+              const uint32_t pa[4] = {pf[mt][2 * x][0], pf[mt][2 * x][1], pf[mt][2 * x + 1][0], pf[mt][2 * x + 1][1]};
+              Mma16<T>::mma(O[mt][j * 8 + d], pa, b0, b1);
+            }
+          }
+      __syncwarp();
+      if (more) ks.fetch(step + PA_STAGES, c.v, ks.vn, off, slot + KB, &landed[1]);
     }
     if (tile == 0 && s.fresh && s0 <= s.psteps && s.psteps < s0 + n) append_rows(c, r, s, b, kvh, D * sizeof(T));
 
@@ -741,7 +793,7 @@ int64_t attend_ws_bytes(int tr, int dim) { return MAX_WORKERS * 4 + (int64_t)att
 // One block an SM.  The shared memory above 48 KB that a kernel needs is asked for once a device.
 template <auto kernel, int D, int TR>
 cudaError_t launch_attend(const AttendArgs& a, cudaStream_t st) {
-  constexpr size_t REGIONS = (size_t)PA_WARPS * Part<D, TR>::STAGE * Part<D, TR>::FLOATS * 4;
+  constexpr size_t REGIONS = (size_t)PA_WARPS * Part<D, TR>::REGION * 4;
   static std::atomic<uint64_t> ready{0};
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
