@@ -241,32 +241,31 @@ template <> struct Mma16<__half> {
 
 template <int D> struct Cfg16 { static constexpr int KS = D == 64 ? 32 : 16; };   // keys a step
 
-// One sequence's share of the work.  Keys come in steps of KS: first the slots
-// in pages, then, where the block's own rows are passed, those rows.
+// One sequence's share of the work: its keys in steps of KS, first the slots in
+// pages, then, where the block's own rows are passed, those rows (whose slots
+// are the next ones).
 struct SeqWork {
   int len, rows;       // committed slots, rows
-  int paged, fresh;    // keys in pages, keys in the block's own rows
-  int psteps, steps, tiles;
+  int paged, keys;     // keys in pages, all keys
+  int steps, tiles;
 };
 template <int KS, int TR>
 __device__ __forceinline__ SeqWork seq_work(const PagedRows& r, int len, int rows) {
   SeqWork s;
   s.len = len;
   s.rows = rows;
-  s.fresh = r.k_new != nullptr ? rows : 0;
-  s.paged = rows == 0 ? 0 : len + (r.causal ? rows - s.fresh : 0);
-  s.psteps = (s.paged + KS - 1) / KS;
-  s.steps = s.psteps + (s.fresh + KS - 1) / KS;
+  const int fresh = r.k_new != nullptr ? rows : 0;
+  s.paged = rows == 0 ? 0 : len + (r.causal ? rows - fresh : 0);
+  s.keys = s.paged + fresh;
+  s.steps = (s.keys + KS - 1) / KS;
   s.tiles = (rows * r.group + TR - 1) / TR;
   return s;
 }
 
-// A warp's reader of one head's keys and values, step by step, as mma B
-// fragments.  A step whose slots are all committed is full; in the others keys
-// past the end are zero.
+// A warp's reader of one head's keys and values, step by step.
 template <typename T, int D>
 struct Keys16 {
-  static constexpr int KS = Cfg16<D>::KS, NG = KS / PG_GROUP, NC = D / 32, NV = D / 64;
+  static constexpr int KS = Cfg16<D>::KS, NG = KS / PG_GROUP, NC = D / 32, NV = D / 64, ROW = D * 2;
   const PagedView& c;
   const PagedRows& r;
   SeqWork s;
@@ -275,10 +274,8 @@ struct Keys16 {
   const char *kn, *vn;   // this sequence's and head's new rows
   int g, t;
 
+  // all of a step's keys are committed, so every row sees them
   __device__ __forceinline__ bool full(int step) const { return (step + 1) * KS <= min(s.len, s.paged); }
-  // slot of a step's first key, and the end of the run of slots that it reads from
-  __device__ __forceinline__ int first(int step) const { return step < s.psteps ? step * KS : s.len + (step - s.psteps) * KS; }
-  __device__ __forceinline__ int end(int step) const { return step < s.psteps ? s.paged : s.len + s.fresh; }
 
   __device__ __forceinline__ int id(int step, int u) const {   // page of group u of a step, fetched ahead
     const int grp = step * NG + u;
@@ -289,10 +286,11 @@ struct Keys16 {
     for (int u = 0; u < NG; ++u) off[u] = paged_offset(c, pid[u], step * NG + u) + head_off;
   }
 
-  // K: kf[key tile][16-byte chunk], lane's key 8 w + g of a group
+  // K from the pages into mma B fragments, kf[key tile][16-byte chunk]: a lane's
+  // keys are 8 w + g of a group, zero past the end.
   __device__ __forceinline__ void load_k(int step, const long long* off, uint4 (&kf)[KS / 8][NC]) const {
+    const int slot = (int)c.slot_stride, lane_off = g * slot + t * 16, left = s.paged - step * KS;
     if (full(step)) {
-      const int slot = (int)c.slot_stride, lane_off = g * slot + t * 16;
 #pragma unroll
       for (int u = 0; u < NG; ++u) {
         const char* p = c.k + off[u] + lane_off;
@@ -302,71 +300,44 @@ struct Keys16 {
           for (int j = 0; j < NC; ++j) kf[u * 2 + w][j] = ldg_stream(p + w * 8 * slot + j * 64);
       }
     } else {
-      const bool paged = step < s.psteps;
-      const int stride = paged ? (int)c.slot_stride : (int)r.n_r, left = end(step) - first(step);
-      const char* rows = kn + (long long)(step - s.psteps) * KS * r.n_r;
 #pragma unroll
       for (int u = 0; u < NG; ++u) {
-        const char* p = (paged ? c.k + off[u] : rows + u * PG_GROUP * stride) + g * stride + t * 16;
+        const char* p = c.k + off[u] + lane_off;
 #pragma unroll
         for (int w = 0; w < 2; ++w)
 #pragma unroll
-          for (int j = 0; j < NC; ++j) kf[u * 2 + w][j] = ldg_if(u * PG_GROUP + w * 8 + g < left, p + w * 8 * stride + j * 64);
+          for (int j = 0; j < NC; ++j) kf[u * 2 + w][j] = ldg_if(u * PG_GROUP + w * 8 + g < left, p + w * 8 * slot + j * 64);
       }
     }
   }
   // A step's K (or V) by bulk copies into shared memory, rows of D in slot
-  // order, counted on `bar`: whole groups where a head's slots are contiguous,
-  // else a row a lane.  Keys past the end are not written.
+  // order, counted on `bar`: a copy a group where a head's slots are
+  // contiguous, else one a row; the block's own rows one a row.  Nothing is
+  // written past the end.
   __device__ __forceinline__ void fetch(int step, const char* pages, const char* fresh, const long long* off, uint32_t dst,
                                         uint64_t* bar) const {
-    constexpr int ROW = D * (int)sizeof(T);
-    const int lane = threadIdx.x & 31, left = end(step) - first(step);
-    if (step < s.psteps && c.slot_stride == ROW) {
-      if (lane == 0) {
-        const int groups = min(NG, (left + PG_GROUP - 1) / PG_GROUP);
-        mbar_arrive_expect_tx(bar, groups * PG_GROUP * ROW);
+    const int lane = threadIdx.x & 31, in_pages = min(KS, s.paged - step * KS);   // rows from the pages, if positive
+    const bool runs = c.slot_stride == ROW;
+    const int rows = min(KS, s.keys - step * KS);
+    if (lane == 0) {
+      mbar_arrive_expect_tx(bar, rows * ROW);
+      if (runs) {
 #pragma unroll
-        for (int u = 0; u < NG; ++u)
-          if (u < groups) bulk_copy(dst + u * PG_GROUP * ROW, pages + off[u], PG_GROUP * ROW, bar);
-      }
-    } else {
-      const int rows = min(KS, left);
-      if (lane == 0) mbar_arrive_expect_tx(bar, rows * ROW);
-      __syncwarp();
-      long long base = off[0];
-      if (NG > 1 && lane >= PG_GROUP) base = off[NG - 1];
-      const char* src = step < s.psteps ? pages + base + (lane % PG_GROUP) * c.slot_stride
-                                        : fresh + (long long)((step - s.psteps) * KS + lane) * r.n_r;
-      if (lane < rows) bulk_copy(dst + lane * ROW, src, ROW, bar);
-    }
-  }
-  // V: vf[group][which of the lane's four keys 2t, 2t+1, 2t+8, 2t+9][64-wide half]
-  __device__ __forceinline__ void load_v(int step, const long long* off, uint4 (&vf)[NG][4][NV]) const {
-    if (full(step)) {
-      const int slot = (int)c.slot_stride, lane_off = 2 * t * slot + g * 16;
-#pragma unroll
-      for (int u = 0; u < NG; ++u) {
-        const char* p = c.v + off[u] + lane_off;
-#pragma unroll
-        for (int w = 0; w < 4; ++w)
-#pragma unroll
-          for (int j = 0; j < NV; ++j) vf[u][w][j] = ldg_stream(p + ((w & 1) + (w >> 1) * 8) * slot + j * 128);
-      }
-    } else {
-      const bool paged = step < s.psteps;
-      const int stride = paged ? (int)c.slot_stride : (int)r.n_r, left = end(step) - first(step);
-      const char* rows = vn + (long long)(step - s.psteps) * KS * r.n_r;
-#pragma unroll
-      for (int u = 0; u < NG; ++u) {
-        const char* p = (paged ? c.v + off[u] : rows + u * PG_GROUP * stride) + 2 * t * stride + g * 16;
-#pragma unroll
-        for (int w = 0; w < 4; ++w) {
-          const int in = (w & 1) + (w >> 1) * 8;
-#pragma unroll
-          for (int j = 0; j < NV; ++j) vf[u][w][j] = ldg_if(u * PG_GROUP + 2 * t + in < left, p + in * stride + j * 128);
+        for (int u = 0; u < NG; ++u) {
+          const int n = min(PG_GROUP, in_pages - u * PG_GROUP);
+          if (n > 0) bulk_copy(dst + u * PG_GROUP * ROW, pages + off[u], n * ROW, bar);
         }
       }
+    }
+    if (runs && in_pages == KS) return;
+    __syncwarp();
+    const int row0 = runs ? max(in_pages, 0) : 0, row = row0 + lane;
+    if (row < rows) {
+      long long base = off[0];
+      if (NG > 1 && row >= PG_GROUP) base = off[NG - 1];
+      const char* src = row < in_pages ? pages + base + (row % PG_GROUP) * c.slot_stride
+                                       : fresh + (long long)(step * KS + row - s.paged) * r.n_r;
+      bulk_copy(dst + row * ROW, src, ROW, bar);
     }
   }
 };

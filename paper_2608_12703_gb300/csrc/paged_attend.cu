@@ -85,8 +85,8 @@ __device__ __forceinline__ uint32_t reg_of(const uint4& v, int i) { return i == 
 // value takes part in the product with weight 0: an infinity or NaN there would
 // reach rows that do not see it.  Such values are taken out of the fragments
 // and added to the rows that do see them.
-template <typename T, int D, int MT>
-__device__ __forceinline__ void guard_values(const Keys16<T, D>& ks, int step, const int (&lim)[MT][2],
+template <typename T, int D, int MT, int E>
+__device__ __forceinline__ void guard_values(const Keys16<T, D>& ks, int step, const int (&lim)[MT][E],
                                              uint4 (&vf)[Keys16<T, D>::NG][4][D / 64], float (&O)[MT][D / 8][4]) {
   using K = Keys16<T, D>;
   // x * 0 is NaN for an infinity or NaN, and stays in the sum
@@ -111,11 +111,10 @@ __device__ __forceinline__ void guard_values(const Keys16<T, D>& ks, int step, c
         v.x &= ~nonfinite_halves<T>(v.x), v.y &= ~nonfinite_halves<T>(v.y);
         v.z &= ~nonfinite_halves<T>(v.z), v.w &= ~nonfinite_halves<T>(v.w);
       }
-  const int first = ks.first(step), end = min(first + K::KS, ks.end(step));
-  for (int key = first; key < end; ++key) {
+  for (int key = step * K::KS; key < min((step + 1) * K::KS, ks.s.keys); ++key) {
     const int grp = key / PG_GROUP;
-    const char* row = step >= ks.s.psteps
-                          ? ks.vn + (long long)(key - ks.s.len) * ks.r.n_r
+    const char* row = key >= ks.s.paged
+                          ? ks.vn + (long long)(key - ks.s.paged) * ks.r.n_r
                           : ks.c.v + paged_offset(ks.c, paged_id(ks.c, ks.table_row, grp), grp) + ks.head_off +
                                 (key % PG_GROUP) * ks.c.slot_stride;
 #pragma unroll
@@ -127,7 +126,7 @@ __device__ __forceinline__ void guard_values(const Keys16<T, D>& ks, int step, c
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-          for (int e = 0; e < 2; ++e)
+          for (int e = 0; e < E; ++e)
             if (key < lim[mt][e]) O[mt][d][2 * e + x] += v;
       }
   }
@@ -448,9 +447,11 @@ __device__ __forceinline__ void attend_items(const AttendArgs& a, F item) {
   }
 }
 
-template <typename T, int D, int MT>
+// MT m-tiles of 8 E rows: up to 8 rows use half of one (E = 1), the softmax of
+// the other half is left out.
+template <typename T, int D, int MT, int E>
 __global__ void __launch_bounds__(PA_WARPS * 32, 1) attend16_kernel(AttendArgs a) {
-  constexpr int KS = Cfg16<D>::KS, NG = KS / PG_GROUP, NC = D / 32, NV = D / 64, TR = 16 * MT;
+  constexpr int KS = Cfg16<D>::KS, NG = KS / PG_GROUP, NC = D / 32, NV = D / 64, TR = 8 * E * MT;
   const PagedView& c = a.c;
   const PagedRows& r = a.r;
   const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
@@ -488,13 +489,13 @@ __global__ void __launch_bounds__(PA_WARPS * 32, 1) attend16_kernel(AttendArgs a
     }
 
     uint32_t qa[MT][NC * 2][4];
-    int lim[MT][2];   // slots that the fragment's rows see
+    int lim[MT][E];   // slots that the fragment's rows see
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const int m = tile * TR + mt * 16 + e * 8 + g, row = m / r.group, hq = kvh * r.group + m - row * r.group;
-        lim[mt][e] = r.causal ? s.len + row + 1 : s.len;
+      for (int e = 0; e < E; ++e) {
+        const int m = tile * TR + mt * 8 * E + e * 8 + g, row = m / r.group, hq = kvh * r.group + m - row * r.group;
+        lim[mt][e] = min(s.keys, r.causal ? s.len + row + 1 : s.len);
 #pragma unroll
         for (int j = 0; j < NC; ++j) {
           const uint4 x = ldg_if(row < s.rows, r.q + b * r.q_b + row * r.q_r + hq * r.q_h + j * 64 + t * 16);
@@ -502,13 +503,14 @@ __global__ void __launch_bounds__(PA_WARPS * 32, 1) attend16_kernel(AttendArgs a
           qa[mt][2 * j][2 + e] = x.y;
           qa[mt][2 * j + 1][e] = x.z;
           qa[mt][2 * j + 1][2 + e] = x.w;
+          if (E == 1) qa[mt][2 * j][1] = qa[mt][2 * j][3] = qa[mt][2 * j + 1][1] = qa[mt][2 * j + 1][3] = 0;
         }
       }
-    float O[MT][D / 8][4], m_run[MT][2], l_run[MT][2];
+    float O[MT][D / 8][4], m_run[MT][E], l_run[MT][E];
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
-      m_run[mt][0] = m_run[mt][1] = -INFINITY;
-      l_run[mt][0] = l_run[mt][1] = 0.f;
+#pragma unroll
+      for (int e = 0; e < E; ++e) m_run[mt][e] = -INFINITY, l_run[mt][e] = 0.f;
 #pragma unroll
       for (int d = 0; d < D / 8; ++d) O[mt][d][0] = O[mt][d][1] = O[mt][d][2] = O[mt][d][3] = 0.f;
     }
@@ -550,22 +552,21 @@ __global__ void __launch_bounds__(PA_WARPS * 32, 1) attend16_kernel(AttendArgs a
 #pragma unroll
           for (int x = 0; x < NG; ++x) next[x] = ks.id(step + PA_STAGES + 1, x);
       }
-      const int first = ks.first(step), end = ks.end(step);
       if (!full) {
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
           for (int kt = 0; kt < KS / 8; ++kt)
 #pragma unroll
-            for (int x = 0; x < 4; ++x)
-              if (first + kt * 8 + 2 * t + (x & 1) >= min(lim[mt][x >> 1], end)) S[mt][kt][x] = -INFINITY;
+            for (int x = 0; x < 2 * E; ++x)
+              if (step * KS + kt * 8 + 2 * t + (x & 1) >= lim[mt][x >> 1]) S[mt][kt][x] = -INFINITY;
       }
-      uint32_t pf[MT][KS / 8][2];
+      uint32_t pf[MT][KS / 8][E];
 #pragma unroll
       for (int mt = 0; mt < MT; ++mt) {
-        float mx[2];
+        float mx[E];
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
+        for (int e = 0; e < E; ++e) {
           float x = fmaxf(S[mt][0][2 * e], S[mt][0][2 * e + 1]);
 #pragma unroll
           for (int kt = 1; kt < KS / 8; ++kt) x = fmaxf(x, fmaxf(S[mt][kt][2 * e], S[mt][kt][2 * e + 1]));
@@ -573,9 +574,9 @@ __global__ void __launch_bounds__(PA_WARPS * 32, 1) attend16_kernel(AttendArgs a
           x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 2));
           mx[e] = fmaxf(m_run[mt][e], x * sc);
         }
-        if (__any_sync(0xffffffffu, mx[0] > m_run[mt][0] || mx[1] > m_run[mt][1])) {
+        if (__any_sync(0xffffffffu, mx[0] > m_run[mt][0] || mx[E - 1] > m_run[mt][E - 1])) {
 #pragma unroll
-          for (int e = 0; e < 2; ++e) {
+          for (int e = 0; e < E; ++e) {
             const float f = mx[e] == -INFINITY ? 1.f : ex2(m_run[mt][e] - mx[e]);
             m_run[mt][e] = mx[e];
             l_run[mt][e] *= f;
@@ -587,7 +588,7 @@ __global__ void __launch_bounds__(PA_WARPS * 32, 1) attend16_kernel(AttendArgs a
           }
         }
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
+        for (int e = 0; e < E; ++e) {
           const float m = m_run[mt][e] == -INFINITY ? 0.f : m_run[mt][e];
 #pragma unroll
           for (int kt = 0; kt < KS / 8; ++kt) {
@@ -608,12 +609,12 @@ __global__ void __launch_bounds__(PA_WARPS * 32, 1) attend16_kernel(AttendArgs a
             const int in = x * PG_GROUP + (w & 1) + (w >> 1) * 8;
 #pragma unroll
             for (int j = 0; j < NV; ++j) vf[x][w][j] = lds16(at + in * (D * 2) + j * 128);
-            if (!full && first + in + 2 * t >= end)   // past the end: whatever the slot held
+            if (!full && step * KS + in + 2 * t >= s.keys)   // past the end: whatever the slot held
 #pragma unroll
               for (int j = 0; j < NV; ++j) vf[x][w][j] = make_uint4(0, 0, 0, 0);
           }
       }
-      if (!full && end > s.len) guard_values<T, D, MT>(ks, step, lim, vf, O);
+      if (!full && s.keys > s.len) guard_values<T, D, MT, E>(ks, step, lim, vf, O);
 #pragma unroll
       for (int x = 0; x < NG; ++x)
 #pragma unroll
@@ -625,24 +626,25 @@ __global__ void __launch_bounds__(PA_WARPS * 32, 1) attend16_kernel(AttendArgs a
             const uint32_t b1 = __byte_perm(reg_of(vf[x][2][j], d >> 1), reg_of(vf[x][3][j], d >> 1), sel);
 #pragma unroll
             for (int mt = 0; mt < MT; ++mt) {
-              const uint32_t pa[4] = {pf[mt][2 * x][0], pf[mt][2 * x][1], pf[mt][2 * x + 1][0], pf[mt][2 * x + 1][1]};
+              const uint32_t pa[4] = {pf[mt][2 * x][0], E > 1 ? pf[mt][2 * x][E - 1] : 0u, pf[mt][2 * x + 1][0],
+                                      E > 1 ? pf[mt][2 * x + 1][E - 1] : 0u};
               Mma16<T>::mma(O[mt][j * 8 + d], pa, b0, b1);
             }
           }
       __syncwarp();
       if (more) ks.fetch(step + PA_STAGES, c.v, ks.vn, off, slot + KB, &landed[1]);
     }
-    if (tile == 0 && s.fresh && s0 <= s.psteps && s.psteps < s0 + n) append_rows(c, r, s, b, kvh, D * sizeof(T));
+    if (tile == 0 && s.keys > s.paged && s0 <= s.paged / KS && s.paged / KS < s0 + n) append_rows(c, r, s, b, kvh, D * sizeof(T));
 
     // of row g (+ 8 e) a lane holds columns 64 j + 16 t .. + 15
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
+      for (int e = 0; e < E; ++e) {
         float l = l_run[mt][e];
         l += __shfl_xor_sync(0xffffffffu, l, 1);
         l += __shfl_xor_sync(0xffffffffu, l, 2);
-        const int in = mt * 16 + e * 8 + g;
+        const int in = mt * 8 * E + e * 8 + g;
         if (t == 0) {
           sm[in] = m_run[mt][e];
           sm[TR + in] = l;
@@ -680,7 +682,7 @@ __global__ void __launch_bounds__(PA_WARPS * 32, 1) attend32_kernel(AttendArgs a
 #pragma unroll
     for (int x = 0; x < TR; ++x) {
       const int m = tile * TR + x, row = m / r.group, hq = kvh * r.group + m - row * r.group;
-      lim[x] = row < s.rows ? (r.causal ? s.len + row + 1 : s.len) : 0;
+      lim[x] = row < s.rows ? min(s.keys, r.causal ? s.len + row + 1 : s.len) : 0;
       m_run[x] = -INFINITY;
       l_run[x] = 0.f;
 #pragma unroll
@@ -694,27 +696,23 @@ __global__ void __launch_bounds__(PA_WARPS * 32, 1) attend32_kernel(AttendArgs a
     }
     for (int i = 0; i < n; ++i) {
       const int step = s0 + i;
-      const bool paged = step < s.psteps;
-      const int first = paged ? step * KS : s.len + (step - s.psteps) * KS, end = paged ? s.paged : s.len + s.fresh;
-      const char *kp, *vp;
-      long long stride;
-      if (paged) {
+      const int first = step * KS;
+      long long page = 0;
+      if (first < s.paged) {
         const int grp = first / PG_GROUP;
-        const long long off = paged_offset(c, paged_id(c, table_row, grp), grp) + kvh * c.head_stride +
-                              (long long)(first % PG_GROUP) * c.slot_stride;
-        kp = c.k + off, vp = c.v + off, stride = c.slot_stride;
-      } else {
-        const long long off = b * r.n_b + (long long)(first - s.len) * r.n_r + kvh * r.n_h;
-        kp = r.k_new + off, vp = r.v_new + off, stride = r.n_r;
+        page = paged_offset(c, paged_id(c, table_row, grp), grp) + kvh * c.head_stride + (first % PG_GROUP) * c.slot_stride;
       }
       float4 kf[IT][NC], vf[IT][NC];
 #pragma unroll
       for (int k = 0; k < IT; ++k) {
-        const bool in = first + 4 * k + kg < end;
-        const long long at = (4 * k + kg) * stride + e * 16;
+        const int key = first + 4 * k + kg;
+        const bool in_page = key < s.paged;
+        const long long at = (in_page ? page + (4 * k + kg) * c.slot_stride
+                                      : b * r.n_b + kvh * r.n_h + (long long)(key - s.paged) * r.n_r) + e * 16;
+        const char *kp = (in_page ? c.k : r.k_new) + at, *vp = (in_page ? c.v : r.v_new) + at;
 #pragma unroll
         for (int j = 0; j < NC; ++j) {
-          const uint4 x = ldg_if(in, kp + at + j * 128), y = ldg_if(in, vp + at + j * 128);
+          const uint4 x = ldg_if(key < s.keys, kp + j * 128), y = ldg_if(key < s.keys, vp + j * 128);
           kf[k][j] = *reinterpret_cast<const float4*>(&x);
           vf[k][j] = *reinterpret_cast<const float4*>(&y);
         }
@@ -732,7 +730,7 @@ __global__ void __launch_bounds__(PA_WARPS * 32, 1) attend32_kernel(AttendArgs a
           d += __shfl_xor_sync(0xffffffffu, d, 1);
           d += __shfl_xor_sync(0xffffffffu, d, 2);
           d += __shfl_xor_sync(0xffffffffu, d, 4);
-          S[k] = first + 4 * k + kg < min(lim[x], end) ? d : -INFINITY;
+          S[k] = first + 4 * k + kg < lim[x] ? d : -INFINITY;
           mx = fmaxf(mx, S[k]);
         }
         const float m = mx == -INFINITY ? 0.f : mx, f = ex2(m_run[x] - m);
@@ -755,7 +753,7 @@ __global__ void __launch_bounds__(PA_WARPS * 32, 1) attend32_kernel(AttendArgs a
         }
       }
     }
-    if (tile == 0 && s.fresh && s0 <= s.psteps && s.psteps < s0 + n) append_rows(c, r, s, b, kvh, D * sizeof(float));
+    if (tile == 0 && s.keys > s.paged && s0 <= s.paged / KS && s.paged / KS < s0 + n) append_rows(c, r, s, b, kvh, D * sizeof(float));
 #pragma unroll
     for (int x = 0; x < TR; ++x) {
       float mx = fmaxf(m_run[x], __shfl_xor_sync(0xffffffffu, m_run[x], 8));
@@ -783,7 +781,9 @@ __global__ void __launch_bounds__(PA_WARPS * 32, 1) attend32_kernel(AttendArgs a
   });
 }
 
-int attend_tile(int dtype, int dim, int m_rows) { return dtype == 0 ? 4 : dim == 64 && m_rows > 16 ? 32 : 16; }
+int attend_tile(int dtype, int dim, int m_rows) {
+  return dtype == 0 ? 4 : m_rows <= 8 ? 8 : dim == 64 && m_rows > 16 ? 32 : 16;
+}
 int attend_grid() {
   const int most = MAX_WORKERS / PA_WARPS, sms = paged_sm_count();
   return sms < most ? sms : most;
@@ -810,9 +810,12 @@ cudaError_t launch_attend(const AttendArgs& a, cudaStream_t st) {
 
 template <typename T>
 cudaError_t launch16(const AttendArgs& a, int dim, int tr, cudaStream_t st) {
-  if (dim == 128) return launch_attend<attend16_kernel<T, 128, 1>, 128, 16>(a, st);
-  if (tr == 32) return launch_attend<attend16_kernel<T, 64, 2>, 64, 32>(a, st);
-  return launch_attend<attend16_kernel<T, 64, 1>, 64, 16>(a, st);
+  if (dim == 128)
+    return tr == 8 ? launch_attend<attend16_kernel<T, 128, 1, 1>, 128, 8>(a, st)
+                   : launch_attend<attend16_kernel<T, 128, 1, 2>, 128, 16>(a, st);
+  if (tr == 32) return launch_attend<attend16_kernel<T, 64, 2, 2>, 64, 32>(a, st);
+  return tr == 16 ? launch_attend<attend16_kernel<T, 64, 1, 2>, 64, 16>(a, st)
+                  : launch_attend<attend16_kernel<T, 64, 1, 1>, 64, 8>(a, st);
 }
 
 }  // namespace

@@ -38,7 +38,8 @@ __device__ __forceinline__ SeqWork weigh_seq(const WeighArgs& a, int len, int ro
     if (a.c.status) set_status(a.c.status, ST_CAPACITY);
     s.len = s.rows = s.paged = s.tiles = 0;
   }
-  s.psteps = s.steps = (s.paged + KS - 1) / KS;
+  s.keys = s.paged;
+  s.steps = (s.paged + KS - 1) / KS;
   return s;
 }
 
