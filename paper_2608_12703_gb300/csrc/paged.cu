@@ -78,6 +78,7 @@ int paged_rows(const asr_paged_cache* c, const asr_paged_rows* r, PagedRows* v) 
   v->max_rows = r->max_rows;
   v->heads = r->heads;
   v->group = r->heads / c->kv_heads;
+  v->groups = make_fastdiv(v->group);
   v->causal = r->causal != 0;
   v->scale = r->scale;
   return ASR_OK;

@@ -50,6 +50,7 @@ struct PagedRows {
   long long n_b, n_r, n_h;
   const int *kv_len, *rows;
   int max_rows, heads, group, causal;
+  FastDiv groups;   // by `group`
   float scale;
 };
 

@@ -167,10 +167,10 @@ struct Acc {   // four columns of a row
 
 template <typename T, int D>
 __device__ __forceinline__ void put_row(const AttendArgs& a, int b, int kvh, int m, int col, const Acc& x) {
-  const int row = m / a.r.group, hq = kvh * a.r.group + m - row * a.r.group;
+  const int row = (int)a.r.groups.div((uint32_t)m), hq = kvh * a.r.group + m - row * a.r.group;
   const size_t at = ((size_t)b * a.r.max_rows + row) * a.r.heads + hq;
-  const float inv = x.l > 0.f ? 1.f / x.l : 0.f;
-  if (a.lse && col == 0) a.lse[at] = (x.m + log2f(x.l)) * LN2;
+  const float inv = x.l > 0.f ? __fdividef(1.f, x.l) : 0.f;
+  if (a.lse && col == 0) a.lse[at] = (x.m + __log2f(x.l)) * LN2;
   T* out = reinterpret_cast<T*>(a.out) + at * D + col;
   if constexpr (sizeof(T) == 4) {
     *reinterpret_cast<float4*>(out) = make_float4(x.o.x * inv, x.o.y * inv, x.o.z * inv, x.o.w * inv);
@@ -185,6 +185,8 @@ __device__ __noinline__ void finish_item(const AttendArgs& a, const WorkPlan& pl
                                          int tile, int rows, int u0, int u1, int worker, bool begins, bool whole) {
   using PT = Part<D, TR>;
   constexpr int PART = PT::FLOATS, C4 = D / 4;
+  // partial results there is room for; more parts than that are joined in runs
+  constexpr int ROOM = (BLOCK ? PA_WARPS : 1) * PT::REGION / PART;
   __shared__ int s_last;
   const int tid = BLOCK ? threadIdx.x : threadIdx.x & 31, nt = BLOCK ? PA_WARPS * 32 : 32;
   const int nr = min(TR, rows - tile * TR);
@@ -192,68 +194,79 @@ __device__ __noinline__ void finish_item(const AttendArgs& a, const WorkPlan& pl
     if (BLOCK) __syncthreads();
     else __syncwarp();
   };
-  sync();
   float* part = a.ws + (size_t)(2 * worker + (begins ? 1 : 0)) * PART;
+  int n = regions, stride = PT::REGION;   // what is added up: first the warps' results, then, by the last to come, the parts
+  int p0 = 0, parts = 0, n0 = 0, n1 = 0, c0 = 0, c1 = 0, wf = 0;
+  bool final = whole;
+  Acc carry[(TR * C4 + (BLOCK ? PA_WARPS * 32 : 32) - 1) / (BLOCK ? PA_WARPS * 32 : 32)];   // from run to run
 #pragma unroll 1
-  for (int x = tid; x < nr * C4; x += nt) {
-    const int in = x / C4, col = (x - in * C4) * 4;
-    Acc acc;
-#pragma unroll 1
-    for (int w = 0; w < regions; ++w) {
-      const float* p = sm + w * PT::REGION;
-      acc.add(p[in], p[TR + in], *reinterpret_cast<const float4*>(p + 2 * TR + in * D + col));
-    }
-    if (whole) {
-      put_row<T, D>(a, b, kvh, tile * TR + in, col, acc);
-    } else {
-      if (col == 0) {
-        __stcg(part + in, acc.m);
-        __stcg(part + TR + in, acc.l);
-      }
-      __stcg(reinterpret_cast<float4*>(part + 2 * TR + in * D + col), acc.o);
-    }
-  }
-  if (whole) {
-    sync();   // the next item's results go to the same shared memory
-    return;
-  }
-  __threadfence();
-  // The parts of the item, in key order: single warps wf .., then blocks c0 ..
-  // c1 whose warps all work on it, then single warps again.
-  const int wf = plan.owner(u0), wl = plan.owner(u1 - 1);
-  const bool from_first = wf % PA_WARPS == 0 && plan.start(wf) == u0;
-  const bool to_last = (wl % PA_WARPS == PA_WARPS - 1 || wl == plan.workers - 1) && plan.start(wl + 1) == u1;
-  const int c0 = wf / PA_WARPS + (from_first ? 0 : 1), c1 = wl / PA_WARPS - (to_last ? 0 : 1);
-  const int n0 = c0 <= c1 ? c0 * PA_WARPS - wf : wl - wf + 1;
-  const int n1 = c0 <= c1 ? c1 - c0 + 1 : 0;
-  const int parts = n0 + n1 + (c0 <= c1 ? max(0, wl + 1 - (c1 + 1) * PA_WARPS) : 0);
-  sync();
-  int last = 0;
-  if (tid == 0) {
-    last = atomicAdd(a.tickets + wf, 1) == parts - 1;
-    if (last) {
-      a.tickets[wf] = 0;   // all have come: as the next call needs it
-      __threadfence();
-    }
-    if (BLOCK) s_last = last;
-  }
-  if (BLOCK) {
-    __syncthreads();
-    last = s_last;
-  } else {
-    last = __shfl_sync(0xffffffffu, last, 0);
-  }
-  if (!last) return;
-
-  // Fetch as many parts at a time as there is room for, and add them up.
-  constexpr int ROOM = (BLOCK ? PA_WARPS : 1) * PT::REGION / PART, MAX_X = (TR * C4 + (BLOCK ? PA_WARPS * 32 : 32) - 1) / (BLOCK ? PA_WARPS * 32 : 32);
-  const int used = 2 * TR + nr * D;   // floats of a part
-  Acc acc[MAX_X];
-  for (int p0 = 0; p0 < parts; p0 += ROOM) {
-    const int np = min(ROOM, parts - p0);
+  for (;;) {
     sync();
+    int e = 0;
 #pragma unroll 1
-    for (int i = 0; i < np; ++i) {
+    for (int x = tid; x < nr * C4; x += nt, ++e) {
+      const int in = x / C4, col = (x - in * C4) * 4;
+      Acc acc;
+      if (p0 > 0) acc = carry[e];
+#pragma unroll 1
+      for (int w = 0; w < n; ++w) {
+        const float* p = sm + w * stride;
+        acc.add(p[in], p[TR + in], *reinterpret_cast<const float4*>(p + 2 * TR + in * D + col));
+      }
+      if (final) {
+        put_row<T, D>(a, b, kvh, tile * TR + in, col, acc);
+      } else if (parts == 0) {
+        __stcg(reinterpret_cast<float4*>(part + 2 * TR + in * D + col), acc.o);
+        if (col == 0) {
+          __stcg(part + in, acc.m);
+          __stcg(part + TR + in, acc.l);
+        }
+      } else {
+        carry[e] = acc;
+      }
+    }
+    if (final) {
+      sync();   // the next item's results go to the same shared memory
+      return;
+    }
+    if (parts == 0) {
+      __threadfence();
+      // The parts of the item, in key order: single warps wf .., then blocks c0
+      // .. c1 whose warps all work on it, then single warps again.
+      wf = plan.owner(u0);
+      const int wl = plan.owner(u1 - 1);
+      const bool from_first = wf % PA_WARPS == 0 && plan.start(wf) == u0;
+      const bool to_last = (wl % PA_WARPS == PA_WARPS - 1 || wl == plan.workers - 1) && plan.start(wl + 1) == u1;
+      c0 = wf / PA_WARPS + (from_first ? 0 : 1), c1 = wl / PA_WARPS - (to_last ? 0 : 1);
+      n0 = c0 <= c1 ? c0 * PA_WARPS - wf : wl - wf + 1;
+      n1 = c0 <= c1 ? c1 - c0 + 1 : 0;
+      parts = n0 + n1 + (c0 <= c1 ? max(0, wl + 1 - (c1 + 1) * PA_WARPS) : 0);
+      sync();
+      int last = 0;
+      if (tid == 0) {
+        last = atomicAdd(a.tickets + wf, 1) == parts - 1;
+        if (last) {
+          a.tickets[wf] = 0;   // all have come: as the next call needs it
+          __threadfence();
+        }
+        if (BLOCK) s_last = last;
+      }
+      if (BLOCK) {
+        __syncthreads();
+        last = s_last;
+      } else {
+        last = __shfl_sync(0xffffffffu, last, 0);
+      }
+      if (!last) return;
+    } else {
+      p0 += ROOM;
+      sync();
+    }
+    n = min(ROOM, parts - p0), stride = PART;
+    final = p0 + ROOM >= parts;
+    const int used = 2 * TR + nr * D;   // floats of a part
+#pragma unroll 1
+    for (int i = 0; i < n; ++i) {
       const int p = p0 + i;
       const int w = p < n0 ? wf + p : p < n0 + n1 ? (c0 + p - n0) * PA_WARPS : (c1 + 1) * PA_WARPS + p - n0 - n1;
       const float* src = a.ws + (size_t)(2 * w + (p == 0 ? 1 : 0)) * PART;
@@ -261,24 +274,7 @@ __device__ __noinline__ void finish_item(const AttendArgs& a, const WorkPlan& pl
       for (int x = tid * 4; x < used; x += nt * 4) copy16(sm + i * PART + x, src + x);
     }
     asm volatile("cp.async.wait_all;" ::: "memory");
-    sync();
-#pragma unroll
-    for (int e = 0; e < MAX_X; ++e) {
-      const int x = tid + e * nt, in = x / C4, col = (x - in * C4) * 4;
-      if (x >= nr * C4) break;
-#pragma unroll 1
-      for (int i = 0; i < np; ++i) {
-        const float* p = sm + i * PART;
-        acc[e].add(p[in], p[TR + in], *reinterpret_cast<const float4*>(p + 2 * TR + in * D + col));
-      }
-    }
   }
-#pragma unroll
-  for (int e = 0; e < MAX_X; ++e) {
-    const int x = tid + e * nt, in = x / C4;
-    if (x < nr * C4) put_row<T, D>(a, b, kvh, tile * TR + in, (x - in * C4) * 4, acc[e]);
-  }
-  sync();   // the next item's results go to the same shared memory
 }
 
 // Rows without keys: zeros, and -inf for the log-sum-exp.
