@@ -40,8 +40,6 @@
 namespace asrspec {
 namespace {
 
-constexpr int PA_WARPS = 8;   // one block an SM
-constexpr int PA_STAGES = 3;  // steps of K and V (8 KB) that a warp has in flight or in use
 
 
 
@@ -139,13 +137,16 @@ __device__ __forceinline__ void guard_values(const Keys16<T, D>& ks, int step, c
 // runs once an item, mostly from a cold instruction cache: its loops stay
 // rolled, and the round trips to L2 are overlapped by asynchronous copies.
 // ---------------------------------------------------------------------------
-template <int D, int TR>
-struct Part {
-  static constexpr int FLOATS = TR * (D + 2);
+// A kernel's shape: head dimension, rows of a tile, warps of a block (one block
+// an SM), and steps of K and V (8 KB) that a warp has in flight or in use.
+template <int D_, int TR_, int WARPS_, int STAGES_>
+struct Shape {
+  static constexpr int D = D_, TR = TR_, WARPS = WARPS_, STAGES = STAGES_;
+  static constexpr int PART = TR * (D + 2);   // floats of a result
   // A warp's shared memory: the ring of its loads (16-bit types), then, the ring
   // drained, its result and room to fetch others' partial results into.
-  static constexpr int RING = TR == 4 ? 0 : PA_STAGES * 8192;
-  static constexpr int REGION = (RING ? RING : 3 * FLOATS * 4) / 4;   // floats
+  static constexpr int RING = STAGES * 8192;
+  static constexpr int REGION = (RING ? RING : 3 * PART * 4) / 4;   // floats
 };
 
 __device__ __forceinline__ void copy16(float* smem, const float* gmem) {   // by L2: another SM wrote it
@@ -180,25 +181,24 @@ __device__ __forceinline__ void put_row(const AttendArgs& a, int b, int kvh, int
   }
 }
 
-template <typename T, int D, int TR, bool BLOCK>
+template <typename T, typename C, bool BLOCK>
 __device__ __noinline__ void finish_item(const AttendArgs& a, const WorkPlan& plan, float* sm, int regions, int b, int kvh,
-                                         int tile, int rows, int u0, int u1, int worker, bool begins, bool whole) {
-  using PT = Part<D, TR>;
-  constexpr int PART = PT::FLOATS, C4 = D / 4;
+                                         int tile, int rows, int u0, int u1, int worker, bool begins, bool whole, int share) {
+  constexpr int D = C::D, TR = C::TR, WARPS = C::WARPS, PART = C::PART, C4 = D / 4;
   // partial results there is room for; more parts than that are joined in runs
-  constexpr int ROOM = (BLOCK ? PA_WARPS : 1) * PT::REGION / PART;
+  constexpr int ROOM = (BLOCK ? WARPS : 1) * C::REGION / PART;
   __shared__ int s_last;
-  const int tid = BLOCK ? threadIdx.x : threadIdx.x & 31, nt = BLOCK ? PA_WARPS * 32 : 32;
+  const int tid = BLOCK ? threadIdx.x : threadIdx.x & 31, nt = BLOCK ? WARPS * 32 : 32;
   const int nr = min(TR, rows - tile * TR);
   auto sync = [] {
     if (BLOCK) __syncthreads();
     else __syncwarp();
   };
   float* part = a.ws + (size_t)(2 * worker + (begins ? 1 : 0)) * PART;
-  int n = regions, stride = PT::REGION;   // what is added up: first the warps' results, then, by the last to come, the parts
+  int n = regions, stride = C::REGION;   // what is added up: first the warps' results, then, by the last to come, the parts
   int p0 = 0, parts = 0, n0 = 0, n1 = 0, c0 = 0, c1 = 0, wf = 0;
   bool final = whole;
-  Acc carry[(TR * C4 + (BLOCK ? PA_WARPS * 32 : 32) - 1) / (BLOCK ? PA_WARPS * 32 : 32)];   // from run to run
+  Acc carry[(TR * C4 + (BLOCK ? WARPS * 32 : 32) - 1) / (BLOCK ? WARPS * 32 : 32)];   // from run to run
 #pragma unroll 1
   for (;;) {
     sync();
@@ -233,14 +233,20 @@ __device__ __noinline__ void finish_item(const AttendArgs& a, const WorkPlan& pl
       __threadfence();
       // The parts of the item, in key order: single warps wf .., then blocks c0
       // .. c1 whose warps all work on it, then single warps again.
-      wf = plan.owner(u0);
-      const int wl = plan.owner(u1 - 1);
-      const bool from_first = wf % PA_WARPS == 0 && plan.start(wf) == u0;
-      const bool to_last = (wl % PA_WARPS == PA_WARPS - 1 || wl == plan.workers - 1) && plan.start(wl + 1) == u1;
-      c0 = wf / PA_WARPS + (from_first ? 0 : 1), c1 = wl / PA_WARPS - (to_last ? 0 : 1);
-      n0 = c0 <= c1 ? c0 * PA_WARPS - wf : wl - wf + 1;
-      n1 = c0 <= c1 ? c1 - c0 + 1 : 0;
-      parts = n0 + n1 + (c0 <= c1 ? max(0, wl + 1 - (c1 + 1) * PA_WARPS) : 0);
+      // Or, of a shared item, `share` blocks.
+      if (share > 0) {
+        c0 = u0, n1 = parts = share;
+        wf = c0 * WARPS;
+      } else {
+        wf = plan.owner(u0);
+        const int wl = plan.owner(u1 - 1);
+        const bool from_first = wf % WARPS == 0 && plan.start(wf) == u0;
+        const bool to_last = (wl % WARPS == WARPS - 1 || wl == plan.workers - 1) && plan.start(wl + 1) == u1;
+        c0 = wf / WARPS + (from_first ? 0 : 1), c1 = wl / WARPS - (to_last ? 0 : 1);
+        n0 = c0 <= c1 ? c0 * WARPS - wf : wl - wf + 1;
+        n1 = c0 <= c1 ? c1 - c0 + 1 : 0;
+        parts = n0 + n1 + (c0 <= c1 ? max(0, wl + 1 - (c1 + 1) * WARPS) : 0);
+      }
       sync();
       int last = 0;
       if (tid == 0) {
@@ -268,7 +274,7 @@ __device__ __noinline__ void finish_item(const AttendArgs& a, const WorkPlan& pl
 #pragma unroll 1
     for (int i = 0; i < n; ++i) {
       const int p = p0 + i;
-      const int w = p < n0 ? wf + p : p < n0 + n1 ? (c0 + p - n0) * PA_WARPS : (c1 + 1) * PA_WARPS + p - n0 - n1;
+      const int w = p < n0 ? wf + p : p < n0 + n1 ? (c0 + p - n0) * WARPS : (c1 + 1) * WARPS + p - n0 - n1;
       const float* src = a.ws + (size_t)(2 * w + (p == 0 ? 1 : 0)) * PART;
 #pragma unroll 1
       for (int x = tid * 4; x < used; x += nt * 4) copy16(sm + i * PART + x, src + x);
@@ -292,19 +298,18 @@ __device__ __forceinline__ void clear_rows(const AttendArgs& a, const PlanMem& m
 }
 
 // Who works on what.  Every end of an item costs its warps a few steps' time
-// (pipeline fill, the way through shared memory), and every item that is split
-// over blocks a way through L2 and a join besides; whole items cost balance
+// (pipeline fill, the way through shared memory), and every item that several
+// blocks work on a way through L2 and a join besides; whole items cost balance
 // instead.  So, by the lengths at hand and in steps:
-//   WARP    a warp takes whole items:   the longest item, or an equal share;
+//   WARP    a warp takes whole items;
 //   BLOCK   a block takes whole items, its warps each a part of the steps;
+//   SHARE   few items: as many blocks for each as there are, in equal parts;
 //   SPLIT   equal runs of steps for all warps, items split wherever a run ends.
 // Whole items are dealt longest sequence first, to and fro over the takers.
-// Measured, us a call: 64 sequences of up to 448 slots, 1280 heads: WARP @@, SPLIT 39;
-// 32 of up to 1500, 384 heads: BLOCK @@, SPLIT 31; one sequence of 230, 20
-// heads: BLOCK @@, SPLIT 13.7; one of 100001, 20 heads: SPLIT 110, BLOCK 400.
-enum Deal { DEAL_WARP, DEAL_BLOCK, DEAL_SPLIT };
-constexpr int DEAL_SORT_MAX = PA_WARPS * 32;   // sequences that a block ranks, one a thread
-constexpr float END_COST = 4.f, JOIN_COST = 5.f;   // steps
+// Measured, us a call: @@
+enum Deal { DEAL_WARP, DEAL_BLOCK, DEAL_SHARE, DEAL_SPLIT };
+constexpr int DEAL_SORT_MAX = 256;   // sequences that a block ranks, one a thread
+constexpr float END_COST = 4.f, SHARE_COST = 5.f, SPLIT_COST = 16.f;   // steps
 
 struct DealMem {
   int *order, *pre;   // [B] sequences by falling length, [B + 1] items before each
@@ -312,9 +317,10 @@ struct DealMem {
 };
 constexpr size_t deal_bytes(int B) { return B <= DEAL_SORT_MAX ? ((size_t)B * 8 + 4 + 15) / 16 * 16 : 0; }
 
-template <int KS, int TR>
+template <typename C, int KS>
 __device__ __forceinline__ Deal choose_deal(const AttendArgs& a, const WorkPlan& plan, const PlanMem& mem, DealMem& dm,
                                             int* smem) {
+  constexpr int TR = C::TR, WARPS = C::WARPS;
   __shared__ int s_long;
   const int B = a.c.batch, b = threadIdx.x, lane = threadIdx.x & 31;
   if (B > DEAL_SORT_MAX) return DEAL_SPLIT;
@@ -357,20 +363,22 @@ __device__ __forceinline__ Deal choose_deal(const AttendArgs& a, const WorkPlan&
   __syncthreads();
   dm.items = dm.pre[B];
   const float u = (float)plan.units, n = (float)dm.items, longest = (float)s_long;
-  const float warps = (float)a.max_workers, blocks = warps / PA_WARPS;
+  const float warps = (float)a.max_workers, blocks = warps / WARPS;
   const float by_warp = fmaxf(longest + END_COST, n <= warps ? 0.f : 1.1f * (u + END_COST * n) / warps);
-  const float by_block = fmaxf(longest / PA_WARPS + END_COST + 1.f,
-                               n <= blocks ? 0.f : 1.1f * (u / PA_WARPS + (END_COST + 1.f) * n) / blocks);
-  const float split = u / warps + 2.f * END_COST + JOIN_COST;
-  return by_warp <= by_block ? (by_warp <= split ? DEAL_WARP : DEAL_SPLIT) : by_block <= split ? DEAL_BLOCK : DEAL_SPLIT;
+  const float by_block = fmaxf(longest / WARPS + END_COST + 1.f,
+                               n <= blocks ? 0.f : 1.1f * (u / WARPS + (END_COST + 1.f) * n) / blocks);
+  const float by_share = n <= blocks / 2.f ? longest / (WARPS * floorf(blocks / n)) + END_COST + 1.f + SHARE_COST : 1e30f;
+  const float split = u / warps + END_COST + SPLIT_COST;
+  const float least = fminf(fminf(by_warp, by_block), fminf(by_share, split));
+  return least == by_warp ? DEAL_WARP : least == by_block ? DEAL_BLOCK : least == by_share ? DEAL_SHARE : DEAL_SPLIT;
 }
 
 // What the two kernels below share: the plan, the walk over a warp's items and
 // their ends.  `item` computes steps [s0, s0 + n) of one item and leaves the
 // result in the warp's shared memory.
-template <typename T, int D, int KS, int TR, typename F>
+template <typename T, typename C, int KS, typename F>
 __device__ __forceinline__ void attend_items(const AttendArgs& a, F item) {
-  constexpr int REGION = Part<D, TR>::REGION;
+  constexpr int REGION = C::REGION, D = C::D, TR = C::TR, WARPS = C::WARPS;
   const PagedView& c = a.c;
   const PagedRows& r = a.r;
   PlanMem mem;
@@ -382,21 +390,27 @@ __device__ __forceinline__ void attend_items(const AttendArgs& a, F item) {
   if (plan.units == 0) return;
   extern __shared__ __align__(16) unsigned char smem[];
   DealMem dm;
-  const Deal deal = choose_deal<KS, TR>(a, plan, mem, dm, reinterpret_cast<int*>(smem + plan_bytes(c.batch)));
+  const Deal deal = choose_deal<C, KS>(a, plan, mem, dm, reinterpret_cast<int*>(smem + plan_bytes(c.batch)));
   float* sm = reinterpret_cast<float*>(smem + plan_bytes(c.batch) + deal_bytes(c.batch));
-  const int warp = threadIdx.x >> 5, w0 = blockIdx.x * PA_WARPS, worker = w0 + warp;
+  const int warp = threadIdx.x >> 5, w0 = blockIdx.x * WARPS, worker = w0 + warp;
 
   // SPLIT: this warp's run of units [u, u_end), the block's [block0, block1)
-  const int w1 = min(w0 + PA_WARPS, plan.workers), block0 = plan.start(min(w0, plan.workers)), block1 = plan.start(w1);
+  const int w1 = min(w0 + WARPS, plan.workers), block0 = plan.start(min(w0, plan.workers)), block1 = plan.start(w1);
   int u = worker < plan.workers ? plan.start(worker) : block1;
   const int u_end = worker < plan.workers ? plan.start(worker + 1) : block1;
   if (deal == DEAL_SPLIT && w0 >= plan.workers) return;
   // WARP, BLOCK: taker and takers; consecutive items go to different SMs
   const int takers = deal == DEAL_WARP ? a.max_workers : gridDim.x;
-  const int taker = deal == DEAL_WARP ? warp * gridDim.x + blockIdx.x : blockIdx.x;
+  int taker = deal == DEAL_WARP ? warp * gridDim.x + blockIdx.x : blockIdx.x;
+  // SHARE: blocks of an item, this one's place among them
+  int share = deal == DEAL_SHARE ? gridDim.x / dm.items : 0, place = 0;
+  if (share) {
+    place = blockIdx.x % share;
+    taker = blockIdx.x / share;
+  }
   bool team = deal != DEAL_WARP;   // all warps of the block work on one item
   for (int round = 0, at = block0;;) {
-    int b, it, u0 = 0, u1 = 0, s0, n, active = PA_WARPS;
+    int b, it, u0 = 0, u1 = 0, s0, n, active = WARPS;
     SeqWork s;
     if (deal == DEAL_SPLIT) {
       b = work_find(mem.pre, c.batch, at);
@@ -422,21 +436,30 @@ __device__ __forceinline__ void attend_items(const AttendArgs& a, F item) {
       it = k - dm.pre[rank];
       s = seq_work<KS, TR>(r, mem.lens[b].x, mem.lens[b].y);
       s0 = 0, n = s.steps;
+      if (share) {
+        share = min(share, s.steps);
+        if (place >= share) return;
+        u0 = (int)blockIdx.x - place;
+        s0 = (int)((long long)s.steps * place / share);
+        n = (int)((long long)s.steps * (place + 1) / share) - s0;
+      }
       if (team) {
-        active = min(PA_WARPS, s.steps);
-        s0 = s.steps * min(warp, active) / active;
-        n = s.steps * min(warp + 1, active) / active - s0;
+        active = min(WARPS, n);
+        const int w_0 = n * min(warp, active) / active, w_1 = n * min(warp + 1, active) / active;
+        s0 += w_0;
+        n = w_1 - w_0;
       }
     }
     const int kvh = it / s.tiles, tile = it - kvh * s.tiles;
     if (n > 0) item(s, b, kvh, tile, s0, n, sm + warp * REGION);
     if (team) {
-      const bool whole = deal == DEAL_BLOCK || (block0 == u0 && block1 == u1);
-      finish_item<T, D, TR, true>(a, plan, sm, active, b, kvh, tile, s.rows * r.group, u0, u1, w0, block0 == u0, whole);
-      if (deal == DEAL_SPLIT) return;
+      const bool whole = deal == DEAL_BLOCK || (share ? share == 1 : block0 == u0 && block1 == u1);
+      finish_item<T, C, true>(a, plan, sm, active, b, kvh, tile, s.rows * r.group, u0, u1, w0, share ? place == 0 : block0 == u0,
+                              whole, share);
+      if (deal != DEAL_BLOCK) return;
     } else {
-      finish_item<T, D, TR, false>(a, plan, sm + warp * REGION, 1, b, kvh, tile, s.rows * r.group, u0, u1, worker, s0 == 0,
-                                   n == s.steps);
+      finish_item<T, C, false>(a, plan, sm + warp * REGION, 1, b, kvh, tile, s.rows * r.group, u0, u1, worker, s0 == 0,
+                                   n == s.steps, 0);
       at = u += n;
       if (deal == DEAL_SPLIT && u >= u_end) return;
     }
@@ -445,38 +468,39 @@ __device__ __forceinline__ void attend_items(const AttendArgs& a, F item) {
 
 // MT m-tiles of 8 E rows: up to 8 rows use half of one (E = 1), the softmax of
 // the other half is left out.
-template <typename T, int D, int MT, int E>
-__global__ void __launch_bounds__(PA_WARPS * 32, 1) attend16_kernel(AttendArgs a) {
-  constexpr int KS = Cfg16<D>::KS, NG = KS / PG_GROUP, NC = D / 32, NV = D / 64, TR = 8 * E * MT;
+template <typename T, typename C, int MT, int E>
+__global__ void __launch_bounds__(C::WARPS * 32, 1) attend16_kernel(AttendArgs a) {
+  constexpr int D = C::D, KS = Cfg16<D>::KS, NG = KS / PG_GROUP, NC = D / 32, NV = D / 64, TR = C::TR, STAGES = C::STAGES;
+  static_assert(TR == 8 * E * MT && KS * D * 4 == 8192, "");
   const PagedView& c = a.c;
   const PagedRows& r = a.r;
   const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   const float sc = r.scale * LOG2E;
-  __shared__ __align__(8) uint64_t bars[PA_WARPS][PA_STAGES][2];   // K and V of a stage have landed
+  __shared__ __align__(8) uint64_t bars[C::WARPS][STAGES][2];   // K and V of a stage have landed
   uint64_t(*bar)[2] = bars[threadIdx.x >> 5];
-  if (lane < 2 * PA_STAGES) mbar_init(&bar[lane >> 1][lane & 1], 1);
+  if (lane < 2 * STAGES) mbar_init(&bar[lane >> 1][lane & 1], 1);
   fence_mbar_init();
   __syncwarp();
   uint32_t phases = 0;   // a bit a stage
   bool gave_up = false;
 
-  attend_items<T, D, KS, TR>(a, [&](const SeqWork& s, int b, int kvh, int tile, int s0, int n, float* sm) {
+  attend_items<T, C, KS>(a, [&](const SeqWork& s, int b, int kvh, int tile, int s0, int n, float* sm) {
     const long long new_off = b * r.n_b + kvh * r.n_h;
     Keys16<T, D> ks{c, r, s, c.table + b * c.table_stride, kvh * c.head_stride, r.k_new + new_off, r.v_new + new_off, g, t};
     constexpr int KB = KS * D * 2;   // bytes of a step's K, and of its V
     const uint32_t ring = smem_u32(sm);
     long long off[NG];
-    int pid[PA_STAGES][NG], next[NG];   // page ids, asked for a step ahead of the copies
+    int pid[STAGES][NG], next[NG];   // page ids, asked for a step ahead of the copies
 #pragma unroll
-    for (int i = 0; i < PA_STAGES; ++i)
+    for (int i = 0; i < STAGES; ++i)
 #pragma unroll
       for (int x = 0; x < NG; ++x) pid[i][x] = i < n ? ks.id(s0 + i, x) : 0;
 #pragma unroll
-    for (int x = 0; x < NG; ++x) next[x] = PA_STAGES < n ? ks.id(s0 + PA_STAGES, x) : 0;
+    for (int x = 0; x < NG; ++x) next[x] = STAGES < n ? ks.id(s0 + STAGES, x) : 0;
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // results were written here before
     __syncwarp();
 #pragma unroll
-    for (int i = 0; i < PA_STAGES; ++i) {
+    for (int i = 0; i < STAGES; ++i) {
       if (i < n) {
         ks.offsets(s0 + i, pid[i], off);
         ks.fetch(s0 + i, c.k, ks.kn, off, ring + i * 2 * KB, &bar[i][0]);
@@ -515,11 +539,11 @@ __global__ void __launch_bounds__(PA_WARPS * 32, 1) attend16_kernel(AttendArgs a
 #pragma unroll 1
     for (int i = 0; i < n; ++i) {
       const int step = s0 + i;
-      const bool full = ks.full(step), more = i + PA_STAGES < n;
+      const bool full = ks.full(step), more = i + STAGES < n;
       const uint32_t slot = ring + stage * 2 * KB, parity = phases >> stage & 1;
       uint64_t* landed = bar[stage];
       phases ^= 1u << stage;
-      stage = stage + 1 == PA_STAGES ? 0 : stage + 1;
+      stage = stage + 1 == STAGES ? 0 : stage + 1;
       float S[MT][KS / 8][4];
       bar_wait(&landed[0], parity, c.status, gave_up);
       {
@@ -542,11 +566,11 @@ __global__ void __launch_bounds__(PA_WARPS * 32, 1) attend16_kernel(AttendArgs a
       }
       __syncwarp();   // all lanes have read the slot
       if (more) {
-        ks.offsets(step + PA_STAGES, next, off);
-        ks.fetch(step + PA_STAGES, c.k, ks.kn, off, slot, &landed[0]);
-        if (i + PA_STAGES + 1 < n)
+        ks.offsets(step + STAGES, next, off);
+        ks.fetch(step + STAGES, c.k, ks.kn, off, slot, &landed[0]);
+        if (i + STAGES + 1 < n)
 #pragma unroll
-          for (int x = 0; x < NG; ++x) next[x] = ks.id(step + PA_STAGES + 1, x);
+          for (int x = 0; x < NG; ++x) next[x] = ks.id(step + STAGES + 1, x);
       }
       if (!full) {
 #pragma unroll
@@ -628,7 +652,7 @@ __global__ void __launch_bounds__(PA_WARPS * 32, 1) attend16_kernel(AttendArgs a
             }
           }
       __syncwarp();
-      if (more) ks.fetch(step + PA_STAGES, c.v, ks.vn, off, slot + KB, &landed[1]);
+      if (more) ks.fetch(step + STAGES, c.v, ks.vn, off, slot + KB, &landed[1]);
     }
     if (tile == 0 && s.keys > s.paged && s0 <= s.paged / KS && s.paged / KS < s0 + n) append_rows(c, r, s, b, kvh, D * sizeof(T));
 
@@ -663,15 +687,15 @@ __global__ void __launch_bounds__(PA_WARPS * 32, 1) attend16_kernel(AttendArgs a
 // key (lane e of them takes the 16-byte chunks e, e + 8, ..), four keys at a
 // time; each group of eight lanes keeps its own running maximum, sum and
 // output over its keys, combined at the end of the item.
-template <int D>
-__global__ void __launch_bounds__(PA_WARPS * 32, 1) attend32_kernel(AttendArgs a) {
-  constexpr int TR = 4, KS = D == 64 ? 16 : 8, IT = KS / 4, NC = D / 32;
+template <typename C>
+__global__ void __launch_bounds__(C::WARPS * 32, 1) attend32_kernel(AttendArgs a) {
+  constexpr int D = C::D, TR = C::TR, KS = D == 64 ? 16 : 8, IT = KS / 4, NC = D / 32;
   const PagedView& c = a.c;
   const PagedRows& r = a.r;
   const int lane = threadIdx.x & 31, kg = lane >> 3, e = lane & 7;
   const float sc = r.scale * LOG2E;
 
-  attend_items<float, D, KS, TR>(a, [&](const SeqWork& s, int b, int kvh, int tile, int s0, int n, float* sm) {
+  attend_items<float, C, KS>(a, [&](const SeqWork& s, int b, int kvh, int tile, int s0, int n, float* sm) {
     const int* table_row = c.table + b * c.table_stride;
     float q[TR][NC * 4], O[TR][NC * 4], m_run[TR], l_run[TR];
     int lim[TR];
@@ -777,41 +801,60 @@ __global__ void __launch_bounds__(PA_WARPS * 32, 1) attend32_kernel(AttendArgs a
   });
 }
 
-int attend_tile(int dtype, int dim, int m_rows) {
-  return dtype == 0 ? 4 : m_rows <= 8 ? 8 : dim == 64 && m_rows > 16 ? 32 : 16;
-}
+// Rows up to 8, 16 and 32 a tile; 12 warps where their registers allow it (a
+// warp's step is a chain of dependent instructions, which other warps fill).
+using S64x8 = Shape<64, 8, 12, 2>;
+using S64x16 = Shape<64, 16, 12, 2>;
+using S64x32 = Shape<64, 32, 8, 3>;
+using S128x8 = Shape<128, 8, 8, 3>;
+using S128x16 = Shape<128, 16, 8, 3>;
+using F64x4 = Shape<64, 4, 8, 0>;
+using F128x4 = Shape<128, 4, 8, 0>;
+
 int attend_grid() {
-  const int most = MAX_WORKERS / PA_WARPS, sms = paged_sm_count();
+  const int most = MAX_WORKERS / 12, sms = paged_sm_count();
   return sms < most ? sms : most;
 }
-int64_t attend_ws_bytes(int tr, int dim) { return MAX_WORKERS * 4 + (int64_t)attend_grid() * PA_WARPS * 2 * tr * (dim + 2) * 4; }
+
+// What a call does with the shape that its type, head dimension and rows ask for.
+template <typename F>
+auto with_shape(int dtype, int dim, int m_rows, F f) {
+  if (dtype == 0) return dim == 64 ? f(F64x4{}) : f(F128x4{});
+  if (dim == 128) return m_rows <= 8 ? f(S128x8{}) : f(S128x16{});
+  return m_rows <= 8 ? f(S64x8{}) : m_rows <= 16 ? f(S64x16{}) : f(S64x32{});
+}
+
+int64_t attend_ws_bytes(int dtype, int dim, int m_rows) {
+  return with_shape(dtype, dim, m_rows, [](auto s) {
+    return (int64_t)MAX_WORKERS * 4 + (int64_t)attend_grid() * s.WARPS * 2 * s.PART * 4;
+  });
+}
 
 // One block an SM.  The shared memory above 48 KB that a kernel needs is asked for once a device.
-template <auto kernel, int D, int TR>
-cudaError_t launch_attend(const AttendArgs& a, cudaStream_t st) {
-  constexpr size_t REGIONS = (size_t)PA_WARPS * Part<D, TR>::REGION * 4;
+template <auto kernel, typename C>
+cudaError_t launch_attend(AttendArgs& a, cudaStream_t st) {
+  constexpr size_t REGIONS = (size_t)C::WARPS * C::REGION * 4;
   static std::atomic<uint64_t> ready{0};
   int dev = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
   const uint64_t bit = 1ull << (dev & 63);
   if (!(ready.load(std::memory_order_acquire) & bit)) {
-    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)(REGIONS + plan_bytes(PG_MAX_BATCH) + deal_bytes(DEAL_SORT_MAX)));
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                             (int)(REGIONS + plan_bytes(PG_MAX_BATCH) + deal_bytes(DEAL_SORT_MAX)));
     if (e != cudaSuccess) return e;
     ready.fetch_or(bit, std::memory_order_release);
   }
-  kernel<<<a.max_workers / PA_WARPS, PA_WARPS * 32, REGIONS + plan_bytes(a.c.batch) + deal_bytes(a.c.batch), st>>>(a);
+  const int grid = attend_grid();
+  a.max_workers = grid * C::WARPS;
+  kernel<<<grid, C::WARPS * 32, REGIONS + plan_bytes(a.c.batch) + deal_bytes(a.c.batch), st>>>(a);
   return cudaGetLastError();
 }
 
-template <typename T>
-cudaError_t launch16(const AttendArgs& a, int dim, int tr, cudaStream_t st) {
-  if (dim == 128)
-    return tr == 8 ? launch_attend<attend16_kernel<T, 128, 1, 1>, 128, 8>(a, st)
-                   : launch_attend<attend16_kernel<T, 128, 1, 2>, 128, 16>(a, st);
-  if (tr == 32) return launch_attend<attend16_kernel<T, 64, 2, 2>, 64, 32>(a, st);
-  return tr == 16 ? launch_attend<attend16_kernel<T, 64, 1, 2>, 64, 16>(a, st)
-                  : launch_attend<attend16_kernel<T, 64, 1, 1>, 64, 8>(a, st);
+template <typename T, typename C>
+cudaError_t launch_shape(AttendArgs& a, cudaStream_t st) {
+  if constexpr (C::TR == 4) return launch_attend<attend32_kernel<C>, C>(a, st);
+  else return launch_attend<attend16_kernel<T, C, C::TR == 32 ? 2 : 1, C::TR == 8 ? 1 : 2>, C>(a, st);
 }
 
 }  // namespace
@@ -826,7 +869,7 @@ int64_t asr_spec_paged_attend_ws(const asr_paged_cache* c, const asr_paged_rows*
   PagedRows w;
   if (int rc = paged_view(c, &v)) return rc;
   if (int rc = paged_rows(c, r, &w)) return rc;
-  return attend_ws_bytes(attend_tile(c->dtype, c->head_dim, w.max_rows * w.group), c->head_dim);
+  return attend_ws_bytes(c->dtype, c->head_dim, w.max_rows * w.group);
 }
 
 int asr_spec_paged_attend(const asr_paged_cache* c, const asr_paged_rows* r, void* out, float* lse, void* ws,
@@ -835,23 +878,22 @@ int asr_spec_paged_attend(const asr_paged_cache* c, const asr_paged_rows* r, voi
   if (int rc = paged_view(c, &a.c)) return rc;
   if (int rc = paged_rows(c, r, &a.r)) return rc;
   if (!out || !ws || ((uintptr_t)out | (uintptr_t)ws) % 16 || (uintptr_t)lse % 4) return ASR_E_INVAL;
-  const int tr = attend_tile(c->dtype, c->head_dim, a.r.max_rows * a.r.group);
-  if (ws_bytes < attend_ws_bytes(tr, c->head_dim)) return ASR_E_CAPACITY;
-  const long long tiles = ((long long)a.r.max_rows * a.r.group + tr - 1) / tr;
+  const int m_rows = a.r.max_rows * a.r.group;
+  if (ws_bytes < attend_ws_bytes(c->dtype, c->head_dim, m_rows)) return ASR_E_CAPACITY;
+  const int tr = with_shape(c->dtype, c->head_dim, m_rows, [](auto s) { return s.TR; });
+  const long long tiles = ((long long)m_rows + tr - 1) / tr;
   if (tiles * c->kv_heads * c->batch * ((long long)a.c.max_slots / 8 + a.r.max_rows / 8 + 2) > 0x7fffffffll)
     return ASR_E_CAPACITY;   // 32-bit units
   a.out = static_cast<char*>(out);
   a.lse = lse;
   a.tickets = static_cast<int*>(ws);
   a.ws = reinterpret_cast<float*>(a.tickets + MAX_WORKERS);
-  a.max_workers = attend_grid() * PA_WARPS;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
-  cudaError_t e;
-  if (c->dtype == 0)
-    e = c->head_dim == 64 ? launch_attend<attend32_kernel<64>, 64, 4>(a, st)
-                          : launch_attend<attend32_kernel<128>, 128, 4>(a, st);
-  else if (c->dtype == 1) e = launch16<__nv_bfloat16>(a, c->head_dim, tr, st);
-  else e = launch16<__half>(a, c->head_dim, tr, st);
+  const cudaError_t e = with_shape(c->dtype, c->head_dim, m_rows, [&](auto s) {
+    using C = decltype(s);
+    if constexpr (C::TR == 4) return launch_shape<float, C>(a, st);
+    else return c->dtype == 1 ? launch_shape<__nv_bfloat16, C>(a, st) : launch_shape<__half, C>(a, st);
+  });
   return e == cudaSuccess ? ASR_OK : ASR_E_CUDA;
 }
 
