@@ -70,13 +70,13 @@ __device__ __forceinline__ void paged_lens(const PagedView& c, const PagedRows& 
 
 // The page of a sequence's 16-slot group `grp`.  An id out of range sets the
 // status word and page 0 stands in, so that reads stay in the pool.
+__device__ __forceinline__ int paged_valid(const PagedView& c, int pid) {
+  if ((unsigned)pid < (unsigned)c.n_pages) return pid;
+  if (c.status) set_status(c.status, ST_BOUNDS);
+  return 0;
+}
 __device__ __forceinline__ int paged_id(const PagedView& c, const int* table_row, int grp) {
-  int pid = __ldg(table_row + c.groups.div((uint32_t)grp));
-  if ((unsigned)pid >= (unsigned)c.n_pages) {
-    if (c.status) set_status(c.status, ST_BOUNDS);
-    pid = 0;
-  }
-  return pid;
+  return paged_valid(c, __ldg(table_row + c.groups.div((uint32_t)grp)));
 }
 // Byte offset of a group's slot 0 in the pool.
 __device__ __forceinline__ long long paged_offset(const PagedView& c, int pid, int grp) {
@@ -312,34 +312,62 @@ struct Keys16 {
     }
   }
   // A step's K (or V) by bulk copies into shared memory, rows of D in slot
-  // order, counted on `bar`: a copy a group where a head's slots are
-  // contiguous, else one a row; the block's own rows one a row.  Nothing is
-  // written past the end.
-  __device__ __forceinline__ void fetch(int step, const char* pages, const char* fresh, const long long* off, uint32_t dst,
+  // order, counted on `bar`.  `off`: the lane's group's offset in the pool (see
+  // Groups), the step's groups being lanes at, at + 1.  A copy a group where a
+  // head's slots are contiguous, else one a row; the block's own rows one a
+  // row.  Nothing is written past the end.
+  __device__ __forceinline__ void fetch(int step, const char* pages, const char* fresh, long long off, int at, uint32_t dst,
                                         uint64_t* bar) const {
-    const int lane = threadIdx.x & 31, in_pages = min(KS, s.paged - step * KS);   // rows from the pages, if positive
+    const int lane = threadIdx.x & 31;
     const bool runs = c.slot_stride == ROW;
-    const int rows = min(KS, s.keys - step * KS);
-    if (lane == 0) {
-      mbar_arrive_expect_tx(bar, rows * ROW);
-      if (runs) {
+    if (runs && (step + 1) * KS <= s.paged) {
+      long long o[NG];
 #pragma unroll
-        for (int u = 0; u < NG; ++u) {
-          const int n = min(PG_GROUP, in_pages - u * PG_GROUP);
-          if (n > 0) bulk_copy(dst + u * PG_GROUP * ROW, pages + off[u], n * ROW, bar);
-        }
+      for (int u = 0; u < NG; ++u) o[u] = __shfl_sync(0xffffffffu, off, at + u);
+      if (lane == 0) {
+        mbar_arrive_expect_tx(bar, KS * ROW);
+#pragma unroll
+        for (int u = 0; u < NG; ++u) bulk_copy(dst + u * PG_GROUP * ROW, pages + o[u], PG_GROUP * ROW, bar);
       }
+      return;
     }
-    if (runs && in_pages == KS) return;
-    __syncwarp();
+    const int in_pages = min(KS, s.paged - step * KS), rows = min(KS, s.keys - step * KS);
+    if (lane == at) mbar_arrive_expect_tx(bar, rows * ROW);
+    if (runs && (unsigned)(lane - at) < NG) {
+      const int n = min(PG_GROUP, in_pages - (lane - at) * PG_GROUP);
+      if (n > 0) bulk_copy(dst + (lane - at) * PG_GROUP * ROW, pages + off, n * ROW, bar);
+    }
     const int row0 = runs ? max(in_pages, 0) : 0, row = row0 + lane;
-    if (row < rows) {
-      long long base = off[0];
-      if (NG > 1 && row >= PG_GROUP) base = off[NG - 1];
-      const char* src = row < in_pages ? pages + base + (row % PG_GROUP) * c.slot_stride
-                                       : fresh + (long long)(step * KS + row - s.paged) * r.n_r;
-      bulk_copy(dst + row * ROW, src, ROW, bar);
+    const long long base = __shfl_sync(0xffffffffu, off, at + (NG > 1 && row >= PG_GROUP ? 1 : 0));
+    if (row < rows)
+      bulk_copy(dst + row * ROW,
+                row < in_pages ? pages + base + (row % PG_GROUP) * c.slot_stride
+                               : fresh + (long long)(step * KS + row - s.paged) * r.n_r,
+                ROW, bar);
+  }
+};
+
+// Where a run of steps lies in the pool: of every 32 groups a lane looks up one,
+// the next 32's page ids a round ahead of their use.
+template <typename T, int D>
+struct Groups {
+  static constexpr int NG = Keys16<T, D>::NG, STEPS = 32 / NG;
+  const Keys16<T, D>& ks;
+  int grp0, next_pid;
+  long long off;
+  __device__ __forceinline__ int page(int round) const {
+    const int grp = grp0 + round * 32 + (threadIdx.x & 31);
+    return grp * PG_GROUP < ks.s.paged ? __ldg(ks.table_row + ks.c.groups.div((uint32_t)grp)) : 0;   // looked at when used
+  }
+  __device__ __forceinline__ Groups(const Keys16<T, D>& k, int s0) : ks(k), grp0(s0 * NG), next_pid(0), off(0) { next_pid = page(0); }
+  // step i of the run: its first lane; the offsets are this round's from here on
+  __device__ __forceinline__ int at(int i) {
+    if (i % STEPS == 0) {
+      const int round = i / STEPS;
+      off = paged_offset(ks.c, paged_valid(ks.c, next_pid), grp0 + round * 32 + (threadIdx.x & 31)) + ks.head_off;
+      next_pid = page(round + 1);
     }
+    return i % STEPS * NG;
   }
 };
 

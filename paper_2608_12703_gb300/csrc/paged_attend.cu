@@ -489,22 +489,15 @@ __global__ void __launch_bounds__(C::WARPS * 32, 1) attend16_kernel(AttendArgs a
     Keys16<T, D> ks{c, r, s, c.table + b * c.table_stride, kvh * c.head_stride, r.k_new + new_off, r.v_new + new_off, g, t};
     constexpr int KB = KS * D * 2;   // bytes of a step's K, and of its V
     const uint32_t ring = smem_u32(sm);
-    long long off[NG];
-    int pid[STAGES][NG], next[NG];   // page ids, asked for a step ahead of the copies
-#pragma unroll
-    for (int i = 0; i < STAGES; ++i)
-#pragma unroll
-      for (int x = 0; x < NG; ++x) pid[i][x] = i < n ? ks.id(s0 + i, x) : 0;
-#pragma unroll
-    for (int x = 0; x < NG; ++x) next[x] = STAGES < n ? ks.id(s0 + STAGES, x) : 0;
+    Groups<T, D> groups(ks, s0);
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // results were written here before
     __syncwarp();
 #pragma unroll
     for (int i = 0; i < STAGES; ++i) {
       if (i < n) {
-        ks.offsets(s0 + i, pid[i], off);
-        ks.fetch(s0 + i, c.k, ks.kn, off, ring + i * 2 * KB, &bar[i][0]);
-        ks.fetch(s0 + i, c.v, ks.vn, off, ring + i * 2 * KB + KB, &bar[i][1]);
+        const int at = groups.at(i);
+        ks.fetch(s0 + i, c.k, ks.kn, groups.off, at, ring + i * 2 * KB, &bar[i][0]);
+        ks.fetch(s0 + i, c.v, ks.vn, groups.off, at, ring + i * 2 * KB + KB, &bar[i][1]);
       }
     }
 
@@ -565,12 +558,10 @@ __global__ void __launch_bounds__(C::WARPS * 32, 1) attend16_kernel(AttendArgs a
         }
       }
       __syncwarp();   // all lanes have read the slot
+      int at = 0;
       if (more) {
-        ks.offsets(step + STAGES, next, off);
-        ks.fetch(step + STAGES, c.k, ks.kn, off, slot, &landed[0]);
-        if (i + STAGES + 1 < n)
-#pragma unroll
-          for (int x = 0; x < NG; ++x) next[x] = ks.id(step + STAGES + 1, x);
+        at = groups.at(i + STAGES);
+        ks.fetch(step + STAGES, c.k, ks.kn, groups.off, at, slot, &landed[0]);
       }
       if (!full) {
 #pragma unroll
@@ -652,7 +643,7 @@ __global__ void __launch_bounds__(C::WARPS * 32, 1) attend16_kernel(AttendArgs a
             }
           }
       __syncwarp();
-      if (more) ks.fetch(step + STAGES, c.v, ks.vn, off, slot + KB, &landed[1]);
+      if (more) ks.fetch(step + STAGES, c.v, ks.vn, groups.off, at, slot + KB, &landed[1]);
     }
     if (tile == 0 && s.keys > s.paged && s0 <= s.paged / KS && s.paged / KS < s0 + n) append_rows(c, r, s, b, kvh, D * sizeof(T));
 
