@@ -94,7 +94,7 @@ struct Stat {   // max and sum of weights relative to it
 // CL blocks a cluster, GROUPS rows at a time in a block.
 template <typename T, int CL, int GROUPS>
 __global__ void __launch_bounds__(AS_ROW * GROUPS, GROUPS == 1 ? 4 : 1) accept_kernel(SampleArgs a) {
-  constexpr int N = Vec16<T>::N, UN = 4, THREADS = AS_ROW * GROUPS, WARPS = THREADS / 32, ROW_WARPS = AS_ROW / 32;
+  constexpr int N = Vec16<T>::N, UN = GROUPS == 1 && sizeof(T) == 4 ? 8 : 4, THREADS = AS_ROW * GROUPS, WARPS = THREADS / 32, ROW_WARPS = AS_ROW / 32;
   __shared__ float2 s_warp[AS_ROWS][ROW_WARPS];          // a warp's part of a row
   __shared__ float2 s_part[AS_ROWS][CL];                 // every block's part of a row
   __shared__ float s_m[AS_ROWS], s_inv[AS_ROWS], s_x[AS_ROWS];   // the row's max, 1 / sum, its draft's logit, then probability
