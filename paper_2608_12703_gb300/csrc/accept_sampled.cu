@@ -60,26 +60,62 @@ __device__ __forceinline__ float clean(float x) { return fminf(fmaxf(x, -INFINIT
 // exp((x - m) / T) for finite m; 0 for a masked x
 __device__ __forceinline__ float weight(float x, float m, float c) { return ex2((x - m) * c); }
 
-template <typename T> struct Vec16 {   // the values of 16 bytes
-  static constexpr int N = 8;
-  static __device__ __forceinline__ void get(const uint4& v, float* f) {
-    const uint32_t r[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const uint32_t lo = r[i] & 0xffffu, hi = r[i] >> 16;
-      const unsigned short a = (unsigned short)lo, b = (unsigned short)hi;
-      f[2 * i] = to_f32(*reinterpret_cast<const T*>(&a));
-      f[2 * i + 1] = to_f32(*reinterpret_cast<const T*>(&b));
-    }
-  }
-};
-
+// The values of 16 bytes, and their maximum (which passes over NaN).
+template <typename T> struct Vec16;
 template <> struct Vec16<float> {
   static constexpr int N = 4;
   static __device__ __forceinline__ void get(const uint4& v, float* f) {
     f[0] = __uint_as_float(v.x), f[1] = __uint_as_float(v.y), f[2] = __uint_as_float(v.z), f[3] = __uint_as_float(v.w);
   }
+  static __device__ __forceinline__ float top(const uint4& v) {
+    return fmaxf(fmaxf(__uint_as_float(v.x), __uint_as_float(v.y)), fmaxf(__uint_as_float(v.z), __uint_as_float(v.w)));
+  }
 };
+template <> struct Vec16<__nv_bfloat16> {
+  static constexpr int N = 8;
+  static __device__ __forceinline__ void get(const uint4& v, float* f) {
+    const uint32_t r[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) f[2 * i] = __uint_as_float(r[i] << 16), f[2 * i + 1] = __uint_as_float(r[i] & 0xffff0000u);
+  }
+  static __device__ __forceinline__ float top(const uint4& v) {
+    const __nv_bfloat162* p = reinterpret_cast<const __nv_bfloat162*>(&v);
+    const float2 f = __bfloat1622float2(__hmax2(__hmax2(p[0], p[1]), __hmax2(p[2], p[3])));
+    return fmaxf(f.x, f.y);
+  }
+};
+template <> struct Vec16<__half> {
+  static constexpr int N = 8;
+  static __device__ __forceinline__ void get(const uint4& v, float* f) {
+    const __half2* p = reinterpret_cast<const __half2*>(&v);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float2 x = __half22float2(p[i]);
+      f[2 * i] = x.x, f[2 * i + 1] = x.y;
+    }
+  }
+  static __device__ __forceinline__ float top(const uint4& v) {
+    const __half2* p = reinterpret_cast<const __half2*>(&v);
+    const float2 f = __half22float2(__hmax2(__hmax2(p[0], p[1]), __hmax2(p[2], p[3])));
+    return fmaxf(f.x, f.y);
+  }
+};
+
+// Weights of two raw logits, two lanes an instruction where there is one: the
+// saturation to [0, 1] turns the NaN of a NaN logit into 0 and the infinity of
+// an infinite one into 1.
+__device__ __forceinline__ uint64_t pair(float x) {
+  const uint32_t b = __float_as_uint(x);
+  return (uint64_t)b << 32 | b;
+}
+__device__ __forceinline__ float weight2(float x, float y, uint64_t minus_m, uint64_t c) {
+  float d, e;
+  asm("{\n\t.reg .b64 t;\n\tmov.b64 t, {%2, %3};\n\tadd.rn.f32x2 t, t, %4;\n\tmul.rn.f32x2 t, t, %5;\n\t"
+      "mov.b64 {%0, %1}, t;\n\t}"
+      : "=f"(d), "=f"(e)
+      : "f"(x), "f"(y), "l"(minus_m), "l"(c));
+  return __saturatef(ex2(d)) + __saturatef(ex2(e));
+}
 
 struct Stat {   // max and sum of weights relative to it
   float m = -INFINITY, l = 0.f;
@@ -151,20 +187,18 @@ __global__ void __launch_bounds__(AS_ROW * GROUPS, GROUPS == 1 ? 4 : 1) accept_k
 #pragma unroll
       for (int j = 0; j < UN; ++j) {
         if (i + j * AS_ROW >= v1) break;
-        float f[N];
-        Vec16<T>::get(v[j], f);
-#pragma unroll
-        for (int y = 0; y < N; ++y) mx = fmaxf(mx, f[y]);   // passes over NaN
+        mx = fmaxf(mx, Vec16<T>::top(v[j]));
       }
       if (mx == -INFINITY) continue;
       mx = fminf(mx, 3.4028234e38f);
+      const uint64_t minus_m = pair(-mx), cc = pair(c);
 #pragma unroll
       for (int j = 0; j < UN; ++j) {
         if (i + j * AS_ROW >= v1) break;
         float f[N];
         Vec16<T>::get(v[j], f);
 #pragma unroll
-        for (int y = 0; y < N; ++y) l += weight(clean(f[y]), mx, c);
+        for (int y = 0; y < N; y += 2) l += weight2(f[y], f[y + 1], minus_m, cc);
       }
       s.l = fmaf(s.l, weight(s.m, mx, c), l);
       s.m = mx;
