@@ -308,48 +308,91 @@ __device__ __forceinline__ void clear_rows(const AttendArgs& a, const PlanMem& m
 // Whole items are dealt longest sequence first, to and fro over the takers.
 // Measured, us a call: @@
 enum Deal { DEAL_WARP, DEAL_BLOCK, DEAL_SHARE, DEAL_SPLIT };
-constexpr int DEAL_SORT_MAX = 256;   // sequences that a block ranks, one a thread
+constexpr int DEAL_SORT_MAX = 224;   // sequences that a block ranks, one a thread of all warps but the first
 constexpr float END_COST = 4.f, SHARE_COST = 5.f, SPLIT_COST = 16.f;   // steps
 
 struct DealMem {
   int *order, *pre;   // [B] sequences by falling length, [B + 1] items before each
   int items;
 };
-constexpr size_t deal_bytes(int B) { return B <= DEAL_SORT_MAX ? ((size_t)B * 8 + 4 + 15) / 16 * 16 : 0; }
+constexpr size_t deal_bytes(int B) { return B <= DEAL_SORT_MAX ? ((size_t)B * 12 + 4 + 16 + 15) / 16 * 16 : 0; }
 
+// The lengths, the units' prefix sums and the deal, the same in every block.
 template <typename C, int KS>
-__device__ __forceinline__ Deal choose_deal(const AttendArgs& a, const WorkPlan& plan, const PlanMem& mem, DealMem& dm,
-                                            int* smem) {
+__device__ __forceinline__ Deal make_plan(const AttendArgs& a, unsigned char* smem, WorkPlan& plan, PlanMem& mem, DealMem& dm) {
   constexpr int TR = C::TR, WARPS = C::WARPS;
-  __shared__ int s_long;
-  const int B = a.c.batch, b = threadIdx.x, lane = threadIdx.x & 31;
-  if (B > DEAL_SORT_MAX) return DEAL_SPLIT;
-  dm.order = smem;
-  dm.pre = smem + B;
-  int steps = 0, items = 0, rank = 0;
-  if (b == 0) s_long = 0;
-  if (b < B) {
-    const SeqWork s = seq_work<KS, TR>(a.r, mem.lens[b].x, mem.lens[b].y);
-    steps = s.steps;
-    items = s.steps ? a.c.kv_heads * s.tiles : 0;
-    dm.pre[b + 1] = steps;
+  __shared__ int s_long, s_items;
+  const int B = a.c.batch, tid = threadIdx.x, lane = tid & 31;
+  const bool sort = B <= DEAL_SORT_MAX;
+  mem.lens = reinterpret_cast<int2*>(smem);
+  mem.pre = reinterpret_cast<int*>(mem.lens + B);
+  int* steps = reinterpret_cast<int*>(smem + plan_bytes(B));   // [B], filled up to whole vectors
+  dm.order = steps + (B + 3) / 4 * 4;
+  dm.pre = dm.order + B;
+  auto work = [&](int b) { return seq_work<KS, TR>(a.r, mem.lens[b].x, mem.lens[b].y); };
+  for (int b = tid; b < B; b += blockDim.x) {
+    paged_lens(a.c, a.r, b, mem.lens[b].x, mem.lens[b].y);
+    const SeqWork s = work(b);
+    mem.pre[b + 1] = a.c.kv_heads * s.tiles * s.steps;
+    if (sort) steps[b] = s.steps;
   }
+  if (sort && tid < 4 && B + tid < (B + 3) / 4 * 4) steps[B + tid] = -1;
   __syncthreads();
-  if (b < B) {
-    for (int x = 0; x < B; ++x) {
-      const int y = dm.pre[x + 1];
-      rank += y > steps || (y == steps && x < b);
+  if (tid < 32) {
+    int base = 0, most = 0, items = 0;
+    for (int b0 = 0; b0 < B; b0 += 32) {
+      int x = 0;
+      if (b0 + lane < B) {
+        x = mem.pre[b0 + lane + 1];
+        const SeqWork s = work(b0 + lane);
+        most = max(most, s.steps);
+        items += s.steps ? a.c.kv_heads * s.tiles : 0;
+      }
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int y = __shfl_up_sync(0xffffffffu, x, o);
+        if (lane >= o) x += y;
+      }
+      if (b0 + lane < B) mem.pre[b0 + lane + 1] = base + x;
+      base += __shfl_sync(0xffffffffu, x, 31);
+    }
+    most = __reduce_max_sync(0xffffffffu, most);
+    items = __reduce_add_sync(0xffffffffu, items);
+    if (lane == 0) mem.pre[0] = 0, s_long = most, s_items = items;
+  } else if (sort && tid - 32 < B) {
+    const int b = tid - 32, mine = steps[b];
+    int rank = 0;
+    for (int x = 0; x < B; x += 4) {
+      const int4 y = *reinterpret_cast<const int4*>(steps + x);
+      rank += (y.x > mine || (y.x == mine && x < b)) + (y.y > mine || (y.y == mine && x + 1 < b)) +
+              (y.z > mine || (y.z == mine && x + 2 < b)) + (y.w > mine || (y.w == mine && x + 3 < b));
     }
     dm.order[rank] = b;
-    if (rank == 0) s_long = steps;
   }
   __syncthreads();
-  if (b < B) dm.pre[rank + 1] = items;
-  __syncthreads();
-  if (threadIdx.x < 32) {
+  plan.units = mem.pre[B];
+  plan.workers = max(1, min(plan.units, a.max_workers));
+  plan.share = plan.units / plan.workers;
+  plan.more = plan.units - plan.share * plan.workers;
+  if (!sort) return DEAL_SPLIT;
+  dm.items = s_items;
+  const float u = (float)plan.units, n = (float)s_items, longest = (float)s_long;
+  const float warps = (float)a.max_workers, blocks = warps / WARPS;
+  const float by_warp = fmaxf(longest + END_COST, n <= warps ? 0.f : 1.1f * (u + END_COST * n) / warps);
+  const float by_block = fmaxf(longest / WARPS + END_COST + 1.f,
+                               n <= blocks ? 0.f : 1.1f * (u / WARPS + (END_COST + 1.f) * n) / blocks);
+  const float by_share = n <= blocks / 2.f ? longest / (WARPS * floorf(blocks / n)) + END_COST + 1.f + SHARE_COST : 1e30f;
+  const float split = u / warps + END_COST + SPLIT_COST;
+  const float least = fminf(fminf(by_warp, by_block), fminf(by_share, split));
+  if (least == split) return DEAL_SPLIT;
+  if (tid < 32) {
     int base = 0;
     for (int b0 = 0; b0 < B; b0 += 32) {
-      int x = b0 + lane < B ? dm.pre[b0 + lane + 1] : 0;
+      int x = 0;
+      if (b0 + lane < B) {
+        const SeqWork s = work(dm.order[b0 + lane]);
+        x = s.steps ? a.c.kv_heads * s.tiles : 0;
+      }
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
         const int y = __shfl_up_sync(0xffffffffu, x, o);
@@ -361,16 +404,7 @@ __device__ __forceinline__ Deal choose_deal(const AttendArgs& a, const WorkPlan&
     if (lane == 0) dm.pre[0] = 0;
   }
   __syncthreads();
-  dm.items = dm.pre[B];
-  const float u = (float)plan.units, n = (float)dm.items, longest = (float)s_long;
-  const float warps = (float)a.max_workers, blocks = warps / WARPS;
-  const float by_warp = fmaxf(longest + END_COST, n <= warps ? 0.f : 1.1f * (u + END_COST * n) / warps);
-  const float by_block = fmaxf(longest / WARPS + END_COST + 1.f,
-                               n <= blocks ? 0.f : 1.1f * (u / WARPS + (END_COST + 1.f) * n) / blocks);
-  const float by_share = n <= blocks / 2.f ? longest / (WARPS * floorf(blocks / n)) + END_COST + 1.f + SHARE_COST : 1e30f;
-  const float split = u / warps + END_COST + SPLIT_COST;
-  const float least = fminf(fminf(by_warp, by_block), fminf(by_share, split));
-  return least == by_warp ? DEAL_WARP : least == by_block ? DEAL_BLOCK : least == by_share ? DEAL_SHARE : DEAL_SPLIT;
+  return least == by_warp ? DEAL_WARP : least == by_block ? DEAL_BLOCK : DEAL_SHARE;
 }
 
 // What the two kernels below share: the plan, the walk over a warp's items and
@@ -381,16 +415,13 @@ __device__ __forceinline__ void attend_items(const AttendArgs& a, F item) {
   constexpr int REGION = C::REGION, D = C::D, TR = C::TR, WARPS = C::WARPS;
   const PagedView& c = a.c;
   const PagedRows& r = a.r;
+  extern __shared__ __align__(16) unsigned char smem[];
+  WorkPlan plan;
   PlanMem mem;
-  const WorkPlan plan = work_plan(c, r, mem, a.max_workers, [&](int len, int rows) {
-    const SeqWork s = seq_work<KS, TR>(r, len, rows);
-    return c.kv_heads * s.tiles * s.steps;
-  });
+  DealMem dm;
+  const Deal deal = make_plan<C, KS>(a, smem, plan, mem, dm);
   clear_rows<T, D>(a, mem);
   if (plan.units == 0) return;
-  extern __shared__ __align__(16) unsigned char smem[];
-  DealMem dm;
-  const Deal deal = choose_deal<C, KS>(a, plan, mem, dm, reinterpret_cast<int*>(smem + plan_bytes(c.batch)));
   float* sm = reinterpret_cast<float*>(smem + plan_bytes(c.batch) + deal_bytes(c.batch));
   const int warp = threadIdx.x >> 5, w0 = blockIdx.x * WARPS, worker = w0 + warp;
 

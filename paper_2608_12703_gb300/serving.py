@@ -28,6 +28,7 @@ from . import asrspec as A
 
 _DTYPE = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 _MAX_LAYOUTS = 1024      # layouts remembered by one operator before it starts anew
+_byref = ctypes.byref
 _raw_stream = torch._C._cuda_getCurrentRawStream
 _current_device = torch._C._cuda_getDevice
 _capturing = torch._C._cuda_isCurrentStreamCapturing
@@ -38,13 +39,9 @@ def _need(ok: bool, what: str):
         raise A.AsrSpecError("ASR_E_INVAL " + what)
 
 
-def _layout(x):
-    if x is None:
-        return None
-    try:
-        return x.shape, x.stride(), x.dtype, x.get_device()
-    except AttributeError:
-        raise A.AsrSpecError(f"ASR_E_INVAL a tensor is required, not {type(x).__name__}") from None
+def _layouts(*args):
+    """The layouts of a call's tensors, other arguments as they are."""
+    return tuple([(x.shape, x.stride(), x.dtype, x.get_device()) if isinstance(x, torch.Tensor) else x for x in args])
 
 
 def _remember(layouts: dict, key, value):
@@ -104,6 +101,8 @@ class PagedCache:
             _DTYPE[self.dtype], self._status.data_ptr())
         self._ref = ctypes.byref(self._c)
         self._lib = A.lib()
+        self._attend, self._weigh, self._evict = (self._lib.asr_spec_paged_attend, self._lib.asr_spec_paged_weigh,
+                                                  self._lib.asr_spec_paged_evict)
         self._attend_layouts, self._weigh_layouts, self._evict_layouts = {}, {}, {}
         self._ws = {}
 
@@ -169,8 +168,7 @@ class PagedCache:
             with torch.cuda.device(self.device):
                 return self.attend(q, kv_len, k_new=k_new, v_new=v_new, rows=rows, causal=causal, scale=scale, out=out,
                                    lse=lse)
-        key = (_layout(q), _layout(kv_len), _layout(k_new), _layout(v_new), _layout(rows), causal, scale, _layout(out),
-               _layout(lse))
+        key = _layouts(q, kv_len, k_new, v_new, rows, causal, scale, out, lse)
         known = self._attend_layouts.get(key)
         if known is None:
             r = self._rows(q, kv_len, rows, k_new, v_new, causal, scale)
@@ -187,8 +185,9 @@ class PagedCache:
         if lse is None:
             lse = torch.empty(lse_shape, dtype=torch.float32, device=self.device)
         stream = _raw_stream(self._index)
-        _check(self._lib.asr_spec_paged_attend(self._ref, ctypes.byref(r), out.data_ptr(), lse.data_ptr(),
-                                               self._workspace("attend", stream, n), n, stream), "asr_spec_paged_attend")
+        rc = self._attend(self._ref, _byref(r), out.data_ptr(), lse.data_ptr(), self._workspace("attend", stream, n), n, stream)
+        if rc:
+            _check(rc, "asr_spec_paged_attend")
         return out, lse
 
     def weigh(self, q, lse, kv_len, score, *, rows=None, causal=True, scale: Optional[float] = None, out=None, pos=None,
@@ -202,8 +201,7 @@ class PagedCache:
                 return self.weigh(q, lse, kv_len, score, rows=rows, causal=causal, scale=scale, out=out, pos=pos,
                                   first_pos=first_pos)
         out = score if out is None else out
-        key = (_layout(q), _layout(kv_len), _layout(rows), causal, scale, _layout(lse), _layout(score), _layout(out),
-               _layout(pos), _layout(first_pos))
+        key = _layouts(q, kv_len, rows, causal, scale, lse, score, out, pos, first_pos)
         known = self._weigh_layouts.get(key)
         if known is None:
             known = _remember(self._weigh_layouts, key, self._weigh_layout(q, lse, kv_len, score, rows, causal, scale, out,
@@ -216,15 +214,16 @@ class PagedCache:
             s.score = score.data_ptr()
         if pos is not None:
             s.pos, s.first_pos = pos.data_ptr(), first_pos.data_ptr()
-        _check(self._lib.asr_spec_paged_weigh(self._ref, ctypes.byref(r), ctypes.byref(s), lse.data_ptr(), *lse_strides,
-                                              _raw_stream(self._index)), "asr_spec_paged_weigh")
+        rc = self._weigh(self._ref, _byref(r), _byref(s), lse.data_ptr(), *lse_strides, _raw_stream(self._index))
+        if rc:
+            _check(rc, "asr_spec_paged_weigh")
         return out
 
     def _weigh_layout(self, q, lse, kv_len, score, rows, causal, scale, out, pos, first_pos):
         r = self._rows(q, kv_len, rows, None, None, causal, scale)
         B, R, H = q.shape[:3]
         _need(out is not None, "out: required without score")
-        _need(out.dim() == 3, "score: [batch, kv_heads, slots] is required")
+        _need(isinstance(out, torch.Tensor) and out.dim() == 3, "score: [batch, kv_heads, slots] is required")
         shape = (B, self.kv_heads, out.shape[2])
         _tensor(out, "out", torch.float32, shape, self.device)
         _need(out.stride(2) == 1, "out: the last axis must be contiguous")
@@ -252,8 +251,7 @@ class PagedCache:
                                   score_out=score_out, pos_out=pos_out)
         score_out = score if score_out is None else score_out
         pos_out = pos if pos_out is None else pos_out
-        key = (_layout(lens), _layout(score), _layout(pos), _layout(seen), budget, recent, first, _layout(lens_out),
-               _layout(score_out), _layout(pos_out))
+        key = _layouts(lens, score, pos, seen, budget, recent, first, lens_out, score_out, pos_out)
         known = self._evict_layouts.get(key)
         if known is None:
             known = _remember(self._evict_layouts, key, self._evict_layout(lens, score, pos, seen, budget, recent, first,
@@ -264,9 +262,10 @@ class PagedCache:
         s = A.AsrPagedScores.from_buffer_copy(slots)
         s.score, s.pos, s.score_out, s.pos_out = score.data_ptr(), pos.data_ptr(), score_out.data_ptr(), pos_out.data_ptr()
         stream = _raw_stream(self._index)
-        _check(self._lib.asr_spec_paged_evict(self._ref, ctypes.byref(s), lens.data_ptr(), seen.data_ptr(), budget, recent,
-                                              first, lens_out.data_ptr(), self._workspace("evict", stream, n), n, stream),
-               "asr_spec_paged_evict")
+        rc = self._evict(self._ref, _byref(s), lens.data_ptr(), seen.data_ptr(), budget, recent, first, lens_out.data_ptr(),
+                         self._workspace("evict", stream, n), n, stream)
+        if rc:
+            _check(rc, "asr_spec_paged_evict")
         return lens_out, score_out, pos_out
 
     def _evict_layout(self, lens, score, pos, seen, budget, recent, first, lens_out, score_out, pos_out):
@@ -299,8 +298,7 @@ def accept_sampled(target, draft, lens, u, race, *, draft_logits=None, temperatu
     [0, 1) and ``race [B, V]`` standard exponential, float32.  Returns ``(accepted [B], token [B], step [B], prob [B, k])``:
     the drafts accepted, the token drawn after them, the positions to commit and each draft's acceptance probability.
     ``status``: an int32 device tensor that collects ``asrspec.ST_*`` bits."""
-    key = (_layout(target), _layout(draft), _layout(lens), _layout(u), _layout(race), _layout(draft_logits),
-           _layout(status), temperature)
+    key = _layouts(target, draft, lens, u, race, draft_logits, status, temperature)
     known = _accept_layouts.get(key)
     if known is None:
         known = _remember(_accept_layouts, key, _accept_layout(target, draft, lens, u, race, draft_logits, temperature, status))
@@ -314,10 +312,12 @@ def accept_sampled(target, draft, lens, u, race, *, draft_logits=None, temperatu
         x.draft_logits = draft_logits.data_ptr()
     accepted = torch.empty(x.batch, dtype=torch.int32, device=device)
     token, step, prob = torch.empty_like(accepted), torch.empty_like(accepted), torch.empty_like(u)
-    _check(_accept(
-        ctypes.byref(x), draft.data_ptr(), None if lens is None else lens.data_ptr(), u.data_ptr(), race.data_ptr(), race_stride,
+    rc = _accept(
+        _byref(x), draft.data_ptr(), None if lens is None else lens.data_ptr(), u.data_ptr(), race.data_ptr(), race_stride,
         temperature, accepted.data_ptr(), token.data_ptr(), step.data_ptr(), prob.data_ptr(),
-        None if status is None else status.data_ptr(), _raw_stream(index)), "asr_spec_accept_sampled")
+        None if status is None else status.data_ptr(), _raw_stream(index))
+    if rc:
+        _check(rc, "asr_spec_accept_sampled")
     return accepted, token, step, prob
 
 
