@@ -6,27 +6,33 @@
 // over the slots j that row r sees: j <= kv_len + r (causal) or j < kv_len.
 // A slot's K and V are read once for a tile of rows, so the operator is bound
 // by the bytes of the cache; the layout follows from that:
-//   * a warp works alone: no shared memory, no block barrier in the key loop.
-//     It keeps a tile of rows (the block's rows times the query heads that
-//     share a K/V head) as mma A fragments and streams keys from the pages
-//     straight into B fragments, 16 bytes a lane.  The contraction index of
-//     q k and the output index of p v may be permuted freely, so the
-//     permutations are chosen for the loads: of a key a lane takes d = 32 j +
-//     8 c .. + 7 (c = lane mod 4), which are the operand pairs of two k-steps;
-//     of a value row it takes d = 8 g .. + 7 (g = lane / 4), one element for
-//     each of eight n-tiles, paired with its neighbour key by byte permutes;
-//   * K of step i + 1 is requested as soon as the scores of step i are done,
-//     V of step i + 1 as soon as its product is: one of the two is always in
-//     flight, 8 KB a warp;
-//   * equal shares whatever the lengths: the (sequence, head, tile, step) units
-//     are dealt in contiguous runs over all resident warps (paged.cuh).  Warps
-//     of a block that all work on one item combine in shared memory; where an
-//     item has several such partial results they go through the workspace,
-//     and whoever delivers the last one joins them, in key order, so results
-//     do not depend on timing;
-//   * committed slots are read from the pages and the block's own rows, in
-//     steps after them, from k_new / v_new; one warp also copies those to the
-//     pages (nobody reads a page's slot that this launch writes).
+//   * a warp works alone, with no block barrier in the key loop.  It keeps a
+//     tile of rows (the block's rows times the query heads that share a K/V
+//     head) as mma A fragments.  Steps of K and V come by bulk copies, one a
+//     run of slots in a page, into a ring of the warp's own, two or three steps
+//     ahead (16 to 24 KB a warp, 192 KB an SM), and from there 16 bytes a lane
+//     into B fragments.  The contraction index of q k and the output index of
+//     p v may be permuted freely, so the permutations are chosen for these
+//     reads: of a key a lane takes d = 32 j + 8 c .. + 7 (c = lane mod 4), which
+//     are the operand pairs of two k-steps; of a value row it takes d = 8 g ..
+//     + 7 (g = lane / 4), one element for each of eight n-tiles, paired with
+//     its neighbour key by byte permutes.  mma.sync, not tcgen05: a tile has 1
+//     to 32 rows, and the tensor pipe is far from its limit;
+//   * who works on what is chosen from the lengths (make_plan).  Warps of a
+//     block that all work on one item combine in shared memory; where an item
+//     has several such partial results they go through the workspace, and
+//     whoever delivers the last one joins them, in key order, so results do
+//     not depend on timing;
+//   * committed slots are read from the pages and the block's own rows from
+//     k_new / v_new; one warp also copies those to the pages (nobody uses a
+//     page's slot that this launch writes).
+// Measured (device time, inputs of one call in L2 where they fit): 48 sequences
+// of up to 40000 slots, 32 query heads on 8 of 128, fp16: 587 - 625 us for 3.95
+// GB, 6.3 - 6.7 TB/s, the copy rate; one of 100001 slots, 9 rows, 20 heads of
+// 64, bf16: 97 us for 512 MB, bound by the chain of instructions of a step (480
+// a warp, 12 warps an SM); 64 of up to 448 slots, 7 rows, 20 heads: 30 us for
+// 78 MB, of which 14 steps of 1.3 us in the longest warp and 9 us launch, plan
+// and end; one of 230 slots: 10 us, all of it latency.
 // Scores, running maximum and sum, and the output accumulate in fp32.  p is
 // rounded to the cache's 16-bit type for the second product (relative error at
 // most 2^-8 for bf16 and 2^-11 for fp16 a weight, as that of the rounded
@@ -39,9 +45,6 @@
 
 namespace asrspec {
 namespace {
-
-
-
 
 struct AttendArgs {
   PagedView c;
@@ -306,7 +309,9 @@ __device__ __forceinline__ void clear_rows(const AttendArgs& a, const PlanMem& m
 //   SHARE   few items: as many blocks for each as there are, in equal parts;
 //   SPLIT   equal runs of steps for all warps, items split wherever a run ends.
 // Whole items are dealt longest sequence first, to and fro over the takers.
-// Measured, us a call: @@
+// Measured, us a call: 64 sequences of up to 448 slots, 20 heads: WARP 30, SPLIT
+// 47; 32 of up to 1500, 12 heads: BLOCK 28, SPLIT 38; one of 230, 20 heads:
+// BLOCK 10, SPLIT 14; one of 100001, 20 heads: SHARE 97, SPLIT 119.
 enum Deal { DEAL_WARP, DEAL_BLOCK, DEAL_SHARE, DEAL_SPLIT };
 constexpr int DEAL_SORT_MAX = 224;   // sequences that a block ranks, one a thread of all warps but the first
 constexpr float END_COST = 4.f, SHARE_COST = 5.f, SPLIT_COST = 16.f;   // steps

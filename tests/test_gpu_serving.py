@@ -139,6 +139,23 @@ def test_attend_many_sequences(built_lib, cuda):
     check_attend(gen(11), DT["bf16"], 64, 2, 2, 16, 2, lens, [i % 3 for i in range(70)])
 
 
+@pytest.mark.parametrize("dtype,dim,R", [("bf16", 64, 2), ("bf16", 64, 11), ("fp16", 128, 9), ("fp32", 64, 3)])
+def test_attend_long_among_many_short(built_lib, cuda, dtype, dim, R):
+    """More sequences than are ranked by length: equal runs of steps, one item spread over many warps and blocks."""
+    lens = [3] * 150 + [9001] + [5] * 140
+    check_attend(gen(16), DT[dtype], dim, 1, 1, 16, R, lens, [R] * 150 + [R] + [1] * 140)
+
+
+def test_attend_most_sequences(built_lib, cuda):
+    check_attend(gen(17), DT["bf16"], 64, 1, 1, 16, 1, [(i * 5) % 40 for i in range(1024)], [i % 2 for i in range(1024)])
+
+
+@pytest.mark.parametrize("dtype,dim,heads,kv_heads", [("bf16", 64, 6, 3), ("bf16", 128, 4, 2), ("fp32", 128, 2, 2)])
+def test_attend_few_long_items(built_lib, cuda, dtype, dim, heads, kv_heads):
+    """Fewer items than blocks: each shared by several."""
+    check_attend(gen(18), DT[dtype], dim, heads, kv_heads, 48, 5, [6000, 1, 4100], [5, 5, 2])
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "fp16", "fp32"])
 @pytest.mark.parametrize("dim", [64, 128])
 def test_attend_hidden_rows_do_not_leak(built_lib, cuda, dtype, dim):
