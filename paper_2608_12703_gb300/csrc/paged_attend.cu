@@ -29,10 +29,10 @@
 // Measured (device time, inputs of one call in L2 where they fit): 48 sequences
 // of up to 40000 slots, 32 query heads on 8 of 128, fp16: 587 - 625 us for 3.95
 // GB, 6.3 - 6.7 TB/s, the copy rate; one of 100001 slots, 9 rows, 20 heads of
-// 64, bf16: 97 us for 512 MB, bound by the chain of instructions of a step (480
-// a warp, 12 warps an SM); 64 of up to 448 slots, 7 rows, 20 heads: 30 us for
-// 78 MB, of which 14 steps of 1.3 us in the longest warp and 9 us launch, plan
-// and end; one of 230 slots: 10 us, all of it latency.
+// 64, bf16: 97 us for 512 MB, 76 of them the key loop at 6.7 TB/s, the rest
+// launch, plan, uneven ends and the join; 64 of up to 448 slots, 7 rows, 20
+// heads: 30 us for 78 MB, of which 14 steps of 1.3 us in the longest warp and 9
+// us launch, plan and end; one of 230 slots: 10 us, all of it latency.
 // Scores, running maximum and sum, and the output accumulate in fp32.  p is
 // rounded to the cache's 16-bit type for the second product (relative error at
 // most 2^-8 for bf16 and 2^-11 for fp16 a weight, as that of the rounded

@@ -7,7 +7,7 @@
 // not causal) and the query heads h of the K/V head.  It runs after the
 // verification, when the number of committed rows is known, on the lse that
 // the attention left: one pass over K, no join.  Bound by the bytes of K and
-// of the scores; keys are read as in the attention (paged.cuh), each warp a
+// of the scores; keys come from the pages into registers a step ahead, each warp a
 // contiguous run of steps.  Products are exact in fp32 accumulators and all
 // sums are fp32 in a fixed order.
 // Measured: 8 sequences of up to 40000 slots, 32 query heads on 8 of 128, bf16:
