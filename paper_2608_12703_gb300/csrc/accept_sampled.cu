@@ -32,7 +32,6 @@
 namespace asrspec {
 namespace {
 
-constexpr int AS_ROW = 256;       // threads on one row at a time
 constexpr int AS_MAX_K = 31;
 constexpr int AS_ROWS = 2 * AS_MAX_K + 1;
 
@@ -132,10 +131,11 @@ struct Stat {   // max and sum of weights relative to it
   }
 };
 
-// CL blocks a cluster, GROUPS rows at a time in a block.
-template <typename T, int CL, int GROUPS>
-__global__ void __launch_bounds__(AS_ROW * GROUPS, GROUPS == 1 ? 4 : 1) accept_kernel(SampleArgs a) {
-  constexpr int N = Vec16<T>::N, UN = GROUPS == 1 && sizeof(T) == 4 ? 8 : 4, THREADS = AS_ROW * GROUPS, WARPS = THREADS / 32, ROW_WARPS = AS_ROW / 32;
+// CL blocks a cluster, GROUPS rows at a time in a block, ROW threads on each.
+template <typename T, int CL, int GROUPS, int ROW>
+__global__ void __launch_bounds__(ROW * GROUPS, 1024 / (ROW * GROUPS)) accept_kernel(SampleArgs a) {
+  constexpr int N = Vec16<T>::N, UN = (GROUPS == 1 || ROW == 32) && sizeof(T) == 4 ? 8 : 4;
+  constexpr int THREADS = ROW * GROUPS, WARPS = THREADS / 32, ROW_WARPS = ROW / 32;
   __shared__ float2 s_warp[AS_ROWS][ROW_WARPS];          // a warp's part of a row
   __shared__ float2 s_part[AS_ROWS][CL];                 // every block's part of a row
   __shared__ float s_m[AS_ROWS], s_inv[AS_ROWS], s_x[AS_ROWS];   // the row's max, 1 / sum, its draft's logit, then probability
@@ -174,8 +174,8 @@ __global__ void __launch_bounds__(AS_ROW * GROUPS, GROUPS == 1 ? 4 : 1) accept_k
     if (a.draft_logits) s_x[n_draft + 1 + lane] = clean(to_f32(row_ptr(n_draft + 1 + lane)[mine]));
   }
 
-  const int rt = tid % AS_ROW;
-  for (int r = tid / AS_ROW; r < n_rows; r += GROUPS) {
+  const int rt = tid % ROW;
+  for (int r = tid / ROW; r < n_rows; r += GROUPS) {
     const T* x = row_ptr(r);
     // elements before the first 16-byte boundary, whole vectors, rest
     const int head = min(a.V, (int)(((16 - (reinterpret_cast<uintptr_t>(x) & 15)) & 15) / sizeof(T)));
@@ -183,15 +183,15 @@ __global__ void __launch_bounds__(AS_ROW * GROUPS, GROUPS == 1 ? 4 : 1) accept_k
     const int v0 = (int)((long long)nv * part / CL), v1 = (int)((long long)nv * (part + 1) / CL);
     const char* xv = reinterpret_cast<const char*>(x + head);
     Stat s;
-    for (int i = v0 + rt; i < v1; i += AS_ROW * UN) {
+    for (int i = v0 + rt; i < v1; i += ROW * UN) {
       uint4 v[UN];
       float mx = s.m, l = 0.f;
 #pragma unroll
       for (int j = 0; j < UN; ++j)
-        if (i + j * AS_ROW < v1) v[j] = ldg_stream(xv + (long long)(i + j * AS_ROW) * 16);
+        if (i + j * ROW < v1) v[j] = ldg_stream(xv + (long long)(i + j * ROW) * 16);
 #pragma unroll
       for (int j = 0; j < UN; ++j) {
-        if (i + j * AS_ROW >= v1) break;
+        if (i + j * ROW >= v1) break;
         mx = fmaxf(mx, Vec16<T>::top(v[j]));
       }
       if (mx == -INFINITY) continue;
@@ -199,7 +199,7 @@ __global__ void __launch_bounds__(AS_ROW * GROUPS, GROUPS == 1 ? 4 : 1) accept_k
       const uint64_t minus_m = pair(-mx), cc = pair(c);
 #pragma unroll
       for (int j = 0; j < UN; ++j) {
-        if (i + j * AS_ROW >= v1) break;
+        if (i + j * ROW >= v1) break;
         float f[N];
         Vec16<T>::get(v[j], f);
 #pragma unroll
@@ -301,8 +301,9 @@ __global__ void __launch_bounds__(AS_ROW * GROUPS, GROUPS == 1 ? 4 : 1) accept_k
   }
 }
 
-template <auto kernel, int CL, int GROUPS>
+template <typename T, int CL, int GROUPS, int ROW>
 cudaError_t launch_accept(const SampleArgs& a, int B, cudaStream_t st) {
+  constexpr auto kernel = accept_kernel<T, CL, GROUPS, ROW>;
   if constexpr (CL > 8) {   // clusters above 8 are asked for once a device
     static std::atomic<uint64_t> ready{0};
     int dev = 0;
@@ -315,16 +316,23 @@ cudaError_t launch_accept(const SampleArgs& a, int B, cudaStream_t st) {
       ready.fetch_or(bit, std::memory_order_release);
     }
   }
-  return launch_ex(kernel, dim3(CL, B), dim3(AS_ROW * GROUPS), 0, st, false, CL, a);
+  return launch_ex(kernel, dim3(CL, B), dim3(ROW * GROUPS), 0, st, false, CL, a);
 }
 
-// A few utterances cannot fill the GPU: wide clusters of large blocks shorten
-// the chain of reads.  From 16 on, blocks of 256 threads, four an SM, keep
-// every SM busy in one wave.
+// Few utterances: wide clusters of large blocks shorten the chain of reads;
+// then the largest blocks of which all fit the SMs at once (1024 threads an SM).
+// A block's share of a short row keeps a warp busy, not a block: a row a warp.
+// Measured, us (wide clusters below 16 utterances, 256 threads a row before): 15
+// of 10 drafts, bf16, 33 -> 16; 25 of 6, fp32, 22 -> 19; 38 of 14 over 2217
+// tokens, fp32, 33 -> 10.5.
 template <typename T>
 cudaError_t launch_accept_t(const SampleArgs& a, int B, cudaStream_t st) {
-  if (B < 16) return launch_accept<accept_kernel<T, 16, 4>, 16, 4>(a, B, st);
-  return launch_accept<accept_kernel<T, 8, 1>, 8, 1>(a, B, st);
+  const int sms = paged_sm_count();
+  if (a.V <= 8192) return launch_accept<T, 4, 8, 32>(a, B, st);
+  if (B <= 8) return launch_accept<T, 16, 4, 256>(a, B, st);
+  if (B * 8 <= sms) return launch_accept<T, 8, 4, 256>(a, B, st);
+  if (B * 4 <= sms) return launch_accept<T, 8, 2, 256>(a, B, st);
+  return launch_accept<T, 8, 1, 256>(a, B, st);
 }
 
 }  // namespace

@@ -306,7 +306,7 @@ __device__ __forceinline__ void clear_rows(const AttendArgs& a, const PlanMem& m
 // instead.  So, by the lengths at hand and in steps:
 //   WARP    a warp takes whole items;
 //   BLOCK   a block takes whole items, its warps each a part of the steps;
-//   SHARE   few items: as many blocks for each as there are, in equal parts;
+//   SHARE   few items: all blocks, each item's number by its length;
 //   SPLIT   equal runs of steps for all warps, items split wherever a run ends.
 // Whole items are dealt longest sequence first, to and fro over the takers.
 // Measured, us a call: 64 sequences of up to 448 slots, 20 heads: WARP 30, SPLIT
@@ -317,9 +317,16 @@ constexpr int DEAL_SORT_MAX = 224;   // sequences that a block ranks, one a thre
 constexpr float END_COST = 4.f, SHARE_COST = 5.f, SPLIT_COST = 16.f;   // steps
 
 struct DealMem {
-  int *order, *pre;   // [B] sequences by falling length, [B + 1] items before each
+  int *order, *pre;   // [B] sequences by falling length, [B + 1] items before each (SHARE: blocks)
   int items;
 };
+// SHARE: blocks of an item of `steps` out of `units`.  Their sum is no more than
+// there are, and no item has more than shorten it: the join takes an eighth of
+// a step a block.
+__device__ __forceinline__ int blocks_of(int steps, int units, int items, int blocks, int warps) {
+  const int most = 1 + (int)sqrtf(8.f * steps / warps);
+  return min(min(steps, most), 1 + (int)((long long)(blocks - items) * steps / units));
+}
 constexpr size_t deal_bytes(int B) { return B <= DEAL_SORT_MAX ? ((size_t)B * 12 + 4 + 16 + 15) / 16 * 16 : 0; }
 
 // The lengths, the units' prefix sums and the deal, the same in every block.
@@ -379,17 +386,21 @@ __device__ __forceinline__ Deal make_plan(const AttendArgs& a, unsigned char* sm
   plan.workers = max(1, min(plan.units, a.max_workers));
   plan.share = plan.units / plan.workers;
   plan.more = plan.units - plan.share * plan.workers;
-  if (!sort) return DEAL_SPLIT;
   dm.items = s_items;
+  if (!sort) return DEAL_SPLIT;
   const float u = (float)plan.units, n = (float)s_items, longest = (float)s_long;
   const float warps = (float)a.max_workers, blocks = warps / WARPS;
   const float by_warp = fmaxf(longest + END_COST, n <= warps ? 0.f : 1.1f * (u + END_COST * n) / warps);
   const float by_block = fmaxf(longest / WARPS + END_COST + 1.f,
                                n <= blocks ? 0.f : 1.1f * (u / WARPS + (END_COST + 1.f) * n) / blocks);
-  const float by_share = n <= blocks / 2.f ? longest / (WARPS * floorf(blocks / n)) + END_COST + 1.f + SHARE_COST : 1e30f;
+  const int grid = a.max_workers / WARPS;
+  const float by_share = dm.items > 0 && 2 * dm.items <= grid
+                             ? longest / (WARPS * blocks_of(s_long, plan.units, dm.items, grid, WARPS)) + END_COST + 1.f + SHARE_COST
+                             : 1e30f;
   const float split = u / warps + END_COST + SPLIT_COST;
   const float least = fminf(fminf(by_warp, by_block), fminf(by_share, split));
-  if (least == split) return DEAL_SPLIT;
+  const Deal deal = least == split ? DEAL_SPLIT : least == by_warp ? DEAL_WARP : least == by_block ? DEAL_BLOCK : DEAL_SHARE;
+  if (deal == DEAL_SPLIT) return deal;
   if (tid < 32) {
     int base = 0;
     for (int b0 = 0; b0 < B; b0 += 32) {
@@ -397,6 +408,7 @@ __device__ __forceinline__ Deal make_plan(const AttendArgs& a, unsigned char* sm
       if (b0 + lane < B) {
         const SeqWork s = work(dm.order[b0 + lane]);
         x = s.steps ? a.c.kv_heads * s.tiles : 0;
+        if (x && deal == DEAL_SHARE) x *= blocks_of(s.steps, plan.units, dm.items, grid, WARPS);
       }
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
@@ -409,7 +421,7 @@ __device__ __forceinline__ Deal make_plan(const AttendArgs& a, unsigned char* sm
     if (lane == 0) dm.pre[0] = 0;
   }
   __syncthreads();
-  return least == by_warp ? DEAL_WARP : least == by_block ? DEAL_BLOCK : DEAL_SHARE;
+  return deal;
 }
 
 // What the two kernels below share: the plan, the walk over a warp's items and
@@ -437,13 +449,9 @@ __device__ __forceinline__ void attend_items(const AttendArgs& a, F item) {
   if (deal == DEAL_SPLIT && w0 >= plan.workers) return;
   // WARP, BLOCK: taker and takers; consecutive items go to different SMs
   const int takers = deal == DEAL_WARP ? a.max_workers : gridDim.x;
-  int taker = deal == DEAL_WARP ? warp * gridDim.x + blockIdx.x : blockIdx.x;
-  // SHARE: blocks of an item, this one's place among them
-  int share = deal == DEAL_SHARE ? gridDim.x / dm.items : 0, place = 0;
-  if (share) {
-    place = blockIdx.x % share;
-    taker = blockIdx.x / share;
-  }
+  const int taker = deal == DEAL_WARP ? warp * gridDim.x + blockIdx.x : blockIdx.x;
+  const int shares = deal == DEAL_SHARE ? dm.pre[c.batch] : dm.items;   // what dm.pre counts
+  int share = 0, place = 0;   // SHARE: blocks of an item, this one's place among them
   bool team = deal != DEAL_WARP;   // all warps of the block work on one item
   for (int round = 0, at = block0;;) {
     int b, it, u0 = 0, u1 = 0, s0, n, active = WARPS;
@@ -465,16 +473,17 @@ __device__ __forceinline__ void attend_items(const AttendArgs& a, F item) {
       active = w1 - w0;
     } else {
       const int k = round * takers + (round & 1 ? takers - 1 - taker : taker);
-      if (k >= dm.items) return;
+      if (k >= shares) return;
       ++round;
       const int rank = work_find(dm.pre, c.batch, k);
       b = dm.order[rank];
       it = k - dm.pre[rank];
       s = seq_work<KS, TR>(r, mem.lens[b].x, mem.lens[b].y);
       s0 = 0, n = s.steps;
-      if (share) {
-        share = min(share, s.steps);
-        if (place >= share) return;
+      if (deal == DEAL_SHARE) {
+        share = blocks_of(s.steps, plan.units, dm.items, gridDim.x, WARPS);
+        place = it % share;
+        it /= share;
         u0 = (int)blockIdx.x - place;
         s0 = (int)((long long)s.steps * place / share);
         n = (int)((long long)s.steps * (place + 1) / share) - s0;
