@@ -311,7 +311,8 @@ __device__ __forceinline__ void clear_rows(const AttendArgs& a, const PlanMem& m
 // Whole items are dealt longest sequence first, to and fro over the takers.
 // Measured, us a call: 64 sequences of up to 448 slots, 20 heads: WARP 30, SPLIT
 // 47; 32 of up to 1500, 12 heads: BLOCK 28, SPLIT 38; one of 230, 20 heads:
-// BLOCK 10, SPLIT 14; one of 100001, 20 heads: SHARE 97, SPLIT 119.
+// BLOCK 10, SPLIT 14; one of 100001, 20 heads: SHARE 97, SPLIT 119; two of 1 and
+// 35129, 16 heads: SHARE 60, with equal numbers of blocks 113.
 enum Deal { DEAL_WARP, DEAL_BLOCK, DEAL_SHARE, DEAL_SPLIT };
 constexpr int DEAL_SORT_MAX = 224;   // sequences that a block ranks, one a thread of all warps but the first
 constexpr float END_COST = 4.f, SHARE_COST = 5.f, SPLIT_COST = 16.f;   // steps

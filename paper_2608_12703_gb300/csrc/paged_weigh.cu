@@ -14,6 +14,8 @@
 // 78 us for 506 MB, 96 % of the copy rate (four blocks of four warps an SM, 4 KB
 // of K a warp in flight); 64 of up to 448 slots, 7 rows, 20 heads of 64: 11.4 us
 // for 40 MB, launch and latency.
+#include <type_traits>
+
 #include "kernels.h"
 #include "paged.cuh"
 
@@ -218,27 +220,45 @@ __global__ void __launch_bounds__(PW_WARPS * 32) weigh32_kernel(WeighArgs a, int
     float w[IT];
 #pragma unroll
     for (int k = 0; k < IT; ++k) w[k] = 0.f;
-    for (int m = 0; m < s.tiles; ++m) {
-      const int row = m / r.group, hq = kvh * r.group + m - row * r.group;
-      const int lim = r.causal ? s.len + row + 1 : s.paged;
-      const float x = a.lse[b * a.lse_b + row * a.lse_r + hq], ls = x == -INFINITY ? INFINITY : x * LOG2E;
-      float d[IT];
+    // Four rows at a time are independent chains of products and exchanges; one
+    // or two rows would pay for four (one row, 128 wide: 20 us against 25).
+    auto add_rows = [&](auto at_once, int m0) {
+      constexpr int MR = decltype(at_once)::value;
+      float d[MR][IT], ls[MR];
+      int lim[MR];
 #pragma unroll
-      for (int k = 0; k < IT; ++k) d[k] = 0.f;
+      for (int x = 0; x < MR; ++x) {
+        const int m = min(m0 + x, s.tiles - 1), row = (int)r.groups.div((uint32_t)m), hq = kvh * r.group + m - row * r.group;
+        lim[x] = m0 + x < s.tiles ? (r.causal ? s.len + row + 1 : s.paged) : 0;
+        const float y = a.lse[b * a.lse_b + row * a.lse_r + hq];
+        ls[x] = y == -INFINITY ? INFINITY : y * LOG2E;
 #pragma unroll
-      for (int j = 0; j < NC; ++j) {
-        const float4 q = __ldg(reinterpret_cast<const float4*>(r.q + b * r.q_b + row * r.q_r + hq * r.q_h + (e + 8 * j) * 16));
+        for (int k = 0; k < IT; ++k) d[x][k] = 0.f;
 #pragma unroll
-        for (int k = 0; k < IT; ++k) d[k] += (q.x * kf[k][j].x + q.y * kf[k][j].y) + (q.z * kf[k][j].z + q.w * kf[k][j].w);
+        for (int j = 0; j < NC; ++j) {
+          const float4 q =
+              __ldg(reinterpret_cast<const float4*>(r.q + b * r.q_b + row * r.q_r + hq * r.q_h + (e + 8 * j) * 16));
+#pragma unroll
+          for (int k = 0; k < IT; ++k)
+            d[x][k] += (q.x * kf[k][j].x + q.y * kf[k][j].y) + (q.z * kf[k][j].z + q.w * kf[k][j].w);
+        }
       }
 #pragma unroll
-      for (int k = 0; k < IT; ++k) {
-        float v = d[k];
-        v += __shfl_xor_sync(0xffffffffu, v, 1);
-        v += __shfl_xor_sync(0xffffffffu, v, 2);
-        v += __shfl_xor_sync(0xffffffffu, v, 4);
-        if (step * KS + 4 * k + kg < lim) w[k] += ex2(fmaf(v, sc, -ls));
-      }
+      for (int o = 1; o < 8; o <<= 1)
+#pragma unroll
+        for (int x = 0; x < MR; ++x)
+#pragma unroll
+          for (int k = 0; k < IT; ++k) d[x][k] += __shfl_xor_sync(0xffffffffu, d[x][k], o);
+#pragma unroll
+      for (int x = 0; x < MR; ++x)
+#pragma unroll
+        for (int k = 0; k < IT; ++k)
+          if (step * KS + 4 * k + kg < lim[x]) w[k] += ex2(fmaf(d[x][k], sc, -ls[x]));
+    };
+    if (s.tiles > 2) {
+      for (int m0 = 0; m0 < s.tiles; m0 += 4) add_rows(std::integral_constant<int, 4>{}, m0);
+    } else {
+      for (int m0 = 0; m0 < s.tiles; ++m0) add_rows(std::integral_constant<int, 1>{}, m0);
     }
 #pragma unroll
     for (int k = 0; k < IT; ++k)
