@@ -22,6 +22,8 @@
 // Measured: 8 sequences of 30001 to 40000 slots, 8 heads of 128, fp16, cut to
 // 16384: 132 us, of which 30 are search and lists and the rest 557 MB of moves;
 // 64 of 200 to 448 slots, 20 heads of 64, bf16, cut to 256: 16 us.
+#include <atomic>
+
 #include "kernels.h"
 #include "paged.cuh"
 
@@ -29,7 +31,8 @@ namespace asrspec {
 namespace {
 
 constexpr int EV_MAX_CLUSTER = 8;
-constexpr int EV_KEYS = 8192;    // slots whose rank a block keeps in shared memory; past them it is taken anew
+// Slots whose rank a block keeps in shared memory; past them it is taken anew.
+constexpr int EV_KEYS = 8192, EV_KEYS_LARGE = 40960;
 
 struct EvictArgs {
   PagedView c;
@@ -297,6 +300,21 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) evict_kernel(EvictArg
   }
 }
 
+// The shared memory above 48 KB of the large blocks, asked for once a device.
+cudaError_t allow_large_keys() {
+  static std::atomic<uint64_t> ready{0};
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  const uint64_t bit = 1ull << (dev & 63);
+  if (!(ready.load(std::memory_order_acquire) & bit)) {
+    e = cudaFuncSetAttribute(evict_kernel<1024>, cudaFuncAttributeMaxDynamicSharedMemorySize, EV_KEYS_LARGE * 4);
+    if (e != cudaSuccess) return e;
+    ready.fetch_or(bit, std::memory_order_release);
+  }
+  return cudaSuccess;
+}
+
 }  // namespace
 }  // namespace asrspec
 
@@ -364,7 +382,13 @@ int asr_spec_paged_evict(const asr_paged_cache* c, const asr_paged_scores* s, co
   const dim3 grid(cluster, c->kv_heads, c->batch);
   cudaError_t e;
   // Few slots a block: smaller blocks, so that more heads share an SM and hide one another's passes.
-  if (part <= 512) e = launch_ex(evict_kernel<128>, grid, dim3(128), a.keys * 4, st, false, cluster, a);
+  // Many slots and no more blocks than SMs: large blocks, which have an SM's shared memory to themselves
+  // (12 heads of up to 120000 slots: 189 us with blocks of 256, 63 with these).
+  if (part > 4096 && tasks * cluster <= paged_sm_count()) {
+    a.keys = part < EV_KEYS_LARGE ? part : EV_KEYS_LARGE;
+    e = allow_large_keys();
+    if (e == cudaSuccess) e = launch_ex(evict_kernel<1024>, grid, dim3(1024), a.keys * 4, st, false, cluster, a);
+  } else if (part <= 512) e = launch_ex(evict_kernel<128>, grid, dim3(128), a.keys * 4, st, false, cluster, a);
   else e = launch_ex(evict_kernel<256>, grid, dim3(256), a.keys * 4, st, false, cluster, a);
   if (e == cudaSuccess && in_place) e = cudaMemcpyAsync(len_out, a.len_out, c->batch * 4, cudaMemcpyDeviceToDevice, st);
   return e == cudaSuccess ? ASR_OK : ASR_E_CUDA;

@@ -575,3 +575,12 @@ def test_refusals(built_lib, cuda):
     refused(lambda: S(*x[:4], x[4][:, :8]))
     refused(lambda: S(z(2, 34, 9, dt=torch.float32), *x[1:]))
     assert c.status() == 0
+
+
+def test_evict_longest_heads(built_lib, cuda):
+    """More slots a block than one of ordinary size keeps ranks of; and, of the same lengths, more than any keeps."""
+    g = gen(44)
+    for n, budget in ((70001, 30000), (330003, 329000)):
+        score = torch.empty((1, 1, n), device="cuda").log_normal_(generator=g)
+        pos = torch.arange(n, device="cuda", dtype=torch.int32).view(1, 1, n).contiguous()
+        check_evict(g, torch.bfloat16, 1, 64, 1024, [n], budget, 64, 4, score, pos, [n])
