@@ -162,6 +162,7 @@ __global__ void __launch_bounds__(ROW * GROUPS, 1024 / (ROW * GROUPS)) accept_ke
     }
     return;
   }
+  cluster_arrive_relaxed();   // this block runs; whether the others do is waited for before anything is stored to them
   // rows: target 0 .. n_draft, then draft 0 .. n_draft - 1
   const int n_rows = n_draft + 1 + (a.draft_logits ? n_draft : 0);
   auto row_ptr = [&](int r) {
@@ -217,6 +218,7 @@ __global__ void __launch_bounds__(ROW * GROUPS, 1024 / (ROW * GROUPS)) accept_ke
     if (lane == 0) s_warp[r][rt >> 5] = make_float2(m, l);
   }
   __syncthreads();
+  cluster_wait();
   for (int x = tid; x < n_rows * CL; x += THREADS) {   // this block's part of every row to every block
     const int r = x / CL, to = x - r * CL;
     Stat s;
