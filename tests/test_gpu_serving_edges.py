@@ -23,3 +23,74 @@ def test_accept_shortest_rows(built_lib, cuda, dtype, B, V):
     for _ in range(50):
         got = serving.accept_sampled(t, d, n, u, r, draft_logits=q)
         assert all(torch.equal(a, b) for a, b in zip(want, got))
+
+
+@pytest.mark.parametrize("dim,R,G,n", [(64, 1, 1, 40000), (64, 3, 1, 40000), (64, 5, 4, 20000), (128, 1, 4, 40000), (128, 3, 4, 20000)])
+def test_attend_long_tail_of_small_weights(built_lib, cuda, dim, R, G, n):
+    """One strong key with a value of 0, and n keys of 2^-24 to 2^-27 of its weight with values of 1: their sum is the output."""
+    from paper_2608_12703_gb300 import serving
+    g = gen(71)
+    k, v, table = pool(g, torch.float16, 1, dim, 256, [n + R])
+    k.zero_()
+    v.fill_(1.0)
+    # slot 7 is the strong one: its score is 0, the others' -8 t with t in steps of 2^-6, exact in every type
+    t = torch.randint(133, 150, (k.shape[0], 256), generator=g, device="cuda") / 64.0      # -8 t / ln 2: 2^-24.0 .. 2^-26.9
+    k[:, 0, :, 0] = -t.half()
+    at = (int(table[0, 0]), 0, 7)
+    k[at], v[at] = 0.0, 0.0
+    q = torch.zeros((1, R, G, dim), dtype=torch.float16, device="cuda")
+    q[..., 0] = 8.0
+    out, lse = serving.PagedCache(k, v, table).attend(q, i32([n]), scale=1.0)
+    x = -8.0 * t[table[0].long()].double().reshape(-1)
+    x[7] = 0.0
+    for i in range(R):
+        w = torch.exp(x[:n + i + 1])
+        want, l = float((w.sum() - w[7]) / w.sum()), float(torch.log(w.sum()))
+        # rounding of a weight and of the output to fp16, of exp2 and its argument, of a sum at every 16 keys
+        rel = 2 * 2.0 ** -11 + 2.0 ** -20 * (1 + 19) + n / 16 * 2.0 ** -23
+        assert float((out[0, i].double() - want).abs().max()) <= rel * want
+        assert float((lse[0, i].double() - l).abs().max()) <= 2.0 ** -20 * (1 + 19)
+
+
+@pytest.mark.parametrize("dim,kv_heads,B", [(64, 32, 60), (128, 16, 90)])
+def test_attend_tail_of_small_weights_walked_by_one_warp(built_lib, cuda, dim, kv_heads, B):
+    """The same with so many heads that nobody splits one: every weight is taken relative to the strong key's."""
+    from paper_2608_12703_gb300 import serving
+    g = gen(80)
+    n, page = 1999, 400
+    k, v, table = pool(g, torch.float16, kv_heads, dim, page, [n + 1] * B)
+    k.zero_()
+    v.fill_(64.0)
+    t = torch.randint(133, 150, (k.shape[0], page), generator=g, device="cuda") / 64.0
+    k[:, :, :, 0] = -t.half()[:, None, :]
+    first = table[:, 0].long()
+    k[first, :, 7], v[first, :, 7] = 0.0, 0.0
+    q = torch.zeros((B, 1, kv_heads, dim), dtype=torch.float16, device="cuda")
+    q[..., 0] = 8.0
+    out, _ = serving.PagedCache(k, v, table).attend(q, i32([n] * B), scale=1.0)
+    x = -8.0 * t[table.long()].double().reshape(B, n + 1)
+    x[:, 7] = 0.0
+    w = torch.exp(x)
+    want = (64.0 * (w.sum(1) - w[:, 7]) / w.sum(1))[:, None, None, None]
+    rel = 2 * 2.0 ** -11 + 2.0 ** -20 * (1 + 19) + n / 16 * 2.0 ** -23
+    assert bool(((out.double() - want).abs() <= rel * want).all())
+
+
+def test_attend_fp16_large_scores(built_lib, cuda):
+    """Scores whose rounding is several powers of two: the weights stay in fp16's range, the strongest keys share the output."""
+    from paper_2608_12703_gb300 import serving
+    g = gen(72)
+    k, v, table = pool(g, torch.float16, 2, 64, 16, [70])
+    k.zero_()
+    v.copy_(torch.randn(v.shape, generator=g, device="cuda"))
+    k[:, :, :, 0] = -1.0
+    for s in (3, 33, 64):       # the same largest score, about 2^35.5
+        k[int(table[0, s // 16]), :, s % 16] = 60000.0
+    q = torch.full((1, 2, 2, 64), 60000.0, dtype=torch.float16, device="cuda")
+    q[:, :, 1] = 59968.0
+    out, lse = serving.PagedCache(k, v, table).attend(q, i32([68]))
+    vv = ref.slots(v, table[0], 70)
+    want = vv[[3, 33, 64]].mean(0)[None, None].expand(1, 2, 2, 64)
+    bound = 3 * 2.0 ** -11 * vv[[3, 33, 64]].abs().sum(0) + 2.0 ** -20
+    assert bool(torch.isfinite(out).all()) and bool(torch.isfinite(lse).all())
+    assert bool(((out.double() - want).abs() <= bound).all())
