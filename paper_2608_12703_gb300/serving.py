@@ -11,15 +11,16 @@ page ids, token ids) is checked by the kernels, which set the status word read
 by ``PagedCache.status``.
 
 A small call's kernels take less time than the checks of its arguments, so a
-call whose tensors have the layouts (shape, strides, type, device) of an
-earlier one goes by that call's checks: layouts are what the checks look at,
-and addresses, the only other thing, are checked by the library.  A captured
-graph needs the cache object that it was captured with.
+call whose tensors have the layouts (shape, strides, type, device) and whose
+numbers have the values of an earlier one goes by that call's checks: these are
+what the checks look at, and addresses, the only other thing, are checked by
+the library.  A captured graph needs the cache object that it was captured with.
 """
 from __future__ import annotations
 
 import ctypes
 import math
+import operator
 from typing import Optional
 
 import torch
@@ -39,8 +40,23 @@ def _need(ok: bool, what: str):
         raise A.AsrSpecError("ASR_E_INVAL " + what)
 
 
+def _number(x, name) -> float:
+    """The value of a number, of a tensor's only element too (which waits for its device)."""
+    try:
+        return float(x + 0.0)
+    except (TypeError, ValueError, RuntimeError):
+        raise A.AsrSpecError(f"ASR_E_INVAL {name}: a number is required") from None
+
+
+def _integer(x, name) -> int:
+    try:
+        return operator.index(x)
+    except (TypeError, ValueError, RuntimeError):
+        raise A.AsrSpecError(f"ASR_E_INVAL {name}: a whole number is required") from None
+
+
 def _layouts(*args):
-    """The layouts of a call's tensors, other arguments as they are."""
+    """The layouts of a call's tensors, other arguments (numbers by value) as they are."""
     return tuple([(x.shape, x.stride(), x.dtype, x.get_device()) if isinstance(x, torch.Tensor) else x for x in args])
 
 
@@ -146,7 +162,7 @@ class PagedCache:
             ns = k_new.stride()[:3]
         s = q.stride()
         return A.AsrPagedRows(q.data_ptr(), s[0], s[1], s[2], A.addr(k_new), A.addr(v_new), *ns, kv_len.data_ptr(),
-                              A.addr(rows), R, H, int(bool(causal)), 1.0 / math.sqrt(D) if scale is None else scale)
+                              A.addr(rows), R, H, int(causal), 1.0 / math.sqrt(D) if scale is None else scale)
 
     @staticmethod
     def _rows_at(layout, q, kv_len, rows, k_new, v_new):
@@ -168,6 +184,9 @@ class PagedCache:
             with torch.cuda.device(self.device):
                 return self.attend(q, kv_len, k_new=k_new, v_new=v_new, rows=rows, causal=causal, scale=scale, out=out,
                                    lse=lse)
+        causal = bool(causal)
+        if scale is not None:
+            scale = _number(scale, "scale")
         key = _layouts(q, kv_len, k_new, v_new, rows, causal, scale, out, lse)
         known = self._attend_layouts.get(key)
         if known is None:
@@ -201,6 +220,9 @@ class PagedCache:
                 return self.weigh(q, lse, kv_len, score, rows=rows, causal=causal, scale=scale, out=out, pos=pos,
                                   first_pos=first_pos)
         out = score if out is None else out
+        causal = bool(causal)
+        if scale is not None:
+            scale = _number(scale, "scale")
         key = _layouts(q, kv_len, rows, causal, scale, lse, score, out, pos, first_pos)
         known = self._weigh_layouts.get(key)
         if known is None:
@@ -251,6 +273,7 @@ class PagedCache:
                                   score_out=score_out, pos_out=pos_out)
         score_out = score if score_out is None else score_out
         pos_out = pos if pos_out is None else pos_out
+        budget, recent, first = _integer(budget, "budget"), _integer(recent, "recent"), _integer(first, "first")
         key = _layouts(lens, score, pos, seen, budget, recent, first, lens_out, score_out, pos_out)
         known = self._evict_layouts.get(key)
         if known is None:
@@ -298,6 +321,7 @@ def accept_sampled(target, draft, lens, u, race, *, draft_logits=None, temperatu
     [0, 1) and ``race [B, V]`` standard exponential, float32.  Returns ``(accepted [B], token [B], step [B], prob [B, k])``:
     the drafts accepted, the token drawn after them, the positions to commit and each draft's acceptance probability.
     ``status``: an int32 device tensor that collects ``asrspec.ST_*`` bits."""
+    temperature = _number(temperature, "temperature")
     key = _layouts(target, draft, lens, u, race, draft_logits, status, temperature)
     known = _accept_layouts.get(key)
     if known is None:

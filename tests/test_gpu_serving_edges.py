@@ -94,3 +94,44 @@ def test_attend_fp16_large_scores(built_lib, cuda):
     bound = 3 * 2.0 ** -11 * vv[[3, 33, 64]].abs().sum(0) + 2.0 ** -20
     assert bool(torch.isfinite(out).all()) and bool(torch.isfinite(lse).all())
     assert bool(((out.double() - want).abs() <= bound).all())
+
+
+def test_numbers_given_as_tensors(built_lib, cuda):
+    """A scale, causal flag, budget or temperature in a tensor is its value at the call, whatever an earlier call's was."""
+    from paper_2608_12703_gb300 import serving
+    g = gen(73)
+    k, v, table = pool(g, torch.bfloat16, 2, 64, 16, [60, 60])
+    fill(g, k, table, [60, 60])
+    fill(g, v, table, [60, 60])
+    q = torch.randn((2, 2, 4, 64), generator=g, device="cuda").bfloat16()
+    n = i32([50, 33])
+    c = serving.PagedCache(k, v, table)
+    score = torch.rand((2, 2, 64), generator=g, device="cuda")
+    fresh = lambda: serving.PagedCache(k.clone(), v.clone(), table)
+    for scale in (0.5, 2.0, 0.125):
+        for causal in (True, False):
+            want, wl = fresh().attend(q, n, scale=scale, causal=causal)
+            got, gl = c.attend(q, n, scale=torch.tensor(scale), causal=torch.tensor(causal))
+            assert same_bits(got, want) and same_bits(gl, wl)
+            ws = fresh().weigh(q, wl, n, score, scale=scale, causal=causal, out=torch.zeros_like(score))
+            gs = c.weigh(q, wl, n, score, scale=torch.tensor(scale), causal=torch.tensor(causal), out=torch.zeros_like(score))
+            assert torch.equal(gs, ws)
+    pos = torch.arange(64, dtype=torch.int32, device="cuda").repeat(2, 2, 1).contiguous()
+    for budget in (2, 30, 8):
+        for recent in (0, 1):
+            want = fresh().evict(n, score.clone(), pos.clone(), n, budget=budget, recent=recent)
+            got = fresh_one(c, k, v).evict(n, score.clone(), pos.clone(), n, budget=torch.tensor(budget), recent=torch.tensor(recent))
+            assert torch.equal(got[0], want[0])
+            assert torch.equal(got[1][:, :, :budget], want[1][:, :, :budget]) and torch.equal(got[2][:, :, :budget], want[2][:, :, :budget])
+    t, d, m, u, r, ql = make_accept(74, torch.float32, 4, 2, 100, True, 1.0)
+    for temperature in (0.3, 2.0):
+        want = serving.accept_sampled(t, d, m, u, r, draft_logits=ql, temperature=temperature)
+        got = serving.accept_sampled(t, d, m, u, r, draft_logits=ql, temperature=torch.tensor(temperature))
+        assert all(torch.equal(x, y) for x, y in zip(want, got))
+
+
+def fresh_one(c, k, v):
+    """The same cache object: its pages as they were, what it remembers kept."""
+    c.k_pages.copy_(k)
+    c.v_pages.copy_(v)
+    return c
