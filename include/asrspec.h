@@ -514,7 +514,8 @@ int asr_spec_paged_weigh(const asr_paged_cache* cache, const asr_paged_rows* row
  * budget are left as they are.
  * Data errors: len outside [0, slots] or the table, or more slots left than
  * slots_out (ASR_ST_CAPACITY): that sequence stays as it is, len_out = len; a
- * bad page id (ASR_ST_BOUNDS): the slot is not moved.
+ * bad page id (ASR_ST_BOUNDS) of either slot of a move: nothing of it is moved,
+ * and the slot below the budget keeps its own K, V, score and position.
  * ws: asr_spec_paged_evict_ws bytes, no initial contents. */
 int64_t asr_spec_paged_evict_ws(const asr_paged_cache* cache, const asr_paged_scores* scores, int32_t budget);
 int asr_spec_paged_evict(const asr_paged_cache* cache, const asr_paged_scores* scores, const int32_t* len,

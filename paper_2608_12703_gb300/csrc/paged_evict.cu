@@ -271,8 +271,10 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) evict_kernel(EvictArg
       const long long head = h * a.c.head_stride;
       s_to[tid] = tp * a.c.page_stride + (to % a.c.page_size) * a.c.slot_stride + head;
       s_of[tid] = ok ? fp * a.c.page_stride + (of % a.c.page_size) * a.c.slot_stride + head : -1;
-      so[to] = sc[of];
-      po[to] = ps[of];
+      if (ok) {   // else the slot keeps its own
+        so[to] = sc[of];
+        po[to] = ps[of];
+      }
     }
     __syncthreads();
     const int m = min(THREADS, moves - j0);

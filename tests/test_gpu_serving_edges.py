@@ -135,3 +135,41 @@ def fresh_one(c, k, v):
     c.k_pages.copy_(k)
     c.v_pages.copy_(v)
     return c
+
+
+@pytest.mark.parametrize("inplace", [False, True])
+@pytest.mark.parametrize("side", ["source", "destination"])
+def test_evict_bad_page(built_lib, cuda, inplace, side):
+    """A slot whose page id, or whose destination's, is out of range is not moved: not its K and V, score or position."""
+    from paper_2608_12703_gb300 import serving
+    g = gen(75)
+    n, budget, page = 96, 40, 16
+    k, v, table = pool(g, torch.bfloat16, 2, 64, page, [n, n])
+    fill(g, k, table, [n, n])
+    fill(g, v, table, [n, n])
+    score = torch.rand((2, 2, n), generator=g, device="cuda")
+    pos = torch.stack([torch.randperm(n, generator=g, device="cuda") for _ in range(4)]).view(2, 2, n).to(torch.int32)
+    bad = table.clone()
+    broken = 3 if side == "source" else 1          # slots 48 .. 63, or 16 .. 31, of the second sequence
+    bad[1, broken] = k.shape[0] if side == "source" else -1
+    k0, v0, s0, p0 = k.clone(), v.clone(), score.clone(), pos.clone()
+    c = serving.PagedCache(k, v, bad)
+    outs = {} if inplace else dict(score_out=torch.full((2, 2, budget), -5.0, device="cuda"),
+                                   pos_out=torch.full((2, 2, budget), -5, dtype=torch.int32, device="cuda"))
+    lens, so, po = c.evict(i32([n, n]), score, pos, i32([n, n]), budget=budget, **outs)
+    assert c.status() == A.ST_BOUNDS and lens.tolist() == [budget, budget]
+    plan = ref.evict([n, n], s0.cpu(), p0.cpu(), [n, n], budget, 0, 0)
+    stuck = 0
+    for b in range(2):
+        for h in range(2):
+            order = list(plan[b][h])
+            for to, of in enumerate(order):
+                if b == 1 and to != of and (to if side == "destination" else of) // page == broken:
+                    order[to] = to
+                    stuck += 1
+            idx = torch.tensor(order, device="cuda")
+            assert torch.equal(so[b, h, :budget], s0[b, h][idx]) and torch.equal(po[b, h, :budget], p0[b, h][idx])
+            for new, old in ((k, k0), (v, v0)):
+                a, o = ref.slots(new, table[b], n)[:, h], ref.slots(old, table[b], n)[:, h]
+                assert torch.equal(a[:budget], o[idx]) and torch.equal(a[budget:], o[budget:])
+    assert stuck > 0
