@@ -21,6 +21,7 @@ from __future__ import annotations
 import ctypes
 import math
 import operator
+import threading
 from typing import Optional
 
 import torch
@@ -120,7 +121,7 @@ class PagedCache:
         self._attend, self._weigh, self._evict = (self._lib.asr_spec_paged_attend, self._lib.asr_spec_paged_weigh,
                                                   self._lib.asr_spec_paged_evict)
         self._attend_layouts, self._weigh_layouts, self._evict_layouts = {}, {}, {}
-        self._ws = {}
+        self._ws, self._lock = {}, threading.Lock()
 
     def status(self) -> int:
         """Wait for the device, then return and clear the status word."""
@@ -130,15 +131,19 @@ class PagedCache:
             self._status.zero_()
         return s
 
-    def _workspace(self, op: str, stream: int, n: int) -> int:
-        """Address of ``n`` bytes, zero at first, that only this operator's calls on this stream use; a capture gets
-        bytes of its graph's own."""
-        ws = None if _capturing() else self._ws.get((op, stream))
+    def _workspace(self, op: str, stream: int, n: int) -> torch.Tensor:
+        """``n`` bytes, zero at first, that only this operator's calls on this stream use; a capture gets bytes of its
+        graph's own.  The caller holds the tensor until it has launched: another host thread's larger call on the stream may
+        replace it here."""
+        if _capturing():
+            return torch.zeros(n, dtype=torch.uint8, device=self.device)
+        ws = self._ws.get((op, stream))
         if ws is None or ws.numel() < n:
-            ws = torch.zeros(n, dtype=torch.uint8, device=self.device)
-            if not _capturing():
-                self._ws[(op, stream)] = ws
-        return ws.data_ptr()
+            with self._lock:
+                ws = self._ws.get((op, stream))
+                if ws is None or ws.numel() < n:
+                    ws = self._ws[(op, stream)] = torch.zeros(n, dtype=torch.uint8, device=self.device)
+        return ws
 
     def _rows(self, q, kv_len, rows, k_new, v_new, causal, scale):
         B, K, D = self.batch, self.kv_heads, self.head_dim
@@ -204,7 +209,8 @@ class PagedCache:
         if lse is None:
             lse = torch.empty(lse_shape, dtype=torch.float32, device=self.device)
         stream = _raw_stream(self._index)
-        rc = self._attend(self._ref, _byref(r), out.data_ptr(), lse.data_ptr(), self._workspace("attend", stream, n), n, stream)
+        ws = self._workspace("attend", stream, n)
+        rc = self._attend(self._ref, _byref(r), out.data_ptr(), lse.data_ptr(), ws.data_ptr(), n, stream)
         if rc:
             _check(rc, "asr_spec_paged_attend")
         return out, lse
@@ -285,8 +291,9 @@ class PagedCache:
         s = A.AsrPagedScores.from_buffer_copy(slots)
         s.score, s.pos, s.score_out, s.pos_out = score.data_ptr(), pos.data_ptr(), score_out.data_ptr(), pos_out.data_ptr()
         stream = _raw_stream(self._index)
+        ws = self._workspace("evict", stream, n)
         rc = self._evict(self._ref, _byref(s), lens.data_ptr(), seen.data_ptr(), budget, recent, first, lens_out.data_ptr(),
-                         self._workspace("evict", stream, n), n, stream)
+                         ws.data_ptr(), n, stream)
         if rc:
             _check(rc, "asr_spec_paged_evict")
         return lens_out, score_out, pos_out

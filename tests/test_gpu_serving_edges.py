@@ -173,3 +173,31 @@ def test_evict_bad_page(built_lib, cuda, inplace, side):
                 a, o = ref.slots(new, table[b], n)[:, h], ref.slots(old, table[b], n)[:, h]
                 assert torch.equal(a[:budget], o[idx]) and torch.equal(a[budget:], o[budget:])
     assert stuck > 0
+
+
+def test_host_threads_share_a_cache(built_lib, cuda):
+    """Threads that call one cache on one stream with growing sizes: every result as a cache of its own gives it."""
+    import threading
+    from paper_2608_12703_gb300 import serving
+    g = gen(81)
+    k, v, table = pool(g, torch.bfloat16, 2, 64, 16, [3000, 2900])
+    fill(g, k, table, [3000, 2900])
+    fill(g, v, table, [3000, 2900])
+    n = i32([2900, 2800])
+    qs = [torch.randn((2, r, 2 * h, 64), generator=g, device="cuda").bfloat16() for r, h in ((1, 1), (4, 2), (9, 1), (9, 4))]
+    want = [serving.PagedCache(k, v, table).attend(q, n) for q in qs]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        c = serving.PagedCache(k, v, table)
+        got, start = [[] for _ in qs], threading.Barrier(len(qs))
+
+        def work(i):
+            start.wait()
+            for _ in range(20):
+                got[i].append(c.attend(qs[i], n))
+        threads = [threading.Thread(target=work, args=(i,)) for i in range(len(qs))]
+        [t.start() for t in threads]
+        [t.join() for t in threads]
+        assert all(len(x) == 20 for x in got) and c.status() == 0
+        for x, (out, lse) in zip(got, want):
+            assert all(same_bits(a, out) and same_bits(b, lse) for a, b in x)

@@ -29,3 +29,48 @@ def test_no_remote_shared_memory_before_the_cluster_has_started(file, name, body
     first = re.search(r"\bdsmem_addr\(|\b(?:ld|st)_cluster\(", body).start()
     barrier = re.search(r"\bcluster_(?:sync|wait)\(\)", body)
     assert barrier and barrier.start() < first
+
+
+def test_workspace_lives_through_its_launch(monkeypatch):
+    """A call on the same stream from another host thread, between this call's look-up of the workspace and its launch, may
+    replace the workspace; the one that this call launches with stays."""
+    import gc
+    import threading
+    import types
+    import weakref
+
+    import torch
+    from paper_2608_12703_gb300 import serving
+
+    made, alive = [], []
+    zeros = torch.zeros
+
+    def tracked(*a, **kw):
+        x = zeros(*a, **kw)
+        made.append((x.data_ptr(), weakref.ref(x)))
+        return x
+
+    monkeypatch.setattr(torch, "zeros", tracked)
+    monkeypatch.setattr(serving, "_capturing", lambda: False)
+    monkeypatch.setattr(serving, "_current_device", lambda: 0)
+    monkeypatch.setattr(serving, "_raw_stream", lambda device: 7)
+    monkeypatch.setattr(serving.PagedCache, "_rows", lambda self, q, *a: serving.A.AsrPagedRows())
+    c = object.__new__(serving.PagedCache)
+    c.device, c.dtype, c._index, c._ref, c._ws = torch.device("cpu"), torch.float32, 0, None, {}
+    c._lock, c._attend_layouts = threading.Lock(), {}
+    c._lib = types.SimpleNamespace(asr_spec_paged_attend_ws=lambda cache, rows: 64 * len(calls))
+    calls = [0]
+    n = zeros(1, dtype=torch.int32)
+
+    def launch(cache, rows, out, lse, ws, size, stream):
+        if len(calls) < 4:              # another thread's call comes first, and needs more
+            calls.append(0)
+            c.attend(zeros(1, len(calls), 2, 64), n)
+            gc.collect()
+        at = [ref for ptr, ref in made if ptr == ws and ref() is not None]
+        alive.append(len(at) == 1 and at[0]().numel() >= size)
+        return 0
+
+    c._attend = launch
+    c.attend(zeros(1, 1, 2, 64), n)
+    assert alive == [True] * 4
