@@ -539,7 +539,8 @@ typedef struct {
  * token[b] = argmax_j w_j / race[b][j] (lowest id on ties) with w = max(0, p_n
  * - q_n) after a rejection and w = p_n after none: with race drawn from the
  * standard exponential distribution and u from [0, 1), accepted drafts and
- * token are distributed as the target's own samples.  Where w has no positive
+ * token are distributed as the target's own samples.  p_n - q_n counts as 0
+ * where it is 2^-18 p_n or less, the rounding of the two.  Where w has no positive
  * entry, w = p_n; where p_n has none either (every logit masked), token = -1.
  * step[b] = n + 1, the positions to commit; 0 where there is no token.
  * prob[b][i] = min(1, p_i(x_i) / q_i(x_i)) for i < lens[b], else 0.

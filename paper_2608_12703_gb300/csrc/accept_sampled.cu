@@ -34,6 +34,11 @@ namespace {
 
 constexpr int AS_MAX_K = 31;
 constexpr int AS_ROWS = 2 * AS_MAX_K + 1;
+// A residual p - q of no more than this part of p is the rounding of p and q:
+// equal rows that are aligned differently add up in different orders, and their
+// sums differ by some 2^-22.  It counts as 0, so that p = q leaves nothing to
+// draw from; what a true residual of that size weighs is 2^-18 of the tokens at most.
+constexpr float NO_RESIDUAL = 1.f / (1 << 18);
 
 struct SampleArgs {
   const char *target, *draft_logits;         // draft_logits may be null
@@ -276,8 +281,8 @@ __global__ void __launch_bounds__(ROW * GROUPS, 1024 / (ROW * GROUPS)) accept_ke
         const int j = min(jj + y * THREADS, j1 - 1);
         float w = weight(clean(p[y]), pm, c) * pi;
         if (residual) {
-          w -= weight(clean(q[y]), qm, c) * qi;
-          if (j == gone) w = 0.f;
+          const float rest = __fsub_rn(w, __fmul_rn(weight(clean(q[y]), qm, c), qi));
+          w = j != gone && rest > w * NO_RESIDUAL ? rest : 0.f;
         }
         // A quotient is off by 2 ulp at most: as good as w itself.
         const float v = __fdividef(w, ej[y]);

@@ -201,3 +201,16 @@ def test_host_threads_share_a_cache(built_lib, cuda):
         assert all(len(x) == 20 for x in got) and c.status() == 0
         for x, (out, lse) in zip(got, want):
             assert all(same_bits(a, out) and same_bits(b, lse) for a, b in x)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("B,V", [(6, 51866), (20, 51865), (70, 51865), (9, 1003), (5, 8), (3, 300001)])
+def test_accept_residual_of_equal_rows(built_lib, cuda, dtype, B, V):
+    """Where p = q nothing is left of p - q: after a rejection (a drafted token masked in both) the token is drawn from p,
+    whatever the rows' alignment."""
+    t, _, _, u, r, _ = make_accept(76 + B, DT[dtype], B, 2, V, False, 0.8)
+    d = torch.full((B, 2), V // 2, dtype=torch.int32, device="cuda")
+    t[:, :, V // 2] = -math.inf
+    x = (t, d, i32([2] * B), u, r, t[:, :2].contiguous())
+    acc, tok, step, _ = check_accept(*x, 0.8)
+    assert bool((acc == 0).all()) and bool((step == 1).all()) and bool((tok != V // 2).all())
