@@ -505,8 +505,9 @@ int asr_spec_paged_weigh(const asr_paged_cache* cache, const asr_paged_rows* row
 
 /* Cut every (sequence, K/V head) to `budget` slots.  Where len[b] > budget the
  * slots that stay are those of highest rank: first the protected ones (pos >=
- * seen[b] - recent, or pos < first; seen = tokens seen so far), then by score,
- * equal scores by lowest slot (NaN last).  The j-th freed slot below the
+ * seen[b] - recent, or pos < first; seen = tokens seen so far), all alike,
+ * whatever their scores, then the others by score (NaN last); equals by lowest
+ * slot, also among more protected ones than the budget holds.  The j-th freed slot below the
  * budget takes K, V, score and position of the j-th kept slot at or past it;
  * other kept slots stay in place.  len_out[b] = min(len[b], budget); may be
  * len itself.  score_out / pos_out receive the entries of the slots in use.

@@ -2,8 +2,8 @@
 //
 // Per (sequence, K/V head) with more than `budget` slots in use, the budget
 // slots of highest rank stay: protected slots first (one of the `recent`
-// newest positions, or of the `first` oldest), then by score, equal scores by
-// lowest slot; a NaN score ranks lowest.  A cached key carries its position in
+// newest positions, or of the `first` oldest), all alike, then the others by
+// score, a NaN lowest; equals by lowest slot.  A cached key carries its position in
 // itself, so the slots' order is free: the j-th freed slot below the budget
 // takes the j-th kept slot at or past it.  Sources and destinations are
 // disjoint, so the moves run in any order over the whole GPU and move the

@@ -270,7 +270,8 @@ class PagedCache:
     def evict(self, lens, score, pos, seen, *, budget: int, recent: int = 0, first: int = 0, lens_out=None, score_out=None,
               pos_out=None):
         """Cut every head to its ``budget`` slots of highest accumulated weight; the ``recent`` newest positions
-        (of ``seen`` ``[B]`` tokens) and the ``first`` oldest go last.  Freed slots below the budget take the kept ones
+        (of ``seen`` ``[B]`` tokens) and the ``first`` oldest go last (of more than the budget holds the lowest slots stay,
+        whatever their scores).  Freed slots below the budget take the kept ones
         past it.  ``score`` / ``pos`` ``[B, K, slots]`` and the pages' K/V move along: into ``score_out`` / ``pos_out``
         (default: in place) and in place.  Returns ``(lens_out, score_out, pos_out)``."""
         if _current_device() != self._index:
