@@ -103,9 +103,9 @@ __global__ void __launch_bounds__(PW_WARPS * 32, 4) weigh16_kernel(WeighArgs a, 
       for (int e = 0; e < 2; ++e) {
         const int m = tile * TR + e * 8 + g, row = m / r.group, hq = kvh * r.group + m - row * r.group;
         const bool in = row < s.rows;
-        lim[e] = !in ? 0 : r.causal ? s.len + row + 1 : s.paged;
         const float x = in ? a.lse[b * a.lse_b + row * a.lse_r + hq] : -INFINITY;
-        ls[e] = x == -INFINITY ? INFINITY : x * LOG2E;   // an empty row weighs nothing
+        lim[e] = x == -INFINITY ? 0 : r.causal ? s.len + row + 1 : s.paged;   // an empty row weighs nothing, whatever its scores
+        ls[e] = x * LOG2E;
 #pragma unroll
         for (int j = 0; j < NC; ++j) {
           const uint4 v = in ? __ldg(reinterpret_cast<const uint4*>(r.q + b * r.q_b + row * r.q_r + hq * r.q_h +
@@ -229,9 +229,9 @@ __global__ void __launch_bounds__(PW_WARPS * 32) weigh32_kernel(WeighArgs a, int
 #pragma unroll
       for (int x = 0; x < MR; ++x) {
         const int m = min(m0 + x, s.tiles - 1), row = (int)r.groups.div((uint32_t)m), hq = kvh * r.group + m - row * r.group;
-        lim[x] = m0 + x < s.tiles ? (r.causal ? s.len + row + 1 : s.paged) : 0;
         const float y = a.lse[b * a.lse_b + row * a.lse_r + hq];
-        ls[x] = y == -INFINITY ? INFINITY : y * LOG2E;
+        lim[x] = m0 + x < s.tiles && y != -INFINITY ? (r.causal ? s.len + row + 1 : s.paged) : 0;
+        ls[x] = y * LOG2E;
 #pragma unroll
         for (int k = 0; k < IT; ++k) d[x][k] = 0.f;
 #pragma unroll

@@ -214,3 +214,25 @@ def test_accept_residual_of_equal_rows(built_lib, cuda, dtype, B, V):
     x = (t, d, i32([2] * B), u, r, t[:, :2].contiguous())
     acc, tok, step, _ = check_accept(*x, 0.8)
     assert bool((acc == 0).all()) and bool((step == 1).all()) and bool((tok != V // 2).all())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16", "fp32"])
+@pytest.mark.parametrize("dim", [64, 128])
+def test_weigh_row_without_weight(built_lib, cuda, dtype, dim):
+    """A row whose lse is -inf weighs nothing, also where its scores are infinite or NaN."""
+    from paper_2608_12703_gb300 import serving
+    g = gen(77)
+    lens, R = [40, 7], 3
+    k, v, table = pool(g, DT[dtype], 2, dim, 16, [n + R for n in lens])
+    fill(g, k, table, [n + R for n in lens])
+    v.zero_()
+    q = torch.randn((2, R, 4, dim), generator=g, device="cuda").to(DT[dtype])
+    c = serving.PagedCache(k, v, table)
+    _, lse = c.attend(q, i32(lens))
+    q[0, 1, :2], q[1, 0, 1], q[1, 2, 3] = math.inf, math.nan, -math.inf
+    lse[0, 1, :2] = lse[1, 0, 1] = lse[1, 2, 3] = -math.inf
+    out = c.weigh(q, lse, i32(lens), None, out=torch.full((2, 2, 48), -5.0, device="cuda"))
+    want, bound = ref.weigh(q, lse, k, table, lens, [R, R], torch.zeros_like(out), True, 1 / math.sqrt(dim))
+    live = ~torch.isnan(want)
+    assert int(live.sum()) == 2 * sum(n + R for n in lens)
+    assert bool(((out.double() - want).abs()[live] <= bound[live]).all())
