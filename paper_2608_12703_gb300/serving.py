@@ -85,6 +85,23 @@ def _check(rc, what):
     return rc
 
 
+_words: dict = {}         # device index: status words made and cleared ahead, and how many are given out
+_words_lock = threading.Lock()
+
+
+def _status_word(device) -> torch.Tensor:
+    """A status word that is clear whichever stream uses it first, without a wait for the current stream at every cache."""
+    with _words_lock:
+        words, at = _words.get(device.index, (None, 0))
+        if words is None or at == words.numel():
+            if _capturing():
+                return torch.zeros(1, dtype=torch.int32, device=device)
+            words, at = torch.zeros(1024, dtype=torch.int32, device=device), 0
+            torch.cuda.current_stream(device).synchronize()
+        _words[device.index] = (words, at + 1)
+        return words[at:at + 1]
+
+
 class PagedCache:
     """A pool of K and V pages ``[n_pages, kv_heads, page_size, head_dim]`` (any strides with a
     contiguous last axis, the same for both) and the sequences' page table ``[batch, max_pages]``.
@@ -111,7 +128,7 @@ class PagedCache:
         self.kv_heads, self.page_size, self.head_dim = kv_heads, page_size, dim
         self.max_slots = self.max_pages * page_size
         self._index = dev.index
-        self._status = torch.zeros(1, dtype=torch.int32, device=dev)
+        self._status = _status_word(dev)
         self._c = A.AsrPagedCache(
             k_pages.data_ptr(), v_pages.data_ptr(), k_pages.stride(0), k_pages.stride(1), k_pages.stride(2),
             page_table.data_ptr(), page_table.stride(0), n_pages, page_size, self.max_pages, kv_heads, dim, self.batch,
@@ -129,6 +146,7 @@ class PagedCache:
         s = int(self._status.item())
         if s:
             self._status.zero_()
+            torch.cuda.current_stream(self.device).synchronize()   # before any stream's next call
         return s
 
     def _workspace(self, op: str, stream: int, n: int) -> torch.Tensor:

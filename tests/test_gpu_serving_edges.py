@@ -236,3 +236,25 @@ def test_weigh_row_without_weight(built_lib, cuda, dtype, dim):
     live = ~torch.isnan(want)
     assert int(live.sum()) == 2 * sum(n + R for n in lens)
     assert bool(((out.double() - want).abs()[live] <= bound[live]).all())
+
+
+def test_status_word_across_streams(built_lib, cuda):
+    """The status word is clear before any stream's first call, and after it was read: what a call sets later stays."""
+    from paper_2608_12703_gb300 import serving
+    k, v = (torch.zeros((4, 2, 16, 64), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    table, q = i32([0, 1]).view(1, 2), torch.zeros((1, 1, 2, 64), dtype=torch.bfloat16, device="cuda")
+    bad = i32([99])
+    torch.cuda.synchronize()
+    made, used = torch.cuda.Stream(), torch.cuda.Stream()
+    with torch.cuda.stream(made):
+        torch.cuda._sleep(200_000_000)          # the stream on which the cache is made is busy for 0.1 s
+        c = serving.PagedCache(k, v, table)
+    with torch.cuda.stream(used):
+        c.attend(q, bad)
+    assert c.status() == A.ST_CAPACITY
+    for _ in range(20):
+        with torch.cuda.stream(used):
+            c.attend(q, bad)
+        with torch.cuda.stream(made):
+            assert c.status() == A.ST_CAPACITY
+            assert made.query()                 # cleared already, not some time later
