@@ -147,7 +147,7 @@ __global__ void __launch_bounds__(ROW * GROUPS, 1024 / (ROW * GROUPS)) accept_ke
   __shared__ unsigned long long s_key[WARPS], s_best[2][CL];   // every block's best, of w and of the second race
   const int b = blockIdx.y, part = blockIdx.x, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int n_draft = live_drafts(a, b);
-  const float c = a.inv_t * LOG2E;
+  const float c = fminf(a.inv_t * LOG2E, 3.4028234e38f);   // finite for the lowest temperatures, so that 0 c is 0
   int mine = 0;   // a lane's draft and its random number
   float u = 1.f;
   if (lane < n_draft) {

@@ -258,3 +258,24 @@ def test_status_word_across_streams(built_lib, cuda):
         with torch.cuda.stream(made):
             assert c.status() == A.ST_CAPACITY
             assert made.query()                 # cleared already, not some time later
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
+@pytest.mark.parametrize("temperature", [1e-30, 3.5e-39, 4e-39, 1e-38, 1e30])
+def test_accept_extreme_temperatures(built_lib, cuda, dtype, temperature):
+    """From the row's maximum alone to every unmasked token alike."""
+    from paper_2608_12703_gb300 import serving
+    t, d, n, u, r, q = make_accept(78, torch.float32, 9, 3, 700, True, 1.0)
+    t, q = t.clamp_(-8, 8).to(DT[dtype]), q.clamp_(-8, 8).to(DT[dtype])
+    for x, rows in ((t, 4), (q, 3)):
+        x[:, :, 5::9] = -math.inf
+        x.scatter_(2, torch.randint(0, 700 // 9, (9, rows, 1), generator=gen(79), device="cuda") * 9, 9.0)
+    d = t[:, :3].float().argmax(2).to(torch.int32)
+    got = serving.accept_sampled(t, d, n, u, r, draft_logits=q, temperature=temperature)
+    acc, tok, step, prob, _ = ref.accept(t.double().cpu().numpy(), d.cpu().numpy(), n.cpu().numpy(), u.double().cpu().numpy(),
+                                         r.cpu().numpy(), q.double().cpu().numpy(), temperature)
+    if temperature < 1:
+        a, k, s, p = (x.cpu().numpy() for x in got)
+        assert np.array_equal(a, acc) and np.array_equal(k, tok) and np.array_equal(s, step) and np.array_equal(p, prob)
+    else:
+        assert bool((got[1][n >= 0] >= 0).all()) and np.allclose(got[3].cpu().numpy(), prob, rtol=1e-5)
