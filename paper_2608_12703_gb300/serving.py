@@ -57,8 +57,10 @@ def _integer(x, name) -> int:
 
 
 def _layouts(*args):
-    """The layouts of a call's tensors, other arguments (numbers by value) as they are."""
-    return tuple([(x.shape, x.stride(), x.dtype, x.get_device()) if isinstance(x, torch.Tensor) else x for x in args])
+    """The layouts of a call's tensors, numbers by value.  Anything else has no place in a call and is like nothing
+    remembered, so that the checks see it and refuse it."""
+    return tuple([(x.shape, x.stride(), x.dtype, x.get_device()) if isinstance(x, torch.Tensor) else
+                  x if x is None or isinstance(x, (int, float)) else object() for x in args])
 
 
 def _remember(layouts: dict, key, value):
@@ -330,6 +332,7 @@ class PagedCache:
             _need(x.stride() == y.stride() and x.stride(2) == 1,
                   "score and pos: the same strides and a contiguous last axis are required")
         _need(budget >= 1 and recent >= 0 and first >= 0, "budget >= 1, recent >= 0 and first >= 0 are required")
+        _need(max(budget, recent, first) < 1 << 31, "budget, recent and first: at most 2^31 - 1")
         s = A.AsrPagedScores(None, None, score.stride(0), score.stride(1), score.shape[2], None, None, score_out.stride(0),
                              score_out.stride(1), score_out.shape[2], None)
         n = _check(self._lib.asr_spec_paged_evict_ws(self._ref, ctypes.byref(s), budget), "asr_spec_paged_evict_ws")

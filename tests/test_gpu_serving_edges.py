@@ -279,3 +279,41 @@ def test_accept_extreme_temperatures(built_lib, cuda, dtype, temperature):
         assert np.array_equal(a, acc) and np.array_equal(k, tok) and np.array_equal(s, step) and np.array_equal(p, prob)
     else:
         assert bool((got[1][n >= 0] >= 0).all()) and np.allclose(got[3].cpu().numpy(), prob, rtol=1e-5)
+
+
+def test_arguments_of_other_kinds_are_refused(built_lib, cuda):
+    """Lists and arrays in place of tensors, texts in place of numbers, whole numbers past 32 bits: an error of the package's
+    own, before and after a call of the same layouts."""
+    from paper_2608_12703_gb300 import serving
+    z = lambda *s, dt=torch.bfloat16: torch.zeros(s, dtype=dt, device="cuda")
+    c = serving.PagedCache(z(4, 2, 16, 64), z(4, 2, 16, 64), z(2, 2, dt=torch.int32))
+    n, q = i32([8, 8]), z(2, 3, 4, 64)
+    lse, s, p = z(2, 3, 4, dt=torch.float32), z(2, 2, 32, dt=torch.float32), z(2, 2, 32, dt=torch.int32)
+    x = (z(2, 3, 9, dt=torch.float32), z(2, 2, dt=torch.int32), n, z(2, 2, dt=torch.float32), z(2, 9, dt=torch.float32) + 1)
+
+    def refused(f):
+        with pytest.raises(A.AsrSpecError, match="ASR_E_INVAL"):
+            f()
+    for _ in range(2):
+        refused(lambda: c.attend(q, [8, 8]))
+        refused(lambda: c.attend(q, n, rows=np.array([1, 1], dtype=np.int32)))
+        refused(lambda: c.attend(None, n))
+        refused(lambda: c.attend(q, n, scale="0.5"))
+        refused(lambda: c.attend(q, n, scale=[0.5]))
+        refused(lambda: c.attend(q, n, scale=torch.ones(2)))
+        refused(lambda: c.weigh(q, lse, [8, 8], s))
+        refused(lambda: c.weigh(q, lse.tolist(), n, s))
+        refused(lambda: c.evict([8, 8], s, p, n, budget=4))
+        refused(lambda: c.evict(n, s, p, n, budget=4.5))
+        refused(lambda: c.evict(n, s, p, n, budget="4"))
+        refused(lambda: c.evict(n, s, p, n, budget=(1 << 32) + 4))
+        refused(lambda: c.evict(n, s, p, n, budget=4, recent=1 << 32))
+        refused(lambda: c.evict(n, s, p, n, budget=4, first=1 << 31))
+        refused(lambda: serving.accept_sampled(*x[:2], [2, 2], *x[3:]))
+        refused(lambda: serving.accept_sampled(*x, temperature="1"))
+        refused(lambda: serving.accept_sampled(*x, status=[0]))
+        c.attend(q, n)
+        c.weigh(q, lse, n, s)
+        c.evict(n, s, p, n, budget=4, recent=(1 << 31) - 1, first=(1 << 31) - 1)
+        serving.accept_sampled(*x)
+    assert c.status() == 0
