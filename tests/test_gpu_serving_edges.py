@@ -317,3 +317,190 @@ def test_arguments_of_other_kinds_are_refused(built_lib, cuda):
         c.evict(n, s, p, n, budget=4, recent=(1 << 31) - 1, first=(1 << 31) - 1)
         serving.accept_sampled(*x)
     assert c.status() == 0
+
+
+def one_head_attend(q, k, v, n, i, scale):
+    """Row i of one head in 64 bits over the slots it sees: output, lse and their bounds (as serving_ref.attend's, of fp32
+    sums of 16-bit products)."""
+    kk, vv, qq = k[:n + i + 1].double(), v[:n + i + 1].double(), q.double()
+    x = scale * (kk @ qq)
+    l = torch.logsumexp(x, 0)
+    p = torch.exp(x - l)
+    ds = ref.score_bound(qq, kk, scale).max()
+    rel = 2 * ds + 2.0 ** -20 * (1 + x.abs().max()) + (n + i + 1) * 2.0 ** -23
+    return p @ vv, l, rel, p @ vv.abs(), ds + 2.0 ** -20 * (1 + l.abs() + x.abs().max())
+
+
+@pytest.mark.parametrize("dtype,dim", [("bf16", 64), ("fp16", 128), ("fp32", 64)])
+@pytest.mark.parametrize("lens,R,rows", [([0, 5, 100], 33, [33, 32, 7]), ([0, 3], 224, [224, 100]), ([1000], 1500, [1500]),
+                                         ([64], 4096, [4096])])
+def test_attend_prompt(built_lib, cuda, dtype, dim, lens, R, rows):
+    """Prompts: many rows at once, into empty pages or behind others, two query heads on each K/V head."""
+    from paper_2608_12703_gb300 import serving
+    g = gen(82 + R)
+    dt, K, G, page = DT[dtype], 2, 2, 80
+    k, v, table = pool(g, dt, K, dim, page, [n + R for n in lens])
+    fill(g, k, table, lens)
+    fill(g, v, table, lens)
+    qkv = torch.randn((len(lens), R, K * G + 2 * K, dim), generator=g, device="cuda").to(dt)
+    q, kn, vn = qkv[:, :, :K * G], qkv[:, :, K * G:K * G + K], qkv[:, :, K * G + K:]
+    c = serving.PagedCache(k, v, table)
+    out, lse = c.attend(q, i32(lens), k_new=kn, v_new=vn, rows=i32(rows))
+    assert c.status() == 0
+    eps = ref.EPS_OUT[dt]
+    for b, (n, r) in enumerate(zip(lens, rows)):
+        ks, vs = (torch.cat([x[int(p)].transpose(0, 1) for p in table[b]])[:n + r] for x in (k, v))
+        assert same_bits(ks[n:], kn[b, :r]) and same_bits(vs[n:], vn[b, :r])
+        assert bool((out[b, r:] == 0).all()) and bool((lse[b, r:] == -math.inf).all())
+        for h in range(K * G):
+            for i in (i for i in sorted({0, 1, 15, 16, 31, 32, r // 2, r - 2, r - 1}) if i < r):
+                want, l, rel, mass, lb = one_head_attend(q[b, i, h], ks[:, h // G], vs[:, h // G], n, i, dim ** -0.5)
+                bound = (rel + (0.0 if dt == torch.float32 else eps)) * mass + 1.01 * eps * want.abs() + 2.0 ** -24
+                assert bool(((out[b, i, h].double() - want).abs() <= bound).all())
+                assert float((lse[b, i, h].double() - l).abs()) <= float(lb)
+
+
+def test_weigh_data_errors(built_lib, cuda):
+    """Bad lengths and rows and more slots than the scores have leave the sequence out; a bad page id is reported; the others
+    are weighed."""
+    from paper_2608_12703_gb300 import serving
+    g = gen(83)
+    k, v, table = pool(g, torch.bfloat16, 2, 64, 16, [48] * 3)
+    fill(g, k, table, [48] * 3)
+    v.zero_()
+    q = torch.randn((3, 2, 2, 64), generator=g, device="cuda").bfloat16()
+    lse = torch.full((3, 2, 2), 3.0, device="cuda")
+    score = torch.rand((3, 2, 40), generator=g, device="cuda")
+    c = serving.PagedCache(k, v, table)
+    good = c.weigh(q, lse, i32([30] * 3), score, out=torch.full_like(score, -5.0))
+    assert c.status() == 0
+    for lens, rows, bit in (([30, 49, 30], [2, 2, 2], A.ST_CAPACITY), ([30, -1, 30], [2, 2, 2], A.ST_CAPACITY),
+                            ([30, 47, 30], [2, 2, 2], A.ST_CAPACITY), ([30, 39, 30], [2, 2, 2], A.ST_CAPACITY),
+                            ([30, 30, 30], [2, 3, 2], A.ST_BAD_LENS), ([30, 30, 30], [2, -1, 2], A.ST_BAD_LENS),
+                            (None, [2, 2, 2], A.ST_BOUNDS)):
+        t = table.clone()
+        if lens is None:
+            lens, t[1, 0] = [30] * 3, -3
+        c = serving.PagedCache(k, v, t)
+        pos = torch.full((3, 2, 40), -7, dtype=torch.int32, device="cuda")
+        out = c.weigh(q, lse, i32(lens), score, rows=i32(rows), out=torch.full_like(score, -5.0), pos=pos, first_pos=i32([9] * 3))
+        assert c.status() == bit and c.status() == 0
+        assert torch.equal(out[0], good[0]) and torch.equal(out[2], good[2])
+        if bit != A.ST_BOUNDS:
+            assert bool((out[1] == -5.0).all()) and bool((pos[1] == -7).all())
+        else:   # the other pages' slots as ever
+            assert torch.equal(out[1, :, 16:32], good[1, :, 16:32])
+        assert bool((out[:, :, 32:] == -5.0).all())
+
+
+def test_operators_on_a_side_stream_and_in_a_graph(built_lib, cuda):
+    """weigh, evict and accept_sampled on another stream, and replayed from a graph: the same results."""
+    from paper_2608_12703_gb300 import serving
+    g = gen(84)
+    k, v, table = pool(g, torch.bfloat16, 4, 64, 16, [320, 100])
+    fill(g, k, table, [320, 100])
+    fill(g, v, table, [320, 100])
+    q = torch.randn((2, 3, 8, 64), generator=g, device="cuda").bfloat16()
+    lse = torch.full((2, 3, 8), 4.0, device="cuda")
+    score = torch.rand((2, 4, 320), generator=g, device="cuda")
+    pos = torch.arange(320, dtype=torch.int32, device="cuda").repeat(2, 4, 1).contiguous()
+    n, new = i32([300, 90]), i32([303, 93])
+    k0, v0 = k.clone(), v.clone()
+    t, d, m, u, r, dl = make_accept(85, torch.float32, 5, 4, 20000, True, 1.0)
+    c = serving.PagedCache(k, v, table)
+    outs = dict(score_out=torch.zeros((2, 4, 64), device="cuda"), pos_out=torch.zeros((2, 4, 64), dtype=torch.int32, device="cuda"))
+    out = torch.zeros_like(score)
+
+    def calls():
+        k.copy_(k0)
+        v.copy_(v0)
+        c.weigh(q, lse, n, score, out=out)
+        lens, so, po = c.evict(new, out, pos, new, budget=64, recent=8, first=2, **outs)
+        return [lens, *serving.accept_sampled(t, d, m, u, r, draft_logits=dl)]
+
+    def results(x):
+        torch.cuda.synchronize()
+        return [y.clone() for y in x + [out[0, :, :303], out[1, :, :93], outs["score_out"], outs["pos_out"], k, v]]
+
+    def clear(x):
+        for y in x + [out, *outs.values(), k, v]:
+            y.zero_()
+    bits = lambda x: x.contiguous().view(torch.uint8)
+    want = results(calls())
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        got = calls()
+    assert all(torch.equal(bits(a), bits(b)) for a, b in zip(want, results(got)))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = calls()
+    for _ in range(2):
+        clear(got)
+        graph.replay()
+        assert all(torch.equal(bits(a), bits(b)) for a, b in zip(want, results(got)))
+    assert c.status() == 0
+
+
+def test_workspaces_grow(built_lib, cuda):
+    """Calls of one cache that need more workspace than the ones before, and less again."""
+    from paper_2608_12703_gb300 import serving
+    g = gen(86)
+    k, v, table = pool(g, torch.float16, 2, 128, 32, [5000, 4000])
+    fill(g, k, table, [5000, 4000])
+    fill(g, v, table, [5000, 4000])
+    n = i32([4900, 3900])
+    score = torch.rand((2, 2, 5000), generator=g, device="cuda")
+    pos = torch.arange(5000, dtype=torch.int32, device="cuda").repeat(2, 2, 1).contiguous()
+    c = serving.PagedCache(k, v, table)
+    for R, G, budget in ((1, 1, 4890), (9, 4, 2500), (1, 1, 16), (17, 2, 3000)):
+        q = torch.randn((2, R, 2 * G, 128), generator=g, device="cuda").half()
+        got, want = c.attend(q, n), serving.PagedCache(k, v, table).attend(q, n)
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+        kk, vv, kw = k.clone(), v.clone(), dict(budget=budget, recent=5, first=1)
+        got = c.evict(n, score.clone(), pos.clone(), n, **kw)
+        want = serving.PagedCache(kk, vv, table).evict(n, score.clone(), pos.clone(), n, **kw)
+        assert torch.equal(got[0], want[0]) and same_bits(k, kk) and same_bits(v, vv)
+        assert torch.equal(got[1][:, :, :budget], want[1][:, :, :budget]) and torch.equal(got[2][:, :, :budget], want[2][:, :, :budget])
+
+
+def test_binding_by_the_library_names(built_lib, cuda):
+    """The functions of the binding with the library's names give what PagedCache and accept_sampled give."""
+    import ctypes
+    from paper_2608_12703_gb300 import serving
+    g = gen(87)
+    k, v, table = pool(g, torch.bfloat16, 2, 64, 16, [64, 64])
+    fill(g, k, table, [64, 64])
+    fill(g, v, table, [64, 64])
+    q = torch.randn((2, 1, 4, 64), generator=g, device="cuda").bfloat16()
+    n = i32([60, 33])
+    c = serving.PagedCache(k, v, table)
+    cache = A.AsrPagedCache(k.data_ptr(), v.data_ptr(), *k.stride()[:3], table.data_ptr(), table.stride(0), k.shape[0], 16,
+                            table.shape[1], 2, 64, 2, 1, None)
+    rows = A.AsrPagedRows(q.data_ptr(), *q.stride()[:3], None, None, 0, 0, 0, n.data_ptr(), None, 1, 4, 1, 0.125)
+    ws = torch.zeros(built_lib.asr_spec_paged_attend_ws(ctypes.byref(cache), ctypes.byref(rows)), dtype=torch.uint8, device="cuda")
+    want, wl = c.attend(q, n)
+    out, lse = torch.zeros_like(want), torch.zeros_like(wl)
+    stream = torch.cuda.current_stream().cuda_stream
+    A.asr_spec_paged_attend(ctypes.byref(cache), rows, out, lse, ws, ws.numel(), stream)
+    assert same_bits(out, want) and same_bits(lse, wl)
+    score, pos = torch.rand((2, 2, 64), generator=g, device="cuda"), torch.arange(64, dtype=torch.int32, device="cuda").repeat(2, 2, 1).contiguous()
+    ws_, got = c.weigh(q, lse, n, score, out=torch.zeros_like(score)), torch.zeros_like(score)
+    s = A.AsrPagedScores(score.data_ptr(), None, 128, 64, 64, got.data_ptr(), None, 0, 0, 0, None)
+    A.asr_spec_paged_weigh(ctypes.byref(cache), rows, s, lse, 4, 4, stream)
+    assert torch.equal(got, ws_)
+    kk, vv = k.clone(), v.clone()
+    so, po, lo = torch.zeros((2, 2, 20), device="cuda"), torch.zeros((2, 2, 20), dtype=torch.int32, device="cuda"), torch.zeros_like(n)
+    s = A.AsrPagedScores(score.data_ptr(), pos.data_ptr(), 128, 64, 64, so.data_ptr(), po.data_ptr(), 40, 20, 20, None)
+    ws = torch.zeros(built_lib.asr_spec_paged_evict_ws(ctypes.byref(cache), ctypes.byref(s), 20), dtype=torch.uint8, device="cuda")
+    A.asr_spec_paged_evict(ctypes.byref(cache), s, n, n, 20, 2, 1, lo, ws, ws.numel(), stream)
+    want = serving.PagedCache(kk, vv, table).evict(n, score, pos, n, budget=20, recent=2, first=1, score_out=torch.zeros_like(so),
+                                                   pos_out=torch.zeros_like(po))
+    assert all(torch.equal(a, b) for a, b in zip((lo, so, po), want)) and same_bits(k, kk) and same_bits(v, vv)
+    t, d, m, u, r, dl = make_accept(88, torch.float32, 3, 2, 500, True, 0.7)
+    x = A.AsrSampledLogits(t.data_ptr(), *t.stride()[:2], dl.data_ptr(), *dl.stride()[:2], 3, 2, 500, 0)
+    i = [torch.zeros(3, dtype=torch.int32, device="cuda") for _ in range(3)]
+    prob = torch.zeros((3, 2), device="cuda")
+    A.asr_spec_accept_sampled(x, d, m, u, r, r.stride(0), 0.7, *i, prob, None, stream)
+    want = serving.accept_sampled(t, d, m, u, r, draft_logits=dl, temperature=0.7)
+    assert all(torch.equal(a, b) for a, b in zip((*i, prob), want))
