@@ -465,8 +465,9 @@ typedef struct {
  * [batch][max_rows][heads] fp32.  ws: asr_spec_paged_attend_ws bytes, 16-byte
  * aligned, zero before its first use; every call leaves it ready for the next
  * on its stream, whatever that one's sizes.  Arithmetic: 16-bit types multiply in 16 bits
- * with fp32 accumulation (weights rounded to the type for the second
- * product); fp32 in fp32 throughout; softmax statistics in fp32.
+ * with fp32 accumulation (weights rounded to the type for the second product;
+ * in fp16 those below 2^-40 of the largest vanish); fp32 in fp32 throughout;
+ * softmax statistics in fp32.
  * Data errors: kv_len or kv_len + rows outside the table (ASR_ST_CAPACITY) and
  * rows outside [0, max_rows] (ASR_ST_BAD_LENS) leave that sequence's rows zero
  * and its pages unwritten; a bad page id (ASR_ST_BOUNDS) reads page 0 in its

@@ -36,7 +36,8 @@
 // Scores, running maximum and sum, and the output accumulate in fp32.  p is
 // rounded to the cache's 16-bit type for the second product (relative error at
 // most 2^-8 for bf16 and 2^-11 for fp16 a weight, as that of the rounded
-// output); the sum takes p before rounding, so the rounding does not reach lse.
+// output); the sum takes p before rounding, so that rounding does not reach lse,
+// which has those of fp32 sums and of the hardware's exp2 and log2, some 2^-20.
 // fp16 has 5 bits of exponent: there p is taken relative to the strongest key
 // times 2^15, the top of the type's range, so that it keeps its precision down
 // to 2^-29 and vanishes below 2^-40 only; and the maximum is subtracted before

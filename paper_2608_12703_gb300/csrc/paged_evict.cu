@@ -20,7 +20,7 @@
 //     thread.  Bound by the bytes of the moved rows where many move, by the
 //     chain of passes where few do.
 // Measured: 8 sequences of 30001 to 40000 slots, 8 heads of 128, fp16, cut to
-// 16384: 132 us, of which 30 are search and lists and the rest 557 MB of moves;
+// 16384: 133 us, of which 30 are search and lists and the rest 557 MB of moves;
 // 64 of 200 to 448 slots, 20 heads of 64, bf16, cut to 256: 16 us.
 #include <atomic>
 
