@@ -40,8 +40,9 @@
 // which has those of fp32 sums and of the hardware's exp2 and log2, some 2^-20.
 // fp16 has 5 bits of exponent: there p is taken relative to the strongest key
 // times 2^15, the top of the type's range, so that it keeps its precision down
-// to 2^-29 and vanishes below 2^-40 only; and the maximum is subtracted before
-// the scale is applied, so that no rounding of large scores lifts p past 2^15.
+// to 2^-29 and vanishes below 2^-40 only.  The maximum is subtracted before the
+// scale is applied: the rounding of a large scaled maximum (scores past 2^31)
+// would move every p by powers of two, out of the types' range or to 0.
 #include <atomic>
 #include <type_traits>
 
@@ -69,12 +70,9 @@ __device__ __forceinline__ uint32_t nonfinite_halves(uint32_t x) {
   return ((x & E) == E ? 0xffffu : 0u) | (((x >> 16) & E) == E ? 0xffff0000u : 0u);
 }
 
-// Weights of the second product are 2^x times the largest's.
-template <typename T> struct WeightScale { static constexpr bool on = false; };
-template <> struct WeightScale<__half> {
-  static constexpr bool on = true;
-  static constexpr float log2 = 15.f, inv = 1.f / 32768.f;
-};
+// The strongest key's weight in the second product, 2^log2.
+template <typename T> struct TopWeight { static constexpr float log2 = 0.f, inv = 1.f; };
+template <> struct TopWeight<__half> { static constexpr float log2 = 15.f, inv = 1.f / 32768.f; };
 
 template <typename T> struct Pair;
 template <> struct Pair<__nv_bfloat16> {
@@ -577,8 +575,8 @@ __global__ void __launch_bounds__(C::WARPS * 32, 1) attend16_kernel(AttendArgs a
           if (E == 1) qa[mt][2 * j][1] = qa[mt][2 * j][3] = qa[mt][2 * j + 1][1] = qa[mt][2 * j + 1][3] = 0;
         }
       }
-    using W = WeightScale<T>;
-    float O[MT][D / 8][4], m_run[MT][E], l_run[MT][E];   // of fp16: the maximum unscaled, sum and output times 2^15
+    using W = TopWeight<T>;
+    float O[MT][D / 8][4], m_run[MT][E], l_run[MT][E];   // the maximum before the scale; sum and output times the top weight
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) {
 #pragma unroll
@@ -642,12 +640,12 @@ __global__ void __launch_bounds__(C::WARPS * 32, 1) attend16_kernel(AttendArgs a
           for (int kt = 1; kt < KS / 8; ++kt) x = fmaxf(x, fmaxf(S[mt][kt][2 * e], S[mt][kt][2 * e + 1]));
           x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 1));
           x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 2));
-          mx[e] = fmaxf(m_run[mt][e], W::on ? x : x * sc);
+          mx[e] = fmaxf(m_run[mt][e], x);
         }
         if (__any_sync(0xffffffffu, mx[0] > m_run[mt][0] || mx[E - 1] > m_run[mt][E - 1])) {
 #pragma unroll
           for (int e = 0; e < E; ++e) {
-            const float d = m_run[mt][e] - mx[e], f = mx[e] == -INFINITY ? 1.f : ex2(W::on ? d * sc : d);
+            const float f = mx[e] == -INFINITY ? 1.f : ex2((m_run[mt][e] - mx[e]) * sc);
             m_run[mt][e] = mx[e];
             l_run[mt][e] *= f;
 #pragma unroll
@@ -662,12 +660,7 @@ __global__ void __launch_bounds__(C::WARPS * 32, 1) attend16_kernel(AttendArgs a
           const float m = m_run[mt][e] == -INFINITY ? 0.f : m_run[mt][e];
 #pragma unroll
           for (int kt = 0; kt < KS / 8; ++kt) {
-            float p0, p1;
-            if constexpr (W::on) {
-              p0 = ex2(fmaf(S[mt][kt][2 * e] - m, sc, W::log2)), p1 = ex2(fmaf(S[mt][kt][2 * e + 1] - m, sc, W::log2));
-            } else {
-              p0 = ex2(fmaf(S[mt][kt][2 * e], sc, -m)), p1 = ex2(fmaf(S[mt][kt][2 * e + 1], sc, -m));
-            }
+            const float p0 = ex2(fmaf(S[mt][kt][2 * e] - m, sc, W::log2)), p1 = ex2(fmaf(S[mt][kt][2 * e + 1] - m, sc, W::log2));
             l_run[mt][e] += p0 + p1;
             pf[mt][kt][e] = Mma16<T>::pack(p0, p1);
           }
@@ -719,8 +712,8 @@ __global__ void __launch_bounds__(C::WARPS * 32, 1) attend16_kernel(AttendArgs a
         float l = l_run[mt][e];
         l += __shfl_xor_sync(0xffffffffu, l, 1);
         l += __shfl_xor_sync(0xffffffffu, l, 2);
-        if constexpr (W::on) {
-          m_run[mt][e] *= sc;
+        m_run[mt][e] *= sc;
+        if constexpr (W::log2 != 0.f) {
           l *= W::inv;
 #pragma unroll
           for (int d = 0; d < D / 8; ++d) O[mt][d][2 * e] *= W::inv, O[mt][d][2 * e + 1] *= W::inv;

@@ -504,3 +504,27 @@ def test_binding_by_the_library_names(built_lib, cuda):
     A.asr_spec_accept_sampled(x, d, m, u, r, r.stride(0), 0.7, *i, prob, None, stream)
     want = serving.accept_sampled(t, d, m, u, r, draft_logits=dl, temperature=0.7)
     assert all(torch.equal(a, b) for a, b in zip((*i, prob), want))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16", "fp32"])
+@pytest.mark.parametrize("dim", [64, 128])
+def test_attend_large_scores(built_lib, cuda, dtype, dim):
+    """Scores of 2^35 and more, a little apart from their own rounding: the strongest keys share the output."""
+    from paper_2608_12703_gb300 import serving
+    g = gen(89)
+    k, v, table = pool(g, DT[dtype], 2, dim, 16, [70])
+    k.zero_()
+    v.copy_(torch.randn(v.shape, generator=g, device="cuda"))
+    k[:, :, :, 0] = -1.0
+    for s in (3, 33, 64):       # the same largest score
+        k[int(table[0, s // 16]), :, s % 16] = 59904.0
+    q = torch.full((1, 2, 4, dim), 59904.0, dtype=DT[dtype], device="cuda")
+    q[:, :, 1], q[:, :, 2] = 58880.0, 32768.0
+    out, lse = serving.PagedCache(k, v, table).attend(q, i32([68]))
+    vv = ref.slots(v, table[0], 70)[[3, 33, 64]]
+    want = vv.mean(0).repeat_interleave(2, 0)[None, None].expand(1, 2, 4, dim)
+    x = (59904.0 * dim * q[..., 0].double()) / math.sqrt(dim)
+    eps = ref.EPS_OUT[DT[dtype]]
+    bound = (eps + 2.0 ** -20) * vv.abs().sum(0).repeat_interleave(2, 0) + 1.01 * eps * want.abs() + 2.0 ** -24
+    assert bool(((out.double() - want).abs() <= bound).all())
+    assert bool(((lse.double() - x).abs() <= ((dim + 8) * 2.0 ** -22 + 2.0 ** -20) * x).all())
