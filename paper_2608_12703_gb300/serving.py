@@ -45,14 +45,14 @@ def _number(x, name) -> float:
     """The value of a number, of a tensor's only element too (which waits for its device)."""
     try:
         return float(x + 0.0)
-    except (TypeError, ValueError, RuntimeError):
+    except (TypeError, ValueError, RuntimeError, OverflowError):
         raise A.AsrSpecError(f"ASR_E_INVAL {name}: a number is required") from None
 
 
 def _integer(x, name) -> int:
     try:
         return operator.index(x)
-    except (TypeError, ValueError, RuntimeError):
+    except (TypeError, ValueError, RuntimeError, OverflowError):
         raise A.AsrSpecError(f"ASR_E_INVAL {name}: a whole number is required") from None
 
 

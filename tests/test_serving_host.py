@@ -74,3 +74,14 @@ def test_workspace_lives_through_its_launch(monkeypatch):
     c._attend = launch
     c.attend(zeros(1, 1, 2, 64), n)
     assert alive == [True] * 4
+
+
+@pytest.mark.parametrize("x", ["1", [1.0], None, 1j, 10 ** 400, b"2"], ids=lambda x: str(x)[:10])
+def test_numbers_are_refused_with_the_package_error(x):
+    from paper_2608_12703_gb300 import asrspec as A
+    from paper_2608_12703_gb300 import serving
+    with pytest.raises(A.AsrSpecError, match="ASR_E_INVAL scale"):
+        serving._number(x, "scale")
+    if not isinstance(x, int):
+        with pytest.raises(A.AsrSpecError, match="ASR_E_INVAL budget"):
+            serving._integer(x, "budget")
