@@ -557,6 +557,153 @@ int asr_spec_accept_sampled(const asr_sampled_logits* logits, const int32_t* dra
                             const float* race, int64_t race_stride, float temperature, int32_t* accepted, int32_t* token,
                             int32_t* step, float* prob, int32_t* status, void* stream);
 
+/* ---- An 8-bit paged cache, its pages, and the logits' adjustment -----------
+ * The same kind of entry as the section above: no handle, device arrays of the
+ * caller's, asynchronous on `stream`, nothing allocated, conditions in device
+ * data reported in the status word.  A round of several samples a prompt is
+ *   fork -> reserve -> attend (per layer) -> adjust_logits -> accept_sampled
+ *   -> kv_len += step -> fork (keep = kv_len) -> now and then compact.
+ *
+ * A pool of pages in 8 bits.  Slot s of sequence b's head h has its codes (e4m3:
+ * 3 bits of mantissa, largest value 448) where asr_paged_cache has its elements;
+ * its values are the codes times
+ *   k_scale[page * scale_page_stride + h * scale_head_stride + s % page_size / 16]
+ * (v_scale alike): one scale for the 16 slots of a group and a head. */
+typedef struct {
+  void *k_pages, *v_pages;
+  int64_t page_stride, head_stride, slot_stride;   /* bytes, > 0, multiples of 16 */
+  float *k_scale, *v_scale;    /* [n_pages][kv_heads][page_size / 16] */
+  int64_t scale_page_stride, scale_head_stride;    /* elements */
+  const int32_t* page_table;   /* as asr_paged_cache's */
+  int64_t table_stride;
+  int32_t n_pages, page_size, max_pages, kv_heads, head_dim, batch;
+  int32_t* status;
+} asr_paged8_cache;
+
+/* Quantise the rows' K/V (k_new, v_new of type dtype: 0 = fp32, 1 = bf16, 2 =
+ * fp16) behind each sequence's kv_len slots; q, heads, causal and scale are not
+ * looked at.  A group that the rows begin takes the scale 2^e, the least (2^-126
+ * at least) with every magnitude at most 448 * 2^e; a group that goes on the larger of that and
+ * its own, and where that is not its own the codes of its earlier slots are
+ * rounded anew (exact but for values below 2^-6 of the new scale, since scales are powers of
+ * two).  code = round to nearest even of value / scale; a NaN or an infinity becomes a
+ * NaN code and counts for no scale.  Slots at or past kv_len + rows are left as they are.
+ * Data errors: as asr_spec_paged_attend's; new rows of a bad page id are not written. */
+int asr_spec_paged8_append(const asr_paged8_cache* cache, const asr_paged_rows* rows, int32_t dtype, void* stream);
+
+/* Attention of the rows over the cache as asr_spec_paged_attend, with K and V
+ * the dequantised ones.  dtype (1 or 2) is that of q, k_new, v_new and out.  With k_new /
+ * v_new (causal only) they are appended first, as by asr_spec_paged8_append, and
+ * the rows see them as they are stored.  Arithmetic: codes and q multiply exactly and
+ * are summed in fp32 (bf16 rows: elements below 2^-38 of a row's largest vanish), softmax statistics in
+ * fp32; weights times the groups' scales are rounded to fp16 for the second product, and
+ * those below 2^-40 of a row's largest vanish.  Scales are positive and finite.
+ * ws: asr_spec_paged8_attend_ws bytes, 16-byte aligned, zero before its first use; every call
+ * leaves it ready for the next on its stream, whatever that one's sizes. */
+int64_t asr_spec_paged8_attend_ws(const asr_paged8_cache* cache, const asr_paged_rows* rows, int32_t dtype);
+int asr_spec_paged8_attend(const asr_paged8_cache* cache, const asr_paged_rows* rows, int32_t dtype, void* out, float* lse,
+                           void* ws, int64_t ws_bytes, void* stream);
+
+/* Who holds which pages.  refs[p] is the number of table entries (and of holders
+ * of the caller's own) of page p; 0 = free.  Entries at or past held[b] mean nothing and are
+ * left as they are.  table_out, held_out and refs_out receive the new state; each
+ * may be its input itself (but not overlap it otherwise). */
+typedef struct {
+  const int32_t* page_table;   /* [batch][table_stride] */
+  int64_t table_stride;
+  const int32_t *held, *refs;  /* [batch], [n_pages] */
+  int32_t* table_out;
+  int64_t table_out_stride;
+  int32_t *held_out, *refs_out;
+  int32_t n_pages, page_size, max_pages, batch;   /* batch 1 .. 1024 */
+  int32_t* status;
+} asr_page_pool;
+
+/* One array that the pages have a part in: [n_pages][heads][rows][row_bytes],
+ * strides in bytes.  A row belongs to row_slots slots (K and V: 1, scales: 16).  Base, strides and
+ * row_bytes are multiples of 4. */
+typedef struct {
+  void* base;
+  int64_t page_stride, head_stride, row_stride;
+  int32_t heads, rows, row_bytes, row_slots;
+} asr_page_array;
+
+/* Checks n (0 .. 1024) arrays of pages of page_size slots and writes what the
+ * kernels read of them, asr_spec_pool_plan_bytes(n) bytes, to host memory, for
+ * the caller to copy to the device once. */
+int64_t asr_spec_pool_plan_bytes(int32_t n);
+int asr_spec_pool_plan(const asr_page_array* arrays, int32_t n, int32_t page_size, void* plan);
+
+/* Pages for rows[b] slots behind lens[b] of each sequence that no other sequence
+ * sees.  Of the pages that hold those slots, a missing one is taken from the pool, and one that
+ * others hold too is replaced by one of the pool's, which takes the slots below
+ * lens[b] along; of sequences that alone share the page of slot lens[b] the
+ * lowest keeps it.  The lowest free pages are taken, in order of sequence and slot.
+ * counts[0] = pages taken, counts[1] = pages free afterwards (those given up by
+ * this call not among them).
+ * Data errors: rows < 0 or lens outside the pages held (ASR_ST_BAD_LENS) and lens + rows past
+ * max_pages (ASR_ST_CAPACITY) leave that sequence out, a held page id outside the
+ * pool (ASR_ST_BOUNDS) counts as the sequence's own; a pool with too few free pages
+ * (ASR_ST_CAPACITY) leaves everything as it is.
+ * plan: the device copy of asr_spec_pool_plan's, or NULL with n_arrays 0.
+ * ws: asr_spec_pool_ws bytes, 16-byte aligned, zero before its first use; every call leaves it
+ * ready for the next on its stream, of any of the three. */
+int64_t asr_spec_pool_ws(const asr_page_pool* pool);
+int asr_spec_pool_reserve(const asr_page_pool* pool, const void* plan, int32_t n_arrays, const int32_t* lens,
+                          const int32_t* rows, int32_t* counts, void* ws, int64_t ws_bytes, void* stream);
+
+/* Sequence b goes on with the pages of sequence parent[b] as they were before
+ * the call (parent NULL: its own; parent[b] = -1: none), of which it holds
+ * those of the first keep[b] slots (keep NULL: all).
+ * Data errors: parent outside [-1, batch) (ASR_ST_BOUNDS) or keep < 0
+ * (ASR_ST_BAD_LENS) leaves that sequence as it is; held outside [0, max_pages]
+ * (ASR_ST_BAD_LENS) counts as 0; a page id outside the pool (ASR_ST_BOUNDS) is
+ * passed on and counted nowhere. */
+int asr_spec_pool_fork(const asr_page_pool* pool, const int32_t* parent, const int32_t* keep, void* ws, int64_t ws_bytes,
+                       void* stream);
+
+/* Live pages (refs > 0) to the front: with n of them the j-th free page below n takes the
+ * contents of the j-th live one at or past it.  live[0] = n; where[p] = page p's
+ * new id, -1 for a free one.  Table entries and refs follow. */
+int asr_spec_pool_compact(const asr_page_pool* pool, const void* plan, int32_t n_arrays, int32_t* where, int32_t* live,
+                          void* ws, int64_t ws_bytes, void* stream);
+
+/* Logits of a block and what is done to them.  Rows need only their element's
+ * alignment; strides in elements, >= 0. */
+typedef struct {
+  const void* logits;          /* [batch][rows][vocab] */
+  int64_t batch_stride, row_stride;
+  void* out;                   /* may be logits itself with its strides */
+  int64_t out_batch_stride, out_row_stride;
+  int32_t batch, rows, vocab, dtype;   /* rows 1 .. 32; dtype 0 = fp32, 1 = bf16, 2 = fp16 */
+  const int32_t* history;      /* [batch][history_stride] tokens before row 0; NULL: history_max 0 */
+  int64_t history_stride;
+  int32_t history_max;         /* tokens a row of history has room for */
+  const int32_t *history_len;  /* [batch] tokens in use; NULL: history_max each */
+  const int32_t *prompt_len;   /* [batch] of these, the prompt's; NULL: 0 */
+  const int32_t *draft;        /* [batch][rows - 1] tokens between the rows, or NULL */
+  const int32_t *lens;         /* [batch] drafts in use, -1 sits out; NULL: rows - 1 each */
+  const float *repetition, *frequency, *presence;   /* [batch], or NULL: the numbers below */
+  float repetition_all, frequency_all, presence_all;
+  const float* bias;           /* [batch][vocab], or NULL */
+  int64_t bias_stride;         /* 0: one for all */
+  const int32_t* mask;         /* [batch][rows][ceil(vocab / 32)], bit j % 32 of word j / 32: token j is allowed; or NULL */
+  int64_t mask_batch_stride, mask_row_stride;
+  int32_t* status;
+} asr_logit_rules;
+
+/* Row i of utterance b comes after its history and its first i drafts.  With
+ * c(j) = how often token j is among them without the prompt, for i <= lens[b]:
+ *   x = logits[b][i][j]
+ *   x = x > 0 ? x / repetition : x * repetition     where j is among them, the prompt included
+ *   x = x - frequency * c(j) - presence * (c(j) > 0)
+ *   out[b][i][j] = x + bias[b][j], or -inf where the mask does not allow j
+ * in fp32, rounded once.  Other rows are left as they are.
+ * Data errors: lens outside [-1, rows - 1], history_len outside [0, history_max]
+ * or prompt_len outside [0, history_len] (ASR_ST_BAD_LENS) leaves the utterance out; a token
+ * outside [0, vocab) (ASR_ST_BAD_TOKEN) is passed over. */
+int asr_spec_adjust_logits(const asr_logit_rules* rules, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -31,7 +31,9 @@ EXPORTED = [
     "asr_spec_verify_tree", "asr_spec_restart", "asr_spec_fewrow_trace", "asr_spec_fewrow_trace_read",
     "asr_spec_debug_anchor_profile", "asr_spec_draft_create", "asr_spec_draft_propose",
     "asr_spec_draft_set_threshold", "asr_spec_paged_attend", "asr_spec_paged_attend_ws", "asr_spec_paged_weigh",
-    "asr_spec_paged_evict", "asr_spec_paged_evict_ws", "asr_spec_accept_sampled",
+    "asr_spec_paged_evict", "asr_spec_paged_evict_ws", "asr_spec_accept_sampled", "asr_spec_paged8_append",
+    "asr_spec_paged8_attend", "asr_spec_paged8_attend_ws", "asr_spec_pool_plan_bytes", "asr_spec_pool_plan",
+    "asr_spec_pool_ws", "asr_spec_pool_reserve", "asr_spec_pool_fork", "asr_spec_pool_compact", "asr_spec_adjust_logits",
 ]
 DRAFT_WIN = {"anchor": 0, "shifted": 1, "random": 2, None: 3}
 PROF_CLASSES = ["qkv", "resid", "query", "mlp_up", "self_attn", "cross_attn", "lm_head", "layernorm", "other",
@@ -92,6 +94,38 @@ class AsrSampledLogits(ctypes.Structure):
                 (n, ctypes.c_int32) for n in ("batch", "k", "vocab", "dtype")]
 
 
+class AsrPaged8Cache(ctypes.Structure):
+    _fields_ = [("k_pages", ctypes.c_void_p), ("v_pages", ctypes.c_void_p), ("page_stride", ctypes.c_int64),
+                ("head_stride", ctypes.c_int64), ("slot_stride", ctypes.c_int64), ("k_scale", ctypes.c_void_p),
+                ("v_scale", ctypes.c_void_p), ("scale_page_stride", ctypes.c_int64), ("scale_head_stride", ctypes.c_int64),
+                ("page_table", ctypes.c_void_p), ("table_stride", ctypes.c_int64)] + [(n, ctypes.c_int32) for n in (
+                    "n_pages", "page_size", "max_pages", "kv_heads", "head_dim", "batch")] + [("status", ctypes.c_void_p)]
+
+
+class AsrPagePool(ctypes.Structure):
+    _fields_ = [("page_table", ctypes.c_void_p), ("table_stride", ctypes.c_int64), ("held", ctypes.c_void_p),
+                ("refs", ctypes.c_void_p), ("table_out", ctypes.c_void_p), ("table_out_stride", ctypes.c_int64),
+                ("held_out", ctypes.c_void_p), ("refs_out", ctypes.c_void_p)] + [(n, ctypes.c_int32) for n in (
+                    "n_pages", "page_size", "max_pages", "batch")] + [("status", ctypes.c_void_p)]
+
+
+class AsrPageArray(ctypes.Structure):
+    _fields_ = [("base", ctypes.c_void_p), ("page_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64),
+                ("row_stride", ctypes.c_int64)] + [(n, ctypes.c_int32) for n in ("heads", "rows", "row_bytes", "row_slots")]
+
+
+class AsrLogitRules(ctypes.Structure):
+    _fields_ = [("logits", ctypes.c_void_p), ("batch_stride", ctypes.c_int64), ("row_stride", ctypes.c_int64),
+                ("out", ctypes.c_void_p), ("out_batch_stride", ctypes.c_int64), ("out_row_stride", ctypes.c_int64)] + [
+                (n, ctypes.c_int32) for n in ("batch", "rows", "vocab", "dtype")] + [
+                ("history", ctypes.c_void_p), ("history_stride", ctypes.c_int64), ("history_max", ctypes.c_int32)] + [
+                (n, ctypes.c_void_p) for n in ("history_len", "prompt_len", "draft", "lens", "repetition", "frequency",
+                                               "presence")] + [
+                (n, ctypes.c_float) for n in ("repetition_all", "frequency_all", "presence_all")] + [
+                ("bias", ctypes.c_void_p), ("bias_stride", ctypes.c_int64), ("mask", ctypes.c_void_p),
+                ("mask_batch_stride", ctypes.c_int64), ("mask_row_stride", ctypes.c_int64), ("status", ctypes.c_void_p)]
+
+
 class AsrSpecError(RuntimeError):
     pass
 
@@ -145,9 +179,19 @@ def lib():
     L.asr_spec_paged_evict.argtypes = [vp, vp, vp, vp, i32, i32, i32, vp, vp, i64, vp]
     L.asr_spec_paged_evict_ws.argtypes = [vp, vp, i32]
     L.asr_spec_accept_sampled.argtypes = [vp, p32, p32, vp, vp, i64, ctypes.c_float, p32, p32, p32, vp, p32, vp]
+    L.asr_spec_paged8_append.argtypes = [vp, vp, i32, vp]
+    L.asr_spec_paged8_attend.argtypes = [vp, vp, i32, vp, vp, vp, i64, vp]
+    L.asr_spec_paged8_attend_ws.argtypes = [vp, vp, i32]
+    L.asr_spec_pool_plan_bytes.argtypes = [i32]
+    L.asr_spec_pool_plan.argtypes = [vp, i32, i32, vp]
+    L.asr_spec_pool_ws.argtypes = [vp]
+    L.asr_spec_pool_reserve.argtypes = [vp, vp, i32, vp, vp, vp, vp, i64, vp]
+    L.asr_spec_pool_fork.argtypes = [vp, vp, vp, vp, i64, vp]
+    L.asr_spec_pool_compact.argtypes = [vp, vp, i32, vp, vp, vp, i64, vp]
+    L.asr_spec_adjust_logits.argtypes = [vp, vp]
     for name in EXPORTED:
         if name not in ("asr_spec_last_error", "asr_spec_destroy"):
-            getattr(L, name).restype = i64 if name.endswith("_ws") else ctypes.c_int
+            getattr(L, name).restype = i64 if name.endswith(("_ws", "_plan_bytes")) else ctypes.c_int
     _lib = L
     return L
 
@@ -349,3 +393,40 @@ def asr_spec_accept_sampled(logits, draft, lens, u, race, race_stride, temperatu
                                                       race_stride, temperature, ptr(accepted), ptr(token), ptr(step),
                                                       ptr(prob), ptr(status), stream),
                   "asr_spec_accept_sampled")
+
+
+def asr_spec_paged8_append(cache, rows, dtype, stream=None):
+    return _check(None, lib().asr_spec_paged8_append(cache, ctypes.byref(rows), dtype, stream), "asr_spec_paged8_append")
+
+
+def asr_spec_paged8_attend(cache, rows, dtype, out, lse, ws, ws_bytes, stream=None):
+    return _check(None, lib().asr_spec_paged8_attend(cache, ctypes.byref(rows), dtype, ptr(out), ptr(lse), ptr(ws), ws_bytes,
+                                                     stream), "asr_spec_paged8_attend")
+
+
+def asr_spec_pool_plan(arrays, page_size) -> np.ndarray:
+    """The bytes that the kernels read of ``arrays`` (a list of AsrPageArray)."""
+    a = (AsrPageArray * max(1, len(arrays)))(*arrays)
+    n = _check(None, lib().asr_spec_pool_plan_bytes(len(arrays)), "asr_spec_pool_plan_bytes")
+    plan = np.zeros((n + 15) // 16 * 2, dtype=np.uint64)
+    _check(None, lib().asr_spec_pool_plan(a, len(arrays), page_size, plan.ctypes.data), "asr_spec_pool_plan")
+    return plan.view(np.uint8)
+
+
+def asr_spec_pool_reserve(pool, plan, n_arrays, lens, rows, counts, ws, ws_bytes, stream=None):
+    return _check(None, lib().asr_spec_pool_reserve(ctypes.byref(pool), ptr(plan), n_arrays, ptr(lens), ptr(rows), ptr(counts),
+                                                    ptr(ws), ws_bytes, stream), "asr_spec_pool_reserve")
+
+
+def asr_spec_pool_fork(pool, parent, keep, ws, ws_bytes, stream=None):
+    return _check(None, lib().asr_spec_pool_fork(ctypes.byref(pool), ptr(parent), ptr(keep), ptr(ws), ws_bytes, stream),
+                  "asr_spec_pool_fork")
+
+
+def asr_spec_pool_compact(pool, plan, n_arrays, where, live, ws, ws_bytes, stream=None):
+    return _check(None, lib().asr_spec_pool_compact(ctypes.byref(pool), ptr(plan), n_arrays, ptr(where), ptr(live), ptr(ws),
+                                                    ws_bytes, stream), "asr_spec_pool_compact")
+
+
+def asr_spec_adjust_logits(rules, stream=None):
+    return _check(None, lib().asr_spec_adjust_logits(ctypes.byref(rules), stream), "asr_spec_adjust_logits")

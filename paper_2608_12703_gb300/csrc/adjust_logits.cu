@@ -1,0 +1,219 @@
+// Penalties for repeated tokens, biases and grammar masks on the logits of a
+// block of rows.
+//
+//   x' = x > 0 ? x / repetition : x * repetition   (tokens seen),
+//   x' - frequency c - presence (c > 0) + bias,  -inf where the mask says so
+//
+// with c the token's count after the prompt, the row's own drafts included.
+// Bound by the logits, read and written once.  A block takes a run of the
+// vocabulary and some or all rows of an utterance: it counts its part of the
+// history in shared memory once, a thread keeps its tokens' counts and biases
+// in registers and walks the rows, so the history is read by each run of the
+// vocabulary instead of by each row, and between two rows only the draft that
+// lies between them is looked at.
+#include "kernels.h"
+#include "paged.cuh"
+
+namespace asrspec {
+namespace {
+
+constexpr int THREADS = 256;
+
+struct AdjustArgs {
+  asr_logit_rules r;
+  long long batch, row, out_batch, out_row;   // bytes
+  int words, rows_each;                       // words of a mask row; rows of a block
+};
+
+template <typename T> __device__ __forceinline__ T from_f32(float v);
+template <> __device__ __forceinline__ float from_f32<float>(float v) { return v; }
+template <> __device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
+template <> __device__ __forceinline__ __half from_f32<__half>(float v) { return __float2half_rn(v); }
+
+template <int BYTES> struct Word;
+template <> struct Word<2> { using type = uint16_t; };
+template <> struct Word<4> { using type = uint32_t; };
+template <> struct Word<8> { using type = uint2; };
+template <> struct Word<16> { using type = uint4; };
+
+// W elements an access, J accesses a thread and row: token base + (j * THREADS + thread) * W + w.
+template <typename T, int W, int J>
+__global__ void __launch_bounds__(THREADS) adjust_kernel(const AdjustArgs a) {
+  constexpr int RUN = THREADS * W * J;
+  using Access = typename Word<W * sizeof(T)>::type;
+  __shared__ int seen[RUN];   // 2 * count + (seen at all)
+  const asr_logit_rules& r = a.r;
+  const int tid = threadIdx.x, b = blockIdx.z, base = blockIdx.x * RUN;
+  const bool reports = blockIdx.x == 0 && blockIdx.y == 0 && r.status;
+  const int n = r.lens ? r.lens[b] : r.rows - 1, have = r.history_len ? r.history_len[b] : r.history_max;
+  const int prompt = r.prompt_len ? r.prompt_len[b] : 0;
+  if (n < -1 || n >= r.rows || have < 0 || have > r.history_max || prompt < 0 || prompt > have) {
+    if (reports && tid == 0) set_status(r.status, ST_BAD_LENS);
+    return;
+  }
+  const int row0 = blockIdx.y * a.rows_each, row1 = min(n + 1, row0 + a.rows_each);
+  if (row0 >= row1 && !reports) return;
+
+  float bias[J][W];
+#pragma unroll
+  for (int j = 0; j < J; ++j)
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+      const int tok = base + (j * THREADS + tid) * W + w;
+      bias[j][w] = r.bias && tok < r.vocab ? __ldg(r.bias + b * r.bias_stride + tok) : 0.f;
+    }
+  for (int i = tid; i < RUN; i += THREADS) seen[i] = 0;
+  __syncthreads();
+  bool bad = false;
+  auto note = [&](int tok, bool said) {
+    bad |= (unsigned)tok >= (unsigned)r.vocab;
+    const int at = tok - base;
+    if ((unsigned)at >= (unsigned)RUN || tok >= r.vocab) return;
+    atomicOr(seen + at, 1);
+    if (said) atomicAdd(seen + at, 2);
+  };
+  for (int i = tid; i < have; i += THREADS) note(__ldg(r.history + b * r.history_stride + i), i >= prompt);
+  const int* draft = r.draft ? r.draft + (long long)b * (r.rows - 1) : nullptr;
+  if (draft && tid < (reports ? n : min(row0, n))) {
+    const int d = __ldg(draft + tid);
+    if (tid < row0) note(d, true);
+    bad |= (unsigned)d >= (unsigned)r.vocab;
+  }
+  if (reports && bad) set_status(r.status, ST_BAD_TOKEN);
+  __syncthreads();
+  if (row0 >= row1) return;
+  int c[J][W];
+#pragma unroll
+  for (int j = 0; j < J; ++j)
+#pragma unroll
+    for (int w = 0; w < W; ++w) c[j][w] = seen[(j * THREADS + tid) * W + w];
+  const float rep = r.repetition ? r.repetition[b] : r.repetition_all;
+  const float freq = r.frequency ? r.frequency[b] : r.frequency_all, pres = r.presence ? r.presence[b] : r.presence_all;
+
+  union Part {
+    Access word;
+    T x[W];
+    __device__ Part() {}
+  };
+  // the next row is on its way while this one is worked on
+  Part in[2][J];
+  uint32_t allowed[2][J];
+  auto load = [&](int row, Part (&x)[J], uint32_t (&m)[J]) {
+    const T* p = reinterpret_cast<const T*>(static_cast<const char*>(r.logits) + b * a.batch + row * a.row);
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+      const int tok = base + (j * THREADS + tid) * W;
+      m[j] = 0xffffffffu;
+      if (r.mask && tok < r.vocab)
+        m[j] = (uint32_t)__ldg(r.mask + b * r.mask_batch_stride + row * r.mask_row_stride + tok / 32) >> (tok % 32);
+      if (tok + W <= r.vocab) {
+        x[j].word = *reinterpret_cast<const Access*>(p + tok);
+      } else {
+#pragma unroll
+        for (int w = 0; w < W; ++w)
+          if (tok + w < r.vocab) x[j].x[w] = p[tok + w];
+      }
+    }
+  };
+  auto work = [&](int row, Part (&x)[J], uint32_t (&m)[J]) {
+    T* p = reinterpret_cast<T*>(static_cast<char*>(r.out) + b * a.out_batch + row * a.out_row);
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+      const int tok = base + (j * THREADS + tid) * W;
+#pragma unroll
+      for (int w = 0; w < W; ++w) {
+        float v = to_f32(x[j].x[w]);
+        if (c[j][w]) {
+          v = v > 0.f ? v / rep : v * rep;
+          const int count = c[j][w] >> 1;
+          if (count) v = v - freq * (float)count - pres;
+        }
+        v += bias[j][w];
+        x[j].x[w] = from_f32<T>(m[j] >> w & 1 ? v : -INFINITY);
+      }
+      if (tok + W <= r.vocab) {
+        *reinterpret_cast<Access*>(p + tok) = x[j].word;
+      } else {
+#pragma unroll
+        for (int w = 0; w < W; ++w)
+          if (tok + w < r.vocab) p[tok + w] = x[j].x[w];
+      }
+    }
+    // the draft that the next row comes after
+    if (draft && row + 1 < row1) {
+      const int d = __ldg(draft + row);
+      if ((unsigned)(d - base) < (unsigned)RUN && d < r.vocab)
+#pragma unroll
+        for (int j = 0; j < J; ++j)
+#pragma unroll
+          for (int w = 0; w < W; ++w)
+            if (base + (j * THREADS + tid) * W + w == d) c[j][w] = (c[j][w] + 2) | 1;
+    }
+  };
+  load(row0, in[0], allowed[0]);
+  for (int row = row0; row < row1; row += 2) {
+    if (row + 1 < row1) load(row + 1, in[1], allowed[1]);
+    work(row, in[0], allowed[0]);
+    if (row + 1 >= row1) break;
+    if (row + 2 < row1) load(row + 2, in[0], allowed[0]);
+    work(row + 1, in[1], allowed[1]);
+  }
+}
+
+// Runs of a utterance's rows: enough blocks for every SM to have some.
+template <typename T, int W, int J>
+cudaError_t launch_adjust(AdjustArgs& a, cudaStream_t st) {
+  const int runs = (a.r.vocab + THREADS * W * J - 1) / (THREADS * W * J), rows = a.r.rows;
+  const long long blocks = (long long)runs * a.r.batch, want = 4ll * paged_sm_count();
+  int parts = (int)((want + blocks - 1) / blocks);
+  if (parts > rows) parts = rows;
+  a.rows_each = (rows + parts - 1) / parts;
+  parts = (rows + a.rows_each - 1) / a.rows_each;
+  adjust_kernel<T, W, J><<<dim3(runs, parts, a.r.batch), THREADS, 0, st>>>(a);
+  return cudaGetLastError();
+}
+
+template <typename T>
+cudaError_t launch_type(AdjustArgs& a, cudaStream_t st) {
+  const uintptr_t all = (uintptr_t)a.r.logits | (uintptr_t)a.r.out | a.batch | a.row | a.out_batch | a.out_row;
+  if constexpr (sizeof(T) == 4)
+    return all % 16 == 0 ? launch_adjust<T, 4, 1>(a, st) : all % 8 == 0 ? launch_adjust<T, 2, 2>(a, st) : launch_adjust<T, 1, 4>(a, st);
+  else
+    return all % 16 == 0  ? launch_adjust<T, 8, 1>(a, st)
+           : all % 8 == 0 ? launch_adjust<T, 4, 2>(a, st)
+           : all % 4 == 0 ? launch_adjust<T, 2, 4>(a, st)
+                          : launch_adjust<T, 1, 8>(a, st);
+}
+
+}  // namespace
+}  // namespace asrspec
+
+using namespace asrspec;
+
+extern "C" int asr_spec_adjust_logits(const asr_logit_rules* r, void* stream) {
+  if (!r || !r->logits || !r->out) return ASR_E_INVAL;
+  if (r->batch < 1 || r->batch > 65535 || r->rows < 1 || r->rows > 32 || r->vocab < 1 || r->vocab > (1 << 30) || r->dtype < 0 || r->dtype > 2)
+    return ASR_E_INVAL;
+  const long long es = r->dtype == 0 ? 4 : 2;
+  if (((uintptr_t)r->logits | (uintptr_t)r->out) % es) return ASR_E_INVAL;
+  if (r->row_stride < r->vocab || r->out_row_stride < r->vocab || r->batch_stride < 0 || r->out_batch_stride < 0) return ASR_E_INVAL;
+  if (r->batch > 1 && (r->batch_stride < r->vocab || r->out_batch_stride < r->vocab)) return ASR_E_INVAL;
+  for (int64_t s : {r->batch_stride, r->row_stride, r->out_batch_stride, r->out_row_stride})
+    if (s >= (1ll << 45)) return ASR_E_INVAL;
+  if (r->out == r->logits && (r->out_batch_stride != r->batch_stride || r->out_row_stride != r->row_stride)) return ASR_E_INVAL;
+  if (r->history_max < 0 || r->history_stride < r->history_max || (!r->history && r->history_max > 0)) return ASR_E_INVAL;
+  if (r->bias_stride < 0 || r->mask_batch_stride < 0 || r->mask_row_stride < 0) return ASR_E_INVAL;
+  for (const void* x : {(const void*)r->history, (const void*)r->history_len, (const void*)r->prompt_len, (const void*)r->draft,
+                        (const void*)r->lens, (const void*)r->repetition, (const void*)r->frequency, (const void*)r->presence,
+                        (const void*)r->bias, (const void*)r->mask, (const void*)r->status})
+    if ((uintptr_t)x % 4) return ASR_E_INVAL;
+  if (!(r->repetition_all > 0.f) || !(r->repetition_all <= 1e30f)) return ASR_E_INVAL;
+  for (float x : {r->frequency_all, r->presence_all})
+    if (!(x >= -1e30f && x <= 1e30f)) return ASR_E_INVAL;
+  AdjustArgs a{*r, r->batch_stride * es, r->row_stride * es, r->out_batch_stride * es, r->out_row_stride * es, (r->vocab + 31) / 32, 0};
+  const cudaStream_t st = static_cast<cudaStream_t>(stream);
+  const cudaError_t e = r->dtype == 0   ? launch_type<float>(a, st)
+                        : r->dtype == 1 ? launch_type<__nv_bfloat16>(a, st)
+                                        : launch_type<__half>(a, st);
+  return e == cudaSuccess ? ASR_OK : ASR_E_CUDA;
+}

@@ -1,0 +1,42 @@
+// A paged K/V cache held in 8 bits: e4m3 codes and one scale for each group of
+// 16 slots and head.
+#pragma once
+
+#include "paged.cuh"
+
+namespace asrspec {
+
+constexpr float E4M3_MAX = 448.f;
+
+// The cache as the kernels see it: the view of its codes (one byte an element)
+// and where the scales lie, in elements.
+struct Paged8View {
+  PagedView c;
+  float *k_scale, *v_scale;
+  long long s_page, s_head;
+  int dim;
+  __device__ __forceinline__ long long scale_at(int pid, int kvh, int grp) const {
+    const int in_page = grp - (int)(c.groups.div((uint32_t)grp) * c.groups.d);
+    return pid * s_page + kvh * s_head + in_page;
+  }
+};
+
+// Two floats to e4m3 (nearest even, magnitudes above 448 become 448, NaN its code): lo in the low byte.
+__device__ __forceinline__ uint32_t e4m3x2(float lo, float hi) {
+  uint16_t v;
+  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(v) : "f"(hi), "f"(lo));
+  return v;
+}
+// The values of two codes, exact.
+__device__ __forceinline__ float2 e4m3x2_value(uint32_t v) {
+  uint32_t h;
+  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((uint16_t)v));
+  return __half22float2(*reinterpret_cast<__half2*>(&h));
+}
+
+// ---- Host: argument checks and launches shared by the entry points -----------
+int paged8_view(const asr_paged8_cache* c, Paged8View* v);
+int paged8_rows(const asr_paged8_cache* c, const asr_paged_rows* r, int dtype, PagedRows* v);
+cudaError_t launch_append8(const Paged8View& c, const PagedRows& r, int dtype, cudaStream_t st);
+
+}  // namespace asrspec
