@@ -34,9 +34,24 @@ __device__ __forceinline__ float2 e4m3x2_value(uint32_t v) {
   return __half22float2(*reinterpret_cast<__half2*>(&h));
 }
 
+// Two codes of the low half of w to fp16: .x the low byte.
+__device__ __forceinline__ uint32_t half2_of(uint32_t w) {
+  uint32_t h;
+  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((uint16_t)w));
+  return h;
+}
+__device__ __forceinline__ float pow2(int e) { return __int_as_float((e + 127) << 23); }   // -126 <= e <= 127
+// Bytes of x that are a NaN code, as a mask.
+__device__ __forceinline__ uint32_t nan_codes(uint32_t x) {
+  const uint32_t top = ((x & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
+  return (top >> 7) * 0xffu;
+}
+
 // ---- Host: argument checks and launches shared by the entry points -----------
 int paged8_view(const asr_paged8_cache* c, Paged8View* v);
 int paged8_rows(const asr_paged8_cache* c, const asr_paged_rows* r, int dtype, PagedRows* v);
 cudaError_t launch_append8(const Paged8View& c, const PagedRows& r, int dtype, cudaStream_t st);
+// Attention of many rows (dtype 1 or 2), whose K/V are in the pages.
+cudaError_t launch_prompt8(const Paged8View& c, const PagedRows& r, int dtype, void* out, float* lse, bool appended, cudaStream_t st);
 
 }  // namespace asrspec

@@ -31,18 +31,11 @@ struct Attend8Args : AttendArgs {
   Paged8View p;
 };
 
-// Two codes of the low half of w to fp16: .x the low byte.
-__device__ __forceinline__ uint32_t half2_of(uint32_t w) {
-  uint32_t h;
-  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((uint16_t)w));
-  return h;
-}
 __device__ __forceinline__ uint32_t transposed(uint32_t x) {   // of an 8 x 8 matrix of 16-bit values
   uint32_t y;
   asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
   return y;
 }
-__device__ __forceinline__ float pow2(int e) { return __int_as_float((e + 127) << 23); }   // -126 <= e <= 127
 
 template <int N> struct Bytes { uint32_t w[N / 4]; };
 template <int N> __device__ __forceinline__ Bytes<N> lds_bytes(uint32_t at) {
@@ -54,12 +47,6 @@ template <int N> __device__ __forceinline__ Bytes<N> lds_bytes(uint32_t at) {
   }
   return v;
 }
-// Bytes of x that are a NaN code, as a mask.
-__device__ __forceinline__ uint32_t nan_codes(uint32_t x) {
-  const uint32_t top = ((x & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
-  return (top >> 7) * 0xffu;
-}
-
 template <int D> struct Cfg8 { static constexpr int KS = 4096 / D, NG = KS / PG_GROUP; };   // keys and groups of a step
 
 // Where a run of steps lies: of every 32 groups a lane looks up one, page ids a
@@ -514,6 +501,8 @@ int asr_spec_paged8_attend(const asr_paged8_cache* c, const asr_paged_rows* r, i
   const bool appends = a.r.k_new != nullptr;
   if (appends && launch_append8(a.p, a.r, dtype, st) != cudaSuccess) return ASR_E_CUDA;
   a.r.k_new = a.r.v_new = nullptr;   // the rows are in the pages from here on
+  if (m_rows >= 64)
+    return launch_prompt8(a.p, a.r, dtype, out, lse, appends, st) == cudaSuccess ? ASR_OK : ASR_E_CUDA;
   a.c = a.p.c;
   a.out = static_cast<char*>(out);
   a.lse = lse;
