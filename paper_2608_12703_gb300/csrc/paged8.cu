@@ -20,18 +20,26 @@ __device__ __forceinline__ float scale_for(float amax) {
   return __int_as_float(max(e, 1) << 23);
 }
 
-template <typename T> __device__ __forceinline__ void unpack8(const char* p, float* x) {
-  uint4 v = __ldg(reinterpret_cast<const uint4*>(p));
-  const T* t = reinterpret_cast<const T*>(&v);
+// 8 elements as they come, and as floats.
+template <typename T> struct Eight {
+  uint4 v[sizeof(T) / 2];
+  __device__ __forceinline__ void load(const char* p) {
 #pragma unroll
-  for (int i = 0; i < 8; ++i) x[i] = to_f32(t[i]);
-}
-template <> __device__ __forceinline__ void unpack8<float>(const char* p, float* x) {
-  reinterpret_cast<float4*>(x)[0] = __ldg(reinterpret_cast<const float4*>(p));
-  reinterpret_cast<float4*>(x)[1] = __ldg(reinterpret_cast<const float4*>(p) + 1);
-}
+    for (int i = 0; i < (int)sizeof(T) / 2; ++i) v[i] = __ldg(reinterpret_cast<const uint4*>(p) + i);
+  }
+  __device__ __forceinline__ float at(int i) const {
+    if constexpr (sizeof(T) == 4) return __uint_as_float(reg_of(v[i / 4], i % 4));
+    else {
+      const uint16_t h = (uint16_t)(reg_of(v[0], i / 2) >> (i % 2 * 16));
+      return to_f32(*reinterpret_cast<const T*>(&h));
+    }
+  }
+};
 
 // Lanes take 8 elements of a row: rows of a group in passes of 32 / (D / 8).
+// Bound by HBM (new rows read, a quarter to half as many bytes of codes
+// written) for prompts, by the chain lengths -> rows -> maximum -> codes for
+// few rows; the rows' loads do not wait for the page's id.
 template <typename T, int D>
 __global__ void __launch_bounds__(256) append8_kernel(const Paged8View p, const PagedRows r, int max_groups, int tasks) {
   constexpr int CH = D / 8, AT_ONCE = 32 / CH, PASSES = PG_GROUP / AT_ONCE;
@@ -45,47 +53,64 @@ __global__ void __launch_bounds__(256) append8_kernel(const Paged8View p, const 
   const int grp = len / PG_GROUP + t2 % max_groups, slot0 = grp * PG_GROUP;
   if (rows == 0 || slot0 >= len + rows) return;
   const int pid = __ldg(p.c.table + b * p.c.table_stride + p.c.groups.div((uint32_t)grp));
+  const char* src = (is_v ? r.v_new : r.k_new) + b * r.n_b + kvh * r.n_h + lane % CH * (8 * (int)sizeof(T));
+  Eight<T> x[PASSES];
+#pragma unroll
+  for (int i = 0; i < PASSES; ++i) {
+    const int row = slot0 + i * AT_ONCE + lane / CH - len;
+    if (row >= 0 && row < rows) x[i].load(src + row * r.n_r);
+  }
   if ((unsigned)pid >= (unsigned)p.c.n_pages) {
     if (p.c.status && lane == 0) set_status(p.c.status, ST_BOUNDS);
     return;
   }
   float* scale_at = (is_v ? p.v_scale : p.k_scale) + p.scale_at(pid, kvh, grp);
-  char* codes = (is_v ? p.c.v : p.c.k) + paged_offset(p.c, pid, grp) + kvh * p.c.head_stride + lane % CH * 8;
-  const char* src = (is_v ? r.v_new : r.k_new) + b * r.n_b + kvh * r.n_h + lane % CH * (8 * (int)sizeof(T));
-  float x[PASSES][8], amax = 0.f;
+  const float own = slot0 < len ? *scale_at : 0.f;
+  float amax = 0.f;
 #pragma unroll
   for (int i = 0; i < PASSES; ++i) {
     const int row = slot0 + i * AT_ONCE + lane / CH - len;
     if (row < 0 || row >= rows) continue;
-    unpack8<T>(src + row * r.n_r, x[i]);
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const float a = fabsf(x[i][j]);
+      const float a = fabsf(x[i].at(j));
       if (a <= 3.4028235e38f) amax = fmaxf(amax, a);
-      else x[i][j] = __int_as_float(0x7fffffff);
     }
   }
-  const float own = slot0 < len ? *scale_at : 0.f;
   const float s = fmaxf(scale_for(warp_max(amax)), own);
   const bool anew = slot0 < len && s != own;
+  // powers of two from 2^-126 to 2^126 have an exact inverse; any other scale came from elsewhere
+  const bool exact = (__float_as_int(s) & 0x807fffff) == 0 && s <= 8.507059173e37f;
+  const float inv = exact ? __int_as_float((254 << 23) - __float_as_int(s)) : 1.f;
+  char* codes = (is_v ? p.c.v : p.c.k) + paged_offset(p.c, pid, grp) + kvh * p.c.head_stride + lane % CH * 8;
 #pragma unroll
   for (int i = 0; i < PASSES; ++i) {
     const int at = i * AT_ONCE + lane / CH, row = slot0 + at - len;
     if (row >= rows || (row < 0 && !anew)) continue;
     uint2* to = reinterpret_cast<uint2*>(codes + at * p.c.slot_stride);
+    float y[8];
     if (row < 0) {
       const uint2 c = *to;
       const uint32_t w[2] = {c.x, c.y};
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const float2 v = e4m3x2_value(w[j / 2] >> (j % 2 * 16));
-        x[i][2 * j] = v.x * own;
-        x[i][2 * j + 1] = v.y * own;
+        y[2 * j] = v.x * own;
+        y[2 * j + 1] = v.y * own;
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        y[j] = x[i].at(j);
+        if (!(fabsf(y[j]) <= 3.4028235e38f)) y[j] = __int_as_float(0x7fffffff);
       }
     }
     uint32_t c[4];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) c[j] = e4m3x2(x[i][2 * j] / s, x[i][2 * j + 1] / s);
+    for (int j = 0; j < 4; ++j) c[j] = e4m3x2(y[2 * j] * inv, y[2 * j + 1] * inv);
+    if (!exact)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) c[j] = e4m3x2(y[2 * j] / s, y[2 * j + 1] / s);
     *to = make_uint2(c[0] | c[1] << 16, c[2] | c[3] << 16);
   }
   __syncwarp();   // every lane has read the group's own scale

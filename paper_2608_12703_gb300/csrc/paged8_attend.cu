@@ -502,7 +502,7 @@ int asr_spec_paged8_attend(const asr_paged8_cache* c, const asr_paged_rows* r, i
   if (appends && launch_append8(a.p, a.r, dtype, st) != cudaSuccess) return ASR_E_CUDA;
   a.r.k_new = a.r.v_new = nullptr;   // the rows are in the pages from here on
   if (m_rows >= 64)
-    return launch_prompt8(a.p, a.r, dtype, out, lse, appends, st) == cudaSuccess ? ASR_OK : ASR_E_CUDA;
+    return launch_prompt8(a.p, a.r, dtype, out, lse, static_cast<int*>(ws), appends, st) == cudaSuccess ? ASR_OK : ASR_E_CUDA;
   a.c = a.p.c;
   a.out = static_cast<char*>(out);
   a.lse = lse;

@@ -1,15 +1,16 @@
 // Attention of prompts over an 8-bit paged cache: many rows a sequence, so that
 // the tensor cores and the exponentials bound it and not the cache's bytes.
 //
-// A block takes 256 rows of a sequence and K/V head (its rows times the query
-// heads that share the head), as two tiles of 128, and walks tiles of 128 keys:
-//   * 4 warps turn codes into fp16 in 128-byte-swizzled shared memory, two
+// One block an SM.  An item is 256 rows of a sequence and K/V head (its rows
+// times the query heads that share the head), as two tiles of 128; a block goes
+// through its items without a break, each part of it at its own pace, in tiles of 128 keys:
+//   * 3 warps turn codes into fp16 in 128-byte-swizzled shared memory, two
 //     stages of K and of V, a tile's loads in flight while the one before is
 //     converted; both row tiles use what they write;
 //   * one thread issues tcgen05.mma: S = q K^T (128 x 128, fp32 in tensor
 //     memory) and O += p V with p read from tensor memory, where it takes the
 //     place of the scores.  The two row tiles alternate, so that one's products
-//     run while the other's scores are being weighed;
+//     run while the other's scores are being weighed, and scores run ahead;
 //   * 4 warps a row tile, a thread a row, weigh the scores.  The first pass over them takes
 //     each group's maximum, the second the exponentials.  Running maximum and
 //     reference of the weights (as in the kernel for few rows) move only when
@@ -27,25 +28,26 @@
 namespace asrspec {
 namespace {
 
-constexpr int BM = 128, BN = 128, THREADS = 416;   // rows and keys of a tile; 8 warps weigh, 4 convert, 1 issues products
+constexpr int BM = 128, BN = 128, THREADS = 512;   // rows and keys of a tile; warps: 8 weigh, 3 convert K, 3 V, 1 issues products
 
 struct Prompt8Args {
   Paged8View p;
   PagedRows r;
   char* out;
   float* lse;
-  int tiles;   // of 256 rows
+  int tiles, items;   // of 256 rows
+  int *next, *done;   // zero between calls: items taken besides each block's first, blocks that are done
 };
 
 template <int D> struct Prompt8Mem {
   static constexpr int HB = D / 64, BLOCK = 16384;             // 64 columns of 128 rows
-  static constexpr int Q = 0, K = 2 * HB * BLOCK, V = K + 2 * HB * BLOCK, END = V + 2 * HB * BLOCK;
+  static constexpr int Q = 0, K = 2 * HB * BLOCK, V = K + 2 * HB * BLOCK, LENS = V + 2 * HB * BLOCK, END = LENS + 8 * PG_MAX_BATCH;
   // one block an SM: each takes all of tensor memory
   static constexpr int BYTES = (END < 120 * 1024 ? 120 * 1024 : END) + 1024;
 };
 
-struct Prompt8Bars {
-  uint64_t q_full[2], k_full[2], k_free[2], v_full[2], v_free[2], sc_full[4], s_full[2], p_full[2], o_full[2];
+struct Prompt8Bars {   // s, p: a buffer of scores; pv, q: a row tile
+  uint64_t q_full[2], k_full[2], k_free[2], v_full[2], v_free[2], sc_full[8], s_full[3], p_full[3], pv_done[2][4], item_full[4], ended[4];
 };
 struct GroupScales {   // of a tile's 8 groups
   float k[8], v[8], lv[8];
@@ -126,370 +128,492 @@ __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
   return d;
 }
 
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float d;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
+
+// A row's 128 scores, 32 at a time, the next ones on their way; f(q, s) for each.
+// Not unrolled further: this code and the other row tile's share an instruction cache.
+template <typename F>
+__device__ __forceinline__ void for_scores(uint32_t at, bool full, int left, F f) {
+  uint32_t s[2][32];
+  tmem_ld32(at, s[0]);
+#pragma unroll 1
+  for (int q2 = 0; q2 < 2; ++q2) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int q = q2 * 2 + h;
+      tmem_wait_ld();
+      if (h == 0 || q2 == 0) tmem_ld32(at + (q + 1) * 32, s[h ^ 1]);
+      if (!full)   // columns that the row does not see
+#pragma unroll
+        for (int i = 0; i < 32; ++i) s[h][i] = q * 32 + i < left ? s[h][i] : 0xff800000u;
+      f(q, s[h]);
+    }
+  }
+}
+
+// First look at a tile's scores: the row's maximum, and log2 of the largest weight
+// relative to the maximum mx.
+__device__ __forceinline__ void look(uint32_t at, bool full, int left, const GroupScales& gs, float mx, float sc, float& most, float& top) {
+  most = top = -INFINITY;
+  for_scores(at, full, left, [&](int q, uint32_t (&s)[32]) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const uint32_t* x = s + h * 16;
+      float g = fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1]));
+#pragma unroll
+      for (int i = 2; i < 16; i += 2) g = max3(g, __uint_as_float(x[i]), __uint_as_float(x[i + 1]));
+      g *= gs.k[q * 2 + h];
+      most = fmaxf(most, g);
+      top = fmaxf(top, (g - mx) * sc + gs.lv[q * 2 + h]);
+    }
+  });
+}
+// Second look: the weights take the scores' place; returns the sum of p.
+__device__ __forceinline__ float weigh(uint32_t at, bool full, int left, const GroupScales& gs, float base, float sc, float inv) {
+  const uint64_t base2 = two(-base, -base), sc2 = two(sc, sc);
+  uint64_t sum2 = 0;
+  for_scores(at, full, left, [&](int q, uint32_t (&s)[32]) {
+    uint32_t p[16];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const float ks = gs.k[q * 2 + h], f = fminf(gs.v[q * 2 + h] * inv, 8.507059173e37f);
+      const uint64_t ks2 = two(ks, ks), f2 = two(f, f);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int x = h * 16 + 2 * i;
+        const float2 t = parts(mul2(fma2(two(__uint_as_float(s[x]), __uint_as_float(s[x + 1])), ks2, base2), sc2));
+        const uint64_t e2 = two(ex2(t.x), ex2(t.y));
+        sum2 = add2(sum2, e2);
+        const float2 w = parts(mul2(e2, f2));
+        p[h * 8 + i] = Mma16<__half>::pack(w.x, w.y);
+      }
+    }
+    tmem_st16(at + q * 16, p);   // over scores that have been read: the next 32 lie past these 16 columns
+  });
+  const float2 sum = parts(sum2);
+  return sum.x + sum.y;
+}
+
+// What a block works on.
+struct Item {
+  int b, kvh, m0, len, rows, keys;
+  int n0, n1;   // key tiles of its two row tiles: up to what the last row sees
+  __device__ __forceinline__ int n() const { return max(n0, n1); }
+};
+__device__ __forceinline__ int seen_by(const PagedRows& r, int len, int m) { return r.causal ? len + (int)r.groups.div(m) + 1 : len; }
+
+// A block's items: the first by its number, each other one the next that no block has, in order of falling row tile (late
+// rows see most).  One thread fetches them, an item ahead, into four slots; a slot is free when everyone has left its item.
+struct Items {
+  const Prompt8Args& a;
+  Prompt8Bars& bars;
+  const int2* lens;
+  int* slots;
+  // item number i; false where it has no work
+  __device__ __forceinline__ bool set(int i, Item& it) const {
+    const int per = a.p.c.kv_heads * a.p.c.batch, tile = i / per, in = i - tile * per;
+    it.b = in / a.p.c.kv_heads, it.kvh = in - it.b * a.p.c.kv_heads;
+    it.m0 = (a.tiles - 1 - tile) * 2 * BM;
+    it.len = lens[it.b].x, it.rows = lens[it.b].y;
+    it.keys = it.rows == 0 ? 0 : it.len + (a.r.causal ? it.rows : 0);
+    const int m_rows = it.rows * a.r.group;
+    it.n0 = it.m0 >= m_rows ? 0 : (seen_by(a.r, it.len, min(it.m0 + BM, m_rows) - 1) + BN - 1) / BN;
+    it.n1 = it.m0 + BM >= m_rows ? 0 : (seen_by(a.r, it.len, min(it.m0 + 2 * BM, m_rows) - 1) + BN - 1) / BN;
+    return it.n0 > 0;
+  }
+  // the block's item k; false past the end
+  __device__ __forceinline__ bool take(int k, Item& it, bool& gave_up) const {
+    bar_wait(&bars.item_full[k & 3], k >> 2 & 1, a.p.c.status, gave_up);
+    const int i = gave_up ? -1 : *reinterpret_cast<volatile int*>(slots + (k & 3));
+    if (i < 0) return false;
+    return set(i, it);
+  }
+  __device__ __forceinline__ void fetch(int k, bool& gave_up) const {   // one thread
+    if (k >= 4) bar_wait(&bars.ended[k & 3], (k >> 2) - 1 & 1, a.p.c.status, gave_up);
+    Item it;
+    int i = k == 0 ? (int)blockIdx.x : (int)gridDim.x + atomicAdd(a.next, 1);
+    while (i < a.items && !set(i, it)) i = (int)gridDim.x + atomicAdd(a.next, 1);
+    slots[k & 3] = i < a.items ? i : -1;
+    mbar_arrive(&bars.item_full[k & 3]);
+  }
+  __device__ __forceinline__ void leave(int k) const { mbar_arrive(&bars.ended[k & 3]); }
+};
+// One arrival a warp, after all its lanes: arrivals at one barrier go one by one.
+__device__ __forceinline__ void warp_arrive(uint64_t* bar) {
+  __syncwarp();
+  if ((threadIdx.x & 31) == 0) mbar_arrive(bar);
+}
+
 template <typename T, int D>
 __global__ void __launch_bounds__(THREADS, 1) prompt8_kernel(const Prompt8Args a) {
   using M = Prompt8Mem<D>;
-  constexpr int HB = M::HB;
+  // Buffers of scores: with a third one a row tile's next scores are there before its weights are.  Tensor memory holds it beside outputs of 64.
+  constexpr int HB = M::HB, NS = D == 64 ? 3 : 2, O_COL = NS * BN;
+  static_assert(O_COL + 2 * D <= 512, "");
   extern __shared__ uint8_t raw[];
   __shared__ __align__(8) Prompt8Bars bars;
-  __shared__ GroupScales scales[4];
-  __shared__ int nan_key[D];      // of a column of V the first key whose code is a NaN
-  __shared__ int s_len, s_rows, s_any_nan;
+  __shared__ GroupScales scales[8];
+  __shared__ int nan_key[4][D];   // by item: of a column of V the first key whose code is a NaN
+  __shared__ int any_nan[4];
   __shared__ uint32_t s_tmem;
+  __shared__ int s_items[4];
   const uint32_t smem = (smem_u32(raw) + 1023) / 1024 * 1024;
+  int2* const lens = reinterpret_cast<int2*>(raw + (smem - smem_u32(raw)) + M::LENS);
   const PagedView& c = a.p.c;
   const PagedRows& r = a.r;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const int kvh = blockIdx.x % c.kv_heads, b = blockIdx.x / c.kv_heads % c.batch;
-  const int m0 = (a.tiles - 1 - (int)(blockIdx.x / c.kv_heads / c.batch)) * 2 * BM;   // late rows, which see most, first
 
   if (tid == 0) {
-    int len, rows;
-    paged_lens(c, r, b, len, rows);
-    s_len = len, s_rows = rows, s_any_nan = 0;
     for (int i = 0; i < 2; ++i) {
-      mbar_init(&bars.q_full[i], BM), mbar_init(&bars.k_full[i], 128), mbar_init(&bars.v_full[i], 128);
-      mbar_init(&bars.k_free[i], 1), mbar_init(&bars.v_free[i], 1), mbar_init(&bars.s_full[i], 1);
-      mbar_init(&bars.p_full[i], BM), mbar_init(&bars.o_full[i], 1);
+      mbar_init(&bars.q_full[i], 4), mbar_init(&bars.k_full[i], 3), mbar_init(&bars.v_full[i], 3);
+      mbar_init(&bars.k_free[i], 1), mbar_init(&bars.v_free[i], 1);
+      for (int j = 0; j < 4; ++j) mbar_init(&bars.pv_done[i][j], 1);
     }
-    for (int i = 0; i < 4; ++i) mbar_init(&bars.sc_full[i], 128);
+    for (int i = 0; i < 3; ++i) mbar_init(&bars.s_full[i], 1), mbar_init(&bars.p_full[i], 4);
+    for (int i = 0; i < 8; ++i) mbar_init(&bars.sc_full[i], 2);
+    for (int i = 0; i < 4; ++i) mbar_init(&bars.item_full[i], 1), mbar_init(&bars.ended[i], 8 + 5 + 1);
     fence_mbar_init();
   }
-  if (tid < D) nan_key[tid] = 0x7fffffff;
-  if (warp == 12) tmem_alloc(&s_tmem, 512), tmem_relinquish();
+  for (int b = tid; b < c.batch; b += THREADS) paged_lens(c, r, b, lens[b].x, lens[b].y);
+  if (warp == 14) tmem_alloc(&s_tmem, 512), tmem_relinquish();
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = s_tmem;
-  const int len = s_len, rows = s_rows, keys = rows == 0 ? 0 : len + (r.causal ? rows : 0), m_rows = rows * r.group;
-  // key tiles of each row tile: up to what its last row sees
-  auto seen_by = [&](int m) { return r.causal ? len + (int)r.groups.div(m) + 1 : len; };
-  auto tiles_of = [&](int x) {
-    const int first = m0 + x * BM;
-    return first >= m_rows ? 0 : (seen_by(min(first + BM, m_rows) - 1) + BN - 1) / BN;
-  };
-  const int n0 = tiles_of(0), n1 = tiles_of(1), n = max(n0, n1);
   bool gave_up = false;
-  pdl_wait();   // the append
+  for (int b = blockIdx.x; b < c.batch; b += gridDim.x) {   // rows past a sequence's own, or without keys
+    const int2 n = lens[b];
+    const int from = n.x + (r.causal ? n.y : 0) == 0 ? 0 : n.y;
+    const size_t heads0 = ((size_t)b * r.max_rows + from) * r.heads, count = (size_t)(r.max_rows - from) * r.heads;
+    uint4* o = reinterpret_cast<uint4*>(a.out + heads0 * D * sizeof(T));
+    for (size_t i = tid; i < count * (D * sizeof(T) / 16); i += THREADS) o[i] = make_uint4(0, 0, 0, 0);
+    if (a.lse)
+      for (size_t i = tid; i < count; i += THREADS) a.lse[heads0 + i] = -INFINITY;
+  }
+  const Items src{a, bars, lens, s_items};
+  pdl_wait();   // the append, and the call before, whose last block sets the counts back
 
+  // 8 warps of 168 registers and 8 of 88: what the block was launched with, 16 of 128
+  if (warp < 8) asm volatile("setmaxnreg.inc.sync.aligned.u32 168;");
+  else asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
   if (warp < 8) {
     // ------------------------------------------------------------ the weights of a row
-    const int x = warp >> 2, row_in = tid & 127, nx = x ? n1 : n0, m = m0 + x * BM + row_in;
-    const int row = (int)r.groups.div(m), hq = kvh * r.group + m - row * r.group;
-    const uint32_t lanes = (uint32_t)(warp & 3) << 21, s_at = tmem + lanes + x * BN, o_at = tmem + lanes + 2 * BN + x * D;
-    const bool mine = m < m_rows;
-    const int lim = mine ? min(keys, seen_by(m)) : 0, all_see = nx ? seen_by(m0 + x * BM) : 0;
-    float sc = r.scale * LOG2E;
-    if (nx > 0) {
-      const char* src = r.q + b * r.q_b + (long long)row * r.q_r + hq * r.q_h;
+    const int x = warp >> 2, row_in = tid & 127;
+    const uint32_t lanes = (uint32_t)(warp & 3) << 21, o_at = tmem + lanes + O_COL + x * D;
+    int pairs = 0, tiles = 0, steps = 0;   // begun before this item: pairs of the block, its key tiles, this row tile's
+    // q of an item, as fp16 rows in shared memory; returns the scale that its scores need.  The products with the q before are
+    // done: the last scores have come.
+    auto take_q = [&](const Item& it) {
+      const int m = it.m0 + x * BM + row_in, row = (int)r.groups.div(m), hq = it.kvh * r.group + m - row * r.group;
+      const bool mine = m < it.rows * r.group;
+      const char* src = r.q + it.b * r.q_b + (long long)row * r.q_r + hq * r.q_h;
       const uint32_t dst = smem + M::Q + x * HB * M::BLOCK + row_in * 128;
-      float f0 = 1.f, f1 = 1.f;
+      float sc = r.scale * LOG2E;
+      uint4 v[D / 8];
+#pragma unroll
+      for (int i = 0; i < D / 8; ++i) v[i] = ldg_if(mine, src + i * 16);
       if constexpr (!std::is_same<T, __half>::value) {   // to fp16 by a power of two: see the kernel for few rows
         uint32_t most = 0;
 #pragma unroll
-        for (int i = 0; i < D / 8; ++i) {
-          const uint4 v = ldg_if(mine, src + i * 16);
+        for (int i = 0; i < D / 8; ++i)
 #pragma unroll
-          for (int y = 0; y < 4; ++y) most = max(most, max(reg_of(v, y) & 0x7fffu, reg_of(v, y) >> 16 & 0x7fffu));
-        }
+          for (int y = 0; y < 4; ++y) most = max(most, max(reg_of(v[i], y) & 0x7fffu, reg_of(v[i], y) >> 16 & 0x7fffu));
         const int e = min(100, 14 - ((int)(most >> 7) - 127));
-        f0 = pow2(e / 2), f1 = pow2(e - e / 2);
+        const float f0 = pow2(e / 2), f1 = pow2(e - e / 2);
         sc = fmaxf(sc * pow2(-(e / 2)) * pow2(-(e - e / 2)), 1.17549435e-38f);
-      }
 #pragma unroll
-      for (int i = 0; i < D / 8; ++i) {
-        uint4 v = ldg_if(mine, src + i * 16);
-        if constexpr (!std::is_same<T, __half>::value) {
+        for (int i = 0; i < D / 8; ++i) {
           uint32_t y[4];
 #pragma unroll
           for (int z = 0; z < 4; ++z) {
-            const uint32_t w = reg_of(v, z);
+            const uint32_t w = reg_of(v[i], z);
             y[z] = Mma16<__half>::pack(__int_as_float(w << 16) * f0 * f1, __int_as_float(w & 0xffff0000u) * f0 * f1);
           }
-          v = make_uint4(y[0], y[1], y[2], y[3]);
+          v[i] = make_uint4(y[0], y[1], y[2], y[3]);
         }
-        sts16(dst + i / 8 * M::BLOCK + ((i % 8) ^ (row_in & 7)) * 16, v.x, v.y, v.z, v.w);
       }
+#pragma unroll
+      for (int i = 0; i < D / 8; ++i) sts16(dst + i / 8 * M::BLOCK + ((i % 8) ^ (row_in & 7)) * 16, v[i].x, v[i].y, v[i].z, v[i].w);
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-      mbar_arrive(&bars.q_full[x]);
-    }
-    float mx = -INFINITY, l = 0.f;   // the maximum, in units of the product; the sum of p
-    int li = 126;                    // log2 of what weights are multiplied by
-    for (int j = 0; j < nx; ++j) {
-      const GroupScales& gs = scales[j & 3];
-      bar_wait(&bars.sc_full[j & 3], j >> 2 & 1, c.status, gave_up);
-      bar_wait(&bars.s_full[x], j & 1, c.status, gave_up);
-      __syncwarp();
-      tc_fence_after();
-      const bool full = (j + 1) * BN <= all_see;   // of every row that counts
-      const int left = lim - j * BN;               // columns that this row sees
-      float gm[8];
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        uint32_t s[32];
-        tmem_ld32(s_at + q * 32, s);
-        tmem_wait_ld();
-        if (!full)
-#pragma unroll
-          for (int i = 0; i < 32; ++i) s[i] = q * 32 + i < left ? s[i] : 0xff800000u;
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          float g0 = __uint_as_float(s[h * 16]), g1 = __uint_as_float(s[h * 16 + 1]);
-#pragma unroll
-          for (int i = 2; i < 16; i += 2) g0 = fmaxf(g0, __uint_as_float(s[h * 16 + i])), g1 = fmaxf(g1, __uint_as_float(s[h * 16 + i + 1]));
-          gm[q * 2 + h] = fmaxf(g0, g1) * gs.k[q * 2 + h];
-        }
-      }
-      float most = gm[0], top = -INFINITY;
-#pragma unroll
-      for (int u = 1; u < 8; ++u) most = fmaxf(most, gm[u]);
-#pragma unroll
-      for (int u = 0; u < 8; ++u) top = fmaxf(top, (gm[u] - mx) * sc + gs.lv[u]);
-      if (__any_sync(0xffffffffu, (most - mx) * sc > 4.f || top + (float)li > 15.f)) {
-        float grown = 0.f;
-        int k = 0;
-        if (most > mx) {
-          grown = mx == -INFINITY ? 0.f : (most - mx) * sc;
-          k = min((int)fminf(grown, 1000.f), 126 - li);
-          mx = most, l *= ex2(-grown), li += k;
-        }
-        top = -INFINITY;
-#pragma unroll
-        for (int u = 0; u < 8; ++u) top = fmaxf(top, (gm[u] - mx) * sc + gs.lv[u]);
-        const int e = top + (float)li > 11.f ? min((int)ceilf(top) + li - 11, li + 126) : 0;
-        li -= e;
-        if (j > 0) {   // the products before have been added up: the scores' came after them
-          const float f = ex2((float)(k - e) - grown);
-          __syncwarp();
-#pragma unroll
-          for (int q = 0; q < D / 32; ++q) {
-            uint32_t o[32];
-            tmem_ld32(o_at + q * 32, o);
-            tmem_wait_ld();
-#pragma unroll
-            for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
-            tmem_st16(o_at + q * 32, o);
-            tmem_st16(o_at + q * 32 + 16, o + 16);
-          }
-        }
-      }
-      const float base = mx == -INFINITY ? 0.f : mx, inv = pow2(li);
-      const uint64_t base2 = two(-base, -base), sc2 = two(sc, sc);
-      uint64_t sum2 = 0;
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        uint32_t s[32], p[16];
-        tmem_ld32(s_at + q * 32, s);
-        tmem_wait_ld();
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const float ks = gs.k[q * 2 + h], f = fminf(gs.v[q * 2 + h] * inv, 8.507059173e37f);
-          const uint64_t ks2 = two(ks, ks), f2 = two(f, f);
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const int at = h * 16 + 2 * i;
-            float2 t = parts(mul2(fma2(two(__uint_as_float(s[at]), __uint_as_float(s[at + 1])), ks2, base2), sc2));
-            if (!full) t = make_float2(q * 32 + at < left ? t.x : -INFINITY, q * 32 + at + 1 < left ? t.y : -INFINITY);
-            const uint64_t e2 = two(ex2(t.x), ex2(t.y));
-            sum2 = add2(sum2, e2);
-            const float2 w = parts(mul2(e2, f2));
-            p[h * 8 + i] = Mma16<__half>::pack(w.x, w.y);
-          }
-        }
-        tmem_st16(s_at + q * 16, p);   // over scores that have been read
-      }
-      const float2 sum = parts(sum2);
-      l += sum.x + sum.y;
-      tmem_wait_st();
-      tc_fence_before();
-      mbar_arrive(&bars.p_full[x]);
-    }
-    // ---------------------------------------------------------------- the row's end
-    if (nx > 0) {
-      bar_wait(&bars.o_full[x], 0, c.status, gave_up);
-      __syncwarp();
-      tc_fence_after();
-    }
-    const size_t at = ((size_t)b * r.max_rows + row) * r.heads + hq;
-    T* out = reinterpret_cast<T*>(a.out) + at * D;
-    const bool there = row < r.max_rows;
-    const bool any_nan = *reinterpret_cast<volatile int*>(&s_any_nan) != 0;
-    const float f = lim > 0 && l != 0.f ? __fdividef(1.f, l) * pow2(-li) : 0.f;
-#pragma unroll
-    for (int q = 0; q < D / 32; ++q) {
-      uint32_t o[32];
-      if (nx > 0) {
+      warp_arrive(&bars.q_full[x]);
+      return sc;
+    };
+    Item it{};
+    float next_sc = 0.f;
+    bool more = true;
+    for (int k = -1; more; ++k) {   // before the first item one without rows
+      const int nx = x ? it.n1 : it.n0, m = it.m0 + x * BM + row_in;
+      const bool mine = m < it.rows * r.group;
+      const int lim = mine ? min(it.keys, seen_by(r, it.len, m)) : 0, all_see = nx ? seen_by(r, it.len, it.m0 + x * BM) : 0;
+      const float sc = next_sc;
+      if (nx == 0)   // keeps step with the other tile's: the waits to come are for the phase after these
+        for (int i = pairs; i < pairs + it.n0 + it.n1; ++i) bar_wait(&bars.s_full[i % NS], i / NS & 1, c.status, gave_up);
+      float mx = -INFINITY, l = 0.f;   // the maximum, in units of the product; the sum of p
+      int li = 126;                    // log2 of what weights are multiplied by
+      for (int j = 0; j < nx; ++j) {
+        const int pair = pairs + min(j, it.n0) + min(j, it.n1) + (x && j < it.n0), buf = pair % NS, tile = tiles + j;
+        const uint32_t s_at = tmem + lanes + buf * BN;
+        const GroupScales& gs = scales[tile & 7];
+        bar_wait(&bars.sc_full[tile & 7], tile >> 3 & 1, c.status, gave_up);
+        bar_wait(&bars.s_full[buf], pair / NS & 1, c.status, gave_up);
         __syncwarp();
-        tmem_ld32(o_at + q * 32, o);
-        tmem_wait_ld();
-      }
-#pragma unroll
-      for (int i = 0; i < 32; ++i) o[i] = lim > 0 ? __float_as_uint(__uint_as_float(o[i]) * f) : 0u;
-      if (any_nan)
-#pragma unroll
-        for (int i = 0; i < 32; ++i)
-          if (nan_key[q * 32 + i] < lim) o[i] = 0x7fffffffu;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        uint32_t w[4];
-#pragma unroll
-        for (int y = 0; y < 4; ++y) w[y] = Mma16<T>::pack(__uint_as_float(o[i * 8 + 2 * y]), __uint_as_float(o[i * 8 + 2 * y + 1]));
-        if (there) *reinterpret_cast<uint4*>(out + q * 32 + i * 8) = make_uint4(w[0], w[1], w[2], w[3]);
-      }
-    }
-    if (there && a.lse) a.lse[at] = lim > 0 ? (mx * sc + __log2f(l)) * LN2 : -INFINITY;
-    tc_fence_before();
-  } else if (warp < 12) {
-    // ------------------------------------------------------------ codes to fp16
-    constexpr int LK = D / 16, KI = 32 / LK, IT = 32 / KI;   // lanes a key, keys an instruction, instructions of a warp's 32 keys
-    const int w = warp - 8, key0 = w * 32 + lane / LK, col = lane % LK, groups = (keys + PG_GROUP - 1) / PG_GROUP;
-    const int* table_row = c.table + b * c.table_stride;
-    const long long head = kvh * c.head_stride + col * 16;
-    uint4 kc[IT], vc[IT];
-    int pid[2];
-    long long off[2];
-    float ks = 1.f, vs = 1.f;
-    auto look_up = [&](int j) {
-#pragma unroll
-      for (int g = 0; g < 2; ++g) {
-        const int grp = j * 8 + w * 2 + g;
-        pid[g] = grp < groups ? __ldg(table_row + c.groups.div((uint32_t)grp)) : 0;   // looked at when used
-      }
-    };
-    auto place = [&](int j) {   // pages of tile j, as looked up; its scales, a group a lane
-      const int g0 = j * 8 + w * 2;
-#pragma unroll
-      for (int g = 0; g < 2; ++g) off[g] = paged_offset(c, pid[g] = paged_valid(c, pid[g]), g0 + g) + head;
-      ks = vs = 1.f;
-      if (lane < 2 && g0 + lane < groups) {
-        const long long at = a.p.scale_at(lane ? pid[1] : pid[0], kvh, g0 + lane);
-        ks = __ldcg(a.p.k_scale + at), vs = __ldcg(a.p.v_scale + at);
-      }
-    };
-    auto load = [&](const char* pages, int j, uint4 (&x)[IT]) {
-#pragma unroll
-      for (int i = 0; i < IT; ++i) {
-        const int in = i * KI + lane / LK;
-        x[i] = ld_if_l2(j * BN + w * 32 + in < keys, pages + off[i * KI / PG_GROUP] + (in % PG_GROUP) * c.slot_stride);
-      }
-    };
-    auto store = [&](uint32_t dst, const uint4 (&x)[IT]) {
-#pragma unroll
-      for (int i = 0; i < IT; ++i) {
-        const int key = key0 + i * KI;
-        const uint32_t at = dst + col / 4 * M::BLOCK + key * 128;
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const uint32_t c0 = reg_of(x[i], 2 * h), c1 = reg_of(x[i], 2 * h + 1);
-          sts16(at + (((col % 4 * 2 + h) ^ (key & 7)) << 4), half2_of(c0), half2_of(c0 >> 16), half2_of(c1), half2_of(c1 >> 16));
+        tc_fence_after();
+        const bool full = (j + 1) * BN <= all_see;   // of every row that counts
+        const int left = lim - j * BN;               // columns that this row sees
+        float most, top;
+        float grown = 0.f;
+        int up = 0;
+#pragma unroll 1
+        for (bool again = false;; again = true) {   // the largest weight is relative to the maximum: where that grows, once more
+          look(s_at, full, left, gs, mx, sc, most, top);
+          if (again || !__any_sync(0xffffffffu, (most - mx) * sc > 4.f)) break;
+          if (most > mx) {
+            grown = mx == -INFINITY ? 0.f : (most - mx) * sc;
+            up = min((int)fminf(grown, 1000.f), 126 - li);
+            mx = most, l *= ex2(-grown), li += up;
+          }
+          __syncwarp();
         }
+        if (__any_sync(0xffffffffu, grown > 0.f || top + (float)li > 15.f)) {
+          const int e = top + (float)li > 11.f ? min((int)ceilf(top) + li - 11, li + 126) : 0;
+          li -= e;
+          if (j > 0) {   // the tile before has been added
+            const float f = ex2((float)(up - e) - grown);
+            // Four barriers in turn: a wait cannot tell a phase from the one after the next, and the tile of four steps ago is
+            // known to be done, since scores run ahead by fewer
+            bar_wait(&bars.pv_done[x][(steps + j - 1) & 3], (steps + j - 1) >> 2 & 1, c.status, gave_up);
+            __syncwarp();
+            tc_fence_after();
+#pragma unroll 1
+            for (int q = 0; q < D / 32; ++q) {
+              uint32_t o[32];
+              tmem_ld32(o_at + q * 32, o);
+              tmem_wait_ld();
+#pragma unroll
+              for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+              tmem_st16(o_at + q * 32, o);
+              tmem_st16(o_at + q * 32 + 16, o + 16);
+            }
+          }
+          __syncwarp();
+        }
+        const float base = mx == -INFINITY ? 0.f : mx, inv = pow2(li);
+        l += weigh(s_at, full, left, gs, base, sc, inv);
+        tmem_wait_st();
+        tc_fence_before();
+        warp_arrive(&bars.p_full[buf]);
+      }
+      pairs += it.n0 + it.n1, tiles += it.n(), steps += nx;
+      const Item was = it;
+      more = src.take(k + 1, it, gave_up);
+      if (more && (x ? it.n1 : it.n0) > 0) next_sc = take_q(it);
+      if (k < 0) continue;
+      // -------------------------------------------------------------- the rows' ends
+      if (nx > 0) {
+        bar_wait(&bars.pv_done[x][(steps - 1) & 3], (steps - 1) >> 2 & 1, c.status, gave_up);
+        __syncwarp();
+        tc_fence_after();
+      }
+      const int row = (int)r.groups.div(m), hq = was.kvh * r.group + m - row * r.group;
+      const size_t at = ((size_t)was.b * r.max_rows + row) * r.heads + hq;
+      T* out = reinterpret_cast<T*>(a.out) + at * D;
+      const bool nans = *reinterpret_cast<volatile int*>(&any_nan[k & 3]) != 0;
+      const float f = l != 0.f ? __fdividef(1.f, l) * pow2(-li) : 0.f;
+#pragma unroll 1
+      for (int q = 0; q < D / 32; ++q) {
+        uint32_t o[32];
+        if (nx > 0) {
+          __syncwarp();
+          tmem_ld32(o_at + q * 32, o);
+          tmem_wait_ld();
+        }
+#pragma unroll
+        for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+        if (nans)
+#pragma unroll
+          for (int i = 0; i < 32; ++i)
+            if (nan_key[k & 3][q * 32 + i] < lim) o[i] = 0x7fffffffu;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          uint32_t w[4];
+#pragma unroll
+          for (int y = 0; y < 4; ++y) w[y] = Mma16<T>::pack(__uint_as_float(o[i * 8 + 2 * y]), __uint_as_float(o[i * 8 + 2 * y + 1]));
+          if (mine) *reinterpret_cast<uint4*>(out + q * 32 + i * 8) = make_uint4(w[0], w[1], w[2], w[3]);
+        }
+      }
+      if (mine && a.lse) a.lse[at] = (mx * sc + __log2f(l)) * LN2;
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) src.leave(k);
+    }
+  } else if (warp < 14) {
+    // ------------------------------------------------------------ codes to fp16
+    // Of K or of V.  A warp takes every third of a tile's 8 groups; LK lanes a key, KI keys an instruction, IT instructions a
+    // group.  Of every 32 groups of an item, four tiles, a lane looks up one: its place, its scale, the next round's page.
+    constexpr int LK = D / 16, KI = 32 / LK, IT = PG_GROUP / KI, MINE = 3;
+    const bool is_v = warp >= 11;
+    const int w = is_v ? warp - 11 : warp - 8, col = lane % LK;
+    const char* pages = (is_v ? c.v : c.k) + col * 16 + lane / LK * c.slot_stride;
+    const float* scale_pages = is_v ? a.p.v_scale : a.p.k_scale;
+    uint64_t *full = is_v ? bars.v_full : bars.k_full, *free = is_v ? bars.v_free : bars.k_free;
+    const uint32_t stages = smem + (is_v ? M::V : M::K);
+    const long long step = KI * c.slot_stride;
+    Item it;
+    int k = -1, j = 0, next_pid = 0;
+    long long off = 0;
+    float scale = 1.f;
+    uint4 x[MINE][IT];
+    bool more;
+    auto take = [&] {
+      ++k;
+      if (tid == 8 * 32) src.fetch(k, gave_up);
+      __syncwarp();
+      more = src.take(k, it, gave_up);
+      j = 0;
+    };
+    auto load = [&] {   // of tile j
+      const int groups = (it.keys + PG_GROUP - 1) / PG_GROUP;
+      if (j % 4 == 0) {
+        const int grp = j * 8 + lane;
+        auto page = [&](int g) { return g < groups ? __ldg(c.table + it.b * c.table_stride + c.groups.div((uint32_t)g)) : 0; };
+        const int pid = paged_valid(c, j == 0 ? page(grp) : next_pid);
+        off = paged_offset(c, pid, grp) + it.kvh * c.head_stride;
+        scale = grp < groups ? __ldcg(scale_pages + a.p.scale_at(pid, it.kvh, grp)) : 1.f;
+        next_pid = page(grp + 32);   // looked at when used
+      }
+      const bool whole = (j + 1) * BN <= it.keys;
+#pragma unroll
+      for (int g = 0; g < MINE; ++g) {
+        const int in = w + 3 * g;
+        const char* at = pages + __shfl_sync(0xffffffffu, off, (j % 4 * 8 + in) & 31);
+        const int left = in >= 8 ? 0 : whole ? PG_GROUP : it.keys - j * BN - in * PG_GROUP;
+#pragma unroll
+        for (int i = 0; i < IT; ++i) x[g][i] = ld_if_l2(i * KI + lane / LK < left, at + i * step);
+      }
+    };
+    take();
+    if (more) load();
+    for (int tile = 0; more; ++tile) {
+      const int st = tile & 1;
+      if (w == 0) {   // the tile's scales
+        GroupScales& gs = scales[tile & 7];
+        if (lane / 8 == j % 4) {
+          if (is_v) gs.v[lane % 8] = scale, gs.lv[lane % 8] = fmaxf(__log2f(scale), -126.f);
+          else gs.k[lane % 8] = fmaxf(scale, 1.17549435e-38f);   // times -inf, where a score is hidden, it must stay that
+        }
+        warp_arrive(&bars.sc_full[tile & 7]);
+      }
+      if (is_v) {
+        const int slot = k & 3;
+        if (j == 0) {   // everyone has left the item that had this slot
+          for (int i = w * 32 + lane; i < D; i += 96) nan_key[slot][i] = 0x7fffffff;
+          if (w == 0 && lane == 0) any_nan[slot] = 0;
+          asm volatile("bar.sync 1, 96;" ::: "memory");
+        }
+        uint32_t bad = 0;
+#pragma unroll
+        for (int g = 0; g < MINE; ++g)
+#pragma unroll
+          for (int i = 0; i < IT; ++i)
+#pragma unroll
+            for (int y = 0; y < 4; ++y) bad |= (reg_of(x[g][i], y) & 0x7f7f7f7fu) + 0x01010101u;
+        if (bad & 0x80808080u) {
+          any_nan[slot] = 1;
+#pragma unroll
+          for (int g = 0; g < MINE; ++g)
+#pragma unroll
+            for (int i = 0; i < IT; ++i) {
+              uint4& v = x[g][i];
+#pragma unroll 1
+              for (int y = 0; y < 16; ++y)
+                if (nan_codes(reg_of(v, y / 4)) >> (y % 4 * 8) & 1)
+                  atomicMin(&nan_key[slot][col * 16 + y], j * BN + (w + 3 * g) * PG_GROUP + i * KI + lane / LK);
+              v.x &= ~nan_codes(v.x), v.y &= ~nan_codes(v.y), v.z &= ~nan_codes(v.z), v.w &= ~nan_codes(v.w);
+            }
+        }
+      }
+      if (tile >= 2) bar_wait(&free[st], (tile >> 1) - 1 & 1, c.status, gave_up);
+      const uint32_t dst = stages + st * HB * M::BLOCK + col / 4 * M::BLOCK + (w * PG_GROUP + lane / LK) * 128;
+#pragma unroll
+      for (int g = 0; g < MINE; ++g) {
+        if (w + 3 * g >= 8) break;
+#pragma unroll
+        for (int i = 0; i < IT; ++i)
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const uint32_t c0 = reg_of(x[g][i], 2 * h), c1 = reg_of(x[g][i], 2 * h + 1);
+            sts16(dst + (3 * g * PG_GROUP + i * KI) * 128 + (((col % 4 * 2 + h) ^ ((i * KI + lane / LK) & 7)) << 4), half2_of(c0),
+                  half2_of(c0 >> 16), half2_of(c1), half2_of(c1 >> 16));
+          }
       }
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-    };
-    if (n > 0) {
-      look_up(0);
-      place(0);
-      load(c.k, 0, kc);
-      load(c.v, 0, vc);
-      look_up(1);
+      warp_arrive(&full[st]);
+      if (++j >= it.n()) {
+        if (warp != 8 && lane == 0) src.leave(k);
+        take();
+      }
+      if (more) load();
     }
-    for (int j = 0; j < n; ++j) {
-      const int st = j & 1;
-      if (lane < 2) {
-        GroupScales& gs = scales[j & 3];
-        gs.k[w * 2 + lane] = ks, gs.v[w * 2 + lane] = vs;
-        gs.lv[w * 2 + lane] = fmaxf(__log2f(vs), -126.f);
-      }
-      mbar_arrive(&bars.sc_full[j & 3]);
-      if (j >= 2) bar_wait(&bars.k_free[st], (j >> 1) - 1 & 1, c.status, gave_up);
-      store(smem + M::K + st * HB * M::BLOCK, kc);
-      mbar_arrive(&bars.k_full[st]);
-      const bool more = j + 1 < n;
-      if (more) {
-        place(j + 1);
-        load(c.k, j + 1, kc);
-      }
-      uint32_t bad = 0;
-#pragma unroll
-      for (int i = 0; i < IT; ++i) bad |= nan_codes(vc[i].x) | nan_codes(vc[i].y) | nan_codes(vc[i].z) | nan_codes(vc[i].w);
-      if (bad) {
-        s_any_nan = 1;
-#pragma unroll 1
-        for (int i = 0; i < IT; ++i) {
-          uint4 v = make_uint4(0, 0, 0, 0);
-#pragma unroll
-          for (int y = 0; y < IT; ++y)
-            if (y == i) v = vc[y];
-#pragma unroll 1
-          for (int y = 0; y < 16; ++y)
-            if (nan_codes(reg_of(v, y / 4)) >> (y % 4 * 8) & 1) atomicMin(&nan_key[col * 16 + y], j * BN + key0 + i * KI);
-        }
-#pragma unroll
-        for (int i = 0; i < IT; ++i) {
-          vc[i].x &= ~nan_codes(vc[i].x), vc[i].y &= ~nan_codes(vc[i].y);
-          vc[i].z &= ~nan_codes(vc[i].z), vc[i].w &= ~nan_codes(vc[i].w);
-        }
-      }
-      if (j >= 2) bar_wait(&bars.v_free[st], (j >> 1) - 1 & 1, c.status, gave_up);
-      store(smem + M::V + st * HB * M::BLOCK, vc);
-      mbar_arrive(&bars.v_full[st]);
-      if (more) {
-        load(c.v, j + 1, vc);
-        look_up(j + 2);
-      }
-    }
-  } else if (lane == 0) {
+  } else if (warp == 14 && lane == 0) {
     // ------------------------------------------------------------ products
     constexpr uint32_t F32 = 1u << 4, M128 = (uint32_t)(BM >> 4) << 24;   // accumulator type; fp16 operands are 0
     constexpr uint32_t id_s = F32 | M128 | (uint32_t)(BN >> 3) << 17, id_o = F32 | M128 | 8u << 17 | 1u << 16;   // V: contraction axis outermost
-    auto scores = [&](int x, int j) {
-      const uint32_t q = smem + M::Q + x * HB * M::BLOCK, k = smem + M::K + (j & 1) * HB * M::BLOCK;
-#pragma unroll
-      for (int h = 0; h < HB; ++h)
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          umma_f16(tmem + x * BN, umma_desc_sw128(q + h * M::BLOCK + i * 32), umma_desc_sw128(k + h * M::BLOCK + i * 32), id_s, h + i > 0);
-      umma_commit(&bars.s_full[x]);
-    };
-    if (n > 0) bar_wait(&bars.k_full[0], 0, c.status, gave_up);
-    for (int x = 0; x < 2; ++x)
-      if ((x ? n1 : n0) > 0) {
-        bar_wait(&bars.q_full[x], 0, c.status, gave_up);
-        tc_fence_after();
-        scores(x, 0);
-      }
-    if (n > 0) umma_commit(&bars.k_free[0]);
-    for (int j = 0; j < n; ++j) {
-      bar_wait(&bars.v_full[j & 1], j >> 1 & 1, c.status, gave_up);
-      if (j + 1 < n) bar_wait(&bars.k_full[j + 1 & 1], (j + 1) >> 1 & 1, c.status, gave_up);
-      for (int x = 0; x < 2; ++x) {
-        const int nx = x ? n1 : n0;
-        if (j < nx) {
-          bar_wait(&bars.p_full[x], j & 1, c.status, gave_up);
+    const uint64_t qd = umma_desc_sw128(smem + M::Q), kd = umma_desc_sw128(smem + M::K), vd = desc_mn(smem + M::V);
+    constexpr uint32_t STEP = HB * M::BLOCK / 16;    // between q's of row tiles, between stages, in a descriptor's units
+    int pairs = 0, tiles = 0, qs0 = 0, qs1 = 0, pv0 = 0, pv1 = 0;   // pairs and key tiles before this item; of each row tile: q's, outputs begun
+    Item it;
+    for (int k = 0; src.take(k, it, gave_up); ++k) {
+      const int n = it.n0 + it.n1;
+      // Scores run ahead of outputs by all buffers but one, within an item: the next one's q comes from threads that may
+      // wait for outputs.  Pair i: key tile i / 2 of row tile i % 2, the last one of row tile 1; of row tile 0 alone i.
+      for (int i = 0; i < n + NS - 1; ++i) {
+        if (i < n) {
+          const int x = it.n1 == 0 ? 0 : i < 2 * it.n0 ? i & 1 : 1, j = it.n1 == 0 ? i : i >> 1, st = tiles + j & 1;
+          if (j == 0) bar_wait(&bars.q_full[x], (x ? qs1++ : qs0++) & 1, c.status, gave_up);
+          bar_wait(&bars.k_full[st], tiles + j >> 1 & 1, c.status, gave_up);
           tc_fence_after();
-          const uint32_t v = smem + M::V + (j & 1) * HB * M::BLOCK;
+          const int buf = (pairs + i) % NS;
 #pragma unroll
           for (int h = 0; h < HB; ++h)
 #pragma unroll
-            for (int i = 0; i < BN / 16; ++i)
-              umma_f16_ts(tmem + 2 * BN + x * D + h * 64, tmem + x * BN + i * 8, desc_mn(v + h * M::BLOCK + i * 2048), id_o, j + i > 0);
-          if (j + 1 == nx) umma_commit(&bars.o_full[x]);
+            for (int y = 0; y < 4; ++y)
+              umma_f16(tmem + buf * BN, qd + x * STEP + h * (M::BLOCK / 16) + y * 2, kd + st * STEP + h * (M::BLOCK / 16) + y * 2, id_s, h + y > 0);
+          umma_commit(&bars.s_full[buf]);
+          if (x == 1 || j >= it.n1) umma_commit(&bars.k_free[st]);
         }
-        if (x) umma_commit(&bars.v_free[j & 1]);
-        if (j + 1 < nx) scores(x, j + 1);
-        if (x && j + 1 < n) umma_commit(&bars.k_free[j + 1 & 1]);
+        if (i >= NS - 1) {
+          const int o = i - (NS - 1), x = it.n1 == 0 ? 0 : o < 2 * it.n0 ? o & 1 : 1, j = it.n1 == 0 ? o : o >> 1, st = tiles + j & 1;
+          const int buf = (pairs + o) % NS;
+          bar_wait(&bars.v_full[st], tiles + j >> 1 & 1, c.status, gave_up);
+          bar_wait(&bars.p_full[buf], (pairs + o) / NS & 1, c.status, gave_up);
+          tc_fence_after();
+#pragma unroll
+          for (int h = 0; h < HB; ++h)
+#pragma unroll
+            for (int y = 0; y < BN / 16; ++y)
+              umma_f16_ts(tmem + O_COL + x * D + h * 64, tmem + buf * BN + y * 8, vd + st * STEP + h * (M::BLOCK / 16) + y * 128, id_o, j + y > 0);
+          umma_commit(&bars.pv_done[x][(x ? pv1++ : pv0++) & 3]);
+          if (x == 1 || j >= it.n1) umma_commit(&bars.v_free[st]);
+        }
       }
+      pairs += n, tiles += it.n();
+      src.leave(k);
     }
   }
   __syncwarp();
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
-  if (warp == 12) tmem_dealloc(tmem, 512);
+  if (warp == 14) tmem_dealloc(tmem, 512);
+  if (tid == 0 && atomicAdd(a.done, 1) == (int)gridDim.x - 1) *a.next = 0, *a.done = 0;   // as the next call needs them
 }
 
 template <typename T, int D>
-cudaError_t launch_d(const Prompt8Args& a, bool appended, cudaStream_t st) {
+cudaError_t launch_d(Prompt8Args& a, bool appended, cudaStream_t st) {
   constexpr auto kernel = prompt8_kernel<T, D>;
   static std::atomic<uint64_t> ready{0};
   int dev = 0;
@@ -501,15 +625,18 @@ cudaError_t launch_d(const Prompt8Args& a, bool appended, cudaStream_t st) {
     if (e != cudaSuccess) return e;
     ready.fetch_or(bit, std::memory_order_release);
   }
-  const long long blocks = (long long)a.tiles * a.p.c.kv_heads * a.p.c.batch;
-  return launch_ex(kernel, dim3((unsigned)blocks), dim3(THREADS), Prompt8Mem<D>::BYTES, st, appended, 1, a);
+  const int sms = paged_sm_count(), grid = a.items < sms ? a.items : sms;
+  return launch_ex(kernel, dim3((unsigned)grid), dim3(THREADS), Prompt8Mem<D>::BYTES, st, appended, 1, a);
 }
 
 }  // namespace
 
-cudaError_t launch_prompt8(const Paged8View& c, const PagedRows& r, int dtype, void* out, float* lse, bool appended, cudaStream_t st) {
-  Prompt8Args a{c, r, static_cast<char*>(out), lse, (r.max_rows * r.group + 2 * BM - 1) / (2 * BM)};
-  if ((long long)a.tiles * c.c.kv_heads * c.c.batch > 0x7fffffffll) return cudaErrorInvalidValue;
+cudaError_t launch_prompt8(const Paged8View& c, const PagedRows& r, int dtype, void* out, float* lse, int* counts, bool appended,
+                           cudaStream_t st) {
+  const int tiles = (r.max_rows * r.group + 2 * BM - 1) / (2 * BM);
+  const long long items = (long long)tiles * c.c.kv_heads * c.c.batch;
+  if (items > 0x7fffffffll - 100000) return cudaErrorInvalidValue;
+  Prompt8Args a{c, r, static_cast<char*>(out), lse, tiles, (int)items, counts, counts + 1};
   if (dtype == 1) return c.dim == 64 ? launch_d<__nv_bfloat16, 64>(a, appended, st) : launch_d<__nv_bfloat16, 128>(a, appended, st);
   return c.dim == 64 ? launch_d<__half, 64>(a, appended, st) : launch_d<__half, 128>(a, appended, st);
 }

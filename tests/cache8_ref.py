@@ -6,7 +6,7 @@ import math
 import numpy as np
 import torch
 
-from serving_ref import EPS_OUT, score_bound
+from serving_ref import EPS_OUT
 
 GROUP = 16
 
@@ -56,35 +56,43 @@ def slots(pages, scales, table_row, n):
 def attend(q, k, v, ks, vs, table, lens, rows, causal, scale):
     """out, lse and bounds on both (float64), of rows whose K/V are in the pages already."""
     B, R, H, D = q.shape
-    K = k.shape[1]
+    G = H // k.shape[1]
     out = torch.zeros((B, R, H, D), dtype=torch.float64, device=q.device)
     lse = torch.full((B, R, H), -math.inf, dtype=torch.float64, device=q.device)
     ob, lb = torch.zeros_like(out), torch.zeros_like(lse)
     for b in range(B):
         n, r = lens[b], rows[b]
-        if r == 0 or n + (r if causal else 0) == 0:
+        end = n + (r if causal else 0)
+        if r == 0 or end == 0:
             continue
-        kk, _ = slots(k, ks, table[b], n + (r if causal else 0))
-        vv, vg = slots(v, vs, table[b], n + (r if causal else 0))
-        for i in range(r):
-            end = n + i + 1 if causal else n
-            for h in range(H):
-                c, qq = h // (H // K), q[b, i, h].double()
-                x = scale * (kk[:end, c] @ qq)
-                l = torch.logsumexp(x, 0)
-                p = torch.exp(x - l)
-                out[b, i, h], lse[b, i, h] = p @ vv[:end, c], l
-                # scores: fp32 sums; exp2 and its argument; statistics in fp32
-                ds = score_bound(qq, kk[:end, c], scale).max()
-                lb[b, i, h] = ds + 2.0 ** -20 * (1 + l.abs() + x.abs().max()) + end * 2.0 ** -23
-                # weights: the scores' error twice (numerator, sum), their rounding to fp16 (half a step, 2^-11 of the weight;
-                # a subnormal one is off by half of 2^-24, the largest being 2^14 or more: 2^-39 of the largest weight times
-                # scale, times codes of 448 at most), sums of `end` fp32 terms, the output's own rounding
-                rel = 2 * ds + 2.0 ** -20 * (1 + x.abs().max()) + 2.0 ** -11 + end * 2.0 ** -23
-                low = end * 2.0 ** -39 * 448 * (p * vg[:end, c]).max()
-                ob[b, i, h] = rel * (p @ vv[:end, c].abs()) + low + EPS_OUT[q.dtype] * out[b, i, h].abs() * 1.01 + 1e-30
-                if q.dtype == torch.float16:
-                    ob[b, i, h] += 2.0 ** -25   # a subnormal output
+        kk, _ = slots(k, ks, table[b], end)
+        vv, vg = slots(v, vs, table[b], end)
+        # slots that row i sees, [r, 1]
+        seen = (torch.arange(r, device=q.device) + n + 1 if causal else torch.full((r,), n, device=q.device))[:, None]
+        hidden = torch.arange(end, device=q.device)[None, :] >= seen
+        for h in range(H):
+            kh, vh, qh = kk[:, h // G], vv[:, h // G], q[b, :r, h].double()
+            x = (scale * (qh @ kh.T)).masked_fill(hidden, -math.inf)
+            l = torch.logsumexp(x, 1)
+            p = torch.exp(x - l[:, None])
+            # a hidden slot adds nothing, whatever it holds
+            bad = ~torch.isfinite(vh)
+            o = p @ vh.masked_fill(bad, 0.0)
+            o = torch.where((~hidden).double() @ bad.double() > 0, math.nan, o)
+            out[b, :r, h], lse[b, :r, h] = o, l
+            # scores: fp32 sums; exp2 and its argument; statistics in fp32
+            ds = (D + 8) * 2.0 ** -22 * scale * (qh.abs() @ kh.abs().T).masked_fill(hidden, 0.0).amax(dim=1)
+            most = x.abs().masked_fill(hidden, 0.0).amax(dim=1)
+            lb[b, :r, h] = ds + 2.0 ** -20 * (1 + l.abs() + most) + seen[:, 0] * 2.0 ** -23
+            # weights: the scores' error twice (numerator, sum), their rounding to fp16 (half a step, 2^-11 of the weight; a
+            # subnormal one is off by half of 2^-24, and the largest of a row is 2^10 or more: 2^-35 of the largest weight times
+            # scale, times codes of 448 at most), sums of `seen` fp32 terms, the output's own rounding
+            rel = 2 * ds + 2.0 ** -20 * (1 + most) + 2.0 ** -11 + seen[:, 0] * 2.0 ** -23
+            low = seen[:, 0] * 2.0 ** -35 * 448 * (p * vg[:, h // G][None, :]).amax(dim=1)
+            bound = rel[:, None] * (p @ vh.abs().masked_fill(bad, 0.0)) + low[:, None] + EPS_OUT[q.dtype] * o.abs() * 1.01 + 1e-30
+            if q.dtype == torch.float16:
+                bound += 2.0 ** -25   # a subnormal output
+            ob[b, :r, h] = bound
     return out, lse, ob, lb
 
 

@@ -145,6 +145,15 @@ def test_attend_prompts(built_lib, cuda, dtype, dim, heads, kv_heads, R):
     check(gen(9), DT[dtype], dim, heads, kv_heads, 16, R, lens, rows, causal=False, fused=False)
 
 
+@pytest.mark.parametrize("dtype,dim,causal", [("bf16", 64, True), ("fp16", 64, False), ("bf16", 128, True), ("fp16", 128, False)])
+def test_attend_many_prompts(built_lib, cuda, dtype, dim, causal):
+    """Many prompts a block, of one row tile and of several, with sequences that sit out and that see nothing between them."""
+    g, B, K = gen(dim), 40, 24
+    R = 290
+    rows = [(0, 70, R, 128, 200, 129, 256, 1, 257, 65)[i % 10] for i in range(B)]
+    check(g, DT[dtype], dim, K, K, 16, R, [(i * 29) % 300 if i % 7 else 0 for i in range(B)], rows, causal=causal)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "fp16"])
 @pytest.mark.parametrize("R", [2, 70])
 def test_attend_scales(built_lib, cuda, dtype, R):
