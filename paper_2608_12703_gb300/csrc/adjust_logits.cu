@@ -38,7 +38,7 @@ template <> struct Word<16> { using type = uint4; };
 
 // W elements an access, J accesses a thread and row: token base + (j * THREADS + thread) * W + w.
 template <typename T, int W, int J>
-__global__ void __launch_bounds__(THREADS) adjust_kernel(const AdjustArgs a) {
+__global__ void __launch_bounds__(THREADS, 6) adjust_kernel(const AdjustArgs a) {
   constexpr int RUN = THREADS * W * J;
   using Access = typename Word<W * sizeof(T)>::type;
   __shared__ int seen[RUN];   // 2 * count + (seen at all)
@@ -54,6 +54,43 @@ __global__ void __launch_bounds__(THREADS) adjust_kernel(const AdjustArgs a) {
   const int row0 = blockIdx.y * a.rows_each, row1 = min(n + 1, row0 + a.rows_each);
   if (row0 >= row1 && !reports) return;
 
+  union Part {
+    Access word;
+    T x[W];
+    __device__ Part() {}
+  };
+  // This thread's accesses: whole, beyond the end, or (one thread, where W does not divide the vocabulary) with a ragged one.
+  const int tok0 = base + tid * W;
+  bool whole[J], ragged = false;
+#pragma unroll
+  for (int j = 0; j < J; ++j) {
+    const int tok = tok0 + j * THREADS * W;
+    whole[j] = tok + W <= r.vocab;
+    ragged |= W > 1 && tok < r.vocab && !whole[j];
+  }
+  const char* src = static_cast<const char*>(r.logits) + b * a.batch + row0 * a.row + tok0 * (long long)sizeof(T);
+  char* dst = static_cast<char*>(r.out) + b * a.out_batch + row0 * a.out_row + tok0 * (long long)sizeof(T);
+  const int* words = r.mask + (b * r.mask_batch_stride + row0 * r.mask_row_stride + tok0 / 32);   // 32 divides THREADS * W
+  const int bit = tok0 % 32;
+  // the next row is on its way while this one is worked on, the first two while the history is counted
+  Part in[2][J];
+  uint32_t allowed[2][J];
+  auto load = [&](Part (&x)[J], uint32_t (&m)[J]) {
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+      m[j] = r.mask && tok0 + j * THREADS * W < r.vocab ? (uint32_t)__ldg(words + j * (THREADS * W / 32)) >> bit : 0xffffffffu;
+      if (whole[j]) x[j].word = *reinterpret_cast<const Access*>(src + j * (THREADS * W * (int)sizeof(T)));
+    }
+    if (ragged)
+#pragma unroll
+      for (int j = 0; j < J; ++j)
+#pragma unroll
+        for (int w = 0; w < W; ++w)
+          if (!whole[j] && tok0 + j * THREADS * W + w < r.vocab) x[j].x[w] = reinterpret_cast<const T*>(src)[j * THREADS * W + w];
+    src += a.row, words += r.mask_row_stride;
+  };
+  if (row0 < row1) load(in[0], allowed[0]);
+  if (row0 + 1 < row1) load(in[1], allowed[1]);
   float bias[J][W];
 #pragma unroll
   for (int j = 0; j < J; ++j)
@@ -90,55 +127,40 @@ __global__ void __launch_bounds__(THREADS) adjust_kernel(const AdjustArgs a) {
   const float rep = r.repetition ? r.repetition[b] : r.repetition_all;
   const float freq = r.frequency ? r.frequency[b] : r.frequency_all, pres = r.presence ? r.presence[b] : r.presence_all;
 
-  union Part {
-    Access word;
-    T x[W];
-    __device__ Part() {}
-  };
-  // the next row is on its way while this one is worked on
-  Part in[2][J];
-  uint32_t allowed[2][J];
-  auto load = [&](int row, Part (&x)[J], uint32_t (&m)[J]) {
-    const T* p = reinterpret_cast<const T*>(static_cast<const char*>(r.logits) + b * a.batch + row * a.row);
+  int any = 0;   // of this thread's tokens
 #pragma unroll
-    for (int j = 0; j < J; ++j) {
-      const int tok = base + (j * THREADS + tid) * W;
-      m[j] = 0xffffffffu;
-      if (r.mask && tok < r.vocab)
-        m[j] = (uint32_t)__ldg(r.mask + b * r.mask_batch_stride + row * r.mask_row_stride + tok / 32) >> (tok % 32);
-      if (tok + W <= r.vocab) {
-        x[j].word = *reinterpret_cast<const Access*>(p + tok);
-      } else {
+  for (int j = 0; j < J; ++j)
 #pragma unroll
-        for (int w = 0; w < W; ++w)
-          if (tok + w < r.vocab) x[j].x[w] = p[tok + w];
-      }
-    }
-  };
+    for (int w = 0; w < W; ++w) any |= c[j][w];
   auto work = [&](int row, Part (&x)[J], uint32_t (&m)[J]) {
-    T* p = reinterpret_cast<T*>(static_cast<char*>(r.out) + b * a.out_batch + row * a.out_row);
+    float v[J][W];
 #pragma unroll
-    for (int j = 0; j < J; ++j) {
-      const int tok = base + (j * THREADS + tid) * W;
+    for (int j = 0; j < J; ++j)
 #pragma unroll
-      for (int w = 0; w < W; ++w) {
-        float v = to_f32(x[j].x[w]);
-        if (c[j][w]) {
-          v = v > 0.f ? v / rep : v * rep;
-          const int count = c[j][w] >> 1;
-          if (count) v = v - freq * (float)count - pres;
-        }
-        v += bias[j][w];
-        x[j].x[w] = from_f32<T>(m[j] >> w & 1 ? v : -INFINITY);
-      }
-      if (tok + W <= r.vocab) {
-        *reinterpret_cast<Access*>(p + tok) = x[j].word;
-      } else {
+      for (int w = 0; w < W; ++w) v[j][w] = to_f32(x[j].x[w]);
+    if (any)
+#pragma unroll
+      for (int j = 0; j < J; ++j)
 #pragma unroll
         for (int w = 0; w < W; ++w)
-          if (tok + w < r.vocab) p[tok + w] = x[j].x[w];
-      }
+          if (c[j][w]) {
+            v[j][w] = v[j][w] > 0.f ? v[j][w] / rep : v[j][w] * rep;
+            const int count = c[j][w] >> 1;
+            if (count) v[j][w] = v[j][w] - freq * (float)count - pres;
+          }
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+#pragma unroll
+      for (int w = 0; w < W; ++w) x[j].x[w] = from_f32<T>(m[j] >> w & 1 ? v[j][w] + bias[j][w] : -INFINITY);
+      if (whole[j]) *reinterpret_cast<Access*>(dst + j * (THREADS * W * (int)sizeof(T))) = x[j].word;
     }
+    if (ragged)
+#pragma unroll
+      for (int j = 0; j < J; ++j)
+#pragma unroll
+        for (int w = 0; w < W; ++w)
+          if (!whole[j] && tok0 + j * THREADS * W + w < r.vocab) reinterpret_cast<T*>(dst)[j * THREADS * W + w] = x[j].x[w];
+    dst += a.out_row;
     // the draft that the next row comes after
     if (draft && row + 1 < row1) {
       const int d = __ldg(draft + row);
@@ -147,20 +169,19 @@ __global__ void __launch_bounds__(THREADS) adjust_kernel(const AdjustArgs a) {
         for (int j = 0; j < J; ++j)
 #pragma unroll
           for (int w = 0; w < W; ++w)
-            if (base + (j * THREADS + tid) * W + w == d) c[j][w] = (c[j][w] + 2) | 1;
+            if (tok0 + j * THREADS * W + w == d) any = c[j][w] = (c[j][w] + 2) | 1;
     }
   };
-  load(row0, in[0], allowed[0]);
   for (int row = row0; row < row1; row += 2) {
-    if (row + 1 < row1) load(row + 1, in[1], allowed[1]);
     work(row, in[0], allowed[0]);
     if (row + 1 >= row1) break;
-    if (row + 2 < row1) load(row + 2, in[0], allowed[0]);
+    if (row + 2 < row1) load(in[0], allowed[0]);
     work(row + 1, in[1], allowed[1]);
+    if (row + 3 < row1) load(in[1], allowed[1]);
   }
 }
 
-// Runs of a utterance's rows: enough blocks for every SM to have some.
+// Rows of an utterance are dealt to several blocks where there are few of them.
 template <typename T, int W, int J>
 cudaError_t launch_adjust(AdjustArgs& a, cudaStream_t st) {
   const int runs = (a.r.vocab + THREADS * W * J - 1) / (THREADS * W * J), rows = a.r.rows;
@@ -173,16 +194,24 @@ cudaError_t launch_adjust(AdjustArgs& a, cudaStream_t st) {
   return cudaGetLastError();
 }
 
+// Elements of an access by the rows' alignment; of a thread and row 4, or 8 of 16 bits
+// where the call is large enough for every SM to have blocks all the same.
+template <typename T, int W>
+cudaError_t launch_width(AdjustArgs& a, cudaStream_t st) {
+  const bool large = (long long)a.r.batch * a.r.rows * a.r.vocab >= 8ll * THREADS * 4 * paged_sm_count();
+  if constexpr (sizeof(T) == 2) {
+    if (W == 8 || large) return launch_adjust<T, W, 8 / W>(a, st);
+  }
+  if constexpr (W <= 4) return launch_adjust<T, W, 4 / W>(a, st);
+  else return cudaErrorInvalidValue;   // 8 of 16 bits: above
+}
 template <typename T>
 cudaError_t launch_type(AdjustArgs& a, cudaStream_t st) {
   const uintptr_t all = (uintptr_t)a.r.logits | (uintptr_t)a.r.out | a.batch | a.row | a.out_batch | a.out_row;
-  if constexpr (sizeof(T) == 4)
-    return all % 16 == 0 ? launch_adjust<T, 4, 1>(a, st) : all % 8 == 0 ? launch_adjust<T, 2, 2>(a, st) : launch_adjust<T, 1, 4>(a, st);
-  else
-    return all % 16 == 0  ? launch_adjust<T, 8, 1>(a, st)
-           : all % 8 == 0 ? launch_adjust<T, 4, 2>(a, st)
-           : all % 4 == 0 ? launch_adjust<T, 2, 4>(a, st)
-                          : launch_adjust<T, 1, 8>(a, st);
+  const int most = 16 / (int)sizeof(T), w = all % 16 == 0 ? most : all % 8 == 0 ? most / 2 : all % 4 == 0 ? most / 4 : 1;
+  if constexpr (sizeof(T) == 2)
+    if (w == 8) return launch_width<T, 8>(a, st);
+  return w == 4 ? launch_width<T, 4>(a, st) : w == 2 ? launch_width<T, 2>(a, st) : launch_width<T, 1>(a, st);
 }
 
 }  // namespace

@@ -19,7 +19,7 @@ namespace asrspec {
 namespace {
 
 constexpr int MAX_ARRAYS = 1024;
-constexpr int PIECE = 256;                     // units that a warp copies at a time, 8 a lane
+constexpr int PIECE = 256;                     // units of the heads that a warp copies together, where one has fewer
 constexpr int PER = 8, CHUNK = 1024 * PER;     // pages that a thread and a block look at
 
 struct PoolView {
@@ -33,17 +33,18 @@ struct PoolView {
   int* status;
 };
 
-// An array as the copy kernel reads it, in units of 16 or 4 bytes.
+// An array as the copy kernels read it, in units of 16 or 4 bytes.
 struct PlanArray {
   char* base;
   long long page_stride, head_stride, row_stride;
-  FastDiv row_units, rows;         // by the units of a row, by the rows of a head
-  int units, row_slots, unit;      // units of a page
-  int whole;                       // a page's units lie side by side
-  int first_piece, pad;            // pieces of the arrays before it
+  FastDiv row_units;               // by the units of a row
+  int heads, rows, row_slots, unit;
+  int runs;                        // a head's rows lie side by side
+  int together;                    // heads of a task
+  int first_task, pad;             // tasks of the arrays before it
 };
 struct PlanHead {
-  int n, pieces, page_size, pad;
+  int n, tasks, page_size, each;   // each: an array's tasks where all have as many, else 0
 };
 
 // A workspace, 16-byte parts in this order.
@@ -150,13 +151,13 @@ struct Pages {
   }
 };
 
-// This block is the last of the grid to come here; it sees what the others wrote.
-__device__ __forceinline__ bool last_block(int* done) {
+// This block is the last of so many to come here; it sees what the others wrote.
+__device__ __forceinline__ bool last_block(int* done, int blocks) {
   __shared__ int s_last;
   __threadfence();
   __syncthreads();
   if (threadIdx.x == 0) {
-    s_last = gridDim.x == 1 || atomicAdd(done, 1) == (int)gridDim.x - 1;
+    s_last = blocks == 1 || atomicAdd(done, 1) == blocks - 1;
     if (s_last) *done = 0;   // as the next call needs it
     __threadfence();
   }
@@ -294,45 +295,53 @@ __device__ __forceinline__ Touched touched(const PoolView& p, const ReserveMem& 
   return t;
 }
 
-// Every block counts the free pages of its chunks and copies what the call does
-// not change; the last one decides.
-__global__ void __launch_bounds__(1024) reserve_kernel(const PoolView p, const int* lens, const int* rows, int* counts, const PoolMem ws) {
+// The first `counters` blocks count the free pages of their chunks, and the last of
+// them to be done decides; the others copy the table entries that the call does not touch.
+__global__ void __launch_bounds__(1024, 1) reserve_kernel(const PoolView p, const int* lens, const int* rows, int* counts, const PoolMem ws,
+                                                       int counters) {
   extern __shared__ __align__(16) unsigned char smem[];
   ReserveMem& m = *reinterpret_cast<ReserveMem*>(smem);
   const int tid = threadIdx.x, chunks = (p.n_pages + CHUNK - 1) / CHUNK;
   pdl_launch();
-  for (int c = blockIdx.x; c < chunks; c += gridDim.x) {
+  if ((int)blockIdx.x >= counters) {   // a warp a sequence
+    for (int b = ((int)blockIdx.x - counters) * 32 + tid / 32; b < p.batch; b += ((int)gridDim.x - counters) * 32) {
+      const int2 w = wanted(p, lens, rows, b);
+      const int held = held_of(p, b);
+      for (int j = tid & 31; j < held; j += 32)
+        if (j < w.x || j > w.y) p.table_out[b * p.out_stride + j] = p.table[b * p.table_stride + j];
+    }
+    return;
+  }
+  // What the sequences touch.  A tail is a first touched page that others hold
+  // too; if all who hold it are about to write there the lowest of them keeps it.
+  // (Read by every counter: its loads overlap the counting.)
+  const int b = tid;
+  int2 w = make_int2(0, -1);
+  int held = 0, was = 0, tail = -1, tail_refs = 0;
+  if (b < p.batch) {
+    w = wanted(p, lens, rows, b);
+    held = held_of(p, b), was = p.held[b];
+    if (w.x <= w.y && w.x < held) {
+      const int id = p.table[b * p.table_stride + w.x];
+      if ((unsigned)id < (unsigned)p.n_pages && (tail_refs = p.refs[id]) > 1) tail = id;
+    }
+  }
+  unsigned free0 = 0;   // of this block's first chunk
+  for (int c = blockIdx.x; c < chunks; c += counters) {
     const Pages g(p, c);
     if (p.refs_out != p.refs)
 #pragma unroll
       for (int k = 0; k < PER; ++k)
         if (k < g.n) p.refs_out[g.first + k] = g.r[k];
+    if (c == (int)blockIdx.x) free0 = g.free();
     int before;
     const int n = block_scan(__popc(g.free()), before, m.warps);
     if (tid == 0) ws.count[c] = n;
   }
-  if (p.table_out != p.table)   // entries that the call replaces are written again below
-    for (int b = blockIdx.x * 32 + tid / 32; b < p.batch; b += gridDim.x * 32) {
-      const int held = held_of(p, b);
-      for (int j = tid & 31; j < held; j += 32) p.table_out[b * p.out_stride + j] = p.table[b * p.table_stride + j];
-    }
-  if (!last_block(ws.ctl + C_DONE)) return;
+  if (!last_block(ws.ctl + C_DONE, counters)) return;
 
-  // What the sequences touch.  A tail is a first touched page that others hold
-  // too; if all who hold it are about to write there the lowest of them keeps it.
-  const int b = tid;
-  int2 w = make_int2(0, -1);
-  int held = 0, tail = -1;
-  if (b < p.batch) {
-    w = wanted(p, lens, rows, b);
-    held = held_of(p, b);
-    m.first[b] = w.x, m.held[b] = held;
-    if (w.x <= w.y && w.x < held) {
-      const int id = p.table[b * p.table_stride + w.x];
-      if ((unsigned)id < (unsigned)p.n_pages && p.refs[id] > 1) tail = id;
-    }
-    if (tail >= 0) ws.src[tail] = 0, ws.low[tail] = p.batch;
-  }
+  if (b < p.batch) m.first[b] = w.x, m.held[b] = held;
+  if (tail >= 0) ws.src[tail] = 0, ws.low[tail] = p.batch;
   int before;
   const int total = block_scan(max(0, w.y - w.x + 1), before, m.warps);
   if (b < p.batch) m.before[b] = before;
@@ -340,13 +349,17 @@ __global__ void __launch_bounds__(1024) reserve_kernel(const PoolView p, const i
   __syncthreads();
   if (tail >= 0) atomicAdd(ws.src + tail, 1), atomicMin(ws.low + tail, b);
   const int free = scan_chunks(ws.count, chunks, m.warps);
-  if (b < p.batch) m.keeps[b] = tail >= 0 && __ldcg(ws.src + tail) == p.refs[tail] && __ldcg(ws.low + tail) == b;
+  if (b < p.batch) m.keeps[b] = tail >= 0 && __ldcg(ws.src + tail) == tail_refs && __ldcg(ws.low + tail) == b;
   __syncthreads();
 
-  int need = 0;
+  int need = 0, before0 = 0;
+  Touched first{0, 0, -1, false};   // of the first round
   for (int i0 = 0; i0 < total; i0 += blockDim.x) {
     const int i = i0 + tid;
-    need += block_scan(i < total && touched(p, m, i).fresh, before, m.warps);
+    Touched t{0, 0, -1, false};
+    if (i < total) t = touched(p, m, i);
+    need += block_scan(t.fresh, before, m.warps);
+    if (i0 == 0) first = t, before0 = before;
   }
   const bool enough = need <= free;
   if (tid == 0) {
@@ -355,20 +368,18 @@ __global__ void __launch_bounds__(1024) reserve_kernel(const PoolView p, const i
     counts[1] = enough ? free - need : free;
     ws.ctl[C_JOBS] = enough ? need : 0;
   }
-  if (b < p.batch) p.held_out[b] = enough && w.x <= w.y ? max(held, w.y + 1) : p.held[b];
-  if (!enough) return;
+  if (b < p.batch) p.held_out[b] = enough && w.x <= w.y ? max(held, w.y + 1) : was;
   // the first `need` free pages
-  for (int c = 0; c < chunks; ++c) {
+  for (int c = 0; enough && c < chunks; ++c) {
     const int at = ws.count[c];
     if (at >= need) break;
-    const Pages g(p, c);
-    const unsigned bits = g.free();
+    const unsigned bits = chunks == 1 ? free0 : Pages(p, c).free();
     block_scan(__popc(bits), before, m.warps);
     before += at;
 #pragma unroll
     for (int k = 0; k < PER; ++k)
       if (bits >> k & 1) {
-        if (before < need) ws.list[before] = g.first + k;
+        if (before < need) ws.list[before] = c * CHUNK + tid * PER + k;
         ++before;
       }
   }
@@ -376,10 +387,17 @@ __global__ void __launch_bounds__(1024) reserve_kernel(const PoolView p, const i
   int base = 0;
   for (int i0 = 0; i0 < total; i0 += blockDim.x) {
     const int i = i0 + tid;
-    Touched t{0, 0, -1, false};
-    if (i < total) t = touched(p, m, i);
-    const int n = block_scan(t.fresh, before, m.warps);
-    if (t.fresh) {
+    Touched t = first;
+    int n = 0;
+    before = before0;
+    if (total > (int)blockDim.x) {   // several rounds: looked up again, before anything of this one is written
+      t = Touched{0, 0, -1, false};
+      if (i < total) t = touched(p, m, i);
+      n = block_scan(t.fresh, before, m.warps);
+    }
+    if (i < total && !(t.fresh && enough)) {
+      if (t.j < m.held[t.b]) p.table_out[t.b * p.out_stride + t.j] = t.old;
+    } else if (i < total) {
       const int id = ws.list[base + before];
       p.table_out[t.b * p.out_stride + t.j] = id;
       // the page of slot lens[b] is copied up to it; pages past it hold nothing
@@ -388,7 +406,7 @@ __global__ void __launch_bounds__(1024) reserve_kernel(const PoolView p, const i
     base += n;
   }
   __syncthreads();   // nobody reads the counts of holders any more, which may be refs_out
-  for (int i = tid; i < need; i += blockDim.x) {
+  for (int i = tid; enough && i < need; i += blockDim.x) {
     const int4 job = ws.job[i];
     if (job.x >= 0) atomicSub(p.refs_out + job.x, 1);
     atomicAdd(p.refs_out + job.y, 1);
@@ -442,7 +460,7 @@ __global__ void __launch_bounds__(1024) compact_count_kernel(const PoolView p, i
     const int n = block_scan(__popc(g.live()), before, warps);
     if (threadIdx.x == 0) ws.count[c] = n;
   }
-  if (!last_block(ws.ctl + C_DONE)) return;
+  if (!last_block(ws.ctl + C_DONE, gridDim.x)) return;
   const int live = scan_chunks(ws.count, chunks, warps);
   int below = live;
   if (live < p.n_pages) {   // those below `live`: of the chunks before its own, and of its own
@@ -467,65 +485,74 @@ __global__ void __launch_bounds__(1024) compact_list_kernel(const PoolView p, in
 }
 
 // ------------------------------------------------------------------ copies
-// A task is PIECE units of an array's part in a page: a warp reads 8 units a
-// lane and writes them.
+// A task is one head of an array's part in a page (some heads where they are
+// small), up to the slots in use: what a page does not hold is neither read nor
+// stepped over.  A warp takes a task, 8 units a lane at a time.
 template <typename U>
-__device__ __forceinline__ void copy_piece(const PlanArray& a, int u0, int src, int dst, int slots, int page_size) {
-  const int lane = threadIdx.x & 31;
-  const char* from = a.base + src * a.page_stride;
-  char* to = a.base + dst * a.page_stride;
-  U x[PIECE / 32];
-  long long off[PIECE / 32];
+__device__ __forceinline__ void copy_heads(const PlanArray& a, int head0, int src, int dst, int slots) {
+  const int rows = min(a.rows, (slots + a.row_slots - 1) / a.row_slots), len = rows * (int)a.row_units.d, heads = min(a.together, a.heads - head0);
+  const char* from = a.base + src * a.page_stride + head0 * a.head_stride;
+  char* to = a.base + dst * a.page_stride + head0 * a.head_stride;
+  const bool plain = heads == 1 && a.runs;
+  for (int u0 = threadIdx.x & 31; u0 < heads * len; u0 += 256) {
+    U x[8];
+    long long off[8];
 #pragma unroll
-  for (int k = 0; k < PIECE / 32; ++k) {
-    const int u = u0 + k * 32 + lane;
-    off[k] = -1;
-    if (u >= a.units) continue;
-    if (a.whole && slots == page_size) {
-      off[k] = (long long)u * (int)sizeof(U);
-    } else {
-      const int r = (int)a.row_units.div(u), h = (int)a.rows.div(r), row = r - h * (int)a.rows.d;
-      if (row * a.row_slots < slots)
-        off[k] = h * a.head_stride + row * a.row_stride + (u - r * (int)a.row_units.d) * (int)sizeof(U);
+    for (int k = 0; k < 8; ++k) {
+      const int u = u0 + k * 32;
+      if (plain) {
+        off[k] = (long long)u * (int)sizeof(U);
+      } else {
+        const int h = heads == 1 ? 0 : u / len, in = u - h * len, r = (int)a.row_units.div(in);
+        off[k] = h * a.head_stride + r * a.row_stride + (in - r * (int)a.row_units.d) * (int)sizeof(U);
+      }
+      if (u < heads * len) x[k] = *reinterpret_cast<const U*>(from + off[k]);
     }
-    if (off[k] >= 0) x[k] = *reinterpret_cast<const U*>(from + off[k]);
-  }
 #pragma unroll
-  for (int k = 0; k < PIECE / 32; ++k)
-    if (off[k] >= 0) *reinterpret_cast<U*>(to + off[k]) = x[k];
+    for (int k = 0; k < 8; ++k)
+      if (u0 + k * 32 < heads * len) *reinterpret_cast<U*>(to + off[k]) = x[k];
+  }
 }
 
-__device__ __forceinline__ void copy_task(const PlanHead* plan, int n_arrays, int piece, int src, int dst, int slots) {
-  const PlanArray* arrays = reinterpret_cast<const PlanArray*>(plan + 1);
-  // the array: first_piece rises from 0
+// The array that holds a task: first_task rises from 0.
+__device__ __forceinline__ int array_of(const PlanArray* arrays, int n, int task) {
   const int lane = threadIdx.x & 31;
-  int lo = 0, n = n_arrays;
+  int lo = 0;
   if (n > 32) {
     const int step = (n + 31) >> 5, at = lane * step;
-    lo = (__popc(__ballot_sync(0xffffffffu, at < n && __ldg(&arrays[at].first_piece) <= piece)) - 1) * step;
+    lo = (__popc(__ballot_sync(0xffffffffu, at < n && __ldg(&arrays[at].first_task) <= task)) - 1) * step;
     n = min(n, lo + step);
   }
-  lo += __popc(__ballot_sync(0xffffffffu, lo + lane < n && __ldg(&arrays[min(lo + lane, n - 1)].first_piece) <= piece)) - 1;
-  const PlanArray a = arrays[lo];
-  const int u0 = (piece - a.first_piece) * PIECE;
-  if (a.unit == 16) copy_piece<uint4>(a, u0, src, dst, slots, plan->page_size);
-  else copy_piece<uint32_t>(a, u0, src, dst, slots, plan->page_size);
+  return lo + __popc(__ballot_sync(0xffffffffu, lo + lane < n && __ldg(&arrays[min(lo + lane, n - 1)].first_task) <= task)) - 1;
+}
+// All tasks of all jobs; job(j): source, destination, slots.
+template <typename F>
+__device__ __forceinline__ void copy_jobs(const PlanHead* plan, int n_arrays, int jobs, F job) {
+  const PlanArray* arrays = reinterpret_cast<const PlanArray*>(plan + 1);
+  const PlanHead head = *plan;
+  const long long tasks = (long long)jobs * head.tasks;
+  for (long long t = (long long)blockIdx.x * 8 + threadIdx.x / 32; t < tasks; t += gridDim.x * 8ll) {
+    const int j = (int)(t / head.tasks), task = (int)(t - (long long)j * head.tasks);
+    const int3 now = job(j);
+    if (now.z <= 0) continue;
+    const PlanArray a = arrays[head.each ? task / head.each : array_of(arrays, n_arrays, task)];   // a copy: stores might alias it
+    const int head0 = (task - a.first_task) * a.together;
+    if (a.unit == 16) copy_heads<uint4>(a, head0, now.x, now.y, now.z);
+    else copy_heads<uint32_t>(a, head0, now.x, now.y, now.z);
+  }
 }
 
-__global__ void __launch_bounds__(256) reserve_copy_kernel(const PlanHead* plan, int n_arrays, const PoolMem ws) {
+__global__ void __launch_bounds__(256, 2) reserve_copy_kernel(const PlanHead* plan, int n_arrays, const PoolMem ws) {
   pdl_wait();
-  const int pieces = __ldg(&plan->pieces);
-  const long long tasks = (long long)ws.ctl[C_JOBS] * pieces;
-  for (long long t = (long long)blockIdx.x * 8 + threadIdx.x / 32; t < tasks; t += gridDim.x * 8ll) {
-    const int j = (int)(t / pieces);
+  copy_jobs(plan, n_arrays, ws.ctl[C_JOBS], [&](int j) {
     const int4 job = ws.job[j];
-    if (job.z > 0) copy_task(plan, n_arrays, (int)(t - (long long)j * pieces), job.x, job.y, job.z);
-  }
+    return make_int3(job.x, job.y, job.z);
+  });
 }
 
 // Copies, counts of holders, table entries and new ids.  The counts may be
 // written in place: of a move one thread reads and writes both.
-__global__ void __launch_bounds__(256) compact_copy_kernel(const PoolView p, const PlanHead* plan, int n_arrays, int* where, const PoolMem ws) {
+__global__ void __launch_bounds__(256, 2) compact_copy_kernel(const PoolView p, const PlanHead* plan, int n_arrays, int* where, const PoolMem ws) {
   pdl_wait();
   const int jobs = ws.ctl[C_JOBS], live = ws.ctl[C_LIVE];
   const int at = blockIdx.x * 256 + threadIdx.x, step = gridDim.x * 256;
@@ -551,12 +578,8 @@ __global__ void __launch_bounds__(256) compact_copy_kernel(const PoolView p, con
     }
   }
   if (!n_arrays) return;
-  const int pieces = __ldg(&plan->pieces), page = __ldg(&plan->page_size);
-  const long long tasks = (long long)jobs * pieces;
-  for (long long t = (long long)blockIdx.x * 8 + threadIdx.x / 32; t < tasks; t += gridDim.x * 8ll) {
-    const int j = (int)(t / pieces);
-    copy_task(plan, n_arrays, (int)(t - (long long)j * pieces), ws.src[j], ws.list[j], page);
-  }
+  const int page = __ldg(&plan->page_size);
+  copy_jobs(plan, n_arrays, jobs, [&](int j) { return make_int3(ws.src[j], ws.list[j], page); });
 }
 
 // ----------------------------------------------------------- host side
@@ -589,7 +612,7 @@ unsigned chunk_blocks(const PoolView& p) {
   const int chunks = (p.n_pages + CHUNK - 1) / CHUNK, sms = paged_sm_count();
   return (unsigned)(chunks < sms ? chunks : sms);
 }
-// Resident blocks of 256 threads, no more than the work could fill.
+// Blocks of 256 threads: a few rounds of the resident ones, no more than the work could fill.
 unsigned copy_blocks(long long warps) {
   const long long most = 8ll * paged_sm_count(), want = (warps + 7) / 8;
   return (unsigned)(want < 1 ? 1 : want < most ? want : most);
@@ -622,19 +645,23 @@ int asr_spec_pool_plan(const asr_page_array* arrays, int32_t n, int32_t page_siz
     const uint64_t all = (uint64_t)(uintptr_t)a.base | a.page_stride | a.head_stride | a.row_stride | (uint64_t)a.row_bytes;
     if (all % 4) return ASR_E_INVAL;
     const int unit = all % 16 ? 4 : 16;
-    const long long units = (long long)a.heads * a.rows * (a.row_bytes / unit);
-    const long long pieces = (units + PIECE - 1) / PIECE;
-    if (units > 0x7fffffffll - PIECE || head.pieces + pieces > 0x7fffffffll) return ASR_E_CAPACITY;
+    const long long per_head = (long long)a.rows * (a.row_bytes / unit);
+    if (per_head * a.heads > 0x7fffffffll) return ASR_E_CAPACITY;
     PlanArray x{};
     x.base = static_cast<char*>(a.base);
     x.page_stride = a.page_stride, x.head_stride = a.head_stride, x.row_stride = a.row_stride;
-    x.row_units = make_fastdiv(a.row_bytes / unit), x.rows = make_fastdiv(a.rows);
-    x.units = (int)units, x.row_slots = a.row_slots, x.unit = unit;
-    x.whole = (a.rows == 1 || a.row_stride == a.row_bytes) && (a.heads == 1 || a.head_stride == (long long)a.rows * a.row_bytes);
-    x.first_piece = head.pieces;
-    head.pieces += (int)pieces;
+    x.row_units = make_fastdiv(a.row_bytes / unit);
+    x.heads = a.heads, x.rows = a.rows, x.row_slots = a.row_slots, x.unit = unit;
+    x.runs = a.rows == 1 || a.row_stride == a.row_bytes;
+    x.together = per_head >= PIECE ? 1 : (int)(PIECE / per_head);
+    x.first_task = head.tasks;
+    const int tasks = (a.heads + x.together - 1) / x.together;
+    if ((long long)head.tasks + tasks > 0x7fffffffll) return ASR_E_CAPACITY;
+    head.tasks += tasks;
+    head.each = i == 0 || head.each == tasks ? tasks : -1;
     memcpy(out + i, &x, sizeof x);
   }
+  if (head.each < 0) head.each = 0;
   memcpy(plan, &head, sizeof head);
   return ASR_OK;
 }
@@ -653,7 +680,9 @@ int asr_spec_pool_reserve(const asr_page_pool* pool, const void* plan, int32_t n
   if (int rc = pool_args(pool, true, plan, n_arrays, ws, ws_bytes, &p, &m)) return rc;
   if (!lens || !rows || !counts || ((uintptr_t)lens | (uintptr_t)rows | (uintptr_t)counts) % 4) return ASR_E_INVAL;
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
-  cudaError_t e = launch_ex(reserve_kernel, dim3(chunk_blocks(p)), dim3(1024), sizeof(ReserveMem), st, false, 1, p, lens, rows, counts, m);
+  const int counters = (int)chunk_blocks(p), copiers = p.table_out == p.table ? 0 : (p.batch + 31) / 32;
+  cudaError_t e = launch_ex(reserve_kernel, dim3(counters + copiers), dim3(1024), sizeof(ReserveMem), st, false, 1, p, lens, rows, counts,
+                            m, counters);
   if (e == cudaSuccess && n_arrays)   // a sequence has one page to copy at most; how many do is known on the device
     e = launch_ex(reserve_copy_kernel, dim3(copy_blocks((long long)p.batch * 1024)), dim3(256), 0, st, true, 1,
                   static_cast<const PlanHead*>(plan), (int)n_arrays, m);
