@@ -38,21 +38,25 @@ template <> struct Word<16> { using type = uint4; };
 
 // W elements an access, J accesses a thread and row: token base + (j * THREADS + thread) * W + w.
 template <typename T, int W, int J>
-__global__ void __launch_bounds__(THREADS, 6) adjust_kernel(const AdjustArgs a) {
+__global__ void __launch_bounds__(THREADS, W * J >= 8 ? 4 : 6) adjust_kernel(const AdjustArgs a) {
   constexpr int RUN = THREADS * W * J;
   using Access = typename Word<W * sizeof(T)>::type;
   __shared__ int seen[RUN];   // 2 * count + (seen at all)
   const asr_logit_rules& r = a.r;
   const int tid = threadIdx.x, b = blockIdx.z, base = blockIdx.x * RUN;
   const bool reports = blockIdx.x == 0 && blockIdx.y == 0 && r.status;
-  const int n = r.lens ? r.lens[b] : r.rows - 1, have = r.history_len ? r.history_len[b] : r.history_max;
-  const int prompt = r.prompt_len ? r.prompt_len[b] : 0;
-  if (n < -1 || n >= r.rows || have < 0 || have > r.history_max || prompt < 0 || prompt > have) {
-    if (reports && tid == 0) set_status(r.status, ST_BAD_LENS);
-    return;
-  }
-  const int row0 = blockIdx.y * a.rows_each, row1 = min(n + 1, row0 + a.rows_each);
-  if (row0 >= row1 && !reports) return;
+  // All of the first loads go out together, before it is known how many tokens and rows there are to look at.
+  const int n = r.lens ? __ldg(r.lens + b) : r.rows - 1, have = r.history_len ? __ldg(r.history_len + b) : r.history_max;
+  const int prompt = r.prompt_len ? __ldg(r.prompt_len + b) : 0;
+  const float rep = r.repetition ? __ldg(r.repetition + b) : r.repetition_all;
+  const float freq = r.frequency ? __ldg(r.frequency + b) : r.frequency_all, pres = r.presence ? __ldg(r.presence + b) : r.presence_all;
+  const int* history = r.history + b * r.history_stride;
+  const int* draft = r.draft ? r.draft + (long long)b * (r.rows - 1) : nullptr;
+  int early[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) early[i] = tid + i * THREADS < r.history_max ? __ldg(history + tid + i * THREADS) : 0;
+  const int between = draft && tid < r.rows - 1 ? __ldg(draft + tid) : 0;
+  const int row0 = blockIdx.y * a.rows_each;
 
   union Part {
     Access word;
@@ -89,8 +93,8 @@ __global__ void __launch_bounds__(THREADS, 6) adjust_kernel(const AdjustArgs a) 
           if (!whole[j] && tok0 + j * THREADS * W + w < r.vocab) x[j].x[w] = reinterpret_cast<const T*>(src)[j * THREADS * W + w];
     src += a.row, words += r.mask_row_stride;
   };
-  if (row0 < row1) load(in[0], allowed[0]);
-  if (row0 + 1 < row1) load(in[1], allowed[1]);
+  if (row0 < r.rows) load(in[0], allowed[0]);
+  if (row0 + 1 < r.rows) load(in[1], allowed[1]);
   float bias[J][W];
 #pragma unroll
   for (int j = 0; j < J; ++j)
@@ -100,6 +104,12 @@ __global__ void __launch_bounds__(THREADS, 6) adjust_kernel(const AdjustArgs a) 
       bias[j][w] = r.bias && tok < r.vocab ? __ldg(r.bias + b * r.bias_stride + tok) : 0.f;
     }
   for (int i = tid; i < RUN; i += THREADS) seen[i] = 0;
+  if (n < -1 || n >= r.rows || have < 0 || have > r.history_max || prompt < 0 || prompt > have) {
+    if (reports && tid == 0) set_status(r.status, ST_BAD_LENS);
+    return;
+  }
+  const int row1 = min(n + 1, row0 + a.rows_each);
+  if (row0 >= row1 && !reports) return;
   __syncthreads();
   bool bad = false;
   auto note = [&](int tok, bool said) {
@@ -109,12 +119,13 @@ __global__ void __launch_bounds__(THREADS, 6) adjust_kernel(const AdjustArgs a) 
     atomicOr(seen + at, 1);
     if (said) atomicAdd(seen + at, 2);
   };
-  for (int i = tid; i < have; i += THREADS) note(__ldg(r.history + b * r.history_stride + i), i >= prompt);
-  const int* draft = r.draft ? r.draft + (long long)b * (r.rows - 1) : nullptr;
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+    if (tid + i * THREADS < have) note(early[i], tid + i * THREADS >= prompt);
+  for (int i = tid + 2 * THREADS; i < have; i += THREADS) note(__ldg(history + i), i >= prompt);
   if (draft && tid < (reports ? n : min(row0, n))) {
-    const int d = __ldg(draft + tid);
-    if (tid < row0) note(d, true);
-    bad |= (unsigned)d >= (unsigned)r.vocab;
+    if (tid < row0) note(between, true);
+    bad |= (unsigned)between >= (unsigned)r.vocab;
   }
   if (reports && bad) set_status(r.status, ST_BAD_TOKEN);
   __syncthreads();
@@ -124,9 +135,6 @@ __global__ void __launch_bounds__(THREADS, 6) adjust_kernel(const AdjustArgs a) 
   for (int j = 0; j < J; ++j)
 #pragma unroll
     for (int w = 0; w < W; ++w) c[j][w] = seen[(j * THREADS + tid) * W + w];
-  const float rep = r.repetition ? r.repetition[b] : r.repetition_all;
-  const float freq = r.frequency ? r.frequency[b] : r.frequency_all, pres = r.presence ? r.presence[b] : r.presence_all;
-
   int any = 0;   // of this thread's tokens
 #pragma unroll
   for (int j = 0; j < J; ++j)

@@ -220,29 +220,34 @@ __global__ void __launch_bounds__(256) fork_stage_kernel(const PoolView p, const
   }
 }
 
-// A block takes 1024 entries of a sequence, 4 a thread.
+// A block takes FORK_RUN entries of a sequence, FORK_PER a thread: most rows whole, so that the look-ups before the entries are
+// paid once.
+constexpr int FORK_PER = 8, FORK_RUN = 256 * FORK_PER;
 __global__ void __launch_bounds__(256) fork_kernel(const PoolView p, const int* parent, const int* keep, const PoolMem ws,
                                                    bool in_place) {
   const int b = blockIdx.x;
   if (in_place) pdl_wait();
   const Fork f = in_place ? Fork{ws.was[b], ws.now[b], ws.from[b]} : fork_of(p, parent, keep, b);
   if (blockIdx.y == 0 && threadIdx.x == 0) p.held_out[b] = f.now;
-  for (int j0 = blockIdx.y * 1024; j0 < max(f.was, f.now); j0 += gridDim.y * 1024) {
-    int old[4], id[4];
+  const int* own = p.table + b * p.table_stride;
+  const int* next = f.from < 0 ? own : in_place ? ws.rows + (long long)b * p.max_pages : p.table + f.from * p.table_stride;
+  const bool writes = p.table_out != p.table || f.from >= 0;
+  for (int j0 = blockIdx.y * FORK_RUN; j0 < max(f.was, f.now); j0 += gridDim.y * FORK_RUN) {
+    int old[FORK_PER], id[FORK_PER];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
+    for (int k = 0; k < FORK_PER; ++k) {
       const int j = j0 + k * 256 + threadIdx.x;
-      old[k] = j < f.was ? p.table[b * p.table_stride + j] : -1;
-      id[k] = j >= f.now ? -1 : f.from < 0 ? old[k] : in_place ? ws.rows[(long long)b * p.max_pages + j] : p.table[f.from * p.table_stride + j];
+      old[k] = j < f.was ? own[j] : -1;
+      id[k] = j < f.now ? f.from < 0 ? old[k] : next[j] : -1;
     }
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
+    for (int k = 0; k < FORK_PER; ++k) {
       const int j = j0 + k * 256 + threadIdx.x;
-      if (j < f.now && (p.table_out != p.table || f.from >= 0)) p.table_out[b * p.out_stride + j] = id[k];
+      if (j < f.now && writes) p.table_out[b * p.out_stride + j] = id[k];
     }
     if (!in_place) pdl_wait();   // the counts are there
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
+    for (int k = 0; k < FORK_PER; ++k) {
       const int j = j0 + k * 256 + threadIdx.x;
       const bool out = j < f.was && in_pool(p, old[k]), in = j < f.now && in_pool(p, id[k]);
       if (out && in && old[k] == id[k]) continue;
@@ -701,7 +706,7 @@ int asr_spec_pool_fork(const asr_page_pool* pool, const int32_t* parent, const i
   const long long most = 8ll * paged_sm_count(), want = stage > counts ? stage : counts;
   cudaError_t e = launch_ex(fork_stage_kernel, dim3((unsigned)(want < most ? want : most)), dim3(256), 0, st, false, 1, p, parent, keep,
                             m, in_place);
-  const int chunks = (p.max_pages + 1023) / 1024;
+  const int chunks = (p.max_pages + FORK_RUN - 1) / FORK_RUN;
   if (e == cudaSuccess)
     e = launch_ex(fork_kernel, dim3(p.batch, chunks < 64 ? chunks : 64), dim3(256), 0, st, true, 1, p, parent, keep, m, in_place);
   return e == cudaSuccess ? ASR_OK : ASR_E_CUDA;

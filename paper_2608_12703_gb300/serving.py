@@ -458,9 +458,9 @@ class PagedCache8(_Paged):
         layout, n, out_shape, lse_shape, dtype = known
         r = self._rows_at(layout, q, kv_len, rows, k_new, v_new)
         if out is None:
-            out = torch.empty(out_shape, dtype=q.dtype, device=self.device)
+            out = q.new_empty(out_shape)
         if lse is None:
-            lse = torch.empty(lse_shape, dtype=torch.float32, device=self.device)
+            lse = self.k_scale.new_empty(lse_shape)
         stream = _raw_stream(self._index)
         ws = self._workspace("attend", stream, n)
         rc = self._attend(self._ref, _byref(r), dtype, out.data_ptr(), lse.data_ptr(), ws.data_ptr(), n, stream)
@@ -517,42 +517,37 @@ class PagePool(_Paged):
                                      refs.data_ptr(), n_pages, self.page_size, self.max_pages, self.batch,
                                      self._status.data_ptr())
         self._bytes = _check(self._lib.asr_spec_pool_ws(ctypes.byref(self._layout)), "asr_spec_pool_ws")
+        self._reserve, self._fork, self._compact = (self._lib.asr_spec_pool_reserve, self._lib.asr_spec_pool_fork,
+                                                    self._lib.asr_spec_pool_compact)
         self._layouts, self._ws, self._lock = {}, {}, threading.Lock()
 
-    def _known(self, op, ints, outs):
-        """Checks of a call's arguments, once a layout: ``ints`` [batch] each, ``outs`` table, held, refs or None."""
-        key = (op, _layouts(*ints, *outs))
-        known = self._layouts.get(key)
-        if known is not None:
-            return known
-        for x, name in zip(ints, op[1]):
+    def _checked(self, key, names, ints, table_out, held_out, refs_out):
+        """Checks of a call's arguments, once a layout: ``ints`` are [batch]."""
+        for x, name in zip(ints, names):
             if x is not None:
                 _whole(x, name, torch.int32, (self.batch,), self.device)
-        table_out, held_out, refs_out = outs
+        layout = A.AsrPagePool.from_buffer_copy(self._layout)
         if table_out is not None:
             _tensor(table_out, "table_out", torch.int32, (self.batch, self.max_pages), self.device)
             _need(table_out.stride(1) == 1 or self.max_pages == 1, "table_out: the last axis must be contiguous")
+            layout.table_out_stride = max(table_out.stride(0), self.max_pages) if self.batch == 1 else table_out.stride(0)
         if held_out is not None:
             _whole(held_out, "held_out", torch.int32, (self.batch,), self.device)
         if refs_out is not None:
             _whole(refs_out, "refs_out", torch.int32, (self.n_pages,), self.device)
-        layout = A.AsrPagePool.from_buffer_copy(self._layout)
-        if table_out is not None:
-            layout.table_out_stride = max(table_out.stride(0), self.max_pages) if self.batch == 1 else table_out.stride(0)
         return _remember(self._layouts, key, layout)
 
-    def _call(self, op, ints, outs):
-        layout = self._known(op, ints, outs)
+    @staticmethod
+    def _at(layout, table_out, held_out, refs_out):
+        """The pool of an earlier call with this call's outputs."""
         p = A.AsrPagePool.from_buffer_copy(layout)
-        table_out, held_out, refs_out = outs
         if table_out is not None:
             p.table_out = table_out.data_ptr()
         if held_out is not None:
             p.held_out = held_out.data_ptr()
         if refs_out is not None:
             p.refs_out = refs_out.data_ptr()
-        stream = _raw_stream(self._index)
-        return p, self._workspace("pool", stream, self._bytes), stream
+        return p
 
     def reserve(self, lens, rows, *, table_out=None, held_out=None, refs_out=None):
         """Private pages for ``rows [B]`` slots behind ``lens [B]`` of each sequence: missing pages are taken from the pool,
@@ -564,11 +559,14 @@ class PagePool(_Paged):
             with torch.cuda.device(self.device):
                 return self.reserve(lens, rows, table_out=table_out, held_out=held_out, refs_out=refs_out)
         _need(lens is not None and rows is not None, "lens and rows are required")
-        outs = (table_out, held_out, refs_out)
-        p, ws, stream = self._call(_RESERVE, (lens, rows), outs)
-        counts = torch.empty(2, dtype=torch.int32, device=self.device)
-        rc = self._lib.asr_spec_pool_reserve(_byref(p), self._plan.data_ptr(), self._n, lens.data_ptr(), rows.data_ptr(),
-                                             counts.data_ptr(), ws.data_ptr(), self._bytes, stream)
+        key = (0, _layouts(lens, rows, table_out, held_out, refs_out))
+        layout = self._layouts.get(key) or self._checked(key, ("lens", "rows"), (lens, rows), table_out, held_out, refs_out)
+        p = self._at(layout, table_out, held_out, refs_out)
+        counts = lens.new_empty(2)
+        stream = _raw_stream(self._index)
+        ws = self._workspace("pool", stream, self._bytes)
+        rc = self._reserve(_byref(p), self._plan.data_ptr(), self._n, lens.data_ptr(), rows.data_ptr(), counts.data_ptr(),
+                           ws.data_ptr(), self._bytes, stream)
         if rc:
             _check(rc, "asr_spec_pool_reserve")
         return (self.page_table if table_out is None else table_out, self.held if held_out is None else held_out,
@@ -581,10 +579,13 @@ class PagePool(_Paged):
         if _current_device() != self._index:
             with torch.cuda.device(self.device):
                 return self.fork(parent, keep, table_out=table_out, held_out=held_out, refs_out=refs_out)
-        outs = (table_out, held_out, refs_out)
-        p, ws, stream = self._call(_FORK, (parent, keep), outs)
-        rc = self._lib.asr_spec_pool_fork(_byref(p), None if parent is None else parent.data_ptr(),
-                                          None if keep is None else keep.data_ptr(), ws.data_ptr(), self._bytes, stream)
+        key = (1, _layouts(parent, keep, table_out, held_out, refs_out))
+        layout = self._layouts.get(key) or self._checked(key, ("parent", "keep"), (parent, keep), table_out, held_out, refs_out)
+        p = self._at(layout, table_out, held_out, refs_out)
+        stream = _raw_stream(self._index)
+        ws = self._workspace("pool", stream, self._bytes)
+        rc = self._fork(_byref(p), None if parent is None else parent.data_ptr(), None if keep is None else keep.data_ptr(),
+                        ws.data_ptr(), self._bytes, stream)
         if rc:
             _check(rc, "asr_spec_pool_fork")
         return (self.page_table if table_out is None else table_out, self.held if held_out is None else held_out,
@@ -597,17 +598,18 @@ class PagePool(_Paged):
         if _current_device() != self._index:
             with torch.cuda.device(self.device):
                 return self.compact(table_out=table_out, refs_out=refs_out)
-        p, ws, stream = self._call(_COMPACT, (), (table_out, None, refs_out))
-        where = torch.empty(self.n_pages, dtype=torch.int32, device=self.device)
-        live = torch.empty(1, dtype=torch.int32, device=self.device)
-        rc = self._lib.asr_spec_pool_compact(_byref(p), self._plan.data_ptr(), self._n, where.data_ptr(), live.data_ptr(),
-                                             ws.data_ptr(), self._bytes, stream)
+        key = (2, _layouts(table_out, refs_out))
+        layout = self._layouts.get(key) or self._checked(key, (), (), table_out, None, refs_out)
+        p = self._at(layout, table_out, None, refs_out)
+        where, live = self.refs.new_empty(self.n_pages), self.refs.new_empty(1)
+        stream = _raw_stream(self._index)
+        ws = self._workspace("pool", stream, self._bytes)
+        rc = self._compact(_byref(p), self._plan.data_ptr(), self._n, where.data_ptr(), live.data_ptr(), ws.data_ptr(),
+                           self._bytes, stream)
         if rc:
             _check(rc, "asr_spec_pool_compact")
         return (self.page_table if table_out is None else table_out, self.refs if refs_out is None else refs_out, where, live)
 
-
-_RESERVE, _FORK, _COMPACT = ("reserve", ("lens", "rows")), ("fork", ("parent", "keep")), ("compact", ())
 
 _adjust_layouts: dict = {}
 
@@ -624,9 +626,12 @@ def adjust_logits(logits, *, history=None, history_len=None, prompt_len=None, dr
     added, and a token whose bit in ``mask`` (int32 ``[B, k + 1, ceil(V / 32)]``, bit j % 32 of word j // 32) is not set
     gets -inf.  ``repetition``, ``frequency`` and ``presence`` are numbers or float32 ``[B]``.  Writes ``out`` (default:
     ``logits`` in place) and returns it; rows past ``lens`` are left as they are."""
-    repetition, frequency, presence = [
-        x if isinstance(x, torch.Tensor) and x.dim() == 1 else _number(x, name)
-        for x, name in ((repetition, "repetition"), (frequency, "frequency"), (presence, "presence"))]
+    if not (type(repetition) is float or isinstance(repetition, torch.Tensor) and repetition.dim() == 1):
+        repetition = _number(repetition, "repetition")
+    if not (type(frequency) is float or isinstance(frequency, torch.Tensor) and frequency.dim() == 1):
+        frequency = _number(frequency, "frequency")
+    if not (type(presence) is float or isinstance(presence, torch.Tensor) and presence.dim() == 1):
+        presence = _number(presence, "presence")
     key = _layouts(logits, history, history_len, prompt_len, draft, lens, repetition, frequency, presence, bias, mask, out, status)
     known = _adjust_layouts.get(key)
     if known is None:
