@@ -117,11 +117,6 @@ __device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
   asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
   return d;
 }
-__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
-  uint64_t d;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-  return d;
-}
 __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
   uint64_t d;
   asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
@@ -172,30 +167,34 @@ __device__ __forceinline__ void look(uint32_t at, bool full, int left, const Gro
     }
   });
 }
-// Second look: the weights take the scores' place; returns the sum of p.
-__device__ __forceinline__ float weigh(uint32_t at, bool full, int left, const GroupScales& gs, float base, float sc, float inv) {
+// Second look: the weights, relative to the maximum, times 2^li and the groups'
+// scales, take the scores' place.  With lf = li + log2 of a group's scale
+//   w = 2^((S t - base) sc + lf),   l = sum over groups of 2^-lf sum w :
+// lf is held at -60, below which fp16 has no weight but the sum still sees it.  Returns the sum.
+__device__ __forceinline__ float weigh(uint32_t at, bool full, int left, const GroupScales& gs, float base, float sc, int li) {
   const uint64_t base2 = two(-base, -base), sc2 = two(sc, sc);
-  uint64_t sum2 = 0;
+  float sum = 0.f;
   for_scores(at, full, left, [&](int q, uint32_t (&s)[32]) {
     uint32_t p[16];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      const float ks = gs.k[q * 2 + h], f = fminf(gs.v[q * 2 + h] * inv, 8.507059173e37f);
-      const uint64_t ks2 = two(ks, ks), f2 = two(f, f);
+      const float ks = gs.k[q * 2 + h], lf = fmaxf(gs.lv[q * 2 + h] + (float)li, -60.f);
+      const uint64_t ks2 = two(ks, ks), lf2 = two(lf, lf);
+      uint64_t sum2 = 0;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const int x = h * 16 + 2 * i;
-        const float2 t = parts(mul2(fma2(two(__uint_as_float(s[x]), __uint_as_float(s[x + 1])), ks2, base2), sc2));
-        const uint64_t e2 = two(ex2(t.x), ex2(t.y));
-        sum2 = add2(sum2, e2);
-        const float2 w = parts(mul2(e2, f2));
-        p[h * 8 + i] = Mma16<__half>::pack(w.x, w.y);
+        const float2 t = parts(fma2(fma2(two(__uint_as_float(s[x]), __uint_as_float(s[x + 1])), ks2, base2), sc2, lf2));
+        const float w0 = ex2(t.x), w1 = ex2(t.y);
+        sum2 = add2(sum2, two(w0, w1));
+        p[h * 8 + i] = Mma16<__half>::pack(w0, w1);
       }
+      const float2 part = parts(sum2);
+      sum = fmaf(part.x + part.y, ex2(-lf), sum);
     }
     tmem_st16(at + q * 16, p);   // over scores that have been read: the next 32 lie past these 16 columns
   });
-  const float2 sum = parts(sum2);
-  return sum.x + sum.y;
+  return sum;
 }
 
 // What a block works on.
@@ -354,6 +353,13 @@ __global__ void __launch_bounds__(THREADS, 1) prompt8_kernel(const Prompt8Args a
         for (int i = pairs; i < pairs + it.n0 + it.n1; ++i) bar_wait(&bars.s_full[i % NS], i / NS & 1, c.status, gave_up);
       float mx = -INFINITY, l = 0.f;   // the maximum, in units of the product; the sum of p
       int li = 126;                    // log2 of what weights are multiplied by
+      Item next;
+      more = src.take(k + 1, next, gave_up);
+      if (more) {   // its rows of q come near
+        const int nm = next.m0 + x * BM + row_in, nrow = (int)r.groups.div(nm), nhq = next.kvh * r.group + nm - nrow * r.group;
+        if (nm < next.rows * r.group)
+          asm volatile("prefetch.global.L2 [%0];" ::"l"(r.q + next.b * r.q_b + (long long)nrow * r.q_r + nhq * r.q_h));
+      }
       for (int j = 0; j < nx; ++j) {
         const int pair = pairs + min(j, it.n0) + min(j, it.n1) + (x && j < it.n0), buf = pair % NS, tile = tiles + j;
         const uint32_t s_at = tmem + lanes + buf * BN;
@@ -401,15 +407,14 @@ __global__ void __launch_bounds__(THREADS, 1) prompt8_kernel(const Prompt8Args a
           }
           __syncwarp();
         }
-        const float base = mx == -INFINITY ? 0.f : mx, inv = pow2(li);
-        l += weigh(s_at, full, left, gs, base, sc, inv);
+        l += weigh(s_at, full, left, gs, mx == -INFINITY ? 0.f : mx, sc, li);
         tmem_wait_st();
         tc_fence_before();
         warp_arrive(&bars.p_full[buf]);
       }
       pairs += it.n0 + it.n1, tiles += it.n(), steps += nx;
       const Item was = it;
-      more = src.take(k + 1, it, gave_up);
+      it = next;
       if (more && (x ? it.n1 : it.n0) > 0) next_sc = take_q(it);
       if (k < 0) continue;
       // -------------------------------------------------------------- the rows' ends
@@ -467,10 +472,13 @@ __global__ void __launch_bounds__(THREADS, 1) prompt8_kernel(const Prompt8Args a
     long long off = 0;
     float scale = 1.f;
     uint4 x[MINE][IT];
-    bool more;
-    auto take = [&] {
+    bool more = true;
+    auto take = [&] {   // the next item, and the one after it is fetched
       ++k;
-      if (tid == 8 * 32) src.fetch(k, gave_up);
+      if (tid == 8 * 32) {
+        if (k == 0) src.fetch(0, gave_up);
+        if (k == 0 || more) src.fetch(k + 1, gave_up);
+      }
       __syncwarp();
       more = src.take(k, it, gave_up);
       j = 0;

@@ -458,9 +458,9 @@ class PagedCache8(_Paged):
         layout, n, out_shape, lse_shape, dtype = known
         r = self._rows_at(layout, q, kv_len, rows, k_new, v_new)
         if out is None:
-            out = q.new_empty(out_shape)
+            out = torch.empty(out_shape, dtype=q.dtype, device=self.device)
         if lse is None:
-            lse = self.k_scale.new_empty(lse_shape)
+            lse = torch.empty(lse_shape, dtype=torch.float32, device=self.device)
         stream = _raw_stream(self._index)
         ws = self._workspace("attend", stream, n)
         rc = self._attend(self._ref, _byref(r), dtype, out.data_ptr(), lse.data_ptr(), ws.data_ptr(), n, stream)
@@ -562,7 +562,7 @@ class PagePool(_Paged):
         key = (0, _layouts(lens, rows, table_out, held_out, refs_out))
         layout = self._layouts.get(key) or self._checked(key, ("lens", "rows"), (lens, rows), table_out, held_out, refs_out)
         p = self._at(layout, table_out, held_out, refs_out)
-        counts = lens.new_empty(2)
+        counts = torch.empty(2, dtype=torch.int32, device=self.device)
         stream = _raw_stream(self._index)
         ws = self._workspace("pool", stream, self._bytes)
         rc = self._reserve(_byref(p), self._plan.data_ptr(), self._n, lens.data_ptr(), rows.data_ptr(), counts.data_ptr(),
@@ -601,7 +601,8 @@ class PagePool(_Paged):
         key = (2, _layouts(table_out, refs_out))
         layout = self._layouts.get(key) or self._checked(key, (), (), table_out, None, refs_out)
         p = self._at(layout, table_out, None, refs_out)
-        where, live = self.refs.new_empty(self.n_pages), self.refs.new_empty(1)
+        where = torch.empty(self.n_pages, dtype=torch.int32, device=self.device)
+        live = torch.empty(1, dtype=torch.int32, device=self.device)
         stream = _raw_stream(self._index)
         ws = self._workspace("pool", stream, self._bytes)
         rc = self._compact(_byref(p), self._plan.data_ptr(), self._n, where.data_ptr(), live.data_ptr(), ws.data_ptr(),
