@@ -594,10 +594,12 @@ int asr_spec_paged8_append(const asr_paged8_cache* cache, const asr_paged_rows* 
 /* Attention of the rows over the cache as asr_spec_paged_attend, with K and V
  * the dequantised ones.  dtype (1 or 2) is that of q, k_new, v_new and out.  With k_new /
  * v_new (causal only) they are appended first, as by asr_spec_paged8_append, and
- * the rows see them as they are stored.  Arithmetic: codes and q multiply exactly and
- * are summed in fp32 (bf16 rows: elements below 2^-38 of a row's largest vanish), softmax statistics in
- * fp32; weights times the groups' scales are rounded to fp16 for the second product, and
- * those below 2^-40 of a row's largest vanish.  Scales are positive and finite.
+ * the rows see them as they are stored.  Arithmetic: codes and q multiply exactly
+ * (bf16 rows are brought to fp16 by a power of two: elements below 2^-30 of a
+ * row's largest lose bits) and are summed in fp32, softmax statistics in fp32; weights times the
+ * groups' scales are rounded to fp16 for the second product, and those below 2^-35 of a row's largest
+ * vanish there (the statistics have them).  Scales are positive and finite; a row of q
+ * that holds an infinity comes out as NaN.
  * ws: asr_spec_paged8_attend_ws bytes, 16-byte aligned, zero before its first use; every call
  * leaves it ready for the next on its stream, whatever that one's sizes. */
 int64_t asr_spec_paged8_attend_ws(const asr_paged8_cache* cache, const asr_paged_rows* rows, int32_t dtype);

@@ -150,6 +150,18 @@ __global__ void __launch_bounds__(C::WARPS * 32, 1) attend8_kernel(const Attend8
   attend_items<T, C, KS>(a, [&](const SeqWork& s, int b, int kvh, int tile, int s0, int n, float* sm) {
     constexpr int KB = KS * D;   // bytes of a step's K, and of its V
     const uint32_t ring = smem_u32(sm);
+    // q, on its way before the pages are looked up and while the append still runs
+    uint4 xq[NT][NJ][2];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      const int m = tile * TR + nt * 8 + g, row = (int)r.groups.div(m), hq = kvh * r.group + m - row * r.group;
+      const char* src = r.q + b * r.q_b + row * r.q_r + hq * r.q_h + t * 32;
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) {
+        xq[nt][j][0] = ldg_if(row < s.rows, src + j * 128);
+        xq[nt][j][1] = ldg_if(row < s.rows, src + j * 128 + 16);
+      }
+    }
     pdl_wait();   // the append
     Groups8<D> groups(a.p, b, kvh, s.keys, s0);
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // results were written here before
@@ -169,14 +181,7 @@ __global__ void __launch_bounds__(C::WARPS * 32, 1) attend8_kernel(const Attend8
     int lim[NT][2];       // slots that they see
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
-      const int m = tile * TR + nt * 8 + g, row = m / r.group, hq = kvh * r.group + m - row * r.group;
-      const char* src = r.q + b * r.q_b + row * r.q_r + hq * r.q_h + t * 32;
-      uint4 x[NJ][2];
-#pragma unroll
-      for (int j = 0; j < NJ; ++j) {
-        x[j][0] = ldg_if(row < s.rows, src + j * 128);
-        x[j][1] = ldg_if(row < s.rows, src + j * 128 + 16);
-      }
+      uint4 (&x)[NJ][2] = xq[nt];
       int e = 0;
       if constexpr (sizeof(T) == 2 && !std::is_same<T, __half>::value) {
         uint32_t most = 0;   // the largest magnitude's bits
@@ -216,7 +221,7 @@ __global__ void __launch_bounds__(C::WARPS * 32, 1) attend8_kernel(const Attend8
         }
 #pragma unroll
       for (int x2 = 0; x2 < 2; ++x2) {
-        const int m2 = tile * TR + nt * 8 + 2 * t + x2, row2 = m2 / r.group;
+        const int m2 = tile * TR + nt * 8 + 2 * t + x2, row2 = (int)r.groups.div(m2);
         lim[nt][x2] = min(s.keys, r.causal ? s.len + row2 + 1 : s.len);
         const int e2 = __shfl_sync(0xffffffffu, e, 8 * t + 4 * x2);
         sc[nt][x2] = fmaxf(r.scale * LOG2E * pow2(-(e2 / 2)) * pow2(-(e2 - e2 / 2)), 1.17549435e-38f);
@@ -496,12 +501,18 @@ int asr_spec_paged8_attend(const asr_paged8_cache* c, const asr_paged_rows* r, i
   if (ws_bytes < attend8_ws_bytes(c->head_dim, m_rows)) return ASR_E_CAPACITY;
   const int tr = with_shape(c->head_dim, m_rows, [](auto s) { return s.TR; });
   const long long tiles = ((long long)m_rows + tr - 1) / tr;
-  if (tiles * c->kv_heads * c->batch * ((long long)a.p.c.max_slots / 32 + 2) > 0x7fffffffll) return ASR_E_CAPACITY;   // 32-bit units
   cudaStream_t st = static_cast<cudaStream_t>(stream);
+  // The kernel for prompts takes 256 rows of a K/V head a block and does not share keys between blocks: it needs rows to fill its
+  // tiles and items to fill the SMs.  Measured, us a call, this kernel and that one: 20 heads of 64, 32 sequences of 448
+  // slots, 64 rows 67 and 68, 96 rows 113 and 84, 256 rows 356 and 117; 40 items of 256 rows by 1000 slots 67 and 40; 8
+  // items of 300 rows by 8000 slots 50 and 151, 6 of 256 by 100000 268 and 1608.
+  const long long items = ((long long)m_rows + 255) / 256 * c->kv_heads * c->batch;
+  const bool prompt = m_rows > 64 && 4 * items >= paged_sm_count();
+  if (!prompt && tiles * c->kv_heads * c->batch * ((long long)a.p.c.max_slots / 32 + 2) > 0x7fffffffll) return ASR_E_CAPACITY;   // 32-bit units
   const bool appends = a.r.k_new != nullptr;
   if (appends && launch_append8(a.p, a.r, dtype, st) != cudaSuccess) return ASR_E_CUDA;
   a.r.k_new = a.r.v_new = nullptr;   // the rows are in the pages from here on
-  if (m_rows >= 64)
+  if (prompt)
     return launch_prompt8(a.p, a.r, dtype, out, lse, static_cast<int*>(ws), appends, st) == cudaSuccess ? ASR_OK : ASR_E_CUDA;
   a.c = a.p.c;
   a.out = static_cast<char*>(out);

@@ -154,10 +154,11 @@ struct Pages {
 // This block is the last of so many to come here; it sees what the others wrote.
 __device__ __forceinline__ bool last_block(int* done, int blocks) {
   __shared__ int s_last;
-  __threadfence();
+  if (blocks > 1) __threadfence();
   __syncthreads();
+  if (blocks == 1) return true;
   if (threadIdx.x == 0) {
-    s_last = blocks == 1 || atomicAdd(done, 1) == blocks - 1;
+    s_last = atomicAdd(done, 1) == blocks - 1;
     if (s_last) *done = 0;   // as the next call needs it
     __threadfence();
   }
@@ -276,6 +277,7 @@ __device__ __forceinline__ int2 wanted(const PoolView& p, const int* lens, const
 
 struct ReserveMem {   // a sequence's first touched page, what it holds, its tail (see below), entries touched before it
   int first[PG_MAX_BATCH], held[PG_MAX_BATCH], keeps[PG_MAX_BATCH], before[PG_MAX_BATCH + 1], warps[32];
+  int list[1024];   // the pages that the call takes, where they are no more than these
 };
 // Entry i of those touched, in order of sequence and slot: its sequence, page and id (-1: none held), and whether it
 // needs another page.
@@ -375,6 +377,7 @@ __global__ void __launch_bounds__(1024, 1) reserve_kernel(const PoolView p, cons
   }
   if (b < p.batch) p.held_out[b] = enough && w.x <= w.y ? max(held, w.y + 1) : was;
   // the first `need` free pages
+  int* const list = need <= 1024 ? m.list : ws.list;
   for (int c = 0; enough && c < chunks; ++c) {
     const int at = ws.count[c];
     if (at >= need) break;
@@ -384,7 +387,7 @@ __global__ void __launch_bounds__(1024, 1) reserve_kernel(const PoolView p, cons
 #pragma unroll
     for (int k = 0; k < PER; ++k)
       if (bits >> k & 1) {
-        if (before < need) ws.list[before] = c * CHUNK + tid * PER + k;
+        if (before < need) list[before] = c * CHUNK + tid * PER + k;
         ++before;
       }
   }
@@ -403,7 +406,7 @@ __global__ void __launch_bounds__(1024, 1) reserve_kernel(const PoolView p, cons
     if (i < total && !(t.fresh && enough)) {
       if (t.j < m.held[t.b]) p.table_out[t.b * p.out_stride + t.j] = t.old;
     } else if (i < total) {
-      const int id = ws.list[base + before];
+      const int id = list[base + before];
       p.table_out[t.b * p.out_stride + t.j] = id;
       // the page of slot lens[b] is copied up to it; pages past it hold nothing
       ws.job[base + before] = make_int4(t.old, id, t.old >= 0 && t.j == m.first[t.b] ? lens[t.b] % p.page_size : 0, 0);

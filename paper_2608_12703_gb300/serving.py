@@ -492,6 +492,7 @@ class PagePool(_Paged):
                   "caches: the same number and size of pages are required")
         _whole(held, "held", torch.int32, (c0.batch,), c0.device)
         _whole(refs, "refs", torch.int32, (n_pages,), c0.device)
+        _need(not _capturing(), "a pool is made outside of a graph capture")
         self.caches, self.page_table, self.held, self.refs = caches, table, held, refs
         self.device, self.batch, self.max_pages, self.page_size = c0.device, c0.batch, c0.max_pages, c0.page_size
         self.n_pages, self._index = n_pages, c0.device.index

@@ -138,9 +138,10 @@ def test_attend_not_causal_and_append_apart(built_lib, cuda, dtype, dim):
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp16"])
 @pytest.mark.parametrize("dim,heads,kv_heads,R", [(64, 3, 3, 130), (128, 4, 2, 70), (64, 8, 1, 40), (64, 2, 2, 300)])
-def test_attend_prompts(built_lib, cuda, dtype, dim, heads, kv_heads, R):
-    """Prompts, on their own and behind what is there already; not causal besides."""
-    lens, rows = [0, 7, 16, 130, 500], [R, R - 1, 17, R, 1]
+@pytest.mark.parametrize("copies", [1, 8])
+def test_attend_prompts(built_lib, cuda, dtype, dim, heads, kv_heads, R, copies):
+    """Prompts, on their own and behind what is there already; not causal besides.  Few of them, and enough to fill the GPU."""
+    lens, rows = [0, 7, 16, 130, 500] * copies, [R, R - 1, 17, R, 1] * copies
     check(gen(8), DT[dtype], dim, heads, kv_heads, 32, R, lens, rows)
     check(gen(9), DT[dtype], dim, heads, kv_heads, 16, R, lens, rows, causal=False, fused=False)
 
@@ -159,8 +160,10 @@ def test_attend_many_prompts(built_lib, cuda, dtype, dim, causal):
 def test_attend_scales(built_lib, cuda, dtype, R):
     for scale in (1e-3, 2.0):
         check(gen(8), DT[dtype], 64, 2, 2, 16, R, [50, 120], [R, R - 1], scale=scale)
+        check(gen(8), DT[dtype], 64, 2, 2, 16, R, [50, 120] * 10, [R, R - 1] * 10, scale=scale)
     # groups whose scales lie far apart
     check(gen(9), DT[dtype], 64, 2, 2, 16, R, [50, 320], [R, R - 1], spread=20, scale=0.01)
+    check(gen(9), DT[dtype], 64, 2, 2, 16, R, [50, 320] * 10, [R, R - 1] * 10, spread=20, scale=0.01)
 
 
 def test_attend_one_long_sequence(built_lib, cuda):
@@ -190,6 +193,7 @@ def test_a_hidden_nan_does_not_reach_a_row(built_lib, cuda, R):
     def spoil(q, kn, vn, v, vs, table):
         vn[0, 2, 0, 3], vn[1, 1, 1, 60], kn[2, 3, 0, 5] = math.nan, math.inf, -math.inf
     check(gen(12), DT["bf16"], 64, 4, 2, 16, R, [0, 14, 29, 61], [R, R, R, R - 1], spoil=spoil)
+    check(gen(12), DT["bf16"], 64, 4, 2, 16, R, [0, 14, 29, 61] * 5, [R, R, R, R - 1] * 5, spoil=spoil)
 
 
 @pytest.mark.parametrize("dtype", ["fp16", "bf16"])
@@ -203,6 +207,7 @@ def test_scales_that_are_no_powers_of_two(built_lib, cuda, R, dtype):
         vs[int(table[1, 0])] = 2.0 ** -126
         vs[int(table[1, 1]), 0, 0] = 2.0 ** 30
     check(gen(13), DT[dtype], 64, 4, 2, 16, R, [64, 96], [R, R], causal=False, spoil=spoil)
+    check(gen(13), DT[dtype], 64, 4, 2, 16, R, [64, 96] * 10, [R, R] * 10, causal=False, spoil=spoil)
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp16"])
@@ -215,7 +220,9 @@ def test_rows_of_wide_range(built_lib, cuda, dtype, R):
         q[1] *= 1e-4 if dtype == "fp16" else 1e-30
         q[2, :, 0, :] *= 0
         q[2, :, 0, 1], q[2, :, 0, 2] = big, -big / 3
-    check(gen(14), DT[dtype], 64, 2, 2, 16, R, [40, 50, 60], [R, R, R], spoil=spoil, scale=1e-30 if dtype == "bf16" else 1e-4)
+    scale = 1e-30 if dtype == "bf16" else 1e-4
+    check(gen(14), DT[dtype], 64, 2, 2, 16, R, [40, 50, 60], [R, R, R], spoil=spoil, scale=scale)
+    check(gen(15), DT[dtype], 64, 8, 2, 16, R, [40, 50, 60] * 7, [R, R, R] * 7, spoil=spoil, scale=scale)      # 4 heads a K/V head
 
 
 @pytest.mark.parametrize("dtype", ["fp32", "bf16", "fp16"])
@@ -263,7 +270,7 @@ def test_append_in_pieces_keeps_what_a_group_holds(built_lib, cuda):
     assert torch.equal(codes(k), codes(kr)) and torch.equal(codes(v), codes(vr)) and same_bits(ks, ksr) and same_bits(vs, vsr)
 
 
-@pytest.mark.parametrize("R", [2, 40])
+@pytest.mark.parametrize("R", [2, 40, 400])
 def test_data_errors(built_lib, cuda, R):
     """Lengths and page ids out of range leave their sequence zero (or read page 0), set the status, and touch nothing else."""
     from paper_2608_12703_gb300 import serving
@@ -272,7 +279,7 @@ def test_data_errors(built_lib, cuda, R):
     k, v, ks, vs, table = pool(g, 2, 64, 16, [n + R for n in lens])
     fill(g, k, ks, table, lens)
     fill(g, v, vs, table, lens)
-    q, kn, vn = make_rows(g, 5, R, 4, 2, 64, torch.bfloat16, True)
+    q, kn, vn = make_rows(g, 5, R, 8, 2, 64, torch.bfloat16, True)      # of 400 rows 7 tiles a head: the kernel for prompts
     lens[2], lens[3] = -1, 16 * table.shape[1] - R + 1
     table[4, 1] = 10 ** 6
     before = codes(k).clone()
@@ -344,3 +351,52 @@ def test_cache_refusals(built_lib, cuda):
               (k, v, ks, vs, table.long()), (k[:, :, :24], v[:, :, :24], ks, vs, table), (k[..., :32], v[..., :32], ks, vs, table)):
         with pytest.raises(A.AsrSpecError, match="INVAL"):
             serving.PagedCache8(*a)
+
+
+def test_calls_of_all_sizes_share_a_workspace(built_lib, cuda):
+    """Few rows, prompts and single tokens in turn on one cache and stream: each finds the workspace as the one before left it."""
+    from paper_2608_12703_gb300 import serving
+    g = gen(24)
+    lens = [700, 3, 90, 0]
+    k, v, ks, vs, table = pool(g, 2, 64, 16, [n + 300 for n in lens])
+    fill(g, k, ks, table, [n + 300 for n in lens])
+    fill(g, v, vs, table, [n + 300 for n in lens])
+    c = serving.PagedCache8(k, v, ks, vs, table)
+    want = {}
+    for turn in range(3):
+        for R in (1, 300, 7, 40, 129):
+            q = torch.randn((4, R, 8, 64), generator=gen(R), device="cuda").half()
+            n = i32([x + 300 - R for x in lens])
+            got = c.attend(q, n)
+            if turn == 0:
+                want[R] = got
+                compare(*got, *ref.attend(q, k, v, ks, vs, table, [x + 300 - R for x in lens], [R] * 4, True, 0.125))
+            assert same_bits(got[0], want[R][0]) and same_bits(got[1], want[R][1])
+    assert c.status() == 0
+
+
+@pytest.mark.parametrize("R,heads", [(2, 2), (70, 2), (300, 20)])
+def test_offsets_past_32_bits(built_lib, cuda, R, heads):
+    """A pool of more than 4 GB, the sequences in its last pages."""
+    from paper_2608_12703_gb300 import serving
+    g, page, K = gen(25), 16, 1
+    n_pages = (9 << 29) // (page * 64)      # 4.5 GiB of codes each
+    k, v = (torch.empty((n_pages, K, page, 64), dtype=torch.uint8, device="cuda").view(torch.float8_e4m3fn) for _ in range(2))
+    ks, vs = (torch.empty((n_pages, K, 1), device="cuda") for _ in range(2))
+    lens = [37, 200]
+    need = [-(-(n + R) // page) for n in lens]
+    ids = [n_pages - 1 - i for i in range(sum(need))]
+    table = torch.zeros((2, max(need)), dtype=torch.int32, device="cuda")
+    table[0, :need[0]], table[1, :need[1]] = i32(ids[:need[0]]), i32(ids[need[0]:])
+    fill(g, k, ks, table, lens)
+    fill(g, v, vs, table, lens)
+    low, small = min(ids), table - min(ids)      # the same pages alone
+    kr, vr, ksr, vsr = (x[low:].clone() for x in (k, v, ks, vs))
+    q, kn, vn = make_rows(g, 2, R, heads, K, 64, torch.bfloat16, True)      # (300, 20): the kernel for prompts
+    ref.append(kr, ksr, small, lens, [R, R], kn)
+    ref.append(vr, vsr, small, lens, [R, R], vn)
+    c = serving.PagedCache8(k, v, ks, vs, table)
+    out, lse = c.attend(q, i32(lens), k_new=kn, v_new=vn)
+    assert c.status() == 0
+    assert torch.equal(codes(k[low:]), codes(kr)) and torch.equal(codes(v[low:]), codes(vr))
+    compare(out, lse, *ref.attend(q, kr, vr, ksr, vsr, small, lens, [R, R], True, 0.125))

@@ -291,3 +291,26 @@ def test_refusals(built_lib, cuda):
         with pytest.raises(A.AsrSpecError):
             serving.PagePool(caches, held, refs)
     assert s.pool.status() == 0
+
+
+def test_offsets_past_32_bits(built_lib, cuda):
+    """A pool of more than 4 GB: copies from its last pages to others of them, and to its front."""
+    from paper_2608_12703_gb300 import serving
+    page, n_pages = 16, (9 << 29) // (16 * 64 * 2)
+    k, v = (torch.empty((n_pages, 1, page, 64), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    refs = torch.full((n_pages,), 1, dtype=torch.int32, device="cuda")      # all others are in use
+    a, b, c = n_pages - 1, n_pages - 2, n_pages - 3
+    refs[a], refs[b], refs[c], refs[5] = 2, 0, 2, 0
+    table = i32([[c, a, 0], [c, a, 0]])
+    held = i32([2, 2])
+    k[a], v[a] = 3.0, 4.0
+    k[c], v[c] = 5.0, 6.0
+    pool = serving.PagePool(serving.PagedCache(k, v, table), held, refs)
+    counts = pool.reserve(i32([20, 20]), i32([1, 1]))[3]
+    # two share the last page and both write: the lower one keeps it, the other takes the lowest free page
+    assert counts.tolist() == [1, 1] and table[:, 1].tolist() == [a, 5] and int(refs[a]) == 1 and int(refs[5]) == 1
+    assert bool((k[5, :, :4] == 3.0).all()) and bool((v[5, :, :4] == 4.0).all())
+    where, live = pool.compact()[2:]
+    assert int(live) == n_pages - 1 and int(where[a]) == b and table.tolist()[0][:2] == [c, b] and table.tolist()[1][:2] == [c, 5]
+    assert bool((k[b, :, :4] == 3.0).all()) and bool((k[c] == 5.0).all()) and refs[-4:].tolist() == [1, 2, 1, 0]
+    assert pool.status() == 0
