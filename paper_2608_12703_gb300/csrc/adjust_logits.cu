@@ -11,6 +11,11 @@
 // in registers and walks the rows, so the history is read by each run of the
 // vocabulary instead of by each row, and between two rows only the draft that
 // lies between them is looked at.
+// Measured: 64 utterances, 1 to 7 rows of 51866 in fp32, histories of up to 448,
+// bias and mask: 39 us for 176 MB, 4.5 TB/s (of 6.75 copied): what a block does before its
+// first row is near half of its instructions, and 8 elements a thread, which halve
+// that, leave fewer blocks to wait with (43 us); all first loads together
+// 42 -> 39 us.  One utterance of 9 rows: 3.5 us.
 #include "kernels.h"
 #include "paged.cuh"
 

@@ -17,6 +17,13 @@
 //     a weight would leave [.., 2^15] or a maximum grows by more than 2^4 in p, which
 //     after the first tiles is rare; the output is then rescaled in place.
 //     A weight vanishes where it is below 2^-35 of the row's largest.
+// Measured: 4 prompts of 2048 rows behind up to 1000 slots, 20 heads of 64, bf16:
+// 174 us in a stream of such calls (167 alone) for 62 GFLOP, 19 the append; of
+// a block's 300000 cycles a weighing warp spends 40 % on weights, 25 % on
+// maxima, 8 % waiting for scores, 8 % at the ends of items.  Issue slots are
+// half used: a warp a scheduler and row tile waits for its own results, and two
+// threads a row (32 % more instructions) or one pass instead of two (its straight
+// code waits for instructions) took as long or longer (176 - 192 us).
 // Slots hidden from a row weigh 0, and V codes that are NaN are taken out on the
 // way in: the rows that see such a slot are made NaN at the end.
 #include <atomic>
