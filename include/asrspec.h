@@ -598,8 +598,8 @@ int asr_spec_paged8_append(const asr_paged8_cache* cache, const asr_paged_rows* 
  * (bf16 rows are brought to fp16 by a power of two: elements below 2^-30 of a
  * row's largest lose bits) and are summed in fp32, softmax statistics in fp32; weights times the
  * groups' scales are rounded to fp16 for the second product, and those below 2^-35 of a row's largest
- * vanish there (the statistics have them).  Scales are positive and finite; a row of q
- * that holds an infinity comes out as NaN.
+ * vanish there (the statistics have them).  Scales are positive and finite, or zero for zeros; rows
+ * that see another one mean nothing.  A row of q that holds an infinity comes out as NaN.
  * ws: asr_spec_paged8_attend_ws bytes, 16-byte aligned, zero before its first use; every call
  * leaves it ready for the next on its stream, whatever that one's sizes. */
 int64_t asr_spec_paged8_attend_ws(const asr_paged8_cache* cache, const asr_paged_rows* rows, int32_t dtype);
@@ -617,7 +617,7 @@ typedef struct {
   int32_t* table_out;
   int64_t table_out_stride;
   int32_t *held_out, *refs_out;
-  int32_t n_pages, page_size, max_pages, batch;   /* batch 1 .. 1024 */
+  int32_t n_pages, page_size, max_pages, batch;   /* batch 1 .. 1024; n_pages and batch * max_pages at most 2^30 */
   int32_t* status;
 } asr_page_pool;
 
@@ -680,7 +680,7 @@ typedef struct {
   int32_t batch, rows, vocab, dtype;   /* rows 1 .. 32; dtype 0 = fp32, 1 = bf16, 2 = fp16 */
   const int32_t* history;      /* [batch][history_stride] tokens before row 0; NULL: history_max 0 */
   int64_t history_stride;
-  int32_t history_max;         /* tokens a row of history has room for */
+  int32_t history_max;         /* tokens a row of history has room for, at most 2^30 */
   const int32_t *history_len;  /* [batch] tokens in use; NULL: history_max each */
   const int32_t *prompt_len;   /* [batch] of these, the prompt's; NULL: 0 */
   const int32_t *draft;        /* [batch][rows - 1] tokens between the rows, or NULL */

@@ -243,7 +243,7 @@ extern "C" int asr_spec_adjust_logits(const asr_logit_rules* r, void* stream) {
   for (int64_t s : {r->batch_stride, r->row_stride, r->out_batch_stride, r->out_row_stride})
     if (s >= (1ll << 45)) return ASR_E_INVAL;
   if (r->out == r->logits && (r->out_batch_stride != r->batch_stride || r->out_row_stride != r->row_stride)) return ASR_E_INVAL;
-  if (r->history_max < 0 || r->history_stride < r->history_max || (!r->history && r->history_max > 0)) return ASR_E_INVAL;
+  if (r->history_max < 0 || r->history_max > (1 << 30) || r->history_stride < r->history_max || (!r->history && r->history_max > 0)) return ASR_E_INVAL;
   if (r->bias_stride < 0 || r->mask_batch_stride < 0 || r->mask_row_stride < 0) return ASR_E_INVAL;
   for (const void* x : {(const void*)r->history, (const void*)r->history_len, (const void*)r->prompt_len, (const void*)r->draft,
                         (const void*)r->lens, (const void*)r->repetition, (const void*)r->frequency, (const void*)r->presence,

@@ -335,20 +335,22 @@ __global__ void __launch_bounds__(C::WARPS * 32, 1) attend8_kernel(const Attend8
             l_run[nt][x & 1] += p[u][x];
           }
         }
-        for (;;) {
+        // One pass but at a first tile or a much larger scale, four at most; the bound is for scales that are infinite.
+        for (int pass = 0;; ++pass) {
           float big[2] = {0.f, 0.f};
 #pragma unroll
           for (int u = 0; u < NG; ++u) {
             float w[4];
 #pragma unroll
             for (int x = 0; x < 4; ++x) {
-              w[x] = p[u][x] * fminf(vs[u] * inv[nt][x & 1], MOST);
+              const float f = vs[u] * inv[nt][x & 1];
+              w[x] = p[u][x] * (f > MOST ? MOST : f);   // a scale that is no number shows
               big[x & 1] = fmaxf(big[x & 1], w[x]);
             }
             pb[nt][u][0] = Mma16<__half>::pack(w[0], w[1]);
             pb[nt][u][1] = Mma16<__half>::pack(w[2], w[3]);
           }
-          if (!__any_sync(0xffffffffu, big[0] > TOP || big[1] > TOP)) break;
+          if (!__any_sync(0xffffffffu, big[0] > TOP || big[1] > TOP) || pass == 4) break;
 #pragma unroll
           for (int x = 0; x < 2; ++x) {
             big[x] = fmaxf(big[x], __shfl_xor_sync(0xffffffffu, big[x], 4));

@@ -603,6 +603,7 @@ int pool_view(const asr_page_pool* c, bool with_held_out, PoolView* v) {
   if (!c || !c->page_table || !c->held || !c->refs || !c->table_out || !c->refs_out || (with_held_out && !c->held_out))
     return ASR_E_INVAL;
   if (c->batch < 1 || c->batch > PG_MAX_BATCH || c->n_pages < 1) return ASR_E_INVAL;
+  if (c->n_pages > (1 << 30) || (long long)c->batch * c->max_pages > (1ll << 30)) return ASR_E_CAPACITY;   // 32-bit counts and steps
   if (c->page_size < PG_GROUP || c->page_size % PG_GROUP || c->page_size > (1 << 20)) return ASR_E_INVAL;
   if (c->max_pages < 1 || (long long)c->max_pages * c->page_size > (1ll << 30)) return ASR_E_INVAL;
   if (c->table_stride < c->max_pages || c->table_out_stride < c->max_pages) return ASR_E_INVAL;

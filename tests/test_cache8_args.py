@@ -120,6 +120,8 @@ def test_pool_arguments(L):
         assert all(rc == INVAL for rc in pool_calls(L, p, **kw)), kw
     assert L.asr_spec_pool_reserve(p, 4096, 1, 64, 64, None, 4096, BIG, None) == INVAL
     assert L.asr_spec_pool_fork(p, 66, None, 4096, BIG, None) == INVAL
+    for large in (dict(n_pages=(1 << 30) + 1), dict(batch=1024, max_pages=(1 << 20) + 1, table_stride=1 << 21, table_out_stride=1 << 21)):
+        assert all(rc == CAPACITY for rc in pool_calls(L, ref(pool(**large)))) and L.asr_spec_pool_ws(ref(pool(**large))) == CAPACITY
     n = L.asr_spec_pool_ws(p)
     assert n > 0 and all(rc == CAPACITY for rc in pool_calls(L, p, size=n - 1))
 
@@ -155,7 +157,7 @@ def test_plans(L):
     dict(logits=None), dict(out=None), dict(batch=0), dict(batch=65536), dict(rows=0), dict(rows=33), dict(vocab=0), dict(dtype=3),
     dict(dtype=-1), dict(logits=4098), dict(out=8193), dict(row_stride=99), dict(out_row_stride=99), dict(batch_stride=99),
     dict(out_batch_stride=0), dict(batch_stride=-400), dict(out=4096, out_row_stride=101), dict(out=4096, out_batch_stride=401),
-    dict(history=None), dict(history_max=-1), dict(history_stride=19), dict(history=66), dict(history_len=66), dict(prompt_len=65),
+    dict(history=None), dict(history_max=-1), dict(history_max=(1 << 30) + 1, history_stride=1 << 31), dict(history_stride=19), dict(history=66), dict(history_len=66), dict(prompt_len=65),
     dict(draft=65), dict(lens=65), dict(repetition=65), dict(frequency=65), dict(presence=65), dict(bias=65), dict(mask=66),
     dict(bias_stride=-1), dict(mask_row_stride=-1), dict(mask_batch_stride=-1), dict(repetition_all=0.0), dict(repetition_all=-1.0),
     dict(repetition_all=float("nan")), dict(frequency_all=float("inf")), dict(presence_all=float("nan")), dict(status=2), None], ids=str)

@@ -400,3 +400,26 @@ def test_offsets_past_32_bits(built_lib, cuda, R, heads):
     assert c.status() == 0
     assert torch.equal(codes(k[low:]), codes(kr)) and torch.equal(codes(v[low:]), codes(vr))
     compare(out, lse, *ref.attend(q, kr, vr, ksr, vsr, small, lens, [R, R], True, 0.125))
+
+
+@pytest.mark.parametrize("R", [1, 20, 70])
+@pytest.mark.parametrize("copies", [1, 10])
+def test_scales_that_are_no_scales(built_lib, cuda, R, copies):
+    """Scales that are zero stand for zeros; infinite, NaN and negative ones spoil no other sequence and end all the same."""
+    from paper_2608_12703_gb300 import serving
+    g = gen(26)
+    lens = [100, 90, 80, 70, 60, 50] * copies
+    k, v, ks, vs, table = pool(g, 2, 64, 16, lens)
+    fill(g, k, ks, table, lens)
+    fill(g, v, vs, table, lens)
+    for b in range(0, len(lens), 6):
+        vs[int(table[b, 1])], ks[int(table[b + 1, 1])] = math.nan, math.inf
+        vs[int(table[b + 2, 0])], vs[int(table[b + 3, 2])] = math.inf, -1.0
+        ks[int(table[b + 4, 0])], vs[int(table[b + 4, 1])] = 0.0, 0.0
+    q = make_rows(g, len(lens), R, 4, 2, 64, torch.bfloat16, True)[0]
+    c = serving.PagedCache8(k, v, ks, vs, table)
+    out, lse = c.attend(q, i32(lens), causal=False)
+    assert c.status() == 0
+    want = ref.attend(q, k, v, ks, vs, table, lens, [R] * len(lens), False, 0.125)
+    good = [b for b in range(len(lens)) if b % 6 > 3]
+    compare(out[good], lse[good], *(x[good] for x in want))
