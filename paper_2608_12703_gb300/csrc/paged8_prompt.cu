@@ -54,7 +54,7 @@ template <int D> struct Prompt8Mem {
 };
 
 struct Prompt8Bars {   // s, p: a buffer of scores; pv, q: a row tile
-  uint64_t q_full[2], k_full[2], k_free[2], v_full[2], v_free[2], sc_full[8], s_full[3], p_full[3], pv_done[2][4], item_full[4], ended[4];
+  uint64_t q_full[2], k_full[2], k_free[2], v_full[2], v_free[2], sc_full[8], s_full[3], p_full[3], pv_done[2][4], item_full[4], begun[4], ended[4];
 };
 struct GroupScales {   // of a tile's 8 groups
   float k[8], v[8], lv[8];
@@ -281,7 +281,7 @@ __global__ void __launch_bounds__(THREADS, 1) prompt8_kernel(const Prompt8Args a
     }
     for (int i = 0; i < 3; ++i) mbar_init(&bars.s_full[i], 1), mbar_init(&bars.p_full[i], 4);
     for (int i = 0; i < 8; ++i) mbar_init(&bars.sc_full[i], 2);
-    for (int i = 0; i < 4; ++i) mbar_init(&bars.item_full[i], 1), mbar_init(&bars.ended[i], 8 + 5 + 1);
+    for (int i = 0; i < 4; ++i) mbar_init(&bars.item_full[i], 1), mbar_init(&bars.begun[i], 1), mbar_init(&bars.ended[i], 8 + 5 + 1);
     fence_mbar_init();
   }
   for (int b = tid; b < c.batch; b += THREADS) paged_lens(c, r, b, lens[b].x, lens[b].y);
@@ -350,14 +350,16 @@ __global__ void __launch_bounds__(THREADS, 1) prompt8_kernel(const Prompt8Args a
     };
     Item it{};
     float next_sc = 0.f;
-    bool more = true;
+    bool more = true, idle = false;
     for (int k = -1; more; ++k) {   // before the first item one without rows
       const int nx = x ? it.n1 : it.n0, m = it.m0 + x * BM + row_in;
       const bool mine = m < it.rows * r.group;
       const int lim = mine ? min(it.keys, seen_by(r, it.len, m)) : 0, all_see = nx ? seen_by(r, it.len, it.m0 + x * BM) : 0;
       const float sc = next_sc;
-      if (nx == 0)   // keeps step with the other tile's: the waits to come are for the phase after these
-        for (int i = pairs; i < pairs + it.n0 + it.n1; ++i) bar_wait(&bars.s_full[i % NS], i / NS & 1, c.status, gave_up);
+      // A wait tells a phase only from the one before.  A row tile that sat out an item has seen none of its phases: it goes
+      // on once the products have come to this item, when all of them have passed.
+      if (nx > 0 && idle) bar_wait(&bars.begun[k & 3], k >> 2 & 1, c.status, gave_up);
+      idle = nx == 0;
       float mx = -INFINITY, l = 0.f;   // the maximum, in units of the product; the sum of p
       int li = 126;                    // log2 of what weights are multiplied by
       Item next;
@@ -583,6 +585,7 @@ __global__ void __launch_bounds__(THREADS, 1) prompt8_kernel(const Prompt8Args a
     Item it;
     for (int k = 0; src.take(k, it, gave_up); ++k) {
       const int n = it.n0 + it.n1;
+      mbar_arrive(&bars.begun[k & 3]);   // nothing of the items before is left to be issued
       // Scores run ahead of outputs by all buffers but one, within an item: the next one's q comes from threads that may
       // wait for outputs.  Pair i: key tile i / 2 of row tile i % 2, the last one of row tile 1; of row tile 0 alone i.
       for (int i = 0; i < n + NS - 1; ++i) {
