@@ -204,6 +204,44 @@ __device__ __forceinline__ float weigh(uint32_t at, bool full, int left, const G
   return sum;
 }
 
+// Both looks at once, the weights to p_at: relative to the maximum and the reference of the tiles before, which the caller
+// compares with what it finds.  ready(): p_at may be written.
+template <typename F>
+__device__ __forceinline__ float weigh_once(uint32_t at, uint32_t p_at, bool full, int left, const GroupScales& gs, float base, float sc,
+                                            int li, float& most, float& top, F ready) {
+  const uint64_t base2 = two(-base, -base), sc2 = two(sc, sc);
+  float sum = 0.f;
+  most = top = -INFINITY;
+  for_scores(at, full, left, [&](int q, uint32_t (&s)[32]) {
+    uint32_t p[16];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const uint32_t* x = s + h * 16;
+      float g = fmaxf(__uint_as_float(x[0]), __uint_as_float(x[1]));
+#pragma unroll
+      for (int i = 2; i < 16; i += 2) g = max3(g, __uint_as_float(x[i]), __uint_as_float(x[i + 1]));
+      const float ks = gs.k[q * 2 + h], lv = gs.lv[q * 2 + h], lf = fmaxf(lv + (float)li, -60.f);
+      g *= ks;
+      most = fmaxf(most, g);
+      top = fmaxf(top, (g - base) * sc + lv);
+      const uint64_t ks2 = two(ks, ks), lf2 = two(lf, lf);
+      uint64_t sum2 = 0;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float2 t = parts(fma2(fma2(two(__uint_as_float(x[2 * i]), __uint_as_float(x[2 * i + 1])), ks2, base2), sc2, lf2));
+        const float w0 = ex2(t.x), w1 = ex2(t.y);
+        sum2 = add2(sum2, two(w0, w1));
+        p[h * 8 + i] = Mma16<__half>::pack(w0, w1);
+      }
+      const float2 part = parts(sum2);
+      sum = fmaf(part.x + part.y, ex2(-lf), sum);
+    }
+    if (q == 0) ready();
+    tmem_st16(p_at + q * 16, p);
+  });
+  return sum;
+}
+
 // What a block works on.
 struct Item {
   int b, kvh, m0, len, rows, keys;
@@ -258,7 +296,9 @@ template <typename T, int D>
 __global__ void __launch_bounds__(THREADS, 1) prompt8_kernel(const Prompt8Args a) {
   using M = Prompt8Mem<D>;
   // Buffers of scores: with a third one a row tile's next scores are there before its weights are.  Tensor memory holds it beside outputs of 64.
-  constexpr int HB = M::HB, NS = D == 64 ? 3 : 2, O_COL = NS * BN;
+  constexpr int HB = M::HB, NS = 2;
+  constexpr bool ONCE = D == 64;
+  constexpr int P_COL = 2 * BN, O_COL = ONCE ? P_COL + BN : 2 * BN, P_STEP = ONCE ? BN / 2 : BN;
   static_assert(O_COL + 2 * D <= 512, "");
   extern __shared__ uint8_t raw[];
   __shared__ __align__(8) Prompt8Bars bars;
@@ -379,44 +419,84 @@ __global__ void __launch_bounds__(THREADS, 1) prompt8_kernel(const Prompt8Args a
         tc_fence_after();
         const bool full = (j + 1) * BN <= all_see;   // of every row that counts
         const int left = lim - j * BN;               // columns that this row sees
-        float most, top;
-        float grown = 0.f;
-        int up = 0;
-#pragma unroll 1
-        for (bool again = false;; again = true) {   // the largest weight is relative to the maximum: where that grows, once more
-          look(s_at, full, left, gs, mx, sc, most, top);
-          if (again || !__any_sync(0xffffffffu, (most - mx) * sc > 4.f)) break;
-          if (most > mx) {
-            grown = mx == -INFINITY ? 0.f : (most - mx) * sc;
-            up = min((int)fminf(grown, 1000.f), 126 - li);
-            mx = most, l *= ex2(-grown), li += up;
-          }
+        // Once a tile's products have been added: a wait cannot tell a phase from the one after the next, but of four barriers
+        // in turn the one of four tiles ago is known to have passed, since scores run ahead by fewer.
+        auto added = [&](int t) {
+          bar_wait(&bars.pv_done[x][(steps + t) & 3], (steps + t) >> 2 & 1, c.status, gave_up);
           __syncwarp();
-        }
-        if (__any_sync(0xffffffffu, grown > 0.f || top + (float)li > 15.f)) {
-          const int e = top + (float)li > 11.f ? min((int)ceilf(top) + li - 11, li + 126) : 0;
-          li -= e;
-          if (j > 0) {   // the tile before has been added
-            const float f = ex2((float)(up - e) - grown);
-            // Four barriers in turn: a wait cannot tell a phase from the one after the next, and the tile of four steps ago is
-            // known to be done, since scores run ahead by fewer
-            bar_wait(&bars.pv_done[x][(steps + j - 1) & 3], (steps + j - 1) >> 2 & 1, c.status, gave_up);
-            __syncwarp();
-            tc_fence_after();
+          tc_fence_after();
+        };
+        auto rescale = [&](float f) {
 #pragma unroll 1
-            for (int q = 0; q < D / 32; ++q) {
-              uint32_t o[32];
-              tmem_ld32(o_at + q * 32, o);
-              tmem_wait_ld();
+          for (int q = 0; q < D / 32; ++q) {
+            uint32_t o[32];
+            tmem_ld32(o_at + q * 32, o);
+            tmem_wait_ld();
 #pragma unroll
-              for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
-              tmem_st16(o_at + q * 32, o);
-              tmem_st16(o_at + q * 32 + 16, o + 16);
-            }
+            for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+            tmem_st16(o_at + q * 32, o);
+            tmem_st16(o_at + q * 32 + 16, o + 16);
           }
-          __syncwarp();
+        };
+        if constexpr (ONCE) {
+          float most, top, sum, shift = 0.f;   // log2 of what the output so far is to be multiplied by
+          bool moved = false;
+#pragma unroll 1
+          for (int pass = 0;; ++pass) {
+            sum = weigh_once(s_at, tmem + lanes + P_COL + buf * P_STEP, full, left, gs, mx == -INFINITY ? 0.f : mx, sc, li, most, top, [&] {
+              if (pass == 0 && j > 0) added(j - 1);
+            });
+            // The first tile brings the first maximum and, once the weights are relative to that, their size.  Later ones move
+            // them only where a weight would leave fp16 or p grows past 2^4.  At most three passes.
+            if (!__any_sync(0xffffffffu, (most - mx) * sc > 4.f || top + (float)li > 15.f || (j == 0 && top + (float)li < 4.f && li < 126)) ||
+                pass == 4)
+              break;
+            moved = true;
+            if (most > mx) {
+              if (mx == -INFINITY) {
+                top = -126.f;
+                for (int u = 0; u < 8; ++u) top = fmaxf(top, gs.lv[u]);
+              } else {
+                const float grown = (most - mx) * sc;
+                const int up = min((int)fminf(grown, 1000.f), 126 - li);
+                top -= grown, shift += (float)up - grown;
+                l *= ex2(-grown), li += up;
+              }
+              mx = most;
+            }
+            const int to = top > -1e4f ? max(-126, min(126, 11 - (int)ceilf(fminf(top, 1000.f)))) : li;
+            if (to < li ? top + (float)li > 11.f : j == 0) shift += (float)(to - li), li = to;
+            __syncwarp();
+          }
+          if (moved && j > 0) rescale(ex2(shift));
+          l += sum;
+        } else {
+          float most, top;
+          float grown = 0.f;
+          int up = 0;
+#pragma unroll 1
+          for (bool again = false;; again = true) {   // the largest weight is relative to the maximum: where that grows, once more
+            look(s_at, full, left, gs, mx, sc, most, top);
+            if (again || !__any_sync(0xffffffffu, (most - mx) * sc > 4.f)) break;
+            if (most > mx) {
+              grown = mx == -INFINITY ? 0.f : (most - mx) * sc;
+              up = min((int)fminf(grown, 1000.f), 126 - li);
+              mx = most, l *= ex2(-grown), li += up;
+            }
+            __syncwarp();
+          }
+          if (__any_sync(0xffffffffu, grown > 0.f || top + (float)li > 15.f)) {
+            const int e = top + (float)li > 11.f ? min((int)ceilf(top) + li - 11, li + 126) : 0;
+            li -= e;
+            if (j > 0) {   // the tile before has been added
+              const float f = ex2((float)(up - e) - grown);
+              added(j - 1);
+              rescale(f);
+            }
+            __syncwarp();
+          }
+          l += weigh(s_at, full, left, gs, mx == -INFINITY ? 0.f : mx, sc, li);
         }
-        l += weigh(s_at, full, left, gs, mx == -INFINITY ? 0.f : mx, sc, li);
         tmem_wait_st();
         tc_fence_before();
         warp_arrive(&bars.p_full[buf]);
@@ -586,15 +666,19 @@ __global__ void __launch_bounds__(THREADS, 1) prompt8_kernel(const Prompt8Args a
     for (int k = 0; src.take(k, it, gave_up); ++k) {
       const int n = it.n0 + it.n1;
       mbar_arrive(&bars.begun[k & 3]);   // nothing of the items before is left to be issued
-      // Scores run ahead of outputs by all buffers but one, within an item: the next one's q comes from threads that may
-      // wait for outputs.  Pair i: key tile i / 2 of row tile i % 2, the last one of row tile 1; of row tile 0 alone i.
-      for (int i = 0; i < n + NS - 1; ++i) {
+      // Scores run ahead of outputs within an item: the next one's q comes from threads that may wait for outputs.  Where weights
+      // have a place of their own, by two pairs, a buffer being free once its scores are weighed; where they take the scores'
+      // place, by one.  Pair i: key tile i / 2 of row tile i % 2, the last one of row tile 1; of row tile 0 alone i.
+      constexpr int LAG = ONCE ? 2 : 1;
+      for (int i = 0; i < n + LAG; ++i) {
+        const int o = i - LAG, o_buf = (pairs + o) & 1;
+        if (ONCE && o >= 0) bar_wait(&bars.p_full[o_buf], (pairs + o) >> 1 & 1, c.status, gave_up);
         if (i < n) {
           const int x = it.n1 == 0 ? 0 : i < 2 * it.n0 ? i & 1 : 1, j = it.n1 == 0 ? i : i >> 1, st = tiles + j & 1;
           if (j == 0) bar_wait(&bars.q_full[x], (x ? qs1++ : qs0++) & 1, c.status, gave_up);
           bar_wait(&bars.k_full[st], tiles + j >> 1 & 1, c.status, gave_up);
           tc_fence_after();
-          const int buf = (pairs + i) % NS;
+          const int buf = (pairs + i) & 1;
 #pragma unroll
           for (int h = 0; h < HB; ++h)
 #pragma unroll
@@ -603,17 +687,16 @@ __global__ void __launch_bounds__(THREADS, 1) prompt8_kernel(const Prompt8Args a
           umma_commit(&bars.s_full[buf]);
           if (x == 1 || j >= it.n1) umma_commit(&bars.k_free[st]);
         }
-        if (i >= NS - 1) {
-          const int o = i - (NS - 1), x = it.n1 == 0 ? 0 : o < 2 * it.n0 ? o & 1 : 1, j = it.n1 == 0 ? o : o >> 1, st = tiles + j & 1;
-          const int buf = (pairs + o) % NS;
+        if (o >= 0) {
+          const int x = it.n1 == 0 ? 0 : o < 2 * it.n0 ? o & 1 : 1, j = it.n1 == 0 ? o : o >> 1, st = tiles + j & 1;
           bar_wait(&bars.v_full[st], tiles + j >> 1 & 1, c.status, gave_up);
-          bar_wait(&bars.p_full[buf], (pairs + o) / NS & 1, c.status, gave_up);
+          if (!ONCE) bar_wait(&bars.p_full[o_buf], (pairs + o) >> 1 & 1, c.status, gave_up);
           tc_fence_after();
 #pragma unroll
           for (int h = 0; h < HB; ++h)
 #pragma unroll
             for (int y = 0; y < BN / 16; ++y)
-              umma_f16_ts(tmem + O_COL + x * D + h * 64, tmem + buf * BN + y * 8, vd + st * STEP + h * (M::BLOCK / 16) + y * 128, id_o, j + y > 0);
+              umma_f16_ts(tmem + O_COL + x * D + h * 64, tmem + (ONCE ? P_COL : 0) + o_buf * P_STEP + y * 8, vd + st * STEP + h * (M::BLOCK / 16) + y * 128, id_o, j + y > 0);
           umma_commit(&bars.pv_done[x][(x ? pv1++ : pv0++) & 3]);
           if (x == 1 || j >= it.n1) umma_commit(&bars.v_free[st]);
         }
