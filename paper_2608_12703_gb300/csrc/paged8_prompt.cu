@@ -269,12 +269,11 @@ struct Items {
     it.n1 = it.m0 + BM >= m_rows ? 0 : (seen_by(a.r, it.len, min(it.m0 + 2 * BM, m_rows) - 1) + BN - 1) / BN;
     return it.n0 > 0;
   }
-  // the block's item k; false past the end
+  // the block's item k, for a warp; false past the end
   __device__ __forceinline__ bool take(int k, Item& it, bool& gave_up) const {
     bar_wait(&bars.item_full[k & 3], k >> 2 & 1, a.p.c.status, gave_up);
     const int i = gave_up ? -1 : *reinterpret_cast<volatile int*>(slots + (k & 3));
-    if (i < 0) return false;
-    return set(i, it);
+    return __all_sync(0xffffffffu, i >= 0 && set(i, it));   // a whole warp: one answer where a wait has given up too
   }
   __device__ __forceinline__ void fetch(int k, bool& gave_up) const {   // one thread
     if (k >= 4) bar_wait(&bars.ended[k & 3], (k >> 2) - 1 & 1, a.p.c.status, gave_up);
@@ -286,6 +285,11 @@ struct Items {
   }
   __device__ __forceinline__ void leave(int k) const { mbar_arrive(&bars.ended[k & 3]); }
 };
+__device__ __forceinline__ bool elect_one() {
+  uint32_t one;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(one));
+  return one != 0;
+}
 // One arrival a warp, after all its lanes: arrivals at one barrier go one by one.
 __device__ __forceinline__ void warp_arrive(uint64_t* bar) {
   __syncwarp();
@@ -655,8 +659,10 @@ __global__ void __launch_bounds__(THREADS, 1) prompt8_kernel(const Prompt8Args a
       }
       if (more) load();
     }
-  } else if (warp == 14 && lane == 0) {
+  } else if (warp == 14) {
     // ------------------------------------------------------------ products
+    // The whole warp walks, one lane issues: what the instructions take stays in uniform registers that way.
+    const bool lead = elect_one();
     constexpr uint32_t F32 = 1u << 4, M128 = (uint32_t)(BM >> 4) << 24;   // accumulator type; fp16 operands are 0
     constexpr uint32_t id_s = F32 | M128 | (uint32_t)(BN >> 3) << 17, id_o = F32 | M128 | 8u << 17 | 1u << 16;   // V: contraction axis outermost
     const uint64_t qd = umma_desc_sw128(smem + M::Q), kd = umma_desc_sw128(smem + M::K), vd = desc_mn(smem + M::V);
@@ -664,8 +670,8 @@ __global__ void __launch_bounds__(THREADS, 1) prompt8_kernel(const Prompt8Args a
     int pairs = 0, tiles = 0, qs0 = 0, qs1 = 0, pv0 = 0, pv1 = 0;   // pairs and key tiles before this item; of each row tile: q's, outputs begun
     Item it;
     for (int k = 0; src.take(k, it, gave_up); ++k) {
-      const int n = it.n0 + it.n1;
-      mbar_arrive(&bars.begun[k & 3]);   // nothing of the items before is left to be issued
+      const int n0 = __shfl_sync(0xffffffffu, it.n0, 0), n1 = __shfl_sync(0xffffffffu, it.n1, 0), n = n0 + n1;
+      if (lead) mbar_arrive(&bars.begun[k & 3]);   // nothing of the items before is left to be issued
       // Scores run ahead of outputs within an item: the next one's q comes from threads that may wait for outputs.  Where weights
       // have a place of their own, by two pairs, a buffer being free once its scores are weighed; where they take the scores'
       // place, by one.  Pair i: key tile i / 2 of row tile i % 2, the last one of row tile 1; of row tile 0 alone i.
@@ -674,35 +680,42 @@ __global__ void __launch_bounds__(THREADS, 1) prompt8_kernel(const Prompt8Args a
         const int o = i - LAG, o_buf = (pairs + o) & 1;
         if (ONCE && o >= 0) bar_wait(&bars.p_full[o_buf], (pairs + o) >> 1 & 1, c.status, gave_up);
         if (i < n) {
-          const int x = it.n1 == 0 ? 0 : i < 2 * it.n0 ? i & 1 : 1, j = it.n1 == 0 ? i : i >> 1, st = tiles + j & 1;
+          const int x = n1 == 0 ? 0 : i < 2 * n0 ? i & 1 : 1, j = n1 == 0 ? i : i >> 1, st = tiles + j & 1;
           if (j == 0) bar_wait(&bars.q_full[x], (x ? qs1++ : qs0++) & 1, c.status, gave_up);
           bar_wait(&bars.k_full[st], tiles + j >> 1 & 1, c.status, gave_up);
           tc_fence_after();
           const int buf = (pairs + i) & 1;
+          if (lead) {
 #pragma unroll
-          for (int h = 0; h < HB; ++h)
+            for (int h = 0; h < HB; ++h)
 #pragma unroll
-            for (int y = 0; y < 4; ++y)
-              umma_f16(tmem + buf * BN, qd + x * STEP + h * (M::BLOCK / 16) + y * 2, kd + st * STEP + h * (M::BLOCK / 16) + y * 2, id_s, h + y > 0);
-          umma_commit(&bars.s_full[buf]);
-          if (x == 1 || j >= it.n1) umma_commit(&bars.k_free[st]);
+              for (int y = 0; y < 4; ++y)
+                umma_f16(tmem + buf * BN, qd + x * STEP + h * (M::BLOCK / 16) + y * 2, kd + st * STEP + h * (M::BLOCK / 16) + y * 2, id_s, h + y > 0);
+            umma_commit(&bars.s_full[buf]);
+            if (x == 1 || j >= n1) umma_commit(&bars.k_free[st]);
+          }
+          __syncwarp();
         }
         if (o >= 0) {
-          const int x = it.n1 == 0 ? 0 : o < 2 * it.n0 ? o & 1 : 1, j = it.n1 == 0 ? o : o >> 1, st = tiles + j & 1;
+          const int x = n1 == 0 ? 0 : o < 2 * n0 ? o & 1 : 1, j = n1 == 0 ? o : o >> 1, st = tiles + j & 1;
           bar_wait(&bars.v_full[st], tiles + j >> 1 & 1, c.status, gave_up);
           if (!ONCE) bar_wait(&bars.p_full[o_buf], (pairs + o) >> 1 & 1, c.status, gave_up);
           tc_fence_after();
+          const int pv = x ? pv1++ : pv0++;
+          if (lead) {
 #pragma unroll
-          for (int h = 0; h < HB; ++h)
+            for (int h = 0; h < HB; ++h)
 #pragma unroll
-            for (int y = 0; y < BN / 16; ++y)
-              umma_f16_ts(tmem + O_COL + x * D + h * 64, tmem + (ONCE ? P_COL : 0) + o_buf * P_STEP + y * 8, vd + st * STEP + h * (M::BLOCK / 16) + y * 128, id_o, j + y > 0);
-          umma_commit(&bars.pv_done[x][(x ? pv1++ : pv0++) & 3]);
-          if (x == 1 || j >= it.n1) umma_commit(&bars.v_free[st]);
+              for (int y = 0; y < BN / 16; ++y)
+                umma_f16_ts(tmem + O_COL + x * D + h * 64, tmem + (ONCE ? P_COL : 0) + o_buf * P_STEP + y * 8, vd + st * STEP + h * (M::BLOCK / 16) + y * 128, id_o, j + y > 0);
+            umma_commit(&bars.pv_done[x][pv & 3]);
+            if (x == 1 || j >= n1) umma_commit(&bars.v_free[st]);
+          }
+          __syncwarp();
         }
       }
-      pairs += n, tiles += it.n();
-      src.leave(k);
+      pairs += n, tiles += max(n0, n1);
+      if (lead) src.leave(k);
     }
   }
   __syncwarp();
