@@ -7,23 +7,27 @@
 //   * 3 warps turn codes into fp16 in 128-byte-swizzled shared memory, two
 //     stages of K and of V, a tile's loads in flight while the one before is
 //     converted; both row tiles use what they write;
-//   * one thread issues tcgen05.mma: S = q K^T (128 x 128, fp32 in tensor
-//     memory) and O += p V with p read from tensor memory, where it takes the
-//     place of the scores.  The two row tiles alternate, so that one's products
+//   * one warp issues tcgen05.mma: S = q K^T (128 x 128, fp32 in tensor
+//     memory) and O += p V with p read from tensor memory: beside the scores for
+//     heads of 64, in their place for heads of 128, whose outputs leave no more
+//     room. The two row tiles alternate, so that one's products
 //     run while the other's scores are being weighed, and scores run ahead;
-//   * 4 warps a row tile, a thread a row, weigh the scores.  The first pass over them takes
-//     each group's maximum, the second the exponentials.  Running maximum and
-//     reference of the weights (as in the kernel for few rows) move only when
-//     a weight would leave [.., 2^15] or a maximum grows by more than 2^4 in p, which
-//     after the first tiles is rare; the output is then rescaled in place.
+//   * 4 warps a row tile, a thread a row, weigh the scores by the maximum and
+//     the reference of the weights (as in the kernel for few rows) of the tiles
+//     before.  Those move only where a weight would leave [.., 2^15] or p grow
+//     past 2^4, which after the first tiles is rare; the output is then rescaled in place.
+//     Heads of 64 see that while they weigh, and weigh such a tile again; heads
+//     of 128, whose weights take the scores' place, look at the scores first.
 //     A weight vanishes where it is below 2^-35 of the row's largest.
 // Measured: 4 prompts of 2048 rows behind up to 1000 slots, 20 heads of 64, bf16:
-// 174 us in a stream of such calls (167 alone) for 62 GFLOP, 19 the append; of
-// a block's 300000 cycles a weighing warp spends 40 % on weights, 25 % on
-// maxima, 8 % waiting for scores, 8 % at the ends of items.  Issue slots are
-// half used: a warp a scheduler and row tile waits for its own results, and two
-// threads a row (32 % more instructions) or one pass instead of two (its straight
-// code waits for instructions) took as long or longer (176 - 192 us).
+// 166 us in a stream of such calls for 62 GFLOP (tensor cores 20 % busy), 19
+// the append; of a block's 280000 cycles a weighing warp spends 60 % on
+// weights, 13 % waiting for scores, 17 % at the ends of items.  Issue slots are
+// half used: a warp a scheduler and row tile waits for its own results.  Two looks at
+// the scores: the same; two threads a row (32 % more instructions): 180 us;
+// products issued by a thread alone instead of a warp with one lane elected: 180, its
+// operands moved to uniform registers one by one; a tile's weights
+// as straight code: 192, it waits for instructions; one item a block at a time: 183.
 // Slots hidden from a row weigh 0, and V codes that are NaN are taken out on the
 // way in: the rows that see such a slot are made NaN at the end.
 #include <atomic>
