@@ -21,13 +21,15 @@
 //     A weight vanishes where it is below 2^-35 of the row's largest.
 // Measured: 4 prompts of 2048 rows behind up to 1000 slots, 20 heads of 64, bf16:
 // 166 us in a stream of such calls for 62 GFLOP (tensor cores 20 % busy), 19
-// the append; of a block's 280000 cycles a weighing warp spends 60 % on
-// weights, 13 % waiting for scores, 17 % at the ends of items.  Issue slots are
-// half used: a warp a scheduler and row tile waits for its own results.  Two looks at
-// the scores: the same; two threads a row (32 % more instructions): 180 us;
-// products issued by a thread alone instead of a warp with one lane elected: 180, its
-// operands moved to uniform registers one by one; a tile's weights
-// as straight code: 192, it waits for instructions; one item a block at a time: 183.
+// the append; of a block's 280000 cycles a weighing warp spends 52 - 59 % on
+// weights, 11 - 16 % waiting for scores, 17 - 19 % between items.  Issue slots are
+// half used: a warp a scheduler and row tile waits for its own results.
+// Append and attention in such a stream, both sides in one run: 186 us, 198
+// where one thread walks and issues the products instead of a warp of which one
+// lane issues.  Before that step 199 us, 201 with two looks at the scores.
+// Tried on earlier forms only, a call each: two threads a row (32 % more
+// instructions) 200.6 us against 200.2; both looks in one as straight code, which
+// waited for its instructions, 224 against 199.
 // Slots hidden from a row weigh 0, and V codes that are NaN are taken out on the
 // way in: the rows that see such a slot are made NaN at the end.
 #include <atomic>
@@ -665,7 +667,7 @@ __global__ void __launch_bounds__(THREADS, 1) prompt8_kernel(const Prompt8Args a
     }
   } else if (warp == 14) {
     // ------------------------------------------------------------ products
-    // The whole warp walks, one lane issues: what the instructions take stays in uniform registers that way.
+    // The whole warp walks, one lane issues: 186 us against 198 where one thread does both (see above).
     const bool lead = elect_one();
     constexpr uint32_t F32 = 1u << 4, M128 = (uint32_t)(BM >> 4) << 24;   // accumulator type; fp16 operands are 0
     constexpr uint32_t id_s = F32 | M128 | (uint32_t)(BN >> 3) << 17, id_o = F32 | M128 | 8u << 17 | 1u << 16;   // V: contraction axis outermost
