@@ -568,7 +568,10 @@ int asr_spec_accept_sampled(const asr_sampled_logits* logits, const int32_t* dra
  * 3 bits of mantissa, largest value 448) where asr_paged_cache has its elements;
  * its values are the codes times
  *   k_scale[page * scale_page_stride + h * scale_head_stride + s % page_size / 16]
- * (v_scale alike): one scale for the 16 slots of a group and a head. */
+ * (v_scale alike): one scale for the 16 slots of a group and a head.  Scales may
+ * share memory (strides of 0: one for all pages or heads; K's and V's the same) in
+ * a cache that is only read; rows are appended only where every group and head has
+ * scales of its own, and K and V codes of their own (ASR_E_INVAL otherwise). */
 typedef struct {
   void *k_pages, *v_pages;
   int64_t page_stride, head_stride, slot_stride;   /* bytes, > 0, multiples of 16 */

@@ -151,7 +151,8 @@ int paged8_view(const asr_paged8_cache* c, Paged8View* v) {
   for (int64_t s : {c->page_stride, c->head_stride, c->slot_stride})
     if (s <= 0 || s % 16 || s >= (1ll << 40)) return ASR_E_INVAL;
   if (c->slot_stride < c->head_dim || c->slot_stride > (1 << 26)) return ASR_E_INVAL;   // 16 slots' offsets fit 32 bits
-  if (c->scale_page_stride < 0 || c->scale_head_stride < 0) return ASR_E_INVAL;
+  for (int64_t s : {c->scale_page_stride, c->scale_head_stride})
+    if (s < 0 || s >= (1ll << 40)) return ASR_E_INVAL;
   v->c.k = static_cast<char*>(c->k_pages);
   v->c.v = static_cast<char*>(c->v_pages);
   v->c.page_stride = c->page_stride;
@@ -174,6 +175,38 @@ int paged8_view(const asr_paged8_cache* c, Paged8View* v) {
   return ASR_OK;
 }
 
+// Whether an element of one array of scales is `apart` elements behind another one of the same array, other than itself:
+//   dp s_page + dh s_head + dg = apart,  |dp| < n_pages, |dh| < kv_heads, |dg| < groups of a page.
+// For each dh only the multiples of s_page next to what is left can come near enough.
+static bool scales_meet(const asr_paged8_cache* c, long long apart) {
+  using Wide = __int128;
+  const Wide groups = c->page_size / PG_GROUP, most = c->n_pages - 1, sp = most ? c->scale_page_stride : 0;
+  const Wide sh = c->kv_heads > 1 ? c->scale_head_stride : 0;
+  if (apart == 0 && most && sp < groups) return true;   // dh = 0: of one head's scales those of two pages
+  for (int dh = apart ? 1 - c->kv_heads : 1; dh < c->kv_heads; ++dh) {
+    const Wide left = apart - dh * sh;
+    Wide at = sp ? left / sp : 0;   // rounded towards 0
+    for (Wide dp : {at - 1, at, at + 1}) {
+      dp = dp < -most ? -most : dp > most ? most : dp;
+      const Wide off = left - dp * sp;
+      if (off < groups && -off < groups) return true;
+    }
+  }
+  return false;
+}
+
+// An append writes scales and codes by (page, head, group), each by a warp of its own: none may share memory with another's.
+// Caches whose scales do (one scale broadcast over pages or heads, K's and V's in one array) can only be read.
+int paged8_writable(const asr_paged8_cache* c) {
+  if (c->k_pages == c->v_pages) return ASR_E_INVAL;
+  const long long apart = (long long)((intptr_t)c->v_scale - (intptr_t)c->k_scale) / 4, groups = c->page_size / PG_GROUP;
+  const __int128 head = c->kv_heads > 1 ? (__int128)(c->kv_heads - 1) * c->scale_head_stride + groups : groups;
+  const __int128 all = c->n_pages > 1 ? (__int128)(c->n_pages - 1) * c->scale_page_stride + head : head;
+  const bool nested = (c->kv_heads == 1 || c->scale_head_stride >= groups) && (c->n_pages == 1 || c->scale_page_stride >= head);
+  if (nested && (apart >= all || -apart >= all)) return ASR_OK;   // as most caches are
+  return apart == 0 || scales_meet(c, 0) || scales_meet(c, apart) ? ASR_E_INVAL : ASR_OK;
+}
+
 // paged_rows of a cache of the rows' type.
 int paged8_rows(const asr_paged8_cache* c, const asr_paged_rows* r, int dtype, PagedRows* v) {
   if (dtype < 0 || dtype > 2) return ASR_E_INVAL;
@@ -192,6 +225,7 @@ extern "C" int asr_spec_paged8_append(const asr_paged8_cache* c, const asr_paged
   PagedRows w;
   if (int rc = paged8_view(c, &v)) return rc;
   if (!r || !r->k_new || !r->v_new) return ASR_E_INVAL;
+  if (int rc = paged8_writable(c)) return rc;
   asr_paged_rows rows = *r;   // the queries are not looked at: the new rows stand in for them
   rows.q = r->k_new;
   rows.q_batch_stride = rows.q_row_stride = rows.q_head_stride = 0;

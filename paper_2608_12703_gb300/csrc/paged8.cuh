@@ -49,6 +49,7 @@ __device__ __forceinline__ uint32_t nan_codes(uint32_t x) {
 
 // ---- Host: argument checks and launches shared by the entry points -----------
 int paged8_view(const asr_paged8_cache* c, Paged8View* v);
+int paged8_writable(const asr_paged8_cache* c);   // of checked ones: whether rows may be appended
 int paged8_rows(const asr_paged8_cache* c, const asr_paged_rows* r, int dtype, PagedRows* v);
 cudaError_t launch_append8(const Paged8View& c, const PagedRows& r, int dtype, cudaStream_t st);
 // Attention of many rows (dtype 1 or 2), whose K/V are in the pages.  counts: 2, zero between calls.

@@ -510,6 +510,8 @@ int asr_spec_paged8_attend(const asr_paged8_cache* c, const asr_paged_rows* r, i
   if (int rc = paged8_view(c, &a.p)) return rc;
   if (dtype < 1) return ASR_E_INVAL;
   if (int rc = paged8_rows(c, r, dtype, &a.r)) return rc;
+  if (a.r.k_new)
+    if (int rc = paged8_writable(c)) return rc;
   if (!out || !ws || ((uintptr_t)out | (uintptr_t)ws) % 16 || (uintptr_t)lse % 4) return ASR_E_INVAL;
   const int m_rows = a.r.max_rows * a.r.group;
   if (ws_bytes < attend8_ws_bytes(c->head_dim, m_rows)) return ASR_E_CAPACITY;

@@ -107,6 +107,10 @@ def _status_word(device) -> torch.Tensor:
         return words[at:at + 1]
 
 
+def _expanded(x) -> bool:
+    return any(n > 1 and s == 0 for n, s in zip(x.shape, x.stride()))
+
+
 class _Paged:
     """What the classes over a pool of pages share: a status word, workspaces, and the rows of a call."""
 
@@ -357,7 +361,8 @@ class PagedCache8(_Paged):
     strides for both), one for the 16 slots of a group and a head, and the page table ``[batch, max_pages]``.
 
     A slot's values are its codes times its group's scale.  The caller owns the tensors.  The scales of appended groups are
-    powers of two; those of groups that were filled in another way need not be."""
+    powers of two; those of groups that were filled in another way need not be.  Scales that share memory (one expanded over
+    pages or heads, the same ones for K and V) can be read but not appended under."""
 
     def __init__(self, k_pages: torch.Tensor, v_pages: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor,
                  page_table: torch.Tensor):
@@ -393,6 +398,12 @@ class PagedCache8(_Paged):
         self._attend, self._append = self._lib.asr_spec_paged8_attend, self._lib.asr_spec_paged8_append
         self._attend_layouts, self._append_layouts = {}, {}
         self._ws, self._lock = {}, threading.Lock()
+        self._read_only = (k_scale.data_ptr() == v_scale.data_ptr() or k_pages.data_ptr() == v_pages.data_ptr() or
+                           _expanded(k_scale))
+
+    def _need_own(self):
+        _need(not self._read_only, "k_new: appended rows need codes and scales of their own; those that K and V, pages or heads "
+                                   "share can only be read")
 
     def _row_type(self, q):
         dtype = getattr(q, "dtype", None)
@@ -409,6 +420,7 @@ class PagedCache8(_Paged):
         key = _layouts(k_new, v_new, kv_len, rows)
         known = self._append_layouts.get(key)
         if known is None:
+            self._need_own()
             B, K, D = self.batch, self.kv_heads, self.head_dim
             _need(isinstance(k_new, torch.Tensor) and k_new.dim() == 4 and k_new.dtype in _DTYPE and k_new.shape[1] >= 1,
                   f"k_new: [{B}, rows, {K}, {D}] of float32, bfloat16 or float16 is required")
@@ -448,6 +460,8 @@ class PagedCache8(_Paged):
         known = self._attend_layouts.get(key)
         if known is None:
             r = self._rows(q, kv_len, rows, k_new, v_new, causal, scale)
+            if k_new is not None:
+                self._need_own()
             if out is not None:
                 _whole(out, "out", q.dtype, q.shape, self.device)
             if lse is not None:
@@ -490,6 +504,9 @@ class PagePool(_Paged):
                   c.device == c0.device, "caches: the same page table is required")
             _need(c.k_pages.shape[0] == n_pages and c.page_size == c0.page_size,
                   "caches: the same number and size of pages are required")
+            if isinstance(c, PagedCache8):
+                _need(not c._read_only, "caches: pages need codes and scales of their own; those that K and V, pages or heads share "
+                                        "cannot be moved")
         _whole(held, "held", torch.int32, (c0.batch,), c0.device)
         _whole(refs, "refs", torch.int32, (n_pages,), c0.device)
         _need(not _capturing(), "a pool is made outside of a graph capture")
