@@ -60,7 +60,7 @@ template <int D> struct Prompt8Mem {
 };
 
 struct Prompt8Bars {   // s, p: a buffer of scores; pv, q: a row tile
-  uint64_t q_full[2], k_full[2], k_free[2], v_full[2], v_free[2], sc_full[8], s_full[3], p_full[3], pv_done[2][4], item_full[4], begun[4], ended[4];
+  uint64_t q_full[2], k_full[2], k_free[2], v_full[2], v_free[2], sc_full[8], s_full[3], p_full[3], pv_done[2][4], item_full[4], begun[4], ended[4], drained;
 };
 struct GroupScales {   // of a tile's 8 groups
   float k[8], v[8], lv[8];
@@ -258,11 +258,15 @@ __device__ __forceinline__ int seen_by(const PagedRows& r, int len, int m) { ret
 
 // A block's items: the first by its number, each other one the next that no block has, in order of falling row tile (late
 // rows see most).  One thread fetches them, an item ahead, into four slots; a slot is free when everyone has left its item.
+// No warp waits for another one but by bar_wait: one whose wait has given up leaves at its next item, and those that stay must
+// find out by waits that end too.
 struct Items {
   const Prompt8Args& a;
   Prompt8Bars& bars;
   const int2* lens;
   int* slots;
+  int4* nan_keys;   // [4][quads], of a slot's item: none yet
+  int *any_nan, quads;
   // item number i; false where it has no work
   __device__ __forceinline__ bool set(int i, Item& it) const {
     const int per = a.p.c.kv_heads * a.p.c.batch, tile = i / per, in = i - tile * per;
@@ -286,6 +290,9 @@ struct Items {
     Item it;
     int i = k == 0 ? (int)blockIdx.x : (int)gridDim.x + atomicAdd(a.next, 1);
     while (i < a.items && !set(i, it)) i = (int)gridDim.x + atomicAdd(a.next, 1);
+#pragma unroll 4
+    for (int q = 0; q < quads; ++q) nan_keys[(k & 3) * quads + q] = make_int4(0x7fffffff, 0x7fffffff, 0x7fffffff, 0x7fffffff);
+    any_nan[k & 3] = 0;
     slots[k & 3] = i < a.items ? i : -1;
     mbar_arrive(&bars.item_full[k & 3]);
   }
@@ -313,7 +320,7 @@ __global__ void __launch_bounds__(THREADS, 1) prompt8_kernel(const Prompt8Args a
   extern __shared__ uint8_t raw[];
   __shared__ __align__(8) Prompt8Bars bars;
   __shared__ GroupScales scales[8];
-  __shared__ int nan_key[4][D];   // by item: of a column of V the first key whose code is a NaN
+  __shared__ __align__(16) int nan_key[4][D];   // by item: of a column of V the first key whose code is a NaN
   __shared__ int any_nan[4];
   __shared__ uint32_t s_tmem;
   __shared__ int s_items[4];
@@ -332,6 +339,7 @@ __global__ void __launch_bounds__(THREADS, 1) prompt8_kernel(const Prompt8Args a
     for (int i = 0; i < 3; ++i) mbar_init(&bars.s_full[i], 1), mbar_init(&bars.p_full[i], 4);
     for (int i = 0; i < 8; ++i) mbar_init(&bars.sc_full[i], 2);
     for (int i = 0; i < 4; ++i) mbar_init(&bars.item_full[i], 1), mbar_init(&bars.begun[i], 1), mbar_init(&bars.ended[i], 8 + 5 + 1);
+    mbar_init(&bars.drained, 1);
     fence_mbar_init();
   }
   for (int b = tid; b < c.batch; b += THREADS) paged_lens(c, r, b, lens[b].x, lens[b].y);
@@ -350,7 +358,7 @@ __global__ void __launch_bounds__(THREADS, 1) prompt8_kernel(const Prompt8Args a
     if (a.lse)
       for (size_t i = tid; i < count; i += THREADS) a.lse[heads0 + i] = -INFINITY;
   }
-  const Items src{a, bars, lens, s_items};
+  const Items src{a, bars, lens, s_items, reinterpret_cast<int4*>(nan_key), any_nan, D / 4};
   pdl_wait();   // the append, and the call before, whose last block sets the counts back
 
   // 8 warps of 168 registers and 8 of 88: what the block was launched with, 16 of 128
@@ -616,11 +624,6 @@ __global__ void __launch_bounds__(THREADS, 1) prompt8_kernel(const Prompt8Args a
       }
       if (is_v) {
         const int slot = k & 3;
-        if (j == 0) {   // everyone has left the item that had this slot
-          for (int i = w * 32 + lane; i < D; i += 96) nan_key[slot][i] = 0x7fffffff;
-          if (w == 0 && lane == 0) any_nan[slot] = 0;
-          asm volatile("bar.sync 1, 96;" ::: "memory");
-        }
         uint32_t bad = 0;
 #pragma unroll
         for (int g = 0; g < MINE; ++g)
@@ -723,6 +726,11 @@ __global__ void __launch_bounds__(THREADS, 1) prompt8_kernel(const Prompt8Args a
       pairs += n, tiles += max(n0, n1);
       if (lead) src.leave(k);
     }
+    // Where a wait has given up products may still be on their way: they end before tensor and shared memory are let go.
+    if (lead) umma_commit(&bars.drained);
+    __syncwarp();
+    bool late = false;
+    bar_wait(&bars.drained, 0, c.status, late);
   }
   __syncwarp();
   tc_fence_before();
