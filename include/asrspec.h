@@ -602,7 +602,7 @@ int asr_spec_paged8_append(const asr_paged8_cache* cache, const asr_paged_rows* 
  * row's largest lose bits) and are summed in fp32, softmax statistics in fp32; weights times the
  * groups' scales are rounded to fp16 for the second product, and those below 2^-35 of a row's largest
  * vanish there (the statistics have them).  Scales are positive and finite, or zero for zeros; rows
- * that see another one mean nothing.  A row of q that holds an infinity comes out as NaN.
+ * that see another one mean nothing.  A row of q that holds an infinity or a NaN comes out as NaN, lse too, where it sees a slot.
  * ws: asr_spec_paged8_attend_ws bytes, 16-byte aligned, zero before its first use; every call
  * leaves it ready for the next on its stream, whatever that one's sizes. */
 int64_t asr_spec_paged8_attend_ws(const asr_paged8_cache* cache, const asr_paged_rows* rows, int32_t dtype);

@@ -40,6 +40,13 @@ __device__ __forceinline__ uint32_t half2_of(uint32_t w) {
   asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((uint16_t)w));
   return h;
 }
+// Two fp16 numbers as they are, infinities as NaN: 0 x + x.  A row of q with an infinity in it then has no score but NaN;
+// left as it is, a row whose scores are all -inf would look like one that sees no slot.
+__device__ __forceinline__ uint32_t nan_for_inf(uint32_t x) {
+  uint32_t y;
+  asm("fma.rn.f16x2 %0, %1, %2, %1;" : "=r"(y) : "r"(x), "r"(0));
+  return y;
+}
 __device__ __forceinline__ float pow2(int e) { return __int_as_float((e + 127) << 23); }   // -126 <= e <= 127
 // Bytes of x that are a NaN code, as a mask.
 __device__ __forceinline__ uint32_t nan_codes(uint32_t x) {

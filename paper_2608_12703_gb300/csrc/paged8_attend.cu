@@ -208,7 +208,7 @@ __global__ void __launch_bounds__(C::WARPS * 32, 1) attend8_kernel(const Attend8
             }
         most = max(most, __shfl_xor_sync(0xffffffffu, most, 1));
         most = max(most, __shfl_xor_sync(0xffffffffu, most, 2));
-        // to [2^14, 2^15); infinities and NaN stay what they are
+        // to [2^14, 2^15); infinities and NaN stay what they are here
         e = min(100, 14 - ((int)(most >> 7) - 127));
         const float f0 = pow2(e / 2), f1 = pow2(e - e / 2);
 #pragma unroll
@@ -228,8 +228,8 @@ __global__ void __launch_bounds__(C::WARPS * 32, 1) attend8_kernel(const Attend8
       for (int j = 0; j < NJ; ++j)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          qb[nt][j][i][0] = reg_of(x[j][i / 2], i % 2 * 2);
-          qb[nt][j][i][1] = reg_of(x[j][i / 2], i % 2 * 2 + 1);
+          qb[nt][j][i][0] = nan_for_inf(reg_of(x[j][i / 2], i % 2 * 2));
+          qb[nt][j][i][1] = nan_for_inf(reg_of(x[j][i / 2], i % 2 * 2 + 1));
         }
 #pragma unroll
       for (int x2 = 0; x2 < 2; ++x2) {

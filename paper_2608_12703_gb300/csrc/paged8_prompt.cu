@@ -401,7 +401,9 @@ __global__ void __launch_bounds__(THREADS, 1) prompt8_kernel(const Prompt8Args a
         }
       }
 #pragma unroll
-      for (int i = 0; i < D / 8; ++i) sts16(dst + i / 8 * M::BLOCK + ((i % 8) ^ (row_in & 7)) * 16, v[i].x, v[i].y, v[i].z, v[i].w);
+      for (int i = 0; i < D / 8; ++i)
+        sts16(dst + i / 8 * M::BLOCK + ((i % 8) ^ (row_in & 7)) * 16, nan_for_inf(v[i].x), nan_for_inf(v[i].y), nan_for_inf(v[i].z),
+              nan_for_inf(v[i].w));
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
       warp_arrive(&bars.q_full[x]);
       return sc;
