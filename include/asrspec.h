@@ -560,7 +560,9 @@ int asr_spec_accept_sampled(const asr_sampled_logits* logits, const int32_t* dra
 /* ---- An 8-bit paged cache, its pages, and the logits' adjustment -----------
  * The same kind of entry as the section above: no handle, device arrays of the
  * caller's, asynchronous on `stream`, nothing allocated, conditions in device
- * data reported in the status word.  A round of several samples a prompt is
+ * data reported in the status word.  A call may be several kernels that hand on
+ * results by ws or by the pages: host threads that share a stream and either of
+ * these make their calls one at a time (serving.py sees to that).  A round of several samples a prompt is
  *   fork -> reserve -> attend (per layer) -> adjust_logits -> accept_sampled
  *   -> kv_len += step -> fork (keep = kv_len) -> now and then compact.
  *

@@ -107,6 +107,16 @@ def _status_word(device) -> torch.Tensor:
         return words[at:at + 1]
 
 
+_turns: dict = {}         # (device index, stream): the lock of calls there
+
+
+def _turn(index: int, stream: int):
+    """Held while a call over pages launches: a call's kernels follow one another on its stream, whatever other host threads
+    launch there.  What one of them leaves in the workspace is the next one's, and pages that a table names already are
+    filled by the last."""
+    return _turns.get((index, stream)) or _turns.setdefault((index, stream), threading.RLock())
+
+
 def _expanded(x) -> bool:
     return any(n > 1 and s == 0 for n, s in zip(x.shape, x.stride()))
 
@@ -246,7 +256,8 @@ class PagedCache(_Paged):
             lse = torch.empty(lse_shape, dtype=torch.float32, device=self.device)
         stream = _raw_stream(self._index)
         ws = self._workspace("attend", stream, n)
-        rc = self._attend(self._ref, _byref(r), out.data_ptr(), lse.data_ptr(), ws.data_ptr(), n, stream)
+        with _turn(self._index, stream):
+            rc = self._attend(self._ref, _byref(r), out.data_ptr(), lse.data_ptr(), ws.data_ptr(), n, stream)
         if rc:
             _check(rc, "asr_spec_paged_attend")
         return out, lse
@@ -278,7 +289,9 @@ class PagedCache(_Paged):
             s.score = score.data_ptr()
         if pos is not None:
             s.pos, s.first_pos = pos.data_ptr(), first_pos.data_ptr()
-        rc = self._weigh(self._ref, _byref(r), _byref(s), lse.data_ptr(), *lse_strides, _raw_stream(self._index))
+        stream = _raw_stream(self._index)
+        with _turn(self._index, stream):
+            rc = self._weigh(self._ref, _byref(r), _byref(s), lse.data_ptr(), *lse_strides, stream)
         if rc:
             _check(rc, "asr_spec_paged_weigh")
         return out
@@ -329,8 +342,9 @@ class PagedCache(_Paged):
         s.score, s.pos, s.score_out, s.pos_out = score.data_ptr(), pos.data_ptr(), score_out.data_ptr(), pos_out.data_ptr()
         stream = _raw_stream(self._index)
         ws = self._workspace("evict", stream, n)
-        rc = self._evict(self._ref, _byref(s), lens.data_ptr(), seen.data_ptr(), budget, recent, first, lens_out.data_ptr(),
-                         ws.data_ptr(), n, stream)
+        with _turn(self._index, stream):
+            rc = self._evict(self._ref, _byref(s), lens.data_ptr(), seen.data_ptr(), budget, recent, first, lens_out.data_ptr(),
+                             ws.data_ptr(), n, stream)
         if rc:
             _check(rc, "asr_spec_paged_evict")
         return lens_out, score_out, pos_out
@@ -441,7 +455,9 @@ class PagedCache8(_Paged):
         r.k_new, r.v_new, r.kv_len = k_new.data_ptr(), v_new.data_ptr(), kv_len.data_ptr()
         if rows is not None:
             r.rows = rows.data_ptr()
-        rc = self._append(self._ref, _byref(r), dtype, _raw_stream(self._index))
+        stream = _raw_stream(self._index)
+        with _turn(self._index, stream):
+            rc = self._append(self._ref, _byref(r), dtype, stream)
         if rc:
             _check(rc, "asr_spec_paged8_append")
 
@@ -477,7 +493,8 @@ class PagedCache8(_Paged):
             lse = torch.empty(lse_shape, dtype=torch.float32, device=self.device)
         stream = _raw_stream(self._index)
         ws = self._workspace("attend", stream, n)
-        rc = self._attend(self._ref, _byref(r), dtype, out.data_ptr(), lse.data_ptr(), ws.data_ptr(), n, stream)
+        with _turn(self._index, stream):
+            rc = self._attend(self._ref, _byref(r), dtype, out.data_ptr(), lse.data_ptr(), ws.data_ptr(), n, stream)
         if rc:
             _check(rc, "asr_spec_paged8_attend")
         return out, lse
@@ -583,8 +600,9 @@ class PagePool(_Paged):
         counts = torch.empty(2, dtype=torch.int32, device=self.device)
         stream = _raw_stream(self._index)
         ws = self._workspace("pool", stream, self._bytes)
-        rc = self._reserve(_byref(p), self._plan.data_ptr(), self._n, lens.data_ptr(), rows.data_ptr(), counts.data_ptr(),
-                           ws.data_ptr(), self._bytes, stream)
+        with _turn(self._index, stream):
+            rc = self._reserve(_byref(p), self._plan.data_ptr(), self._n, lens.data_ptr(), rows.data_ptr(), counts.data_ptr(),
+                               ws.data_ptr(), self._bytes, stream)
         if rc:
             _check(rc, "asr_spec_pool_reserve")
         return (self.page_table if table_out is None else table_out, self.held if held_out is None else held_out,
@@ -602,8 +620,9 @@ class PagePool(_Paged):
         p = self._at(layout, table_out, held_out, refs_out)
         stream = _raw_stream(self._index)
         ws = self._workspace("pool", stream, self._bytes)
-        rc = self._fork(_byref(p), None if parent is None else parent.data_ptr(), None if keep is None else keep.data_ptr(),
-                        ws.data_ptr(), self._bytes, stream)
+        with _turn(self._index, stream):
+            rc = self._fork(_byref(p), None if parent is None else parent.data_ptr(), None if keep is None else keep.data_ptr(),
+                            ws.data_ptr(), self._bytes, stream)
         if rc:
             _check(rc, "asr_spec_pool_fork")
         return (self.page_table if table_out is None else table_out, self.held if held_out is None else held_out,
@@ -623,8 +642,9 @@ class PagePool(_Paged):
         live = torch.empty(1, dtype=torch.int32, device=self.device)
         stream = _raw_stream(self._index)
         ws = self._workspace("pool", stream, self._bytes)
-        rc = self._compact(_byref(p), self._plan.data_ptr(), self._n, where.data_ptr(), live.data_ptr(), ws.data_ptr(),
-                           self._bytes, stream)
+        with _turn(self._index, stream):
+            rc = self._compact(_byref(p), self._plan.data_ptr(), self._n, where.data_ptr(), live.data_ptr(), ws.data_ptr(),
+                               self._bytes, stream)
         if rc:
             _check(rc, "asr_spec_pool_compact")
         return (self.page_table if table_out is None else table_out, self.refs if refs_out is None else refs_out, where, live)
