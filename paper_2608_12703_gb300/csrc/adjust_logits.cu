@@ -27,7 +27,7 @@ constexpr int THREADS = 256;
 struct AdjustArgs {
   asr_logit_rules r;
   long long batch, row, out_batch, out_row;   // bytes
-  int words, rows_each;                       // words of a mask row; rows of a block
+  int rows_each;                              // of a block
 };
 
 template <typename T> __device__ __forceinline__ T from_f32(float v);
@@ -252,7 +252,7 @@ extern "C" int asr_spec_adjust_logits(const asr_logit_rules* r, void* stream) {
   if (!(r->repetition_all > 0.f) || !(r->repetition_all <= 1e30f)) return ASR_E_INVAL;
   for (float x : {r->frequency_all, r->presence_all})
     if (!(x >= -1e30f && x <= 1e30f)) return ASR_E_INVAL;
-  AdjustArgs a{*r, r->batch_stride * es, r->row_stride * es, r->out_batch_stride * es, r->out_row_stride * es, (r->vocab + 31) / 32, 0};
+  AdjustArgs a{*r, r->batch_stride * es, r->row_stride * es, r->out_batch_stride * es, r->out_row_stride * es, 0};
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
   const cudaError_t e = r->dtype == 0   ? launch_type<float>(a, st)
                         : r->dtype == 1 ? launch_type<__nv_bfloat16>(a, st)

@@ -60,7 +60,7 @@ template <int D> struct Prompt8Mem {
 };
 
 struct Prompt8Bars {   // s, p: a buffer of scores; pv, q: a row tile
-  uint64_t q_full[2], k_full[2], k_free[2], v_full[2], v_free[2], sc_full[8], s_full[3], p_full[3], pv_done[2][4], item_full[4], begun[4], ended[4], drained;
+  uint64_t q_full[2], k_full[2], k_free[2], v_full[2], v_free[2], sc_full[8], s_full[2], p_full[2], pv_done[2][4], item_full[4], begun[4], ended[4], drained;
 };
 struct GroupScales {   // of a tile's 8 groups
   float k[8], v[8], lv[8];
@@ -312,7 +312,8 @@ __device__ __forceinline__ void warp_arrive(uint64_t* bar) {
 template <typename T, int D>
 __global__ void __launch_bounds__(THREADS, 1) prompt8_kernel(const Prompt8Args a) {
   using M = Prompt8Mem<D>;
-  // Buffers of scores: with a third one a row tile's next scores are there before its weights are.  Tensor memory holds it beside outputs of 64.
+  // Tensor memory, 512 columns: two buffers of scores, for heads of 64 the weights of each beside them, the outputs of both row
+  // tiles.  Heads of 64 fill 512, heads of 128 too: no room for a third buffer of scores.
   constexpr int HB = M::HB, NS = 2;
   constexpr bool ONCE = D == 64;
   constexpr int P_COL = 2 * BN, O_COL = ONCE ? P_COL + BN : 2 * BN, P_STEP = ONCE ? BN / 2 : BN;
@@ -334,9 +335,9 @@ __global__ void __launch_bounds__(THREADS, 1) prompt8_kernel(const Prompt8Args a
     for (int i = 0; i < 2; ++i) {
       mbar_init(&bars.q_full[i], 4), mbar_init(&bars.k_full[i], 3), mbar_init(&bars.v_full[i], 3);
       mbar_init(&bars.k_free[i], 1), mbar_init(&bars.v_free[i], 1);
+      mbar_init(&bars.s_full[i], 1), mbar_init(&bars.p_full[i], 4);
       for (int j = 0; j < 4; ++j) mbar_init(&bars.pv_done[i][j], 1);
     }
-    for (int i = 0; i < 3; ++i) mbar_init(&bars.s_full[i], 1), mbar_init(&bars.p_full[i], 4);
     for (int i = 0; i < 8; ++i) mbar_init(&bars.sc_full[i], 2);
     for (int i = 0; i < 4; ++i) mbar_init(&bars.item_full[i], 1), mbar_init(&bars.begun[i], 1), mbar_init(&bars.ended[i], 8 + 5 + 1);
     mbar_init(&bars.drained, 1);
