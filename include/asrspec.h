@@ -593,6 +593,9 @@ typedef struct {
  * rounded anew (exact but for values below 2^-6 of the new scale, since scales are powers of
  * two).  code = round to nearest even of value / scale; a NaN or an infinity becomes a
  * NaN code and counts for no scale.  Slots at or past kv_len + rows are left as they are.
+ * Rows that are appended and never counted by a later kv_len (rejected drafts) leave the scale that they raised, and the
+ * codes of the group's earlier slots rounded to it: by less than 2^-9 of the scale over all such calls, 2^-16 of the largest
+ * value that the group was given.  What is written over them takes that scale, or a larger one.
  * Data errors: as asr_spec_paged_attend's; new rows of a bad page id are not written. */
 int asr_spec_paged8_append(const asr_paged8_cache* cache, const asr_paged_rows* rows, int32_t dtype, void* stream);
 
@@ -600,8 +603,8 @@ int asr_spec_paged8_append(const asr_paged8_cache* cache, const asr_paged_rows* 
  * the dequantised ones.  dtype (1 or 2) is that of q, k_new, v_new and out.  With k_new /
  * v_new (causal only) they are appended first, as by asr_spec_paged8_append, and
  * the rows see them as they are stored.  Arithmetic: codes and q multiply exactly
- * (bf16 rows are brought to fp16 by a power of two: elements below 2^-30 of a
- * row's largest lose bits) and are summed in fp32, softmax statistics in fp32; weights times the
+ * (bf16 rows are brought to fp16 by a power of two: elements below 2^-31 of a
+ * row's largest, or below 2^-117, lose bits) and are summed in fp32, softmax statistics in fp32; weights times the
  * groups' scales are rounded to fp16 for the second product, and those below 2^-35 of a row's largest
  * vanish there (the statistics have them).  Scales are positive and finite, or zero for zeros; rows
  * that see another one mean nothing.  A row of q that holds an infinity or a NaN comes out as NaN, lse too, where it sees a slot.
@@ -611,7 +614,9 @@ int64_t asr_spec_paged8_attend_ws(const asr_paged8_cache* cache, const asr_paged
 int asr_spec_paged8_attend(const asr_paged8_cache* cache, const asr_paged_rows* rows, int32_t dtype, void* out, float* lse,
                            void* ws, int64_t ws_bytes, void* stream);
 
-/* Who holds which pages.  refs[p] is the number of table entries (and of holders
+/* Who holds which pages.  A page that several sequences hold is read by all and
+ * written by none: reserve comes before an append, and asr_spec_paged_evict,
+ * which moves slots within their pages, only where every page is held once.  refs[p] is the number of table entries (and of holders
  * of the caller's own) of page p; 0 = free.  Entries at or past held[b] mean nothing and are
  * left as they are.  table_out, held_out and refs_out receive the new state; each
  * may be its input itself (but not overlap it otherwise). */
@@ -676,7 +681,9 @@ int asr_spec_pool_compact(const asr_page_pool* pool, const void* plan, int32_t n
                           void* ws, int64_t ws_bytes, void* stream);
 
 /* Logits of a block and what is done to them.  Rows need only their element's
- * alignment; strides in elements, >= 0. */
+ * alignment; strides in elements.  Those of logits and out are at least vocab (of
+ * the batch where it is more than 1), history's at least history_max; bias's and
+ * the mask's may be 0. */
 typedef struct {
   const void* logits;          /* [batch][rows][vocab] */
   int64_t batch_stride, row_stride;

@@ -427,7 +427,8 @@ class PagedCache8(_Paged):
     def append(self, k_new, v_new, kv_len, *, rows=None):
         """Quantise ``k_new`` / ``v_new`` ``[B, R, K, D]`` (float32, bfloat16 or float16) behind each sequence's ``kv_len``
         slots; ``rows`` (int32 ``[B]``) are the rows in use.  A group that the rows begin takes the least power of two that
-        holds its values; one that goes on keeps its scale, or takes a larger one and its codes are rounded anew."""
+        holds its values; one that goes on keeps its scale, or takes a larger one and its codes are rounded anew.  Rows that are
+        rejected later leave the scale that they raised (see ``asr_spec_paged8_append``)."""
         if _current_device() != self._index:
             with torch.cuda.device(self.device):
                 return self.append(k_new, v_new, kv_len, rows=rows)
@@ -504,6 +505,9 @@ class PagePool(_Paged):
     """Who holds which pages of one or more caches (one a layer) that share a page table: ``held [batch]``, the entries in
     use of each table row, and ``refs [n_pages]``, how many table entries (and holders of the caller's own) a page has; 0 is
     free.  Both int32, contiguous.
+
+    A page that several rows hold may be read by all and written by none: ``reserve`` comes before an append, and
+    ``PagedCache.evict``, which moves slots within their pages, only where no page is shared.
 
     The calls decide from these arrays alone and keep nothing: each takes the lowest free pages in order of sequence and
     slot.  They write the caches' table, ``held`` and ``refs`` in place unless outputs are given (which take all of the new
@@ -715,6 +719,7 @@ def _adjust_layout(logits, history, history_len, prompt_len, draft, lens, repeti
         _need(isinstance(history, torch.Tensor) and history.dim() == 2, f"history: int32 [{B}, tokens] is required")
         _tensor(history, "history", torch.int32, (B, history.shape[1]), dev)
         _need(history.stride(1) == 1 or history.shape[1] <= 1, "history: the last axis must be contiguous")
+        _need(history.stride(0) >= history.shape[1], "history: rows must lie apart (an expanded history: contiguous() first)")
     _need(history is not None or (history_len is None and prompt_len is None), "history_len, prompt_len: history is required")
     for x, name in ((history_len, "history_len"), (prompt_len, "prompt_len"), (lens, "lens")):
         if x is not None:

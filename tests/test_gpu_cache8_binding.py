@@ -141,3 +141,16 @@ def test_too_many_arrays(built_lib, cuda):
     with pytest.raises(A.AsrSpecError, match="1024"):
         serving.PagePool([c] * 257, s.h, s.r)
     assert np.array_equal(raw(s.arrays[0][0]).cpu().numpy(), raw(s.before[0]).cpu().numpy())
+
+
+def test_an_expanded_history_is_refused(built_lib, cuda):
+    """Rows of a history lie apart; one for all utterances is made contiguous first."""
+    from paper_2608_12703_gb300 import serving
+    x = torch.randn((3, 2, 50), generator=gen(95), device="cuda")
+    h = torch.arange(7, dtype=torch.int32, device="cuda")
+    with pytest.raises(A.AsrSpecError, match="contiguous"):
+        serving.adjust_logits(x, history=h.expand(3, 7), repetition=2.0, out=torch.zeros_like(x))
+    got = serving.adjust_logits(x, history=h.expand(3, 7).contiguous(), repetition=2.0, out=torch.zeros_like(x))
+    want = x.clone()
+    want[:, :, :7] = torch.where(want[:, :, :7] > 0, want[:, :, :7] / 2, want[:, :, :7] * 2)
+    assert torch.equal(got, want)
