@@ -8,8 +8,8 @@
 // ring of its own.  What differs:
 //   * codes become fp16 on the way to the tensor cores, two an instruction and
 //     exactly.  q is taken to fp16 too: fp16 rows as they are; bf16 rows by a power of two
-//     that brings their largest element to the top of the range, which keeps all 8 bits
-//     of elements down to 2^-29 of it;
+//     that brings their largest element to [2^14, 2^15), which keeps all 8 bits of
+//     elements down to 2^-31 of it (at most 2^100: below 2^-117 they lose bits);
 //   * keys are the first index of both products (S^T = K q^T, O^T = V^T p^T), so
 //     that 16 of them meet 8 rows in an instruction and no half of a tile is left
 //     empty by blocks of up to 8 rows, which are most.  p^T changes
@@ -519,7 +519,8 @@ int asr_spec_paged8_attend(const asr_paged8_cache* c, const asr_paged_rows* r, i
   const long long tiles = ((long long)m_rows + tr - 1) / tr;
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   // The kernel for prompts takes 256 rows of a K/V head a block and does not share keys between blocks: it needs rows to fill its
-  // tiles and items to fill the SMs.  Measured, us a call, this kernel and that one: 20 heads of 64, 32 sequences of 448
+  // tiles and items to fill the SMs.  Rows are those that a call has room for: a prompt among single rows takes all of them
+  // there.  Measured for heads of 64 and sequences of one length (heads of 128 and uneven ones follow unmeasured), us a call, this kernel and that one: 20 heads of 64, 32 sequences of 448
   // slots, 64 rows 67 and 68, 96 rows 113 and 84, 256 rows 356 and 117; 40 items of 256 rows by 1000 slots 67 and 40; 8
   // items of 300 rows by 8000 slots 50 and 151, 6 of 256 by 100000 268 and 1608.
   const long long items = ((long long)m_rows + 255) / 256 * c->kv_heads * c->batch;

@@ -12,9 +12,9 @@
 // CHUNK pages, so that its steps are block barriers and not launches.
 // Measured, device time: private pages for 256 sequences after a fork, 6 layers
 // of 12 heads of 64, bf16: 46 us for 227 MB, 10 of them the plan; for 8 samples 13
-// us, latency; 1024 sequences' rows of up to 2500 entries forked: 15 us, 8 the
+// us, latency; 1024 sequences' rows of up to 2500 entries forked: 9 us, 8 the
 // second kernel (three dependent look-ups, then 13 MB); 32 layers of 20 heads of 64 in 8
-// bits compacted: 105 us for 590 MB, 5.6 TB/s.  Copies in pieces of a page
+// bits compacted: 103 us for 590 MB, 5.7 TB/s.  Copies in pieces of a page
 // whatever it holds took 70 us where 46 are needed; runs of neighbouring pieces
 // a warp, to look job and array up less often, 10 % longer than tasks dealt in turn.
 #include <cstring>
