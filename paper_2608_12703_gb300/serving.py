@@ -526,8 +526,7 @@ class PagePool(_Paged):
             _need(c.k_pages.shape[0] == n_pages and c.page_size == c0.page_size,
                   "caches: the same number and size of pages are required")
             if isinstance(c, PagedCache8):
-                _need(not c._read_only, "caches: pages need codes and scales of their own; those that K and V, pages or heads share "
-                                        "cannot be moved")
+                _need(not _expanded(c.k_scale), "caches: pages need scales of their own; those that pages or heads share cannot be moved")
         _whole(held, "held", torch.int32, (c0.batch,), c0.device)
         _whole(refs, "refs", torch.int32, (n_pages,), c0.device)
         _need(not _capturing(), "a pool is made outside of a graph capture")
