@@ -117,13 +117,14 @@ __device__ __forceinline__ void bulk_copy(uint32_t smem, const char* p, uint32_t
                : "memory");
 }
 // Waits for a phase, at most about a second; then it gives up: the status word
-// says so and the results are invalid.  From there on a wait takes half a
-// millisecond at most: copies that are on their way still end before the block does.
+// says so and the results are invalid.  From there on a wait takes 2^17 cycles
+// at most, far longer than a copy does: those on their way end before the block,
+// and a block that waits in vain at every step still ends soon.
 __device__ __forceinline__ void bar_wait(uint64_t* bar, uint32_t parity, int* status, bool& gave_up) {
   if (mbar_try_wait(bar, parity)) return;
   const uint32_t t0 = (uint32_t)clock();
   while (!mbar_try_wait(bar, parity)) {
-    if ((uint32_t)clock() - t0 > (gave_up ? 1u << 20 : 1u << 31)) {
+    if ((uint32_t)clock() - t0 > (gave_up ? 1u << 17 : 1u << 31)) {
       if (status) set_status(status, ST_WAIT_TIMEOUT);
       gave_up = true;
       return;

@@ -61,7 +61,7 @@ def test_a_phase_that_does_not_end(waits):
     first, copy, lost, again, there = waits((end, 1000), (10 ** 5, 100), (end, 100), (10 ** 5, 100), (0, 20))
     assert first[1:] == (0, 1, 1, 1) and 1 << 31 < first[0] < (1 << 31) + 10 ** 4
     assert copy[1] == again[1] == there[1] == 1 and copy[4] == again[4] == there[4] == 0
-    assert lost[1] == 0 and 1 << 20 < lost[0] < (1 << 20) + 10 ** 4
+    assert lost[1] == 0 and 1 << 17 < lost[0] < (1 << 17) + 10 ** 4
 
 
 def test_without_a_status_word(waits):
